@@ -45,7 +45,7 @@ typedef enum {
   FD_ERR_UNSUPPORTED = 7      /* device is not sm_103 / sm_100 class                      */
 } fd_status;
 
-typedef enum { FD_DTYPE_F32 = 0, FD_DTYPE_BF16 = 1, FD_DTYPE_U8 = 2 } fd_dtype;
+typedef enum { FD_DTYPE_F32 = 0, FD_DTYPE_BF16 = 1, FD_DTYPE_U8 = 2, FD_DTYPE_F16 = 3 } fd_dtype;
 
 /*
  * Decoder shape (names follow the paper: Sec. 3, Algorithm 1, Table "Model scaling").

@@ -205,6 +205,143 @@ fd_status fd_op_l1_pixel_bwd(const float* F, const float* target, int frames, in
                              int grid_w, int channels, int rs, float* dF, float* loss,
                              float* work, void* stream);
 
+/* ---- rotary positions ---- */
+
+/* How a head's leading rot_dim elements are paired: pair i is elements (2i, 2i + 1) or
+ * (i, i + rot_dim / 2). */
+typedef enum { FD_ROTARY_INTERLEAVED = 0, FD_ROTARY_HALF = 1 } fd_rotary_layout;
+
+/* How the frequencies f = base^(-2i/d) of an axis of d elements are stretched to contexts
+ * `factor` times longer than those trained on:
+ *   LINEAR  f / factor (positions interpolated)
+ *   BASE    base * factor^(d / (d - 2)) for base: the slowest pair of the axis is slowed by
+ *           `factor`, the fastest not at all (axes of 2 elements keep their one frequency)
+ *   BLEND   g f + (1 - g) f / factor with g = clamp((n - slow_turns) / (fast_turns -
+ *           slow_turns), 0, 1) and n = trained_len f / (2 pi), the pair's turns over the
+ *           trained context: fast pairs as they are, slow ones interpolated */
+typedef enum {
+  FD_ROTARY_SCALE_NONE = 0,
+  FD_ROTARY_SCALE_LINEAR = 1,
+  FD_ROTARY_SCALE_BASE = 2,
+  FD_ROTARY_SCALE_BLEND = 3
+} fd_rotary_scaling;
+
+typedef struct {
+  int32_t head_dim;      /* elements of a head, 2..256                                      */
+  int32_t rot_dim;       /* leading elements that are turned, even, 2..head_dim             */
+  int32_t layout;        /* fd_rotary_layout                                                */
+  int32_t axes;          /* position axes, 1..3 (time, row, column for video tokens)        */
+  int32_t axis_dims[3];  /* elements turned by each axis, even, >= 2, their sum is rot_dim  */
+  int32_t scaling;       /* fd_rotary_scaling                                               */
+  float base;            /* > 0                                                             */
+  float factor;          /* > 0; used unless scaling is NONE                                */
+  int32_t trained_len;   /* >= 1; BLEND                                                     */
+  float fast_turns;      /* > slow_turns; BLEND                                             */
+  float slow_turns;
+  float amplitude;       /* turned elements are multiplied by it, finite (1: a rotation)    */
+} fd_rotary_config;
+
+/* The frequencies of one configuration. A host object: it holds no device memory, any number of
+ * calls on any streams and devices may use it at once. */
+typedef struct fd_rotary_s* fd_rotary;
+fd_status fd_rotary_create(const fd_rotary_config* cfg, fd_rotary* out);
+fd_status fd_rotary_destroy(fd_rotary plan);
+
+/* Turns queries and keys by their positions, in one launch: for pair (a, b) of axis x at
+ * frequency f and angle t = positions[token][x] f
+ *   a' = amplitude (a cos t - b sin t),  b' = amplitude (a sin t + b cos t)
+ * and with backward = 1 the gradient (the transposed turn: t negated), from the gradients of
+ * the outputs to those of the inputs. Elements past rot_dim are copied. A position's phase
+ * is an integer product modulo one turn, so no int32 position, negative ones too, loses its
+ * angle to rounding.
+ * dtype FD_DTYPE_F32 / BF16 / F16 of q, k and the outputs; positions int32 [tokens][axes].
+ * Element (token, head, i) of q is at q[token q_token_stride + head q_head_stride + i], of q_out
+ * with the out strides (in elements, any values that keep the heads apart), k likewise; k with 0 heads is
+ * left out (pointers may be NULL). An output may be its input (same pointer and strides), no
+ * other overlap is allowed. tokens may be 0. */
+fd_status fd_op_rotary(fd_rotary plan, int backward, int dtype, int tokens,
+                       const int32_t* positions, int q_heads, const void* q,
+                       int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                       int64_t q_out_token_stride, int64_t q_out_head_stride, int k_heads,
+                       const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
+                       int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/* ---- a cache of bounded size that keeps what attention uses ----
+ *
+ * For streams that are not served by the last W chunks alone: every (stream, KV group) has
+ * `capacity` slots, each holding a key, a value, the position that they belong to and the
+ * attention weight that the entry has gathered so far. Slots are in no order. New tokens take
+ * the slots of the entries with the least weight (fd_op_cache_insert), attention reads the
+ * slots and adds to their weights (fd_op_cache_attention), a long first pass is cut down once
+ * (fd_op_cache_compact). An empty slot has a negative position; the caller sets all positions to
+ * -1 before the first insert. Whatever an empty slot's key, value and weight hold (NaN too) has
+ * no effect. Entries that are in use have finite keys and values. */
+typedef struct {
+  int32_t streams, groups, capacity;  /* >= 0, >= 1, >= 0                                   */
+  int32_t head_dim;                   /* 64 or 128                                          */
+  int32_t dtype;                      /* FD_DTYPE_BF16 or FD_DTYPE_F16                      */
+  int32_t reserved;                   /* 0                                                  */
+  void* k;                            /* element i of slot j: k[stream stream_stride + group */
+  void* v;                            /*   group_stride + j slot_stride + i]; v the same     */
+  int64_t stream_stride, group_stride, slot_stride; /* elements, multiples of 8, >= 0; slot_stride >=
+                                         head_dim; k and v 16-byte aligned                  */
+  int32_t* pos;                       /* [streams][groups][capacity]                        */
+  float* weight;                      /* [streams][groups][capacity]                        */
+} fd_cache;
+
+/* Attention of n_q queries a stream over the first `used` slots of its cache, and the weights
+ * that they give to each slot:
+ *   p[t][h][j] = softmax over the visible slots j of scale q[t][h] . k[j];  KV group h / (heads / groups)
+ *   out[t][h]  = sum_j p[t][h][j] v[j]
+ *   weight_out[j] = decay weight[j] + sum over the queries t and the group's heads h of p[t][h][j]
+ * Slot j is visible to query t if 0 <= pos[j] <= q_pos[t] (one position for all tokens of a
+ * chunk lets each see the whole chunk). A query that sees no slot gives zeros and adds nothing.
+ * q, out of the cache's type: element (stream, t, h, i) of q at q[stream q_stream_stride + t
+ * q_token_stride + h q_head_stride + i], of out with the out strides (elements; 16-byte
+ * aligned, strides multiples of 8). q_pos int32 [streams][n_q]. weight_out fp32
+ * [streams][groups][capacity], entries past `used` are not written; it may be cache->weight;
+ * NULL: the weights are not gathered. Softmax, sums and weights are in fp32, P is rounded to the
+ * cache's type for its product with V. The order of every sum is fixed: equal calls give equal
+ * bits. workspace: fd_cache_attention_workspace_bytes(...) bytes of device memory (16-byte
+ * aligned) that the call overwrites; calls that may overlap need one each. err_dev as for
+ * fd_op_linear. streams, n_q and used may be 0 (with used = 0 out is zeros). */
+size_t fd_cache_attention_workspace_bytes(const fd_cache* cache, int used, int heads, int n_q);
+fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int n_q,
+                                const void* q, int64_t q_stream_stride, int64_t q_token_stride,
+                                int64_t q_head_stride, const int32_t* q_pos, float scale,
+                                float decay, void* out, int64_t out_stream_stride,
+                                int64_t out_token_stride, int64_t out_head_stride,
+                                float* weight_out, void* workspace, int* err_dev, void* stream);
+
+/* New tokens into the cache, evicting what they displace. For each (stream, group), the slots
+ * are ranked by (class, weight, slot index): class 0 empty slots (weights ignored), class 1
+ * entries that nothing protects, class 2 protected ones (pos < sinks, or pos >= new_pos[0] -
+ * recent of the stream). The first n_new in this order are given up, so ties go to the lowest
+ * index, -0 ranks as +0 and NaN above every number, and the n_new new tokens take them in the order
+ * of their slot index. slots int32 [streams][groups][n_new]: the slots taken, ascending.
+ * The new entries' positions are new_pos int32 [streams][n_new] (>= 0) and their weight is 0.
+ * k_new, v_new of the cache's type: element (stream, t, group, i) at k_new[stream
+ * new_stream_stride + t new_token_stride + group new_group_stride + i] (elements; 16-byte
+ * aligned, strides multiples of 8). pos_out, weight_out: [streams][groups][capacity] arrays
+ * that receive all positions and weights; they may be cache->pos and cache->weight. Keys and
+ * values are written in place. 0 <= n_new <= capacity <= 1,048,576; sinks, recent >= 0. */
+fd_status fd_op_cache_insert(const fd_cache* cache, int n_new, const void* k_new,
+                             const void* v_new, int64_t new_stream_stride,
+                             int64_t new_token_stride, int64_t new_group_stride,
+                             const int32_t* new_pos, int sinks, int recent, int32_t* pos_out,
+                             float* weight_out, int32_t* slots, void* stream);
+
+/* Cuts a cache down: for each (stream, group), of the first `used` slots of src the
+ * dst->capacity that rank last in the order of fd_op_cache_insert (recency counts from
+ * now[stream], int32) are copied to dst with their positions and weights, in the order of their
+ * slots; where src has fewer entries, the slots at dst's end are empty (position -1, weight 0,
+ * key and value zero). src_slots int32 [streams][groups][dst->capacity]: the slot that each came
+ * from, -1 for an empty one. src and dst have the same streams, groups, head_dim and dtype and
+ * share no memory. 0 <= used <= src->capacity, dst->capacity <= used <= 1,048,576. */
+fd_status fd_op_cache_compact(const fd_cache* src, int used, const fd_cache* dst,
+                              const int32_t* now, int sinks, int recent, int32_t* src_slots,
+                              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -284,6 +284,15 @@ bool band_attention_maps(AttnStream* host, int T, int W, int rows_per_chunk, int
 bool attention_q_maps(CUtensorMap* q, CUtensorMap* q8, const __nv_bfloat16* base, int rows,
                       int heads);
 
+// ---- hooks of the operators with their own C entries (fd_rotary.cu, fd_cache_*.cu)
+// FD_OK on an sm_103 device; SMs of the device
+fd_status check_device();
+int num_sms();
+// 4D map over 16-bit elements (is_f16: fp16, else bf16): dims innermost first, strides in bytes
+// of dims 1..3, 128-byte swizzled boxes of 64 x rows x 1 x 1; reads past the dims give zeros
+bool tmap_16bit_4d(CUtensorMap* m, bool is_f16, const void* base, const uint64_t dims[4],
+                   const uint64_t strides[3], uint32_t rows);
+
 // GEMM tile widths compiled in
 inline bool gemm_bn_supported(int bn) {
   return bn == 64 || bn == 96 || bn == 128 || bn == 192 || bn == 256;

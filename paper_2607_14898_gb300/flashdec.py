@@ -20,7 +20,7 @@ FD_OK = 0
 STATUS = {0: "FD_OK", 1: "FD_ERR_INVALID_ARG", 2: "FD_ERR_CONFIG", 3: "FD_ERR_OOM",
           4: "FD_ERR_CUDA", 5: "FD_ERR_STATE", 6: "FD_ERR_DEVICE_TIMEOUT",
           7: "FD_ERR_UNSUPPORTED"}
-DTYPE_F32, DTYPE_BF16, DTYPE_U8 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_U8, DTYPE_F16 = 0, 1, 2, 3
 # fd_rope_mode, keyed like the oracle's rope_mode argument
 ROPE_MODES = {"abs": 0, "window": 1}
 EPI_F32, EPI_RESID, EPI_GELU, EPI_TUP, EPI_SWIGLU = 0, 1, 2, 3, 4
@@ -48,9 +48,27 @@ class fd_config(ctypes.Structure):
                                       ("rope_mode", ctypes.c_int32)]
 
 
+class fd_rotary_config(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("axis_dims", ctypes.c_int32 * 3), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_float), ("factor", ctypes.c_float),
+                ("trained_len", ctypes.c_int32), ("fast_turns", ctypes.c_float),
+                ("slow_turns", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class fd_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("streams", "groups", "capacity", "head_dim",
+                                              "dtype", "reserved")] + [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("stream_stride", "group_stride", "slot_stride")] + [
+        ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
+_L = ctypes.c_int64
 _SIGS = {
     "fd_status_str": (ctypes.c_char_p, [_I]),
     "fd_weights_blob_elems": (ctypes.c_size_t, [ctypes.POINTER(fd_config)]),
@@ -111,6 +129,18 @@ _SIGS = {
     "fd_op_linear_e4m3": (_I, [_I, _I, _I, _I, _P, _P, _P, _P, _P, _F, _I, _P, _P]),
     "fd_op_unshuffle": (_I, [_P, _I, _I, _I, _I, _P, _P]),
     "fd_op_pixel_head": (_I, [_P, _I, _I, _I, _I, _I, _I, _P, _P]),
+    "fd_rotary_create": (_I, [ctypes.POINTER(fd_rotary_config), ctypes.POINTER(_P)]),
+    "fd_rotary_destroy": (_I, [_P]),
+    "fd_op_rotary": (_I, [_P, _I, _I, _I, _P, _I, _P, _L, _L, _P, _L, _L, _I, _P, _L, _L, _P, _L,
+                          _L, _P]),
+    "fd_cache_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(fd_cache), _I, _I,
+                                                             _I]),
+    "fd_op_cache_attention": (_I, [ctypes.POINTER(fd_cache), _I, _I, _I, _P, _L, _L, _L, _P, _F,
+                                   _F, _P, _L, _L, _L, _P, _P, _P, _P]),
+    "fd_op_cache_insert": (_I, [ctypes.POINTER(fd_cache), _I, _P, _P, _L, _L, _L, _P, _I, _I, _P,
+                                _P, _P, _P]),
+    "fd_op_cache_compact": (_I, [ctypes.POINTER(fd_cache), _I, ctypes.POINTER(fd_cache), _P, _I,
+                                 _I, _P, _P]),
 }
 
 
@@ -619,3 +649,200 @@ def op_l1_pixel_bwd(F, target, frames, grid_h, grid_w, channels, rs, dF, loss,
     _check(lib().fd_op_l1_pixel_bwd(_ptr(F), _ptr(target), frames, grid_h, grid_w, channels, rs,
                                     _ptr(dF), _ptr(loss), _ptr(work), _stream_ptr(stream)),
            "fd_op_l1_pixel_bwd")
+
+
+# ------------------------------------------- rotary positions and the cache of bounded size
+ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "blend": 3}
+
+
+def _dtype_code(t) -> int:
+    import torch
+    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16,
+            torch.float16: DTYPE_F16}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"dtype {t.dtype}: float32, bfloat16 or float16 is required")
+    return code
+
+
+def _check_tensor(t, what: str, shape, dtype, device, contiguous: bool = True) -> None:
+    """The library receives raw pointers: refuse a tensor that a call would misread or overrun."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what}: a CUDA tensor is required")
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {t.dtype}, the call takes {dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the other arguments are on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, the call takes {tuple(shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous tensor is required")
+    if not contiguous and t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+
+
+class Rotary:
+    """Frequencies of a rotary embedding (fd_rotary_create): the leading rot_dim elements of a
+    head (all by default) in pairs of the given layout, split over the position axes by axis_dims."""
+
+    def __init__(self, head_dim, rot_dim=None, layout="interleaved", axis_dims=None,
+                 base=10000.0, scaling="none", factor=1.0, trained_len=1, fast_turns=32.0,
+                 slow_turns=1.0, amplitude=1.0):
+        rot_dim = int(head_dim if rot_dim is None else rot_dim)
+        dims = [rot_dim] if axis_dims is None else [int(d) for d in axis_dims]
+        if not 1 <= len(dims) <= 3:
+            raise ValueError("1 to 3 position axes")
+        c = fd_rotary_config(int(head_dim), rot_dim, ROTARY_LAYOUTS[layout], len(dims),
+                             (ctypes.c_int32 * 3)(*dims), ROTARY_SCALINGS[scaling], float(base),
+                             float(factor), int(trained_len), float(fast_turns),
+                             float(slow_turns), float(amplitude))
+        self.head_dim, self.axes = int(head_dim), len(dims)
+        out = _P()
+        _check(lib().fd_rotary_create(ctypes.byref(c), ctypes.byref(out)), "fd_rotary_create")
+        self.handle = out
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            _check(lib().fd_rotary_destroy(self.handle), "fd_rotary_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def op_rotary(plan: Rotary, positions, q, q_out, k=None, k_out=None, backward=False,
+              stream=None) -> None:
+    """Turns q [T][heads][head_dim] (and k) by positions int32 [T][axes] ([T] for one axis) into
+    q_out (k_out), which may be q (k) itself; with backward=True the gradient (fd_op_rotary)."""
+    import torch
+    T, D = q.shape[0], plan.head_dim
+    dev = q.device
+    pos_shape = (T, plan.axes) if positions.dim() == 2 or plan.axes > 1 else (T,)
+    _check_tensor(positions, "positions", pos_shape, torch.int32, dev)
+    views = []
+    for x, y, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            views += [0, 0, 0, 0, 0, 0, 0]
+            continue
+        if x.dim() != 3:
+            raise ValueError(f"{what}: [tokens][heads][head_dim] is required")
+        shape = (T, x.shape[1], D)
+        _check_tensor(x, what, shape, q.dtype, dev, contiguous=False)
+        _check_tensor(y, what + "_out", shape, q.dtype, dev, contiguous=False)
+        views += [x.shape[1], x.data_ptr(), x.stride(0), x.stride(1), y.data_ptr(), y.stride(0),
+                  y.stride(1)]
+    _check(lib().fd_op_rotary(plan.handle, 1 if backward else 0, _dtype_code(q), T,
+                              positions.data_ptr(), *views, _stream_ptr(stream)), "fd_op_rotary")
+
+
+class Cache:
+    """A cache of bounded size (fd_cache) over the caller's tensors: k, v bf16 or fp16
+    [streams][groups][capacity][head_dim] (any strides that fd_cache allows, the same for both),
+    pos int32 and weight fp32 [streams][groups][capacity]; empty slots have pos < 0."""
+
+    def __init__(self, k, v, pos, weight):
+        import torch
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k: [streams][groups][capacity][head_dim] is required")
+        if k.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"k: {k.dtype}, a cache holds bfloat16 or float16")
+        S, G, C, D = k.shape
+        _check_tensor(k, "k", k.shape, k.dtype, None, contiguous=False)
+        _check_tensor(v, "v", k.shape, k.dtype, k.device, contiguous=False)
+        if v.stride() != k.stride():
+            raise ValueError("v: the strides of k are required")
+        _check_tensor(pos, "pos", (S, G, C), torch.int32, k.device)
+        _check_tensor(weight, "weight", (S, G, C), torch.float32, k.device)
+        self.k, self.v, self.pos, self.weight = k, v, pos, weight
+        self.streams, self.groups, self.capacity, self.head_dim = S, G, C, D
+        self.device, self.dtype = k.device, k.dtype
+        self.view = fd_cache(S, G, C, D, _dtype_code(k), 0, k.data_ptr(), v.data_ptr(),
+                             k.stride(0), k.stride(1), k.stride(2), pos.data_ptr(),
+                             weight.data_ptr())
+        self.ref = ctypes.byref(self.view)
+
+
+def cache_attention_workspace_bytes(cache: Cache, heads, n_q, used=None) -> int:
+    return lib().fd_cache_attention_workspace_bytes(
+        cache.ref, cache.capacity if used is None else int(used), heads, n_q)
+
+
+def op_cache_attention(cache: Cache, q, q_pos, out, weight_out=None, used=None, scale=None,
+                       decay=1.0, workspace=None, err=None, stream=None) -> None:
+    """Attention of q [streams][n_q][heads][head_dim] at positions q_pos int32 [streams][n_q] over
+    the cache's first `used` slots (all by default) into out; weight_out fp32
+    [streams][groups][capacity] (may be cache.weight) receives decay times the slots' weights plus
+    what this call gives them. scale: 1 / sqrt(head_dim) by default (fd_op_cache_attention)."""
+    import torch
+    S, D = cache.streams, cache.head_dim
+    if q.dim() != 4:
+        raise ValueError("q: [streams][n_q][heads][head_dim] is required")
+    n, H = q.shape[1], q.shape[2]
+    dev = cache.device
+    _check_tensor(q, "q", (S, n, H, D), cache.dtype, dev, contiguous=False)
+    _check_tensor(out, "out", (S, n, H, D), cache.dtype, dev, contiguous=False)
+    _check_tensor(q_pos, "q_pos", (S, n), torch.int32, dev)
+    used = cache.capacity if used is None else int(used)
+    if weight_out is not None:
+        _check_tensor(weight_out, "weight_out", (S, cache.groups, cache.capacity), torch.float32,
+                      dev)
+    need = lib().fd_cache_attention_workspace_bytes(cache.ref, used, H, n)
+    if need:
+        if workspace is None or not workspace.is_cuda or not workspace.is_contiguous() or \
+                workspace.device != dev:
+            raise ValueError(f"workspace: {need} bytes of contiguous memory on {dev} are required")
+        if workspace.numel() * workspace.element_size() < need:
+            raise ValueError(f"workspace: {need} bytes are required")
+    _check(lib().fd_op_cache_attention(
+        cache.ref, used, H, n, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2),
+        q_pos.data_ptr(), D ** -0.5 if scale is None else scale, decay, out.data_ptr(),
+        out.stride(0), out.stride(1), out.stride(2), _ptr(weight_out), _ptr(workspace), _ptr(err),
+        _stream_ptr(stream)), "fd_op_cache_attention")
+
+
+def op_cache_insert(cache: Cache, k_new, v_new, new_pos, slots, pos_out=None, weight_out=None,
+                    sinks=0, recent=0, stream=None) -> None:
+    """New tokens k_new, v_new [streams][n][groups][head_dim] at new_pos int32 [streams][n] take
+    the n slots of each (stream, group) that rank first by (class, weight, slot), written to
+    slots int32 [streams][groups][n]; positions and weights go to pos_out and weight_out (the
+    cache's own by default) (fd_op_cache_insert)."""
+    import torch
+    S, G, C, D = cache.streams, cache.groups, cache.capacity, cache.head_dim
+    if k_new.dim() != 4:
+        raise ValueError("k_new: [streams][n][groups][head_dim] is required")
+    n = k_new.shape[1]
+    dev = cache.device
+    _check_tensor(k_new, "k_new", (S, n, G, D), cache.dtype, dev, contiguous=False)
+    _check_tensor(v_new, "v_new", (S, n, G, D), cache.dtype, dev, contiguous=False)
+    if v_new.stride() != k_new.stride():
+        raise ValueError("v_new: the strides of k_new are required")
+    _check_tensor(new_pos, "new_pos", (S, n), torch.int32, dev)
+    _check_tensor(slots, "slots", (S, G, n), torch.int32, dev)
+    pos_out = cache.pos if pos_out is None else pos_out
+    weight_out = cache.weight if weight_out is None else weight_out
+    _check_tensor(pos_out, "pos_out", (S, G, C), torch.int32, dev)
+    _check_tensor(weight_out, "weight_out", (S, G, C), torch.float32, dev)
+    _check(lib().fd_op_cache_insert(
+        cache.ref, n, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1),
+        k_new.stride(2), new_pos.data_ptr(), sinks, recent, pos_out.data_ptr(),
+        weight_out.data_ptr(), slots.data_ptr(), _stream_ptr(stream)), "fd_op_cache_insert")
+
+
+def op_cache_compact(src: Cache, dst: Cache, now, src_slots, used=None, sinks=0, recent=0,
+                     stream=None) -> None:
+    """The dst.capacity entries of src's first `used` slots (all by default) that rank last by
+    (class, weight, slot), recency counted from now int32 [streams], into dst in slot order;
+    src_slots int32 [streams][groups][dst.capacity]: where each came from (fd_op_cache_compact)."""
+    import torch
+    dev = src.device
+    if dst.device != dev:
+        raise ValueError(f"dst: on {dst.device}, src is on {dev}")
+    _check_tensor(now, "now", (src.streams,), torch.int32, dev)
+    _check_tensor(src_slots, "src_slots", (src.streams, src.groups, dst.capacity), torch.int32, dev)
+    _check(lib().fd_op_cache_compact(
+        src.ref, src.capacity if used is None else int(used), dst.ref, now.data_ptr(), sinks,
+        recent, src_slots.data_ptr(), _stream_ptr(stream)), "fd_op_cache_compact")

@@ -1,6 +1,6 @@
 """Build the CUDA library libflashdec.so in-tree (sm_103a only).
 
-Nine translation units compiled in parallel with nvcc, then linked into
+Ten translation units compiled in parallel with nvcc, then linked into
 ``paper_2607_14898_gb300/_build/libflashdec.so``. Rebuilds only when a source or header is
 newer than the library.
 """
@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libflashdec.so")
 SOURCES = ["flashdec.cu", "fd_gemm.cu", "fd_gemm_qkv.cu", "fd_attn.cu", "fd_small.cu",
-           "fd_train.cu", "fd_rotary.cu", "fd_cache_evict.cu", "fd_cache_attn.cu"]
+           "fd_train.cu", "fd_rotary.cu", "fd_cache_evict.cu", "fd_cache_attn.cu",
+           "fd_cache_chunk.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -9,59 +9,13 @@
 #include <algorithm>
 #include <cmath>
 
-#include "fd_internal.h"
-#include "fd_ptx.cuh"
-#include "flashdec_ops.h"
+#include "fd_cache_attn.cuh"
 
 namespace fd {
 
 bool valid_cache(const fd_cache* c);  // fd_cache_evict.cu
 
 namespace {
-
-constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kSms = 152;  // of the GPU that the library is built for
-
-// one launch's shapes, pointers and workspace
-struct CacheAttn {
-  int groups, heads, per;     // per: heads of a group
-  int used, n_q, rows;        // rows = n_q * per
-  int capacity;
-  const void *k, *v;
-  int64_t stream_stride, group_stride, slot_stride;
-  const int32_t* pos;
-  const float* weight;
-  float* weight_out;
-  const void* q;
-  int64_t q_stream, q_token, q_head;
-  const int32_t* q_pos;
-  void* out;
-  int64_t out_stream, out_token, out_head;
-  float scale_log2, decay;
-  // few rows: logits [lists][rows][pitch] (log2 domain, -inf where not visible), and per
-  // (list, row, split) the maximum and sum, and the unnormalised output
-  int splits, chunk;          // slots of a split
-  int64_t logit_pitch;
-  float* logits;
-  float2* part_ml;            // [lists][splits][rows]
-  float* part_o;              // [lists][splits][rows][D]
-};
-
-template <bool F16>
-struct Elem;
-template <>
-struct Elem<false> {
-  using type = __nv_bfloat16;
-  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
-};
-template <>
-struct Elem<true> {
-  using type = __half;
-  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-};
 
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
@@ -464,7 +418,7 @@ cudaError_t launch_few(const CacheAttn& p, int lists, cudaStream_t s) {
 
 bool valid_shape(const fd_cache* c, int used, int heads, int n_q) {
   if (!valid_cache(c) || used < 0 || used > c->capacity || n_q < 0 || n_q > (1 << 20)) return false;
-  if (heads < c->groups || heads % c->groups || heads / c->groups > 1024) return false;
+  if (heads < c->groups || heads % c->groups || heads / c->groups > 128) return false;
   const int64_t lists = static_cast<int64_t>(c->streams) * c->groups;
   return lists <= 65535 && static_cast<int64_t>(n_q) * (heads / c->groups) <= 16ll * 65535;
 }
@@ -505,7 +459,9 @@ extern "C" {
 size_t fd_cache_attention_workspace_bytes(const fd_cache* cache, int used, int heads, int n_q) {
   if (!fd::valid_shape(cache, used, heads, n_q)) return 0;
   if (cache->streams == 0 || used == 0 || n_q == 0) return 0;
-  return fd::layout_of(cache, used, heads, n_q).total;
+  const int per = heads / cache->groups;
+  return fd::chunk_form(n_q * per, used) ? fd::chunk_plan(cache, used, per, n_q).total
+                                         : fd::layout_of(cache, used, heads, n_q).total;
 }
 
 fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int n_q,
@@ -555,9 +511,29 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
   p.out_head = out_head_stride;
   p.scale_log2 = scale * fd::kLog2e;
   p.decay = decay;
+  p.lists = cache->streams * cache->groups;
+  p.err = err_dev;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (used > 0 && fd::chunk_form(p.rows, used)) {
+    const fd::ChunkPlan y = fd::chunk_plan(cache, used, p.per, n_q);
+    p.tile_tokens = y.tile_tokens;
+    p.tile_rows = y.tile_rows;
+    p.row_tiles = y.row_tiles;
+    p.key_tiles = y.key_tiles;
+    p.parts = y.parts;
+    p.row_splits = y.row_splits;
+    p.part_ml = reinterpret_cast<float2*>(ws + y.ml);
+    p.part_o = reinterpret_cast<float*>(ws + y.o);
+    p.lse = reinterpret_cast<float*>(ws + y.lse);
+    p.part_w = reinterpret_cast<float*>(ws + y.w);
+    p.flip = scale < 0.f ? -1.f : (scale == 0.f ? 0.f : 1.f);
+    p.scale_log2 = scale == 0.f ? 1.f : fabsf(p.scale_log2);
+    return fd::launch_chunk(p, cache, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? FD_OK
+               : FD_ERR_CUDA;
+  }
   if (used > 0 && n_q > 0) {
     const fd::Layout y = fd::layout_of(cache, used, heads, n_q);
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
     p.splits = y.splits;
     p.chunk = y.chunk;
     p.logit_pitch = y.logit_pitch;

@@ -289,9 +289,9 @@ bool attention_q_maps(CUtensorMap* q, CUtensorMap* q8, const __nv_bfloat16* base
 fd_status check_device();
 int num_sms();
 // 4D map over 16-bit elements (is_f16: fp16, else bf16): dims innermost first, strides in bytes
-// of dims 1..3, 128-byte swizzled boxes of 64 x rows x 1 x 1; reads past the dims give zeros
+// of dims 1..3, 128-byte swizzled boxes of 64 x box1 x box2 x 1; reads past the dims give zeros
 bool tmap_16bit_4d(CUtensorMap* m, bool is_f16, const void* base, const uint64_t dims[4],
-                   const uint64_t strides[3], uint32_t rows);
+                   const uint64_t strides[3], uint32_t box1, uint32_t box2);
 
 // GEMM tile widths compiled in
 inline bool gemm_bn_supported(int bn) {

@@ -962,8 +962,8 @@ namespace fd {
 fd_status check_device() { return ::check_device(); }
 int num_sms() { return ::num_sms(); }
 bool tmap_16bit_4d(CUtensorMap* m, bool is_f16, const void* base, const uint64_t dims[4],
-                   const uint64_t strides[3], uint32_t rows) {
-  const uint32_t box[4] = {64, rows, 1, 1};
+                   const uint64_t strides[3], uint32_t box1, uint32_t box2) {
+  const uint32_t box[4] = {64, box1, box2, 1};
   return tmap_nd(m, is_f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
                  base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }

@@ -275,11 +275,12 @@ __global__ void __launch_bounds__(few::kWarps * 32)
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * kRows + r].x);
+    const float off = top == -INFINITY ? 0.f : top;
     float sum = 0.f, acc = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const float2 x = ml[w * kRows + r];
-      const float f = x.x == -INFINITY ? 0.f : ex2_approx(x.x - top);
+      const float f = ex2_approx(x.x - off);
       sum = fmaf(f, x.y, sum);
       acc = fmaf(f, po[(w * kRows + r) * D + d], acc);
     }
@@ -308,14 +309,15 @@ __global__ void __launch_bounds__(kJoinThreads)
     for (int s = lane; s < p.splits; s += 32) top = fmaxf(top, ml[static_cast<int64_t>(s) * p.rows + r].x);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    if (top == -INFINITY) top = 0.f;
     float sum = 0.f;
     for (int s = lane; s < p.splits; s += 32) {
       const float2 x = ml[static_cast<int64_t>(s) * p.rows + r];
-      if (x.x != -INFINITY) sum = fmaf(ex2_approx(x.x - top), x.y, sum);
+      sum = fmaf(ex2_approx(x.x - top), x.y, sum);
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    return top == -INFINITY ? INFINITY : top + log2f(sum);
+    return sum == 0.f ? INFINITY : top + log2f(sum);
   };
   if (static_cast<int>(blockIdx.x) < out_blocks) {
     const int r = blockIdx.x * (kJoinThreads / 32) + warp;
@@ -326,9 +328,7 @@ __global__ void __launch_bounds__(kJoinThreads)
       float acc[D / 32] = {};
       for (int s = 0; s < p.splits; ++s) {
         const int64_t at = (static_cast<int64_t>(lst) * p.splits + s) * p.rows + r;
-        const float top = p.part_ml[at].x;
-        if (top == -INFINITY) continue;
-        const float f = ex2_approx(top - lse);
+        const float f = ex2_approx(p.part_ml[at].x - lse);
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
           const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + 64 * j + 2 * lane);
@@ -520,6 +520,7 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
     p.tile_rows = y.tile_rows;
     p.row_tiles = y.row_tiles;
     p.key_tiles = y.key_tiles;
+    p.attend_blocks = y.attend_blocks;
     p.parts = y.parts;
     p.row_splits = y.row_splits;
     p.part_ml = reinterpret_cast<float2*>(ws + y.ml);

@@ -33,11 +33,12 @@ struct CacheAttn {
   int splits, chunk;          // slots of a split
   int64_t logit_pitch;
   float* logits;
-  float2* part_ml;            // [lists][splits][rows]; many rows: [ctas][2][2][128]
-  float* part_o;              // [lists][splits][rows][D]; many rows: [ctas][2][2][D / 4][128] float4
+  float2* part_ml;            // [lists][splits][rows]; many rows: [ctas][2][128]
+  float* part_o;              // [lists][splits][rows][D]; many rows: [ctas][2][D / 4][128] float4
   // many rows: tiles of whole tokens, tile_rows = tile_tokens * per <= 128 rows each
   int tile_tokens, tile_rows, row_tiles;
   int key_tiles;              // of 128 slots
+  int attend_blocks;          // of 256 slots
   int parts;                  // CTAs of the attention
   int row_splits;             // of the weights
   float* lse;                 // [lists][row_tiles * tile_rows], log2; +inf: sees nothing
@@ -65,7 +66,7 @@ struct Elem<true> {
 // whether a call runs on the many-rows form: a rule on its sizes, and its plan and workspace
 bool chunk_form(int rows, int used);
 struct ChunkPlan {
-  int tile_tokens, tile_rows, row_tiles, key_tiles, parts, row_splits;
+  int tile_tokens, tile_rows, row_tiles, key_tiles, attend_blocks, parts, row_splits;
   size_t ml, o, lse, w, total;  // byte offsets
 };
 ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q);

@@ -55,11 +55,18 @@ __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint3
       "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t accumulate) {
+// 64 steps of K: A from TMEM (16 steps are 8 columns), B MN-major (16 steps are 2048 bytes)
+__device__ __forceinline__ void mma4_ts_mn(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                           uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "{\n\t.reg .pred p, q;\n\t.reg .b32 a1, a2, a3;\n\t.reg .b64 b1, b2, b3;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 q, %4, %4;\n\t"
+      "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"
+      "add.s64 b1, %2, 128;\n\tadd.s64 b2, %2, 256;\n\tadd.s64 b3, %2, 384;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, q;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, q;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, q;\n\t}" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
@@ -74,45 +81,66 @@ __device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t lead
          (static_cast<uint64_t>(2) << 61);
 }
 
+// The waits of this file: one try inline, the bounded loop in a function of its own. Inlined at
+// every wait it made the attend kernel 132 KB of code, and a third of its issue slots went to
+// instruction fetches.
+__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, int* err, int code) {
+  return mbar_wait_for(bar, parity, err, code, kWaitLimitNs);
+}
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code) {
+  return mbar_try_wait(bar, parity) || wait_more(bar, parity, err, code);
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, int code) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, wait_more(bar, parity, err, code));
+}
+
 constexpr int kTile = 128;      // rows of a tile, slots of a block
 constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swizzled sub-tile
 
 // ------------------------------------------------------------------------------ attend
 //
-// Persistent CTAs (one per SM), each with an equal run of the (tile pair, block) units, pair
-// after pair: a segment is a pair's consecutive blocks. A pair that is cut between CTAs leaves
+// Persistent CTAs (one per SM), each with an equal run of the (tile, block of 256 slots) units,
+// tile after tile: a segment is a tile's consecutive blocks. A tile that is cut between CTAs leaves
 // partial results, which join_parts adds up in the order of the blocks.
 //
-// Per CTA two tiles, so that one tile's exponentials run while the tensor cores work for the other:
-//   warps 0-3 / 4-7   softmax of tile 0 / 1, a row (TMEM lane) per thread
-//   warp 8            TMA: Q of the segment, K and V blocks into a ring
-//   warps 9 / 10      issue tile 0's / tile 1's products
-//   warp 11           positions of each block, and zeros for the values of empty slots (their
-//                     probability is 0, but 0 times NaN is NaN)
-// TMEM (512 columns): S 2 x 128, O 2 x D, P (two 16-bit values a column) 2 x 64: for D = 64 beside S,
-// for D = 128 over the first half of its own S, which then takes the next scores only
-// after P V.
+// The softmax is the longest chain of a block (scores out of TMEM, maximum, exponentials, P into
+// TMEM), so sixteen warps share it, four on every SM sub-partition: each of four groups of 128
+// threads has a quarter of a block's slots, a row (TMEM lane) per thread. The row's running
+// maximum is handed from quarter to quarter, which sets the groups a step apart: the exponentials
+// of one run beside the loads, masks and maxima of the others.
+//   warps 0-15    softmax: warps 4 q .. 4 q + 3 quarter q
+//   warp 16       TMA: Q of the segment, K and V blocks into a ring
+//   warps 17, 18  products: a thread issues one tcgen05.mma per 104 to 158 cycles whatever its
+//                 size, so two of them share the work. D = 64: those of the block's first and
+//                 second half, each half with a running maximum and an O of its own; D = 128: S of
+//                 both halves, and P V into the one O that TMEM has room for.
+//   warp 19       positions of each block, and zeros for the values of empty slots (their
+//                 probability is 0, but 0 times NaN is NaN)
+// TMEM (512 columns): S 2 x 128, P 2 x 64 (two 16-bit values a column), O 2 x 64 or 128. S takes the
+// next scores once the softmax has it in registers.
 template <int D>
 struct AttendCfg {
-  static constexpr bool kAlias = D == 128;
-  static constexpr int kTileBytes = kTile * D * 2;
-  static constexpr int kSlots = D == 128 ? 4 : 8;  // ring of K, V, K, V, ..
-  static constexpr int kPosStages = 4;
-  static constexpr int kOffRing = 2 * kTileBytes;  // after the two Q tiles
-  static constexpr int kOffPos = kOffRing + kSlots * kTileBytes;
-  static constexpr int kOffTop = kOffPos + kPosStages * kTile * 4;  // largest position per stage
-  static constexpr int kOffBar = kOffTop + 64;
+  static constexpr int kKeys = 256;
+  static constexpr int kQBytes = kTile * D * 2;
+  static constexpr int kSub2 = kKeys * 128;        // 64 elements of a block's rows
+  static constexpr int kBlockBytes = kKeys * D * 2;
+  static constexpr int kSlots = D == 128 ? 3 : 6;  // ring of K, V, K, V, ..
+  static constexpr bool kTwoO = D == 64;
+  static constexpr int kOffRing = kQBytes;
+  static constexpr int kOffPos = kOffRing + kSlots * kBlockBytes;
+  static constexpr int kOffMax = kOffPos + 2 * kKeys * 4;  // two blocks' positions before it
+  static constexpr int kOffBar = kOffMax + (kTwoO ? 4 : 1) * kTile * 4;  // D = 64: [half][m, l]
   static constexpr int kSmem = kOffBar + 512;
-  static constexpr int kThreads = 384;
-  static constexpr uint32_t kColS = 0, kColP = kAlias ? 0 : 256, kColO = kAlias ? 256 : 384;
-  static constexpr uint32_t kStepP = kAlias ? 128 : 64;
-  // barriers
+  static constexpr int kThreads = 640;
+  static constexpr uint32_t kColS = 0, kColP = 256, kColO = 384;
+  // barriers: kSFull, kSRead of the halves, kPFull, kPv, kMax of the quarters, kPos* of the stages
   static constexpr int kQFull = 0, kQFree = 1, kKvFull = 2, kKvFree = kKvFull + kSlots,
-                       kVReady = kKvFree + kSlots, kSFull = kVReady + kSlots,
-                       kSRead = kSFull + 2, kPFull = kSRead + 2, kPv = kPFull + 2,
-                       kORead = kPv + 2, kPosFull = kORead + 2, kPosFree = kPosFull + kPosStages,
-                       kDone = kPosFree + kPosStages, kBars = kDone + 2;
-  static_assert(kBars * 8 + 8 <= 512, "barriers");
+                       kVReady = kKvFree + kSlots, kSFull = kVReady + 4, kSRead = kSFull + 2,
+                       kPFull = kSRead + 2, kPv = kPFull + 4, kMax = kPv + 4, kORead = kMax + 4,
+                       kPosFull = kORead + 1, kPosFree = kPosFull + 2, kDone = kPosFree + 2,
+                       kBars = kDone + 2;
+  static_assert(kBars * 8 + 24 <= 512, "barriers, TMEM slot, largest positions");
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -128,14 +156,14 @@ struct Units {
 
 // a walk over a CTA's units
 struct Walk {
-  int64_t pair;
+  int tile;              // over all lists
   int block, left, seg;  // left: units after this one
   bool first, last;      // of its segment
   __device__ Walk(const Units& w, int cta, int blocks) {
     const int64_t u = w.start(cta);
     left = static_cast<int>(w.start(cta + 1) - u) - 1;
-    pair = u / blocks;
-    block = static_cast<int>(u - pair * blocks);
+    tile = static_cast<int>(u / blocks);
+    block = static_cast<int>(u - static_cast<int64_t>(tile) * blocks);
     seg = 0;
     first = true;
     last = block == blocks - 1 || left == 0;
@@ -146,7 +174,7 @@ struct Walk {
     first = ++block == blocks;
     if (first) {
       block = 0;
-      ++pair;
+      ++tile;
       ++seg;
     }
     last = block == blocks - 1 || left <= 0;
@@ -168,37 +196,39 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
-  int32_t* pos_ring = reinterpret_cast<int32_t*>(smem + C::kOffPos);
-  uint32_t* pos_top = reinterpret_cast<uint32_t*>(smem + C::kOffTop);
-  const int blocks = p.key_tiles;
-  const int pairs_list = (p.row_tiles + 1) / 2;
-  const Units units{static_cast<int64_t>(p.lists) * pairs_list * blocks, p.parts};
+  volatile uint32_t* pos_top = tmem_slot + 1;  // largest position, [stage][half]
+  int32_t* pos_ring = reinterpret_cast<int32_t*>(smem + C::kOffPos);  // [stage][256]
+  // the rows' running maximum (D = 64: of each half); at a segment's end their sums
+  volatile float* row_max = reinterpret_cast<volatile float*>(smem + C::kOffMax);
+  const int blocks = p.attend_blocks;
+  const Units units{static_cast<int64_t>(p.lists) * p.row_tiles * blocks, p.parts};
 
   // rows past tile_rows are never loaded
-  for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += C::kThreads)
+  for (int i = threadIdx.x; i < C::kQBytes / 16; i += C::kThreads)
     reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   fence_proxy_async_smem();
   if (threadIdx.x == 0) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
     mbar_init(bar(C::kQFull), 1);
-    mbar_init(bar(C::kQFree), 2);
+    mbar_init(bar(C::kQFree), C::kTwoO ? 2 : 1);
     for (int i = 0; i < C::kSlots; ++i) {
       mbar_init(bar(C::kKvFull + i), 1);
-      mbar_init(bar(C::kKvFree + i), 2);
-      mbar_init(bar(C::kVReady + i), 1);
+      mbar_init(bar(C::kKvFree + i), C::kTwoO ? 2 : 1);  // warps that read it
     }
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(bar(C::kSFull + x), 1);
-      mbar_init(bar(C::kSRead + x), 128);
-      mbar_init(bar(C::kPFull + x), 128);
-      mbar_init(bar(C::kPv + x), 1);
-      mbar_init(bar(C::kORead + x), 128);
-      mbar_init(bar(C::kDone + x), 1);
+    for (int i = 0; i < 4; ++i) mbar_init(bar(C::kVReady + i), 1);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(bar(C::kSFull + h), 1);
+      mbar_init(bar(C::kSRead + h), 256);
+      mbar_init(bar(C::kPosFull + h), 1);
+      mbar_init(bar(C::kPosFree + h), 16);
+      mbar_init(bar(C::kDone + h), 1);
     }
-    for (int i = 0; i < C::kPosStages; ++i) {
-      mbar_init(bar(C::kPosFull + i), 1);
-      mbar_init(bar(C::kPosFree + i), 8);
+    for (int q = 0; q < 4; ++q) {
+      mbar_init(bar(C::kPFull + q), 128);
+      mbar_init(bar(C::kPv + q), 1);
+      mbar_init(bar(C::kMax + q), 128);
     }
+    mbar_init(bar(C::kORead), 512);
     fence_barrier_init();
   }
   grid_dep_wait();
@@ -211,204 +241,206 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  // tile x of a pair holds rows (an odd number of tiles leaves the last pair's second one empty)
-  auto has_tile = [&](int64_t pair, int x) {
-    return static_cast<int>(pair % pairs_list) * 2 + x < p.row_tiles;
-  };
   if (!aligned) {
     // nothing is loaded or computed; the status word says why
-  } else if (warp == 8) {
+  } else if (warp == 16) {
     if (lane == 0) {
       prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
       prefetch_tmap(&tmV);
-      int J = 0, segs = 0;
+      int i = 0, segs = 0;  // i: loads of K and V so far
       bool ok = true;
-      for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks), ++J) {
-        const int lst = static_cast<int>(w.pair / pairs_list);
+      for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks)) {
+        const int lst = w.tile / p.row_tiles;
         const int stream = lst / p.groups, group = lst - stream * p.groups;
         if (w.first) {
-          if (w.seg > 0 && !mbar_wait(bar(C::kQFree), (w.seg - 1) & 1, p.err, ERR_WAIT_MMA)) break;
-          const int n = 1 + has_tile(w.pair, 1);
-          mbar_expect_tx(bar(C::kQFull), n * p.tile_rows * D * 2);
-          for (int x = 0; x < n; ++x)
-            for (int d = 0; d < D / 64; ++d)
-              tma_load_4d(base + x * C::kTileBytes + d * kSub, &tmQ, bar(C::kQFull), 64 * d,
-                          group * p.per,
-                          (static_cast<int>(w.pair % pairs_list) * 2 + x) * p.tile_tokens, stream);
+          ok = w.seg == 0 || wait(bar(C::kQFree), (w.seg - 1) & 1, p.err, ERR_WAIT_MMA);
+          if (!ok) break;
+          mbar_expect_tx(bar(C::kQFull), p.tile_rows * D * 2);
+          for (int d = 0; d < D / 64; ++d)
+            tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.per,
+                        (w.tile - lst * p.row_tiles) * p.tile_tokens, stream);
           segs = w.seg + 1;
         }
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const int i = 2 * J + kv, s = i % C::kSlots;
-          if (!mbar_wait(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA)) {
-            ok = false;
-            break;
-          }
-          mbar_expect_tx(bar(C::kKvFull + s), C::kTileBytes);
+        for (int kv = 0; kv < 2; ++kv, ++i) {
+          const int s = i % C::kSlots;
+          ok = wait(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA);
+          if (!ok) break;
+          mbar_expect_tx(bar(C::kKvFull + s), C::kBlockBytes);
           for (int d = 0; d < D / 64; ++d)
-            tma_load_4d(base + C::kOffRing + s * C::kTileBytes + d * kSub, kv ? &tmV : &tmK,
-                        bar(C::kKvFull + s), 64 * d, w.block * kTile, group, stream);
-        }
-        if (!ok) {  // a K without its V: wait for what was started
-          const int i = 2 * J, s = i % C::kSlots;
-          mbar_wait(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+            tma_load_4d(base + C::kOffRing + s * C::kBlockBytes + d * C::kSub2, kv ? &tmV : &tmK,
+                        bar(C::kKvFull + s), 64 * d, w.block * C::kKeys, group, stream);
         }
       }
       // nothing may be in flight when the CTA exits
-      if (segs > 0) mbar_wait(bar(C::kQFull), (segs - 1) & 1, p.err, ERR_WAIT_TMA);
-      for (int i = 2 * J - 1; i >= 0 && i >= 2 * J - C::kSlots; --i)
-        mbar_wait(bar(C::kKvFull + i % C::kSlots), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+      if (segs > 0) wait(bar(C::kQFull), (segs - 1) & 1, p.err, ERR_WAIT_TMA);
+      for (int j = i - 1; j >= 0 && j >= i - C::kSlots; --j)
+        wait(bar(C::kKvFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
     }
-  } else if (warp == 11) {
+  } else if (warp == 19) {
     // ---- positions and empty slots' values
     int J = 0;
     bool ok = true;
     for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks), ++J) {
-      const int lst = static_cast<int>(w.pair / pairs_list);
+      const int lst = w.tile / p.row_tiles;
       const int32_t* pos = p.pos + static_cast<int64_t>(lst) * p.capacity;
-      int32_t v[4];
+      const int slot0 = w.block * C::kKeys + lane;
+      int32_t v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int slot = w.block * kTile + 32 * i + lane;
-        v[i] = slot < p.used ? __ldg(pos + slot) : -1;
-      }
-      const int st = J % C::kPosStages;
-      ok = mbar_wait_warp(bar(C::kPosFree + st), ((J / C::kPosStages) & 1) ^ 1, p.err, ERR_WAIT_EPI);
+      for (int i = 0; i < 8; ++i) v[i] = slot0 + 32 * i < p.used ? __ldg(pos + slot0 + 32 * i) : -1;
+      const int st = J & 1;
+      ok = wait_warp(bar(C::kPosFree + st), ((J >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI);
       if (!ok) break;
-      uint32_t top = 0;
+      uint32_t top[2] = {0, 0};
       bool hole = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        pos_ring[st * kTile + 32 * i + lane] = v[i];
-        top = max(top, static_cast<uint32_t>(v[i]));
-        hole |= v[i] < 0 && w.block * kTile + 32 * i + lane < p.used;
+      for (int i = 0; i < 8; ++i) {
+        pos_ring[st * C::kKeys + 32 * i + lane] = v[i];
+        top[i / 4] = max(top[i / 4], static_cast<uint32_t>(v[i]));
+        hole |= v[i] < 0 && slot0 + 32 * i < p.used;
       }
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (lane == 0) pos_top[st] = top;
+      top[0] = __reduce_max_sync(0xffffffffu, top[0]);
+      top[1] = __reduce_max_sync(0xffffffffu, top[1]);
+      if (lane < 2) pos_top[2 * st + lane] = lane ? top[1] : top[0];
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kPosFull + st));
       const int i = 2 * J + 1, s = i % C::kSlots;
-      ok = mbar_wait_warp(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+      ok = wait_warp(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
       if (!ok) break;
       if (__any_sync(0xffffffffu, hole)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < 8; ++r) {
           if (v[r] >= 0) continue;
-          uint4* row = reinterpret_cast<uint4*>(smem + C::kOffRing + s * C::kTileBytes +
+          uint4* row = reinterpret_cast<uint4*>(smem + C::kOffRing + s * C::kBlockBytes +
                                                 (32 * r + lane) * 128);
 #pragma unroll
           for (int d = 0; d < D / 64; ++d)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) row[d * (kSub / 16) + c] = make_uint4(0, 0, 0, 0);
+            for (int c = 0; c < 8; ++c) row[d * (C::kSub2 / 16) + c] = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kVReady + s));
+      if (lane == 0) mbar_arrive(bar(C::kVReady + (J & 3)));
     }
-  } else if (warp >= 9) {
-    // ---- products of tile x
-    const int x = warp - 9;
+  } else if (warp >= 17) {
     if (lane == 0) {
       constexpr uint32_t is = Mma<F16, D>::idesc(kTile, false), io = Mma<F16, D>::idesc(D, true);
-      const uint32_t s_col = tmem + C::kColS + 128u * x;
-      const uint32_t p_col = tmem + C::kColP + C::kStepP * x;
-      const uint32_t o_col = tmem + C::kColO + static_cast<uint32_t>(D) * x;
-      const uint64_t q0 = sdesc_k_sw128(base + x * C::kTileBytes);
-      // scores of the walk's block (number J); leaves the K slot
-      auto scores = [&](const Walk& w, int J) -> bool {
-        if (w.first && !mbar_wait(bar(C::kQFull), w.seg & 1, p.err, ERR_WAIT_TMA)) return false;
-        const int i = 2 * J, s = i % C::kSlots;
-        if (!mbar_wait(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
-        if (!has_tile(w.pair, x)) {
-          mbar_arrive(bar(C::kKvFree + s));
-          if (w.last) mbar_arrive(bar(C::kQFree));
-          return true;
-        }
+      const uint32_t s_col = tmem + C::kColS, p_col = tmem + C::kColP, o_col = tmem + C::kColO;
+      const uint64_t q0 = sdesc_k_sw128(base);
+      // Q and K of the walk's block, number J, are there
+      auto loaded = [&](int J, const Walk& w) -> bool {
+        const int i = 2 * J;
+        return (!w.first || wait(bar(C::kQFull), w.seg & 1, p.err, ERR_WAIT_TMA)) &&
+               wait(bar(C::kKvFull + i % C::kSlots), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+      };
+      auto scores = [&](int J, int h) {
         tc_fence_after();
-        const uint64_t k0 = sdesc_k_sw128(base + C::kOffRing + s * C::kTileBytes);
+        const uint64_t k0 = sdesc_k_sw128(base + C::kOffRing + (2 * J) % C::kSlots * C::kBlockBytes +
+                                          h * kSub);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          const uint64_t at = static_cast<uint64_t>((d / 4) * (kSub >> 4) + (d % 4) * 2);
-          mma_ss(s_col, q0 + at, k0 + at, is, d > 0);
-        }
-        mma_commit(bar(C::kSFull + x));
-        mma_commit(bar(C::kKvFree + s));
+        for (int d = 0; d < D / 64; ++d)
+          mma4_bf16_ss(s_col + 128u * h, q0 + static_cast<uint64_t>(d * (kSub >> 4)),
+                       k0 + static_cast<uint64_t>(d * (C::kSub2 >> 4)), is, d > 0);
+        mma_commit(bar(C::kSFull + h));
+      };
+      // this warp's last scores of the block are issued: K, and Q after a segment, may go
+      auto leave = [&](int J, const Walk& w) {
+        mma_commit(bar(C::kKvFree + (2 * J) % C::kSlots));
         if (w.last) mma_commit(bar(C::kQFree));
+      };
+      // V of block J has arrived; O of the previous segment has been read
+      auto ready = [&](int J, const Walk& w) -> bool {
+        return wait(bar(C::kVReady + (J & 3)), (J >> 2) & 1, p.err, ERR_WAIT_TMA) &&
+               (!w.first || w.seg == 0 ||
+                wait(bar(C::kORead), (w.seg - 1) & 1, p.err, ERR_WAIT_EPI));
+      };
+      // P V of quarter q of block J into O (the half's own for D = 64)
+      auto values = [&](int J, int q, bool first) -> bool {
+        if (!wait(bar(C::kPFull + q), J & 1, p.err, ERR_WAIT_EPI)) return false;
+        tc_fence_after();
+        const uint64_t v0 = sdesc_mn_sw128(
+            base + C::kOffRing + (2 * J + 1) % C::kSlots * C::kBlockBytes + q * (kSub / 2), C::kSub2);
+        const bool fresh = first && (C::kTwoO ? q % 2 == 0 : q == 0);
+        mma4_ts_mn(o_col + (C::kTwoO ? 64u * (q / 2) : 0u), p_col + 32u * q, v0, io, !fresh);
+        mma_commit(bar(C::kPv + q));
         return true;
       };
+      const int h = warp - 17;
       Walk w(units, blockIdx.x, blocks);
-      // T: blocks of this tile so far, the phase of its own barriers (a pair without this tile
-      // has none), E: segments that it has had
-      int J = 0, T = 0, E = 0;
-      bool ok = !w.valid() || scores(w, 0);
-      for (; w.valid() && ok; ++J) {
-        const Walk here = w;
-        const bool mine = has_tile(here.pair, x);
-        w.next(blocks);
-        if (!C::kAlias && w.valid()) {
-          // S is free once the softmax has read it
-          if (mine) ok = mbar_wait(bar(C::kSRead + x), T & 1, p.err, ERR_WAIT_EPI);
-          ok = ok && scores(w, J + 1);
-          if (!ok) break;
+      if (C::kTwoO) {
+        bool ok = w.valid() && loaded(0, w);
+        if (ok) {
+          scores(0, h);
+          leave(0, w);
         }
-        const int i = 2 * J + 1, s = i % C::kSlots;
-        ok = mbar_wait(bar(C::kVReady + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
-        if (!ok) break;
-        if (mine) {
-          ok = mbar_wait(bar(C::kPFull + x), T & 1, p.err, ERR_WAIT_EPI);
-          // the first product of a segment overwrites O
-          if (ok && here.first && E > 0)
-            ok = mbar_wait(bar(C::kORead + x), (E - 1) & 1, p.err, ERR_WAIT_EPI);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t v0 = sdesc_mn_sw128(base + C::kOffRing + s * C::kTileBytes, kSub);
-#pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)
-            mma_ts(o_col, p_col + 8u * k, v0 + static_cast<uint64_t>(k * (2048 >> 4)), io,
-                   !here.first || k > 0);
-          mma_commit(bar(C::kPv + x));
-          mma_commit(bar(C::kKvFree + s));
-          if (here.last) ++E;
-          if (C::kAlias) ok = mbar_wait(bar(C::kPv + x), T & 1, p.err, ERR_WAIT_MMA);
-          ++T;
-        } else {
-          mbar_arrive(bar(C::kKvFree + s));
+        for (int J = 0; w.valid() && ok; ++J) {
+          const Walk here = w;
+          w.next(blocks);
+          if (w.valid()) {
+            ok = wait(bar(C::kSRead + h), J & 1, p.err, ERR_WAIT_EPI) && loaded(J + 1, w);
+            if (!ok) break;
+            scores(J + 1, h);
+            leave(J + 1, w);
+          }
+          ok = ready(J, here) && values(J, 2 * h, here.first) && values(J, 2 * h + 1, false);
+          if (ok) mma_commit(bar(C::kKvFree + (2 * J + 1) % C::kSlots));
         }
-        if (C::kAlias && ok && w.valid()) ok = scores(w, J + 1);
+      } else if (h == 0) {
+        bool ok = true;
+        for (int J = 0; w.valid() && ok; w.next(blocks), ++J) {
+          ok = loaded(J, w);
+          for (int x = 0; x < 2 && ok; ++x) {
+            ok = J == 0 || wait(bar(C::kSRead + x), (J - 1) & 1, p.err, ERR_WAIT_EPI);
+            if (ok) scores(J, x);
+          }
+          if (ok) leave(J, w);
+        }
+      } else {
+        bool ok = true;
+        for (int J = 0; w.valid() && ok; w.next(blocks), ++J) {
+          ok = ready(J, w) && values(J, 0, w.first) && values(J, 1, false) &&
+               values(J, 2, false) && values(J, 3, false);
+          if (ok) mma_commit(bar(C::kKvFree + (2 * J + 1) % C::kSlots));
+        }
       }
-      mma_commit(bar(C::kDone + x));
-      mbar_wait(bar(C::kDone + x), 0, p.err, ERR_WAIT_MMA);
+      mma_commit(bar(C::kDone + h));
+      wait(bar(C::kDone + h), 0, p.err, ERR_WAIT_MMA);
     }
   } else {
-    // ---- softmax of tile x
-    const int x = warp >> 2, quarter = warp & 3;
-    const int row = quarter * 32 + lane;
-    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t s_col = tmem + lane_off + C::kColS + 128u * x;
-    const uint32_t p_col = tmem + lane_off + C::kColP + C::kStepP * x;
-    const uint32_t o_col = tmem + lane_off + C::kColO + static_cast<uint32_t>(D) * x;
+    // ---- softmax of quarter q of the blocks
+    const int q = warp >> 2, h = q >> 1, lanes = warp & 3;
+    const int row = lanes * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(lanes * 32) << 16;
+    const uint32_t s_col = tmem + lane_off + C::kColS + 64u * q;
+    const uint32_t p_col = tmem + lane_off + C::kColP + 32u * q;
+    const uint32_t o_col = tmem + lane_off + C::kColO;
+    // the quarters that share an O and a running maximum: the one before this, in the same block
+    // or (the first one) the last in the block before
+    constexpr int kShare = C::kTwoO ? 2 : 4;
+    const bool lead = q % kShare == 0;
+    const int prev = lead ? q + kShare - 1 : q - 1;
+    volatile float* const my_max = row_max + (C::kTwoO ? 2 * h * kTile : 0) + row;
     const float c = p.scale_log2;
+    const uint64_t c2 = pack_f32x2(c, c);
     float m = -INFINITY, l = 0.f;
+    // the segment's tile and this thread's row in it
+    int lst = 0, stream = 0, group = 0, token = 0;
+    bool valid = false;
     uint32_t limit = 0;  // a slot is visible if its position, unsigned, is below this
-    int J = 0, T = 0;
-    bool ok = true;
-    for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks), ++J) {
-      const int st = J % C::kPosStages;
-      ok = mbar_wait_warp(bar(C::kPosFull + st), (J / C::kPosStages) & 1, p.err, ERR_WAIT_EPI);
-      if (!ok) break;
-      if (!has_tile(w.pair, x)) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::kPosFree + st));
-        continue;
-      }
-      const int lst = static_cast<int>(w.pair / pairs_list);
-      const int stream = lst / p.groups, group = lst - stream * p.groups;
-      const int tile = static_cast<int>(w.pair % pairs_list) * 2 + x;
-      const int token = tile * p.tile_tokens + row / p.per;
-      const bool valid = row < p.tile_rows && token < p.n_q;
+    // the warp's different limits: lane i has the i-th of n_limits, which is this row's if my_limit = i
+    uint32_t limits = 0;
+    int n_limits = 0, my_limit = 0;
+    // A wait that gives up has set the status word, and every wait after it returns at once: the
+    // warps walk on to the end, since they have to meet at the segments' barriers.
+    int J = 0;
+    for (Walk w(units, blockIdx.x, blocks); w.valid(); w.next(blocks), ++J) {
       if (w.first) {
+        lst = w.tile / p.row_tiles;
+        stream = lst / p.groups;
+        group = lst - stream * p.groups;
+        token = (w.tile - lst * p.row_tiles) * p.tile_tokens + row / p.per;
+        valid = row < p.tile_rows && token < p.n_q;
         m = -INFINITY;
         l = 0.f;
         // (rows that are none see every entry: their results go nowhere, and they do not send the
@@ -416,117 +448,192 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         const int qp = valid ? __ldg(p.q_pos + static_cast<int64_t>(stream) * p.n_q + token)
                              : 0x7fffffff;
         limit = qp < 0 ? 0u : static_cast<uint32_t>(qp) + 1u;
+        n_limits = 0;
+        for (uint32_t todo = 0xffffffffu; todo != 0; ++n_limits) {
+          const uint32_t x = __shfl_sync(0xffffffffu, limit, __ffs(todo) - 1);
+          todo &= ~__ballot_sync(0xffffffffu, limit == x);
+          if (limit == x) my_limit = n_limits;
+          if (lane == n_limits) limits = x;
+        }
       }
-      ok = mbar_wait_warp(bar(C::kSFull + x), T & 1, p.err, ERR_WAIT_MMA);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t sr[4][32];
+      const int st = J & 1;
+      wait_warp(bar(C::kPosFull + st), (J >> 1) & 1, p.err, ERR_WAIT_EPI);
+      const bool all_seen = __all_sync(0xffffffffu, pos_top[2 * st + h] < limit);
+      uint32_t seen[2] = {0, 0};
+      if (!all_seen) {
+        uint32_t at[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(s_col + 32 * i, sr[i]);
-      tmem_ld_wait();
-      if (!C::kAlias) {
-        tc_fence_before();
-        mbar_arrive(bar(C::kSRead + x));
+        for (int i = 0; i < 2; ++i)
+          at[i] = static_cast<uint32_t>(pos_ring[st * C::kKeys + 64 * q + 32 * i + lane]);
+#pragma unroll 4
+        for (int k = 0; k < n_limits; ++k) {
+          const uint32_t x = __shfl_sync(0xffffffffu, limits, k);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t b = __ballot_sync(0xffffffffu, at[i] < x);
+            if (my_limit == k) seen[i] = b;
+          }
+        }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::kPosFree + st));
+      wait_warp(bar(C::kSFull + h), J & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      uint32_t sr[2][32];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) tmem_ld_32x32b_x32(s_col + 32 * i, sr[i]);
+      tmem_ld_wait();
+      tc_fence_before();
+      mbar_arrive(bar(C::kSRead + h));
       if (p.flip != 1.f) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 32; ++e)
             sr[i][e] = __float_as_uint(__uint_as_float(sr[i][e]) * p.flip);
       }
-      if (!__all_sync(0xffffffffu, pos_top[st] < limit)) {
-        const int4* ps = reinterpret_cast<const int4*>(pos_ring + st * kTile);
+      if (!all_seen) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const int4 v = ps[8 * i + e / 4];
-            if (static_cast<uint32_t>(v.x) >= limit) sr[i][e] = 0xff800000u;
-            if (static_cast<uint32_t>(v.y) >= limit) sr[i][e + 1] = 0xff800000u;
-            if (static_cast<uint32_t>(v.z) >= limit) sr[i][e + 2] = 0xff800000u;
-            if (static_cast<uint32_t>(v.w) >= limit) sr[i][e + 3] = 0xff800000u;
-          }
+          for (int e = 0; e < 32; ++e)
+            if (!(seen[i] & (1u << e))) sr[i][e] = 0xff800000u;
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kPosFree + st));
       float mx[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        mx[i] = __uint_as_float(sr[i][0]);
+        const uint32_t* x = sr[i / 2] + 16 * (i % 2);
+        mx[i] = __uint_as_float(x[0]);
 #pragma unroll
-        for (int e = 1; e < 31; e += 2)
-          mx[i] = fmax3(mx[i], __uint_as_float(sr[i][e]), __uint_as_float(sr[i][e + 1]));
-        mx[i] = fmaxf(mx[i], __uint_as_float(sr[i][31]));
+        for (int e = 1; e < 15; e += 2)
+          mx[i] = fmax3(mx[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+        mx[i] = fmaxf(mx[i], __uint_as_float(x[15]));
       }
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-      const bool grow = top > m + kSlack;
-      const float now = grow ? top : m;
-      const float off = now == -INFINITY ? 0.f : now;
-      // O and P: the previous block's product is done
-      if (!w.first) {
-        ok = mbar_wait_warp(bar(C::kPv + x), (T - 1) & 1, p.err, ERR_WAIT_MMA);
-        if (!ok) break;
-        tc_fence_after();
-        if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? ex2_approx(m - off) : 1.f;
-          l *= f;
-#pragma unroll 1
-          for (int d = 0; d < D; d += 16) {
-            uint32_t o[16];
-            tmem_ld_32x32b_x16(o_col + d, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st_32x32b_x16(o_col + d, o);
-          }
-        }
+      // the maximum that O stands for now
+      const bool fresh = w.first && lead;  // O holds nothing yet
+      float before = -INFINITY;
+      if (!lead || J > 0) {
+        wait_warp(bar(C::kMax + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_EPI);
+        if (!fresh) before = *my_max;
       }
+      const bool grow = top > before + kSlack;
+      const float now = grow ? top : before;
+      const float off = now == -INFINITY ? 0.f : now;
+      *my_max = now;
+      mbar_arrive(bar(C::kMax + q));
+      const float f = grow ? ex2_approx(before - off) : 1.f;  // of O
+      l *= m == now ? 1.f : ex2_approx(m - off);
       m = now;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint64_t off2 = pack_f32x2(-off, -off);
+      uint64_t sum2[2] = {0, 0};
+      uint32_t pk[2][16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t pk[16];
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-          const float a = ex2_approx(fmaf(__uint_as_float(sr[i][e]), c, -off));
-          const float b = ex2_approx(fmaf(__uint_as_float(sr[i][e + 1]), c, -off));
-          sum[e / 2 % 2] += a;
-          sum[2 + e / 2 % 2] += b;
-          pk[e / 2] = pack16<F16>(a, b);
+          uint64_t x;
+          asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(sr[i][e]), "r"(sr[i][e + 1]));
+          asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(x), "l"(c2), "l"(off2));
+          float a, b;
+          asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+          a = ex2_approx(a);
+          b = ex2_approx(b);
+          asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[e / 2 % 2]) : "l"(pack_f32x2(a, b)));
+          pk[i][e / 2] = pack16<F16>(a, b);
         }
-        tmem_st_32x32b_x16(p_col + 16 * i, pk);
+      // the previous block's product has read this quarter's P
+      if (!w.first) wait_warp(bar(C::kPv + q), (J - 1) & 1, p.err, ERR_WAIT_MMA);
+      if (!fresh && __any_sync(0xffffffffu, grow)) {
+        // O as the products of all quarters before left it
+        wait_warp(bar(C::kPv + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          uint32_t o[16];
+          const uint32_t at = o_col + (C::kTwoO ? 64u * h : 0u) + d;
+          tmem_ld_32x32b_x16(at, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+          tmem_st_32x32b_x16(at, o);
+        }
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tc_fence_after();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(p_col + 16 * i, pk[i]);
+      {
+        float a0, b0, a1, b1;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(b0) : "l"(sum2[0]));
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(a1), "=f"(b1) : "l"(sum2[1]));
+        l += (a0 + b0) + (a1 + b1);
+      }
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(bar(C::kPFull + x));
-      ++T;
+      mbar_arrive(bar(C::kPFull + q));
       if (!w.last) continue;
 
-      // ---- the segment's result
-      ok = mbar_wait_warp(bar(C::kPv + x), (T - 1) & 1, p.err, ERR_WAIT_MMA);
-      if (!ok) break;
-      tc_fence_after();
-      const int lo = units.owner(w.pair * blocks), hi = units.owner(w.pair * blocks + blocks - 1);
-      const bool whole = lo == hi;
-      // a cut pair's part: the CTA's first segment (slot 0) unless the pair began in this CTA
-      const int slot = units.start(blockIdx.x) > w.pair * blocks ? 0 : 1;
-      const int64_t part = (static_cast<int64_t>(blockIdx.x) * 2 + slot) * 2 + x;
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      using T16 = uint16_t;
-      T16* out = static_cast<T16*>(p.out) + stream * p.out_stream +
-                 static_cast<int64_t>(token) * p.out_token +
-                 static_cast<int64_t>(group * p.per + row % p.per) * p.out_head;
+      // ---- the segment's result: this thread's quarter of the row's elements
 #pragma unroll
-      for (int d = 0; d < D; d += 32) {
-        uint32_t o[32];
+      for (int i = 0; i < 4; ++i) wait_warp(bar(C::kPv + i), J & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      // the sums on the last maximum, added up in the order of the quarters (named barriers of
+      // the row's four warps between the steps)
+      wait_warp(bar(C::kMax + q / kShare * kShare + kShare - 1), J & 1, p.err, ERR_WAIT_EPI);
+      const float last = *my_max;
+      l *= m == last ? 1.f : ex2_approx(m - last);
+      m = last;
+      named_barrier(1 + lanes, 128);
+      float all, f0 = 1.f, f1 = 1.f;
+      if (C::kTwoO) {  // [half][m, l]: the halves on the larger maximum
+        volatile float* const my_sum = my_max + kTile;
+        if (lead) *my_sum = l;
+        named_barrier(1 + lanes, 128);
+        if (!lead) *my_sum = *my_sum + l;
+        named_barrier(1 + lanes, 128);
+        const float m0 = row_max[row], l0 = row_max[kTile + row];
+        const float m1 = row_max[2 * kTile + row], l1 = row_max[3 * kTile + row];
+        m = fmaxf(m0, m1);
+        const float at = m == -INFINITY ? 0.f : m;
+        f0 = ex2_approx(m0 - at);
+        f1 = ex2_approx(m1 - at);
+        all = fmaf(f0, l0, f1 * l1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (q == i) *my_max = i == 0 ? l : *my_max + l;
+          named_barrier(1 + lanes, 128);
+        }
+        all = *my_max;
+      }
+      named_barrier(1 + lanes, 128);  // read by all before the next segment writes
+      const int64_t unit = static_cast<int64_t>(w.tile) * blocks;
+      const bool whole = units.owner(unit) == units.owner(unit + blocks - 1);
+      // a cut tile's part: the CTA's first segment (slot 0) unless the tile began in this CTA
+      const int64_t part = static_cast<int64_t>(blockIdx.x) * 2 + (units.start(blockIdx.x) > unit ? 0 : 1);
+      const float inv = all == 0.f ? 0.f : 1.f / all;
+      uint16_t* out = static_cast<uint16_t*>(p.out) + stream * p.out_stream +
+                      static_cast<int64_t>(token) * p.out_token +
+                      static_cast<int64_t>(group * p.per + row % p.per) * p.out_head;
+#pragma unroll
+      for (int d0 = 0; d0 < D / 4; d0 += 16) {
+        const int d = q * (D / 4) + d0;
+        uint32_t o[16];
         __syncwarp();
-        tmem_ld_32x32b_x32(o_col + d, o);
-        tmem_ld_wait();
+        tmem_ld_32x32b_x16(o_col + d, o);
+        if (C::kTwoO) {
+          uint32_t o2[16];
+          tmem_ld_32x32b_x16(o_col + 64 + d, o2);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            o[e] = __float_as_uint(fmaf(f0, __uint_as_float(o[e]), f1 * __uint_as_float(o2[e])));
+        } else {
+          tmem_ld_wait();
+        }
         if (whole && valid) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
+          for (int e = 0; e < 16; e += 8) {
             uint4 v;
             v.x = pack16<F16>(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
             v.y = pack16<F16>(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
@@ -537,17 +644,18 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         } else if (!whole) {
           uint4* po = reinterpret_cast<uint4*>(p.part_o) + part * (D / 4) * kTile + row;
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
+          for (int e = 0; e < 16; e += 4)
             po[(d + e) / 4 * kTile] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
       }
       tc_fence_before();
-      mbar_arrive(bar(C::kORead + x));
-      if (!whole) {
-        p.part_ml[part * kTile + row] = make_float2(m, l);
-      } else if (row < p.tile_rows) {
-        p.lse[(static_cast<int64_t>(lst) * p.row_tiles + tile) * p.tile_rows + row] =
-            valid && l > 0.f ? m + log2f(l) : INFINITY;
+      mbar_arrive(bar(C::kORead));
+      if (q == 0) {
+        if (!whole)
+          p.part_ml[part * kTile + row] = make_float2(m, all);
+        else if (row < p.tile_rows)
+          p.lse[static_cast<int64_t>(w.tile) * p.tile_rows + row] =
+              !valid || all == 0.f ? INFINITY : m + log2f(all);
       }
     }
   }
@@ -560,21 +668,20 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
   }
 }
 
-// The cut pairs' parts added up: blockIdx.x = (pair, tile of it), blockIdx.y = 4 elements of the
-// head, a thread per row.
+// The cut tiles' parts added up: blockIdx.x = tile, blockIdx.y = 4 elements of the head, a thread per
+// row.
 template <bool F16, int D>
 __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant__ CacheAttn p) {
   grid_dep_wait();
-  const int blocks = p.key_tiles, pairs_list = (p.row_tiles + 1) / 2;
-  const Units units{static_cast<int64_t>(p.lists) * pairs_list * blocks, p.parts};
-  const int64_t pair = blockIdx.x >> 1;
-  const int x = blockIdx.x & 1, k = blockIdx.y, row = threadIdx.x;
-  const int lst = static_cast<int>(pair / pairs_list);
-  const int tile = static_cast<int>(pair % pairs_list) * 2 + x;
-  const int lo = units.owner(pair * blocks), hi = units.owner(pair * blocks + blocks - 1);
-  if (lo != hi && tile < p.row_tiles) {
+  const int blocks = p.attend_blocks;
+  const Units units{static_cast<int64_t>(p.lists) * p.row_tiles * blocks, p.parts};
+  const int k = blockIdx.y, row = threadIdx.x;
+  const int lst = blockIdx.x / p.row_tiles, tile = blockIdx.x - lst * p.row_tiles;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * blocks;
+  const int lo = units.owner(unit), hi = units.owner(unit + blocks - 1);
+  if (lo != hi) {
     auto part_of = [&](int c) {
-      return (static_cast<int64_t>(c) * 2 + (units.start(c) > pair * blocks ? 0 : 1)) * 2 + x;
+      return static_cast<int64_t>(c) * 2 + (units.start(c) > unit ? 0 : 1);
     };
     float top = -INFINITY;
     for (int c = lo; c <= hi; ++c) top = fmaxf(top, __ldcg(p.part_ml + part_of(c) * kTile + row).x);
@@ -597,7 +704,7 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
     const int stream = lst / p.groups, group = lst - stream * p.groups;
     const int token = tile * p.tile_tokens + row / p.per;
     const bool valid = row < p.tile_rows && token < p.n_q;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     if (valid) {
       uint16_t* out = static_cast<uint16_t*>(p.out) + stream * p.out_stream +
                       static_cast<int64_t>(token) * p.out_token +
@@ -606,8 +713,8 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
                                                   pack16<F16>(acc.z * inv, acc.w * inv));
     }
     if (k == 0 && row < p.tile_rows)
-      p.lse[(static_cast<int64_t>(lst) * p.row_tiles + tile) * p.tile_rows + row] =
-          valid && l > 0.f ? top + log2f(l) : INFINITY;
+      p.lse[static_cast<int64_t>(blockIdx.x) * p.tile_rows + row] =
+          !valid || l == 0.f ? INFINITY : off + log2f(l);
   }
   grid_dep_launch();
 }
@@ -706,25 +813,25 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
       int i = 0;
       for (; i < tiles; ++i) {
         const int s = i % C::kStages;
-        if (!mbar_wait(bar(C::kQFree + s), ((i / C::kStages) & 1) ^ 1, p.err, ERR_WAIT_MMA)) break;
+        if (!wait(bar(C::kQFree + s), ((i / C::kStages) & 1) ^ 1, p.err, ERR_WAIT_MMA)) break;
         mbar_expect_tx(bar(C::kQFull + s), p.tile_rows * D * 2);
         for (int d = 0; d < D / 64; ++d)
           tma_load_4d(base + C::kOffQ + s * C::kTileBytes + d * kSub, &tmQ, bar(C::kQFull + s),
                       64 * d, group * p.per, (first + i) * p.tile_tokens, stream);
       }
-      mbar_wait(bar(C::kKFull), 0, p.err, ERR_WAIT_TMA);
+      wait(bar(C::kKFull), 0, p.err, ERR_WAIT_TMA);
       for (int j = i - 1; j >= 0 && j >= i - C::kStages; --j)
-        mbar_wait(bar(C::kQFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA);
+        wait(bar(C::kQFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA);
     }
   } else if (warp == 9) {
     if (lane == 0) {
       constexpr uint32_t idesc = Mma<F16, D>::idesc(kTile, false);
       const uint64_t k0 = sdesc_k_sw128(base);
-      bool ok = mbar_wait(bar(C::kKFull), 0, p.err, ERR_WAIT_TMA);
+      bool ok = wait(bar(C::kKFull), 0, p.err, ERR_WAIT_TMA);
       for (int i = 0; i < tiles && ok; ++i) {
         const int s = i % C::kStages, x = i & 1;
-        ok = mbar_wait(bar(C::kTFree + x), ((i >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI) &&
-             mbar_wait(bar(C::kQFull + s), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
+        ok = wait(bar(C::kTFree + x), ((i >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI) &&
+             wait(bar(C::kQFull + s), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
         if (!ok) break;
         tc_fence_after();
         const uint64_t q0 = sdesc_k_sw128(base + C::kOffQ + s * C::kTileBytes);
@@ -737,7 +844,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
         mma_commit(bar(C::kQFree + s));
       }
       mma_commit(bar(C::kDone));
-      mbar_wait(bar(C::kDone), 0, p.err, ERR_WAIT_MMA);
+      wait(bar(C::kDone), 0, p.err, ERR_WAIT_MMA);
     }
   } else if (warp == 10) {
     bool ok = true;
@@ -757,7 +864,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
         if (in) low = min(low, lim[j]);
       }
       low = __reduce_min_sync(0xffffffffu, low);
-      ok = mbar_wait_warp(bar(C::kRowFree + st), ((i / C::kRowStages) & 1) ^ 1, p.err, ERR_WAIT_EPI);
+      ok = wait_warp(bar(C::kRowFree + st), ((i / C::kRowStages) & 1) ^ 1, p.err, ERR_WAIT_EPI);
       if (!ok) break;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -777,8 +884,8 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
     bool ok = true;
     for (int i = x; i < tiles && ok; i += 2) {
       const int st = i % C::kRowStages;
-      ok = mbar_wait_warp(bar(C::kRowFull + st), (i / C::kRowStages) & 1, p.err, ERR_WAIT_EPI) &&
-           mbar_wait_warp(bar(C::kTFull + x), (i >> 1) & 1, p.err, ERR_WAIT_MMA);
+      ok = wait_warp(bar(C::kRowFull + st), (i / C::kRowStages) & 1, p.err, ERR_WAIT_EPI) &&
+           wait_warp(bar(C::kTFull + x), (i >> 1) & 1, p.err, ERR_WAIT_MMA);
       if (!ok) break;
       tc_fence_after();
       // an empty slot's sum is not used, so it does not matter here
@@ -876,23 +983,24 @@ cudaError_t launch_t(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {
                                 W::kSmem);
   }();
   if (attr != cudaSuccess) return attr;
-  CUtensorMap tq, tk, tv;
+  CUtensorMap tq, tk, tv, tk1;
   if (!make_map(&tq, F16, p.q, D, p.heads, p.n_q, c->streams, p.q_head, p.q_token, p.q_stream,
                 p.per, p.tile_tokens) ||
       !make_map(&tk, F16, p.k, D, p.used, p.groups, c->streams, p.slot_stride, p.group_stride,
-                p.stream_stride, kTile, 1) ||
+                p.stream_stride, A::kKeys, 1) ||
       !make_map(&tv, F16, p.v, D, p.used, p.groups, c->streams, p.slot_stride, p.group_stride,
+                p.stream_stride, A::kKeys, 1) ||
+      !make_map(&tk1, F16, p.k, D, p.used, p.groups, c->streams, p.slot_stride, p.group_stride,
                 p.stream_stride, kTile, 1))
     return cudaErrorInvalidValue;
   cudaError_t e = launch_pdl(attend_kernel<F16, D>, dim3(p.parts), dim3(A::kThreads), A::kSmem, s,
                              tq, tk, tv, p);
-  const int pairs = p.lists * ((p.row_tiles + 1) / 2);
-  // the pairs fall on whole CTAs only if the units divide evenly
   if (e == cudaSuccess && p.parts > 1)
-    e = launch_pdl(join_parts_kernel<F16, D>, dim3(2 * pairs, D / 4), dim3(kTile), 0, s, p);
+    e = launch_pdl(join_parts_kernel<F16, D>, dim3(p.lists * p.row_tiles, D / 4), dim3(kTile), 0, s,
+                   p);
   if (e != cudaSuccess || p.weight_out == nullptr) return e;
   e = launch_pdl(weigh_kernel<F16, D>, dim3(p.key_tiles, p.row_splits, p.lists), dim3(W::kThreads),
-                 W::kSmem, s, tq, tk, p);
+                 W::kSmem, s, tq, tk1, p);
   if (e != cudaSuccess || p.row_splits == 1) return e;
   const int64_t n = static_cast<int64_t>(p.lists) * p.used;
   return launch_pdl(sum_weights_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0,
@@ -910,9 +1018,10 @@ ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q) {
   y.tile_rows = y.tile_tokens * per;
   y.row_tiles = (n_q + y.tile_tokens - 1) / y.tile_tokens;
   y.key_tiles = (used + kTile - 1) / kTile;
-  const int64_t units = lists * ((y.row_tiles + 1) / 2) * y.key_tiles;
-  // a CTA for every SM, of 4 blocks at least: its fixed cost is about that of 2 blocks
-  y.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kSms, units / 4)));
+  y.attend_blocks = (used + 255) / 256;
+  const int64_t units = lists * y.row_tiles * y.attend_blocks;
+  // a CTA for every SM, of 2 blocks at least: its fixed cost is about that of 2 blocks
+  y.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kSms, units / 2)));
   // row splits: the fewest waves of two CTAs an SM, counted in tiles one after the other
   const int64_t ctas = lists * y.key_tiles;
   int64_t best = INT64_MAX;
@@ -927,9 +1036,9 @@ ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t at = 0;
   y.ml = at;
-  at += up(static_cast<size_t>(y.parts) * 4 * kTile * 8);
+  at += up(static_cast<size_t>(y.parts) * 2 * kTile * 8);
   y.o = at;
-  at += up(static_cast<size_t>(y.parts) * 4 * kTile * c->head_dim * 4);
+  at += up(static_cast<size_t>(y.parts) * 2 * kTile * c->head_dim * 4);
   y.lse = at;
   at += up(static_cast<size_t>(lists) * y.row_tiles * y.tile_rows * 4);
   y.w = at;

@@ -277,7 +277,7 @@ fd_status fd_op_rotary(fd_rotary plan, int backward, int dtype, int tokens,
  * -1 before the first insert. Whatever an empty slot's key, value and weight hold (NaN too) has
  * no effect. Entries that are in use have finite keys and values. */
 typedef struct {
-  int32_t streams, groups, capacity;  /* >= 0, >= 1, >= 0                                   */
+  int32_t streams, groups, capacity;  /* >= 0, >= 1, 0..1,048,576                            */
   int32_t head_dim;                   /* 64 or 128                                          */
   int32_t dtype;                      /* FD_DTYPE_BF16 or FD_DTYPE_F16                      */
   int32_t reserved;                   /* 0                                                  */
@@ -298,7 +298,8 @@ typedef struct {
  * chunk lets each see the whole chunk). A query that sees no slot gives zeros and adds nothing.
  * q, out of the cache's type: element (stream, t, h, i) of q at q[stream q_stream_stride + t
  * q_token_stride + h q_head_stride + i], of out with the out strides (elements; 16-byte
- * aligned, strides multiples of 8). q_pos int32 [streams][n_q]. weight_out fp32
+ * aligned, strides multiples of 8). q_pos int32 [streams][n_q]. scale > 0, finite; decay finite;
+ * heads / groups <= 128. weight_out fp32
  * [streams][groups][capacity], entries past `used` are not written; it may be cache->weight;
  * NULL: the weights are not gathered. Softmax, sums and weights are in fp32, P is rounded to the
  * cache's type for its product with V. The order of every sum is fixed: equal calls give equal

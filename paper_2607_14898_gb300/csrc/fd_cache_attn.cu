@@ -470,7 +470,8 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
                                 float decay, void* out, int64_t out_stream_stride,
                                 int64_t out_token_stride, int64_t out_head_stride,
                                 float* weight_out, void* workspace, int* err_dev, void* stream) {
-  if (!fd::valid_shape(cache, used, heads, n_q) || !std::isfinite(scale) || !std::isfinite(decay))
+  if (!fd::valid_shape(cache, used, heads, n_q) || !std::isfinite(scale) || !(scale > 0.f) ||
+      !std::isfinite(decay))
     return FD_ERR_INVALID_ARG;
   if (cache->streams == 0 || (n_q == 0 && (used == 0 || weight_out == nullptr))) return FD_OK;
   if (weight_out != nullptr && !fd::ok_ptr(weight_out, 4)) return FD_ERR_INVALID_ARG;
@@ -527,8 +528,6 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
     p.part_o = reinterpret_cast<float*>(ws + y.o);
     p.lse = reinterpret_cast<float*>(ws + y.lse);
     p.part_w = reinterpret_cast<float*>(ws + y.w);
-    p.flip = scale < 0.f ? -1.f : (scale == 0.f ? 0.f : 1.f);
-    p.scale_log2 = scale == 0.f ? 1.f : fabsf(p.scale_log2);
     return fd::launch_chunk(p, cache, static_cast<cudaStream_t>(stream)) == cudaSuccess
                ? FD_OK
                : FD_ERR_CUDA;

@@ -43,7 +43,6 @@ struct CacheAttn {
   int row_splits;             // of the weights
   float* lse;                 // [lists][row_tiles * tile_rows], log2; +inf: sees nothing
   float* part_w;              // [row_splits][lists][used], where row_splits > 1
-  float flip;                 // -1: the scores change sign (negative scale), 0: scale 0, else 1
 };
 
 template <bool F16>

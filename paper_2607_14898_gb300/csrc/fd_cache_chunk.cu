@@ -81,18 +81,54 @@ __device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t lead
          (static_cast<uint64_t>(2) << 61);
 }
 
-// The waits of this file: one try inline, the bounded loop in a function of its own. Inlined at
-// every wait it made the attend kernel 132 KB of code, and a third of its issue slots went to
-// instruction fetches.
-__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, int* err, int code) {
-  return mbar_wait_for(bar, parity, err, code, kWaitLimitNs);
+// The waits of this file. A try suspends the thread for up to kSuspendNs, so that waiting warps
+// leave the issue slots to the others, and kTries of them bound a wait (to seconds; a wait that
+// succeeds takes microseconds). The loops are short on purpose: with the 64-fold unrolled loop of
+// mbar_wait at every wait the attend kernel was 132 KB of code, and a third of its issue slots went
+// to instruction fetches.
+constexpr uint32_t kSuspendNs = 20000;
+constexpr int kTries = 1 << 18;
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(kSuspendNs)
+      : "memory");
+  return ok != 0;
 }
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code) {
-  return mbar_try_wait(bar, parity) || wait_more(bar, parity, err, code);
+// Gives up after kTries, or at once when another wait of this launch (or an earlier one on the
+// same status word) has given up; not so a drain, which waits for the CTA's own copies and
+// products in flight.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code,
+                                     bool drain = false) {
+  bool ok = try_wait(bar, parity);
+#pragma unroll 1
+  for (int n = 0; !ok; ++n) {
+    if (n == kTries || (!drain && *reinterpret_cast<volatile int*>(err) != 0)) {
+      atomicOr(err, code);
+      break;
+    }
+    ok = try_wait(bar, parity);
+  }
+  return ok;
 }
+// The same for a whole warp that stays together (tcgen05 loads and stores, which follow such
+// waits, have to be executed by all its lanes at once): every decision is the warp's.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, int code) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return __all_sync(0xffffffffu, wait_more(bar, parity, err, code));
+  bool ok = __all_sync(0xffffffffu, try_wait(bar, parity));
+#pragma unroll 1
+  for (int n = 0; !ok; ++n) {
+    if (__any_sync(0xffffffffu, n == kTries || *reinterpret_cast<volatile int*>(err) != 0)) {
+      atomicOr(err, code);
+      break;
+    }
+    ok = __all_sync(0xffffffffu, try_wait(bar, parity));
+  }
+  __syncwarp();
+  return ok;
 }
 
 constexpr int kTile = 128;      // rows of a tile, slots of a block
@@ -127,6 +163,11 @@ struct AttendCfg {
   static constexpr int kBlockBytes = kKeys * D * 2;
   static constexpr int kSlots = D == 128 ? 3 : 6;  // ring of K, V, K, V, ..
   static constexpr bool kTwoO = D == 64;
+  // An odd ring's slots hold K and V in turn, and a slot's full barrier has waiters for every
+  // other phase only. A parity tells a phase from its neighbours and no further: such a waiter first
+  // waits until the slot's use before its own is over (the wait of the loader), or it would
+  // take the phase before that one for its own.
+  static constexpr bool kMixed = kSlots % 2 != 0;
   static constexpr int kOffRing = kQBytes;
   static constexpr int kOffPos = kOffRing + kSlots * kBlockBytes;
   static constexpr int kOffMax = kOffPos + 2 * kKeys * 4;  // two blocks' positions before it
@@ -273,9 +314,9 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         }
       }
       // nothing may be in flight when the CTA exits
-      if (segs > 0) wait(bar(C::kQFull), (segs - 1) & 1, p.err, ERR_WAIT_TMA);
+      if (segs > 0) wait(bar(C::kQFull), (segs - 1) & 1, p.err, ERR_WAIT_TMA, true);
       for (int j = i - 1; j >= 0 && j >= i - C::kSlots; --j)
-        wait(bar(C::kKvFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+        wait(bar(C::kKvFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
     }
   } else if (warp == 19) {
     // ---- positions and empty slots' values
@@ -305,7 +346,9 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kPosFull + st));
       const int i = 2 * J + 1, s = i % C::kSlots;
-      ok = wait_warp(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+      ok = (!C::kMixed || wait_warp(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err,
+                                    ERR_WAIT_MMA)) &&
+           wait_warp(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
       if (!ok) break;
       if (__any_sync(0xffffffffu, hole)) {
 #pragma unroll
@@ -330,9 +373,11 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       const uint64_t q0 = sdesc_k_sw128(base);
       // Q and K of the walk's block, number J, are there
       auto loaded = [&](int J, const Walk& w) -> bool {
-        const int i = 2 * J;
+        const int i = 2 * J, s = i % C::kSlots;
         return (!w.first || wait(bar(C::kQFull), w.seg & 1, p.err, ERR_WAIT_TMA)) &&
-               wait(bar(C::kKvFull + i % C::kSlots), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+               (!C::kMixed || wait(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err,
+                                   ERR_WAIT_MMA)) &&
+               wait(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
       };
       auto scores = [&](int J, int h) {
         tc_fence_after();
@@ -405,7 +450,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         }
       }
       mma_commit(bar(C::kDone + h));
-      wait(bar(C::kDone + h), 0, p.err, ERR_WAIT_MMA);
+      wait(bar(C::kDone + h), 0, p.err, ERR_WAIT_MMA, true);
     }
   } else {
     // ---- softmax of quarter q of the blocks
@@ -485,13 +530,6 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       tmem_ld_wait();
       tc_fence_before();
       mbar_arrive(bar(C::kSRead + h));
-      if (p.flip != 1.f) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            sr[i][e] = __float_as_uint(__uint_as_float(sr[i][e]) * p.flip);
-      }
       if (!all_seen) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -560,6 +598,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         }
       }
       tc_fence_after();
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(p_col + 16 * i, pk[i]);
       {
@@ -583,14 +622,19 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       const float last = *my_max;
       l *= m == last ? 1.f : ex2_approx(m - last);
       m = last;
-      named_barrier(1 + lanes, 128);
+      // (the warp together at each of them)
+      auto meet = [&]() {
+        __syncwarp();
+        named_barrier(1 + lanes, 128);
+      };
+      meet();
       float all, f0 = 1.f, f1 = 1.f;
       if (C::kTwoO) {  // [half][m, l]: the halves on the larger maximum
         volatile float* const my_sum = my_max + kTile;
         if (lead) *my_sum = l;
-        named_barrier(1 + lanes, 128);
+        meet();
         if (!lead) *my_sum = *my_sum + l;
-        named_barrier(1 + lanes, 128);
+        meet();
         const float m0 = row_max[row], l0 = row_max[kTile + row];
         const float m1 = row_max[2 * kTile + row], l1 = row_max[3 * kTile + row];
         m = fmaxf(m0, m1);
@@ -602,11 +646,11 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (q == i) *my_max = i == 0 ? l : *my_max + l;
-          named_barrier(1 + lanes, 128);
+          meet();
         }
         all = *my_max;
       }
-      named_barrier(1 + lanes, 128);  // read by all before the next segment writes
+      meet();  // read by all before the next segment writes
       const int64_t unit = static_cast<int64_t>(w.tile) * blocks;
       const bool whole = units.owner(unit) == units.owner(unit + blocks - 1);
       // a cut tile's part: the CTA's first segment (slot 0) unless the tile began in this CTA
@@ -819,9 +863,9 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
           tma_load_4d(base + C::kOffQ + s * C::kTileBytes + d * kSub, &tmQ, bar(C::kQFull + s),
                       64 * d, group * p.per, (first + i) * p.tile_tokens, stream);
       }
-      wait(bar(C::kKFull), 0, p.err, ERR_WAIT_TMA);
+      wait(bar(C::kKFull), 0, p.err, ERR_WAIT_TMA, true);
       for (int j = i - 1; j >= 0 && j >= i - C::kStages; --j)
-        wait(bar(C::kQFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA);
+        wait(bar(C::kQFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA, true);
     }
   } else if (warp == 9) {
     if (lane == 0) {
@@ -844,7 +888,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
         mma_commit(bar(C::kQFree + s));
       }
       mma_commit(bar(C::kDone));
-      wait(bar(C::kDone), 0, p.err, ERR_WAIT_MMA);
+      wait(bar(C::kDone), 0, p.err, ERR_WAIT_MMA, true);
     }
   } else if (warp == 10) {
     bool ok = true;
@@ -880,7 +924,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
     const uint32_t col = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * x;
     const uint32_t pos =
         key < p.used ? static_cast<uint32_t>(__ldg(p.pos + list_at + key)) : 0xffffffffu;
-    const float c = p.scale_log2 * p.flip;  // flip 0: every score is 0
+    const float c = p.scale_log2;
     bool ok = true;
     for (int i = x; i < tiles && ok; i += 2) {
       const int st = i % C::kRowStages;

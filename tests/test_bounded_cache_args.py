@@ -111,7 +111,8 @@ def test_attention_arguments():
                 dict(n_q=-1), dict(q=None), dict(q=P + 2), dict(qt=1023), dict(qh=4), dict(qs=2),
                 dict(q_pos=None), dict(out=None), dict(out=P + 4), dict(oh=60), dict(ot=2),
                 dict(os=2), dict(weight_out=P + 1), dict(work=None), dict(work=P + 4),
-                dict(err=None), dict(scale=float("nan")), dict(scale=float("inf")),
+                dict(err=None), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=0.0),
+                dict(scale=-1.0),
                 dict(decay=float("nan"))):
         assert attend(c, L, **bad) == INVALID, bad
     assert attend(cache(streams=0), L) == 0

@@ -9,11 +9,14 @@
 // integers: the choice does not depend on the order in which threads run.
 //
 // One cluster of 1 to 8 CTAs per list. Keys are read once into registers, each warp
-// holding consecutive slots; histograms are counted in shared memory and summed over the cluster
-// through distributed shared memory; one scan of counts over warps and CTAs gives every slot
-// that is taken (or kept) its place in slot order. Then the cluster writes the list's positions and
-// weights and moves the rows, 16 bytes a thread. For one new token the selection is a minimum
-// over (class, weight, slot) packed into 54 bits.
+// holding consecutive slots, and histograms are counted in shared memory. Up to kAloneSlots every
+// CTA of the cluster selects from the whole list by itself, and the cluster only shares the
+// writing: 50 KB more reads from L2 a CTA, but no exchange, whose steps (a cluster barrier and a
+// round trip through distributed shared memory, three times) took longer than all else. Longer
+// lists are cut between the CTAs and the histograms summed over the cluster. One scan of
+// counts over warps (and CTAs) gives every slot that is taken (or kept) its place in slot order.
+// Then the cluster writes the list's positions and weights and moves the rows, 16 bytes a thread.
+// For one new token the selection is a minimum over (class, weight, slot) packed into 54 bits.
 //
 // Bound by memory for long rows (the copied keys and values) and by the latency of the dependent steps for
 // short ones: the positions and weights of a list are 8 bytes a slot.
@@ -33,13 +36,14 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMaxSlots = 1 << 20;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxKeys = 32;  // keys a thread holds in registers
+constexpr int kAloneSlots = 8 * kThreads;
 // radix digits of the 34-bit key: bits 23.., 11..22, 0..10
 constexpr int kBins0 = 2048, kBins1 = 4096, kBins2 = 2048;
 constexpr int kBins = kBins0 + kBins1 + kBins2;
 
 struct EvictParams {
   int groups, slots, n;      // slots looked at, slots given up, per list
-  int iters;                 // slots a thread has: kThreads * iters * cluster size >= slots
+  int iters;                 // slots a thread has: kThreads * iters (* cluster size) >= slots
   int sinks, recent;
   const int32_t* newest;     // per stream, newest_stride apart: the position recency counts from
   int newest_stride;
@@ -110,7 +114,7 @@ struct Keys<0> {
 };
 
 struct Shared {
-  uint32_t hist[kBins];
+  alignas(16) uint32_t hist[kBins];
   uint32_t warp_a[kWarps], warp_b[kWarps];
   uint64_t warp_min[kWarps];
   uint64_t cta_min;
@@ -142,8 +146,9 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, 
 }
 
 // COMPACT: the slots that are not given up go to the destination; else the given-up slots are
-// taken by new tokens.
-template <int KPT, bool COMPACT>
+// taken by new tokens. ALONE: each CTA selects from the whole list, and writes for its share of
+// the warps.
+template <int KPT, bool COMPACT, bool ALONE>
 __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constant__ EvictParams p) {
   __shared__ Shared sm;
   cg::cluster_group cluster = cg::this_cluster();
@@ -153,7 +158,10 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
   const int stream = lst / p.groups, group = lst - stream * p.groups;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int iters = p.iters;
-  const int slot0 = (rank * kWarps + warp) * 32 * iters + lane;  // this thread's i-th: + 32 i
+  const int slot0 = ((ALONE ? 0 : rank * kWarps) + warp) * 32 * iters + lane;  // i-th: + 32 i
+  // the warps whose slots this CTA writes
+  const int warps = ALONE ? kWarps / ctas : kWarps, warp_lo = ALONE ? rank * warps : 0;
+  const bool writes = warp >= warp_lo && warp < warp_lo + warps;
   const int64_t at = static_cast<int64_t>(lst) * p.pitch;
 
   for (int i = tid; i < kBins; i += kThreads) sm.hist[i] = 0;
@@ -163,6 +171,11 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       p.recent;
   Keys<KPT> keys;
   keys.load(p, at, slot0, protect);
+  // positions and weights may be written in place: not before every CTA has read them
+  if (ALONE) {
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  }
   auto key_of = [&](int i) { return keys.get(p, at, slot0, protect, i); };
 #define FOR_KEYS(i) _Pragma("unroll") for (int i = 0; i < (KPT > 0 ? KPT : iters); ++i) if (KPT == 0 || i < iters)
 
@@ -191,11 +204,18 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       }
       if (lane == 0) sm.cta_min = best;
     }
-    cluster.sync();
-    best = ~0ull;
-    for (int c = 0; c < ctas; ++c) {
-      const uint64_t o = *cluster.map_shared_rank(&sm.cta_min, c);
-      best = o < best ? o : best;
+    if (ALONE) {
+      __syncthreads();
+      best = sm.cta_min;
+    } else {
+      cluster.sync();
+      best = ~0ull;
+#pragma unroll
+      for (int c = 0; c < kMaxCluster; ++c)
+        if (c < ctas) {
+          const uint64_t o = *cluster.map_shared_rank(&sm.cta_min, c);
+          best = o < best ? o : best;
+        }
     }
     only = static_cast<int>(best & (kMaxSlots - 1));
   } else if (p.n > 0) {
@@ -205,21 +225,32 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
       uint32_t* hist = sm.hist + (pass == 0 ? 0 : pass == 1 ? kBins0 : kBins0 + kBins1);
-      const int bins = pass == 1 ? kBins1 : kBins0;
       FOR_KEYS(i) {
         const uint64_t k = key_of(i);
         const uint32_t hi = static_cast<uint32_t>(k >> 23), mid = static_cast<uint32_t>(k >> 11) & 0xfff;
         const bool in = (k >> 32) < 3 && (pass < 1 || hi == d0) && (pass < 2 || mid == d1);
         if (in) atomicAdd(hist + (pass == 0 ? hi : pass == 1 ? mid : static_cast<uint32_t>(k) & 0x7ff), 1u);
       }
-      cluster.sync();
-      const int per = bins / kThreads;  // 2 or 4 bins a thread
+      constexpr int kPer[3] = {kBins0 / kThreads, kBins1 / kThreads, kBins2 / kThreads};
+      const int per = kPer[pass];  // 2 or 4 bins a thread
       uint32_t c[4] = {0, 0, 0, 0}, sum = 0;
-      for (int r = 0; r < ctas; ++r) {
-        const uint32_t* h = cluster.map_shared_rank(hist, r) + tid * per;
+      auto add = [&](const uint32_t* h) {
+        if (per == 4) {
+          const uint4 x = *reinterpret_cast<const uint4*>(h + 4 * tid);
+          c[0] += x.x, c[1] += x.y, c[2] += x.z, c[3] += x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(h + 2 * tid);
+          c[0] += x.x, c[1] += x.y;
+        }
+      };
+      if (ALONE) {
+        __syncthreads();
+        add(hist);
+      } else {
+        cluster.sync();
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j < per) c[j] += h[j];
+        for (int r = 0; r < kMaxCluster; ++r)
+          if (r < ctas) add(cluster.map_shared_rank(hist, r));
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum += c[j];
@@ -251,10 +282,11 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
   const int64_t out_at = static_cast<int64_t>(lst) * p.out_pitch;
   const bool copy_pos = p.pos_out != p.pos, copy_weight = p.weight_out != p.weight;
   uint32_t kept = 0;  // entries of the whole list (compact)
+  if (ALONE) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (only >= 0) {
     FOR_KEYS(i) {
       const int slot = slot0 + 32 * i;
-      if (slot < p.slots) {
+      if (writes && slot < p.slots) {
         const bool take = slot == only;
         if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[0] : p.pos[at + slot];
         if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : p.weight[at + slot];
@@ -262,8 +294,8 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       }
     }
     // the CTA that holds the slot moves the row
-    const int base = rank * kWarps * 32 * iters;
-    if (only >= base && only < base + kWarps * 32 * iters) count = 1;
+    const int base = rank * warps * 32 * iters;
+    if (only >= base && only < base + warps * 32 * iters) count = 1;
   } else {
     // counts of this warp: slots that are taken (kept) whatever the ties, and ties
     const uint32_t tie_cls = static_cast<uint32_t>(limit >> 32);
@@ -287,19 +319,32 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
     const uint32_t ca = __reduce_add_sync(0xffffffffu, wa), cb = __reduce_add_sync(0xffffffffu, wb);
     wa = __reduce_add_sync(0xffffffffu, lane < warp ? wa : 0u);
     wb = __reduce_add_sync(0xffffffffu, lane < warp ? wb : 0u);
-    if (tid == 0) {
-      sm.cta_a = ca;
-      sm.cta_b = cb;
-    }
-    cluster.sync();
-    uint32_t before_a = 0, before_b = 0, all_a = 0, all_b = 0;
-    for (int r = 0; r < ctas; ++r) {
-      const uint32_t ra = *cluster.map_shared_rank(&sm.cta_a, r);
-      const uint32_t rb = *cluster.map_shared_rank(&sm.cta_b, r);
-      before_a += r < rank ? ra : 0;
-      before_b += r < rank ? rb : 0;
-      all_a += ra;
-      all_b += rb;
+    // before this CTA's slots, in them, and in the whole list
+    uint32_t before_a = 0, before_b = 0, mine_a = ca, mine_b = cb, all_a = ca, all_b = cb;
+    if (ALONE) {
+      const uint32_t la = sm.warp_a[lane], lb = sm.warp_b[lane];
+      before_a = __reduce_add_sync(0xffffffffu, lane < warp_lo ? la : 0u);
+      before_b = __reduce_add_sync(0xffffffffu, lane < warp_lo ? lb : 0u);
+      const bool own = lane >= warp_lo && lane < warp_lo + warps;
+      mine_a = __reduce_add_sync(0xffffffffu, own ? la : 0u);
+      mine_b = __reduce_add_sync(0xffffffffu, own ? lb : 0u);
+    } else {
+      if (tid == 0) {
+        sm.cta_a = ca;
+        sm.cta_b = cb;
+      }
+      cluster.sync();
+      all_a = all_b = 0;
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r)
+        if (r < ctas) {
+          const uint32_t ra = *cluster.map_shared_rank(&sm.cta_a, r);
+          const uint32_t rb = *cluster.map_shared_rank(&sm.cta_b, r);
+          before_a += r < rank ? ra : 0;
+          before_b += r < rank ? rb : 0;
+          all_a += ra;
+          all_b += rb;
+        }
     }
     // list entries among the slots before a point with na sure ones and nb ties before it
     auto place = [&](uint32_t na, uint32_t nb) -> uint32_t {
@@ -307,10 +352,10 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       return na + (nb < ties ? nb : ties);
     };
     first = place(before_a, before_b);
-    count = place(before_a + ca, before_b + cb) - first;
+    count = place(before_a + mine_a, before_b + mine_b) - first;
     kept = place(all_a, all_b);
-    uint32_t na = before_a + wa, nb = before_b + wb;
-    FOR_KEYS(i) {
+    uint32_t na = (ALONE ? 0 : before_a) + wa, nb = (ALONE ? 0 : before_b) + wb;
+    if (writes) FOR_KEYS(i) {
       const uint64_t k = key_of(i);
       const int slot = slot0 + 32 * i;
       const bool is_a = sure(k), is_b = k == limit;
@@ -384,10 +429,10 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
     }
   }
   grid_dep_launch();
-  cluster.sync();  // no CTA leaves while another may still read its shared memory
+  if (!ALONE) cluster.sync();  // no CTA leaves while another may still read its shared memory
 }
 
-template <int KPT, bool COMPACT>
+template <int KPT, bool COMPACT, bool ALONE>
 cudaError_t launch_evict(const EvictParams& p, int lists, int ctas, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(lists) * ctas);
@@ -402,7 +447,7 @@ cudaError_t launch_evict(const EvictParams& p, int lists, int ctas, cudaStream_t
   at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, evict_kernel<KPT, COMPACT>, p);
+  return cudaLaunchKernelEx(&cfg, evict_kernel<KPT, COMPACT, ALONE>, p);
 }
 
 // CTAs of a cluster: as many as keep the lists' clusters on the GPU at once, but no fewer than
@@ -413,13 +458,16 @@ cudaError_t launch(EvictParams& p, int lists, cudaStream_t s) {
   while (ctas < kMaxCluster && 2 * ctas * static_cast<int64_t>(lists) <= num_sms() &&
          p.slots > 1024 * ctas)
     ctas *= 2;
-  const int per = kThreads * ctas;
+  const bool alone = p.slots <= kAloneSlots;
+  const int per = alone ? kThreads : kThreads * ctas;
   p.iters = (p.slots + per - 1) / per;
   if (p.iters < 1) p.iters = 1;
-  if (p.iters <= 2) return launch_evict<2, COMPACT>(p, lists, ctas, s);
-  if (p.iters <= 8) return launch_evict<8, COMPACT>(p, lists, ctas, s);
-  if (p.iters <= kMaxKeys) return launch_evict<kMaxKeys, COMPACT>(p, lists, ctas, s);
-  return launch_evict<0, COMPACT>(p, lists, ctas, s);
+  if (alone)
+    return p.iters <= 2 ? launch_evict<2, COMPACT, true>(p, lists, ctas, s)
+                        : launch_evict<8, COMPACT, true>(p, lists, ctas, s);
+  if (p.iters <= 12) return launch_evict<12, COMPACT, false>(p, lists, ctas, s);
+  if (p.iters <= kMaxKeys) return launch_evict<kMaxKeys, COMPACT, false>(p, lists, ctas, s);
+  return launch_evict<0, COMPACT, false>(p, lists, ctas, s);
 }
 
 bool aligned(const void* x, uintptr_t a) { return reinterpret_cast<uintptr_t>(x) % a == 0; }

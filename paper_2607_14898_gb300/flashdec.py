@@ -656,30 +656,67 @@ ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "blend": 3}
 
 
-def _dtype_code(t) -> int:
-    import torch
-    code = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16,
-            torch.float16: DTYPE_F16}.get(t.dtype)
+_DTYPE_CODES: dict = {}
+
+
+def _dtype_code(dtype) -> int:
+    if not _DTYPE_CODES:
+        import torch
+        _DTYPE_CODES.update({torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16,
+                             torch.float16: DTYPE_F16})
+    code = _DTYPE_CODES.get(dtype)
     if code is None:
-        raise TypeError(f"dtype {t.dtype}: float32, bfloat16 or float16 is required")
+        raise TypeError(f"dtype {dtype}: float32, bfloat16 or float16 is required")
     return code
 
 
-def _check_tensor(t, what: str, shape, dtype, device, contiguous: bool = True) -> None:
-    """The library receives raw pointers: refuse a tensor that a call would misread or overrun."""
+def _stream_on(device: int, stream) -> int:
+    """The stream's handle; of the device's current stream where none is given. (The handle alone:
+    a torch.cuda.Stream object takes 3 us to make, half of what a small call takes in all.)"""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device)
+    return int(getattr(stream, "cuda_stream", stream))
+
+
+def _refuse(t, what: str, shape, dtype, device: int, contiguous: bool) -> None:
+    """Says what is wrong with a tensor that a check has turned down."""
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{what}: a CUDA tensor is required")
     if t.dtype != dtype:
         raise TypeError(f"{what}: {t.dtype}, the call takes {dtype}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what}: on {t.device}, the other arguments are on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, the call works on cuda:{device}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, the call takes {tuple(shape)}")
-    if contiguous and not t.is_contiguous():
+    if contiguous:
         raise ValueError(f"{what}: a contiguous tensor is required")
-    if not contiguous and t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{what}: the last dimension must be contiguous")
+    raise ValueError(f"{what}: the last dimension must be contiguous")
+
+
+def _dense(t, what: str, shape, dtype, device: int) -> int:
+    """Address of a contiguous tensor of this shape, type and device. The library receives raw
+    pointers: anything else would be misread or overrun."""
+    try:
+        if (t.dtype is dtype and t.shape == shape and t.get_device() == device
+                and t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, what, shape, dtype, device, True)
+
+
+def _rows(t, what: str, shape, dtype, device: int):
+    """(address, strides) of a tensor whose last dimension is contiguous."""
+    try:
+        st = t.stride()
+        if (t.dtype is dtype and t.shape == shape and t.get_device() == device
+                and (st[-1] == 1 or shape[-1] < 2)):
+            return t.data_ptr(), st
+    except AttributeError:
+        pass
+    _refuse(t, what, shape, dtype, device, False)
 
 
 class Rotary:
@@ -697,7 +734,8 @@ class Rotary:
                              (ctypes.c_int32 * 3)(*dims), ROTARY_SCALINGS[scaling], float(base),
                              float(factor), int(trained_len), float(fast_turns),
                              float(slow_turns), float(amplitude))
-        self.head_dim, self.axes = int(head_dim), len(dims)
+        import torch
+        self.head_dim, self.axes, self.int32 = int(head_dim), len(dims), torch.int32
         out = _P()
         _check(lib().fd_rotary_create(ctypes.byref(c), ctypes.byref(out)), "fd_rotary_create")
         self.handle = out
@@ -718,25 +756,29 @@ def op_rotary(plan: Rotary, positions, q, q_out, k=None, k_out=None, backward=Fa
               stream=None) -> None:
     """Turns q [T][heads][head_dim] (and k) by positions int32 [T][axes] ([T] for one axis) into
     q_out (k_out), which may be q (k) itself; with backward=True the gradient (fd_op_rotary)."""
-    import torch
-    T, D = q.shape[0], plan.head_dim
-    dev = q.device
-    pos_shape = (T, plan.axes) if positions.dim() == 2 or plan.axes > 1 else (T,)
-    _check_tensor(positions, "positions", pos_shape, torch.int32, dev)
-    views = []
-    for x, y, what in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            views += [0, 0, 0, 0, 0, 0, 0]
-            continue
-        if x.dim() != 3:
-            raise ValueError(f"{what}: [tokens][heads][head_dim] is required")
-        shape = (T, x.shape[1], D)
-        _check_tensor(x, what, shape, q.dtype, dev, contiguous=False)
-        _check_tensor(y, what + "_out", shape, q.dtype, dev, contiguous=False)
-        views += [x.shape[1], x.data_ptr(), x.stride(0), x.stride(1), y.data_ptr(), y.stride(0),
-                  y.stride(1)]
-    _check(lib().fd_op_rotary(plan.handle, 1 if backward else 0, _dtype_code(q), T,
-                              positions.data_ptr(), *views, _stream_ptr(stream)), "fd_op_rotary")
+    shape, dtype, dev = q.shape, q.dtype, q.get_device()
+    if len(shape) != 3 or shape[2] != plan.head_dim:
+        raise ValueError(f"q: shape {tuple(shape)}, [tokens][heads][{plan.head_dim}] is required")
+    T = shape[0]
+    pos = _dense(positions, "positions",
+                 (T,) if plan.axes == 1 and positions.dim() == 1 else (T, plan.axes),
+                 plan.int32, dev)
+    qp, qs = _rows(q, "q", shape, dtype, dev)
+    op, os_ = _rows(q_out, "q_out", shape, dtype, dev)
+    if k is None:
+        args = (0, 0, 0, 0, 0, 0, 0)
+    else:
+        ks = k.shape
+        if len(ks) != 3 or ks[0] != T or ks[2] != plan.head_dim:
+            raise ValueError(f"k: shape {tuple(ks)}, [{T}][heads][{plan.head_dim}] is required")
+        kp, kst = _rows(k, "k", ks, dtype, dev)
+        ko, kot = _rows(k_out, "k_out", ks, dtype, dev)
+        args = (ks[1], kp, kst[0], kst[1], ko, kot[0], kot[1])
+    code = lib().fd_op_rotary(plan.handle, 1 if backward else 0, _dtype_code(dtype), T, pos,
+                              shape[1], qp, qs[0], qs[1], op, os_[0], os_[1], *args,
+                              _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_rotary")
 
 
 class Cache:
@@ -751,24 +793,35 @@ class Cache:
         if k.dtype not in (torch.bfloat16, torch.float16):
             raise TypeError(f"k: {k.dtype}, a cache holds bfloat16 or float16")
         S, G, C, D = k.shape
-        _check_tensor(k, "k", k.shape, k.dtype, None, contiguous=False)
-        _check_tensor(v, "v", k.shape, k.dtype, k.device, contiguous=False)
-        if v.stride() != k.stride():
+        dev = k.get_device()
+        kp, st = _rows(k, "k", k.shape, k.dtype, dev)
+        vp, vst = _rows(v, "v", k.shape, k.dtype, dev)
+        if dev < 0:
+            raise TypeError("k: a CUDA tensor is required")
+        if vst != st:
             raise ValueError("v: the strides of k are required")
-        _check_tensor(pos, "pos", (S, G, C), torch.int32, k.device)
-        _check_tensor(weight, "weight", (S, G, C), torch.float32, k.device)
         self.k, self.v, self.pos, self.weight = k, v, pos, weight
         self.streams, self.groups, self.capacity, self.head_dim = S, G, C, D
-        self.device, self.dtype = k.device, k.dtype
-        self.view = fd_cache(S, G, C, D, _dtype_code(k), 0, k.data_ptr(), v.data_ptr(),
-                             k.stride(0), k.stride(1), k.stride(2), pos.data_ptr(),
-                             weight.data_ptr())
+        self.device, self.dtype, self.int32, self.float32 = dev, k.dtype, torch.int32, torch.float32
+        self.view = fd_cache(S, G, C, D, _dtype_code(k.dtype), 0, kp, vp, st[0], st[1], st[2],
+                             _dense(pos, "pos", (S, G, C), torch.int32, dev),
+                             _dense(weight, "weight", (S, G, C), torch.float32, dev))
         self.ref = ctypes.byref(self.view)
+        self._workspace: dict = {}  # bytes by (used, heads, n_q)
+
+    def workspace_bytes(self, used: int, heads: int, n_q: int) -> int:
+        key = (used, heads, n_q)
+        need = self._workspace.get(key)
+        if need is None:
+            if len(self._workspace) > 1000:
+                self._workspace.clear()
+            need = self._workspace[key] = lib().fd_cache_attention_workspace_bytes(
+                self.ref, used, heads, n_q)
+        return need
 
 
 def cache_attention_workspace_bytes(cache: Cache, heads, n_q, used=None) -> int:
-    return lib().fd_cache_attention_workspace_bytes(
-        cache.ref, cache.capacity if used is None else int(used), heads, n_q)
+    return cache.workspace_bytes(cache.capacity if used is None else int(used), heads, n_q)
 
 
 def op_cache_attention(cache: Cache, q, q_pos, out, weight_out=None, used=None, scale=None,
@@ -777,31 +830,25 @@ def op_cache_attention(cache: Cache, q, q_pos, out, weight_out=None, used=None, 
     the cache's first `used` slots (all by default) into out; weight_out fp32
     [streams][groups][capacity] (may be cache.weight) receives decay times the slots' weights plus
     what this call gives them. scale: 1 / sqrt(head_dim) by default (fd_op_cache_attention)."""
-    import torch
-    S, D = cache.streams, cache.head_dim
-    if q.dim() != 4:
-        raise ValueError("q: [streams][n_q][heads][head_dim] is required")
-    n, H = q.shape[1], q.shape[2]
-    dev = cache.device
-    _check_tensor(q, "q", (S, n, H, D), cache.dtype, dev, contiguous=False)
-    _check_tensor(out, "out", (S, n, H, D), cache.dtype, dev, contiguous=False)
-    _check_tensor(q_pos, "q_pos", (S, n), torch.int32, dev)
+    shape, dev, D = q.shape, cache.device, cache.head_dim
+    if len(shape) != 4 or shape[0] != cache.streams or shape[3] != D:
+        raise ValueError(f"q: shape {tuple(shape)}, [{cache.streams}][n_q][heads][{D}] is required")
+    n, H = shape[1], shape[2]
+    qp, qs = _rows(q, "q", shape, cache.dtype, dev)
+    op, os_ = _rows(out, "out", shape, cache.dtype, dev)
+    pos = _dense(q_pos, "q_pos", (cache.streams, n), cache.int32, dev)
     used = cache.capacity if used is None else int(used)
-    if weight_out is not None:
-        _check_tensor(weight_out, "weight_out", (S, cache.groups, cache.capacity), torch.float32,
-                      dev)
-    need = lib().fd_cache_attention_workspace_bytes(cache.ref, used, H, n)
-    if need:
-        if workspace is None or not workspace.is_cuda or not workspace.is_contiguous() or \
-                workspace.device != dev:
-            raise ValueError(f"workspace: {need} bytes of contiguous memory on {dev} are required")
-        if workspace.numel() * workspace.element_size() < need:
-            raise ValueError(f"workspace: {need} bytes are required")
-    _check(lib().fd_op_cache_attention(
-        cache.ref, used, H, n, q.data_ptr(), q.stride(0), q.stride(1), q.stride(2),
-        q_pos.data_ptr(), D ** -0.5 if scale is None else scale, decay, out.data_ptr(),
-        out.stride(0), out.stride(1), out.stride(2), _ptr(weight_out), _ptr(workspace), _ptr(err),
-        _stream_ptr(stream)), "fd_op_cache_attention")
+    wp = 0 if weight_out is None else _dense(
+        weight_out, "weight_out", (cache.streams, cache.groups, cache.capacity), cache.float32, dev)
+    need = cache.workspace_bytes(used, H, n)
+    if need and (workspace is None or workspace.get_device() != dev
+                 or not workspace.is_contiguous() or workspace.nbytes < need):
+        raise ValueError(f"workspace: {need} bytes of contiguous memory on cuda:{dev} are required")
+    code = lib().fd_op_cache_attention(
+        cache.ref, used, H, n, qp, qs[0], qs[1], qs[2], pos, D ** -0.5 if scale is None else scale,
+        decay, op, os_[0], os_[1], os_[2], wp, _ptr(workspace), _ptr(err), _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_cache_attention")
 
 
 def op_cache_insert(cache: Cache, k_new, v_new, new_pos, slots, pos_out=None, weight_out=None,
@@ -810,26 +857,24 @@ def op_cache_insert(cache: Cache, k_new, v_new, new_pos, slots, pos_out=None, we
     the n slots of each (stream, group) that rank first by (class, weight, slot), written to
     slots int32 [streams][groups][n]; positions and weights go to pos_out and weight_out (the
     cache's own by default) (fd_op_cache_insert)."""
-    import torch
-    S, G, C, D = cache.streams, cache.groups, cache.capacity, cache.head_dim
-    if k_new.dim() != 4:
-        raise ValueError("k_new: [streams][n][groups][head_dim] is required")
-    n = k_new.shape[1]
-    dev = cache.device
-    _check_tensor(k_new, "k_new", (S, n, G, D), cache.dtype, dev, contiguous=False)
-    _check_tensor(v_new, "v_new", (S, n, G, D), cache.dtype, dev, contiguous=False)
-    if v_new.stride() != k_new.stride():
+    shape, dev = k_new.shape, cache.device
+    S, G, C = cache.streams, cache.groups, cache.capacity
+    if len(shape) != 4 or shape[0] != S or shape[2] != G or shape[3] != cache.head_dim:
+        raise ValueError(f"k_new: shape {tuple(shape)}, [{S}][n][{G}][{cache.head_dim}] is required")
+    n = shape[1]
+    kp, st = _rows(k_new, "k_new", shape, cache.dtype, dev)
+    vp, vst = _rows(v_new, "v_new", shape, cache.dtype, dev)
+    if vst != st:
         raise ValueError("v_new: the strides of k_new are required")
-    _check_tensor(new_pos, "new_pos", (S, n), torch.int32, dev)
-    _check_tensor(slots, "slots", (S, G, n), torch.int32, dev)
-    pos_out = cache.pos if pos_out is None else pos_out
-    weight_out = cache.weight if weight_out is None else weight_out
-    _check_tensor(pos_out, "pos_out", (S, G, C), torch.int32, dev)
-    _check_tensor(weight_out, "weight_out", (S, G, C), torch.float32, dev)
-    _check(lib().fd_op_cache_insert(
-        cache.ref, n, k_new.data_ptr(), v_new.data_ptr(), k_new.stride(0), k_new.stride(1),
-        k_new.stride(2), new_pos.data_ptr(), sinks, recent, pos_out.data_ptr(),
-        weight_out.data_ptr(), slots.data_ptr(), _stream_ptr(stream)), "fd_op_cache_insert")
+    code = lib().fd_op_cache_insert(
+        cache.ref, n, kp, vp, st[0], st[1], st[2],
+        _dense(new_pos, "new_pos", (S, n), cache.int32, dev), sinks, recent,
+        _dense(cache.pos if pos_out is None else pos_out, "pos_out", (S, G, C), cache.int32, dev),
+        _dense(cache.weight if weight_out is None else weight_out, "weight_out", (S, G, C),
+               cache.float32, dev),
+        _dense(slots, "slots", (S, G, n), cache.int32, dev), _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_cache_insert")
 
 
 def op_cache_compact(src: Cache, dst: Cache, now, src_slots, used=None, sinks=0, recent=0,
@@ -837,12 +882,13 @@ def op_cache_compact(src: Cache, dst: Cache, now, src_slots, used=None, sinks=0,
     """The dst.capacity entries of src's first `used` slots (all by default) that rank last by
     (class, weight, slot), recency counted from now int32 [streams], into dst in slot order;
     src_slots int32 [streams][groups][dst.capacity]: where each came from (fd_op_cache_compact)."""
-    import torch
     dev = src.device
     if dst.device != dev:
-        raise ValueError(f"dst: on {dst.device}, src is on {dev}")
-    _check_tensor(now, "now", (src.streams,), torch.int32, dev)
-    _check_tensor(src_slots, "src_slots", (src.streams, src.groups, dst.capacity), torch.int32, dev)
-    _check(lib().fd_op_cache_compact(
-        src.ref, src.capacity if used is None else int(used), dst.ref, now.data_ptr(), sinks,
-        recent, src_slots.data_ptr(), _stream_ptr(stream)), "fd_op_cache_compact")
+        raise ValueError(f"dst: on cuda:{dst.device}, src is on cuda:{dev}")
+    code = lib().fd_op_cache_compact(
+        src.ref, src.capacity if used is None else int(used), dst.ref,
+        _dense(now, "now", (src.streams,), src.int32, dev), sinks, recent,
+        _dense(src_slots, "src_slots", (src.streams, src.groups, dst.capacity), src.int32, dev),
+        _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_cache_compact")

@@ -99,15 +99,15 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Gives up after kTries, or at once when another wait of this launch (or an earlier one on the
-// same status word) has given up; not so a drain, which waits for the CTA's own copies and
+// Gives up after kTries, or soon after another wait of this launch (or an earlier one on the
+// same status word) has given up (looked up every 64 tries: the word is a trip to L2 away); not so a drain, which waits for the CTA's own copies and
 // products in flight.
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code,
                                      bool drain = false) {
   bool ok = try_wait(bar, parity);
 #pragma unroll 1
   for (int n = 0; !ok; ++n) {
-    if (n == kTries || (!drain && *reinterpret_cast<volatile int*>(err) != 0)) {
+    if (n == kTries || (!drain && n % 64 == 63 && *reinterpret_cast<volatile int*>(err) != 0)) {
       atomicOr(err, code);
       break;
     }
@@ -121,7 +121,8 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* er
   bool ok = __all_sync(0xffffffffu, try_wait(bar, parity));
 #pragma unroll 1
   for (int n = 0; !ok; ++n) {
-    if (__any_sync(0xffffffffu, n == kTries || *reinterpret_cast<volatile int*>(err) != 0)) {
+    if (n == kTries ||
+        (n % 64 == 63 && __any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(err) != 0))) {
       atomicOr(err, code);
       break;
     }

@@ -3,20 +3,23 @@
 //
 // Per list (one KV group of one stream) the n slots that rank first by (class, weight, slot)
 // are given up: class 0 empty, 1 unprotected, 2 protected. A slot's rank key is 34 bits, class
-// and the weight's bits made monotone; the n-th smallest key T is found by radix selection
-// (digits of 11, 12 and 11 bits), and of the slots whose key is T the first e in slot order are
-// given up, so equal weights fall to the lowest index. Keys are integers and counts are sums of
+// and the weight's bits made monotone; the n-th smallest key T is found by radix selection (class
+// with 11 bits, then 11 and 10 bits), and of the slots whose key is T the first e in slot order are
+// given up, so equal weights fall to the lowest index. (The first digit reaches two bits into
+// the mantissa: with the class as bits of the digit it ended at the exponent, most slots fell
+// into some twenty counters, and counting them took longer than all else.) Keys are integers and counts are sums of
 // integers: the choice does not depend on the order in which threads run.
 //
 // One cluster of 1 to 8 CTAs per list. Keys are read once into registers, each warp
 // holding consecutive slots, and histograms are counted in shared memory. Up to kAloneSlots every
 // CTA of the cluster selects from the whole list by itself, and the cluster only shares the
-// writing: 50 KB more reads from L2 a CTA, but no exchange, whose steps (a cluster barrier and a
-// round trip through distributed shared memory, three times) took longer than all else. Longer
-// lists are cut between the CTAs and the histograms summed over the cluster. One scan of
-// counts over warps (and CTAs) gives every slot that is taken (or kept) its place in slot order.
-// Then the cluster writes the list's positions and weights and moves the rows, 16 bytes a thread.
-// For one new token the selection is a minimum over (class, weight, slot) packed into 54 bits.
+// writing: more reads from L2, but no exchange, whose steps (a cluster barrier and a round
+// trip through distributed shared memory, three times) took longer than the rest. Longer lists are
+// cut between the CTAs and the histograms summed over the cluster. One scan of counts over
+// warps (and CTAs) gives every slot that is taken (or kept) its place in slot order. Then the
+// cluster writes the list's positions and weights and moves the rows, 16 bytes a thread. For one
+// new token the selection is a minimum over (class, weight, slot) packed into 54 bits, one exchange
+// only, so there the list is always cut.
 //
 // Bound by memory for long rows (the copied keys and values) and by the latency of the dependent steps for
 // short ones: the positions and weights of a list are 8 bytes a slot.
@@ -37,9 +40,11 @@ constexpr int kMaxSlots = 1 << 20;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxKeys = 32;  // keys a thread holds in registers
 constexpr int kAloneSlots = 8 * kThreads;
-// radix digits of the 34-bit key: bits 23.., 11..22, 0..10
-constexpr int kBins0 = 2048, kBins1 = 4096, kBins2 = 2048;
-constexpr int kBins = kBins0 + kBins1 + kBins2;
+// Radix digits: class 0 is bin 0 of the first, classes 1 and 2 have 2048 bins each for bits 21..31 (the
+// last of them is never used: the largest key, NaN, is below it); then bits 10..20 and 0..9.
+constexpr int kBins0 = 4096, kBins1 = 2048, kBins2 = 1024;
+constexpr int kHist = kAloneSlots;  // counters; afterwards the list of a CTA that selects alone
+static_assert(kBins0 + kBins1 + kBins2 <= kHist, "counters");
 
 struct EvictParams {
   int groups, slots, n;      // slots looked at, slots given up, per list
@@ -69,7 +74,7 @@ __device__ __forceinline__ uint64_t rank_key(int32_t pos, float w, int sinks, in
   if (pos < 0) return 0;
   uint32_t b = __float_as_uint(w);
   if (b == 0x80000000u) b = 0;
-  b = w != w ? 0xffffffffu : (b & 0x80000000u ? ~b : b | 0x80000000u);
+  b = w != w ? 0xffc00000u : (b & 0x80000000u ? ~b : b | 0x80000000u);
   const uint64_t cls = pos < sinks || pos >= protect ? 2 : 1;
   return (cls << 32) | b;
 }
@@ -114,7 +119,7 @@ struct Keys<0> {
 };
 
 struct Shared {
-  alignas(16) uint32_t hist[kBins];
+  alignas(16) uint32_t hist[kHist];
   uint32_t warp_a[kWarps], warp_b[kWarps];
   uint64_t warp_min[kWarps];
   uint64_t cta_min;
@@ -159,12 +164,9 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int iters = p.iters;
   const int slot0 = ((ALONE ? 0 : rank * kWarps) + warp) * 32 * iters + lane;  // i-th: + 32 i
-  // the warps whose slots this CTA writes
-  const int warps = ALONE ? kWarps / ctas : kWarps, warp_lo = ALONE ? rank * warps : 0;
-  const bool writes = warp >= warp_lo && warp < warp_lo + warps;
   const int64_t at = static_cast<int64_t>(lst) * p.pitch;
 
-  for (int i = tid; i < kBins; i += kThreads) sm.hist[i] = 0;
+  for (int i = tid; i < kBins0 + kBins1 + kBins2; i += kThreads) sm.hist[i] = 0;
   grid_dep_wait();
   const int64_t protect =
       static_cast<int64_t>(p.newest ? p.newest[static_cast<int64_t>(stream) * p.newest_stride] : 0) -
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
   uint64_t limit = 0;   // T: the n-th smallest key
   uint32_t ties = 0;    // e: so many of the slots with key T are given up
   int only = -1;        // the slot, where a minimum tells it
-  if (!COMPACT && p.n == 1) {
+  if (!COMPACT && !ALONE && p.n == 1) {
     uint64_t best = ~0ull;
     FOR_KEYS(i) {
       const uint64_t k = (key_of(i) << 20) | static_cast<uint32_t>(slot0 + 32 * i);
@@ -204,43 +206,42 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       }
       if (lane == 0) sm.cta_min = best;
     }
-    if (ALONE) {
-      __syncthreads();
-      best = sm.cta_min;
-    } else {
-      cluster.sync();
-      best = ~0ull;
+    cluster.sync();
+    best = ~0ull;
 #pragma unroll
-      for (int c = 0; c < kMaxCluster; ++c)
-        if (c < ctas) {
-          const uint64_t o = *cluster.map_shared_rank(&sm.cta_min, c);
-          best = o < best ? o : best;
-        }
-    }
+    for (int c = 0; c < kMaxCluster; ++c)
+      if (c < ctas) {
+        const uint64_t o = *cluster.map_shared_rank(&sm.cta_min, c);
+        best = o < best ? o : best;
+      }
     only = static_cast<int>(best & (kMaxSlots - 1));
   } else if (p.n > 0) {
     __syncthreads();
     uint32_t rest = static_cast<uint32_t>(p.n);
-    uint32_t d0 = 0, d1 = 0;
+    uint64_t high = 0;  // the digits found so far, in their places
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
+      if (pass > 0 && high == 0) break;  // class 0: equal keys
       uint32_t* hist = sm.hist + (pass == 0 ? 0 : pass == 1 ? kBins0 : kBins0 + kBins1);
       FOR_KEYS(i) {
         const uint64_t k = key_of(i);
-        const uint32_t hi = static_cast<uint32_t>(k >> 23), mid = static_cast<uint32_t>(k >> 11) & 0xfff;
-        const bool in = (k >> 32) < 3 && (pass < 1 || hi == d0) && (pass < 2 || mid == d1);
-        if (in) atomicAdd(hist + (pass == 0 ? hi : pass == 1 ? mid : static_cast<uint32_t>(k) & 0x7ff), 1u);
+        const uint32_t cls = static_cast<uint32_t>(k >> 32), low = static_cast<uint32_t>(k);
+        if (pass == 0 ? cls < 3 : (k >> (pass == 1 ? 21 : 10)) == high)
+          atomicAdd(hist + (pass == 0 ? (cls == 0 ? 0 : 1 + (cls - 1) * 2048 + (low >> 21))
+                                      : pass == 1 ? (low >> 10) & 0x7ff : low & 0x3ff), 1u);
       }
       constexpr int kPer[3] = {kBins0 / kThreads, kBins1 / kThreads, kBins2 / kThreads};
-      const int per = kPer[pass];  // 2 or 4 bins a thread
+      const int per = kPer[pass];  // 4, 2 or 1 bins a thread
       uint32_t c[4] = {0, 0, 0, 0}, sum = 0;
       auto add = [&](const uint32_t* h) {
         if (per == 4) {
           const uint4 x = *reinterpret_cast<const uint4*>(h + 4 * tid);
           c[0] += x.x, c[1] += x.y, c[2] += x.z, c[3] += x.w;
-        } else {
+        } else if (per == 2) {
           const uint2 x = *reinterpret_cast<const uint2*>(h + 2 * tid);
           c[0] += x.x, c[1] += x.y;
+        } else {
+          c[0] += h[tid];
         }
       };
       if (ALONE) {
@@ -267,11 +268,13 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       __syncthreads();
       const uint32_t digit = sm.digit;
       rest = sm.rest;
+      if (pass == 0)
+        high = digit == 0 ? 0 : (static_cast<uint64_t>(1 + (digit - 1) / 2048) << 11) | ((digit - 1) % 2048);
+      else
+        high = (high << (pass == 1 ? 11 : 10)) | digit;
       __syncthreads();
-      if (pass == 0) d0 = digit;
-      else if (pass == 1) d1 = digit;
-      else limit = (static_cast<uint64_t>(d0) << 23) | (static_cast<uint64_t>(d1) << 11) | digit;
     }
+    limit = high;
     ties = rest;
   }
 
@@ -281,12 +284,12 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
   int32_t* list = p.list + static_cast<int64_t>(lst) * p.list_len;
   const int64_t out_at = static_cast<int64_t>(lst) * p.out_pitch;
   const bool copy_pos = p.pos_out != p.pos, copy_weight = p.weight_out != p.weight;
-  uint32_t kept = 0;  // entries of the whole list (compact)
+  uint32_t kept = 0;  // entries of the whole list
   if (ALONE) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (only >= 0) {
     FOR_KEYS(i) {
       const int slot = slot0 + 32 * i;
-      if (writes && slot < p.slots) {
+      if (slot < p.slots) {
         const bool take = slot == only;
         if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[0] : p.pos[at + slot];
         if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : p.weight[at + slot];
@@ -294,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       }
     }
     // the CTA that holds the slot moves the row
-    const int base = rank * warps * 32 * iters;
-    if (only >= base && only < base + warps * 32 * iters) count = 1;
+    const int base = rank * kWarps * 32 * iters;
+    if (only >= base && only < base + kWarps * 32 * iters) count = 1;
   } else {
     // counts of this warp: slots that are taken (kept) whatever the ties, and ties
     const uint32_t tie_cls = static_cast<uint32_t>(limit >> 32);
@@ -319,16 +322,9 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
     const uint32_t ca = __reduce_add_sync(0xffffffffu, wa), cb = __reduce_add_sync(0xffffffffu, wb);
     wa = __reduce_add_sync(0xffffffffu, lane < warp ? wa : 0u);
     wb = __reduce_add_sync(0xffffffffu, lane < warp ? wb : 0u);
-    // before this CTA's slots, in them, and in the whole list
-    uint32_t before_a = 0, before_b = 0, mine_a = ca, mine_b = cb, all_a = ca, all_b = cb;
-    if (ALONE) {
-      const uint32_t la = sm.warp_a[lane], lb = sm.warp_b[lane];
-      before_a = __reduce_add_sync(0xffffffffu, lane < warp_lo ? la : 0u);
-      before_b = __reduce_add_sync(0xffffffffu, lane < warp_lo ? lb : 0u);
-      const bool own = lane >= warp_lo && lane < warp_lo + warps;
-      mine_a = __reduce_add_sync(0xffffffffu, own ? la : 0u);
-      mine_b = __reduce_add_sync(0xffffffffu, own ? lb : 0u);
-    } else {
+    // before this CTA's slots, and in the whole list
+    uint32_t before_a = 0, before_b = 0, all_a = ca, all_b = cb;
+    if (!ALONE) {
       if (tid == 0) {
         sm.cta_a = ca;
         sm.cta_b = cb;
@@ -351,34 +347,61 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       if (COMPACT) return na + (tie_cls >= 1 && nb > ties ? nb - ties : 0u);
       return na + (nb < ties ? nb : ties);
     };
-    first = place(before_a, before_b);
-    count = place(before_a + mine_a, before_b + mine_b) - first;
     kept = place(all_a, all_b);
-    uint32_t na = (ALONE ? 0 : before_a) + wa, nb = (ALONE ? 0 : before_b) + wb;
-    if (writes) FOR_KEYS(i) {
-      const uint64_t k = key_of(i);
-      const int slot = slot0 + 32 * i;
-      const bool is_a = sure(k), is_b = k == limit;
-      const uint32_t ma = __ballot_sync(0xffffffffu, is_a), mb = __ballot_sync(0xffffffffu, is_b);
-      const uint32_t below = (1u << lane) - 1;
-      const uint32_t la = na + __popc(ma & below), lb = nb + __popc(mb & below);
-      const bool tie_in = is_b && (COMPACT ? tie_cls >= 1 && lb >= ties : lb < ties);
-      const bool take = is_a || tie_in;
-      if (slot < p.slots) {
-        const uint32_t v = place(la, lb);
-        if (take) list[v] = slot;
-        if (COMPACT) {
-          if (take) {
-            p.pos_out[out_at + v] = p.pos[at + slot];
-            p.weight_out[out_at + v] = p.weight[at + slot];
-          }
-        } else {
-          if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[v] : p.pos[at + slot];
-          if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : p.weight[at + slot];
-        }
+    if (ALONE) {  // an equal share
+      first = static_cast<uint32_t>(static_cast<uint64_t>(kept) * rank / ctas);
+      count = static_cast<uint32_t>(static_cast<uint64_t>(kept) * (rank + 1) / ctas) - first;
+    } else {
+      first = place(before_a, before_b);
+      count = place(before_a + ca, before_b + cb) - first;
+    }
+    uint32_t na = before_a + wa, nb = before_b + wb;
+    if (ALONE) __syncthreads();  // the counters have been read
+    // positions and weights first, so that no load waits for the store before it
+    constexpr int kGroup = 4;
+#pragma unroll
+    for (int i0 = 0; i0 < (KPT > 0 ? KPT : iters); i0 += kGroup) {
+      if (i0 >= iters) break;
+      int32_t ps[kGroup];
+      float ws[kGroup];
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) {
+        const int i = i0 + u, slot = slot0 + 32 * i;
+        // alone: the CTAs write for the warps' rounds in turn
+        const bool mine = i < iters && slot < p.slots && (!ALONE || i % ctas == rank);
+        ps[u] = mine && (COMPACT || copy_pos) ? p.pos[at + slot] : 0;
+        ws[u] = mine && (COMPACT || copy_weight) ? p.weight[at + slot] : 0.f;
       }
-      na += __popc(ma);
-      nb += __popc(mb);
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) {
+        const int i = i0 + u, slot = slot0 + 32 * i;
+        if (i >= iters) break;
+        const uint64_t k = key_of(KPT > 0 && i >= KPT ? 0 : i);
+        const bool is_a = sure(k), is_b = k == limit;
+        const uint32_t ma = __ballot_sync(0xffffffffu, is_a), mb = __ballot_sync(0xffffffffu, is_b);
+        const uint32_t below = (1u << lane) - 1;
+        const uint32_t la = na + __popc(ma & below), lb = nb + __popc(mb & below);
+        const bool tie_in = is_b && (COMPACT ? tie_cls >= 1 && lb >= ties : lb < ties);
+        const bool take = is_a || tie_in;
+        const uint32_t v = place(la, lb);
+        if (slot < p.slots) {
+          if (ALONE && take) sm.hist[v] = slot;
+          if (!ALONE && take) list[v] = slot;
+          if (!ALONE || i % ctas == rank) {
+            if (COMPACT) {
+              if (take) {
+                p.pos_out[out_at + v] = ps[u];
+                p.weight_out[out_at + v] = ws[u];
+              }
+            } else {
+              if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[v] : ps[u];
+              if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : ws[u];
+            }
+          }
+        }
+        na += __popc(ma);
+        nb += __popc(mb);
+      }
     }
     if (COMPACT) {  // the destination's empty end
       for (int v = static_cast<int>(kept) + rank * kThreads + tid; v < p.list_len; v += ctas * kThreads) {
@@ -392,6 +415,8 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
 
   // ---- rows: the entries of this CTA, 16 bytes of a key and of a value per thread and step
   __syncthreads();  // this CTA's part of the list is written
+  if (ALONE)
+    for (uint32_t v = first + tid; v < first + count; v += kThreads) list[v] = sm.hist[v];
   const int64_t src0 = stream * p.src_stream + group * p.src_group;
   const int64_t dst0 = stream * p.dst_stream + group * p.dst_group;
   const int r16 = p.row16;  // 8 or 16
@@ -406,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       if (it >= items) continue;
       const int64_t v = first + it / r16;
       const int part = static_cast<int>(it % r16);
-      const int64_t slot = list[v];
+      const int64_t slot = ALONE ? static_cast<int64_t>(sm.hist[v]) : list[v];
       const int64_t from = src0 + (COMPACT ? slot : v) * p.src_row + part;
       to[u] = dst0 + (COMPACT ? v : slot) * p.dst_row + part;
       xk[u] = p.src_k[from];
@@ -458,13 +483,14 @@ cudaError_t launch(EvictParams& p, int lists, cudaStream_t s) {
   while (ctas < kMaxCluster && 2 * ctas * static_cast<int64_t>(lists) <= num_sms() &&
          p.slots > 1024 * ctas)
     ctas *= 2;
-  const bool alone = p.slots <= kAloneSlots;
+  const bool alone = p.slots <= kAloneSlots && (COMPACT || p.n != 1);
   const int per = alone ? kThreads : kThreads * ctas;
   p.iters = (p.slots + per - 1) / per;
   if (p.iters < 1) p.iters = 1;
   if (alone)
     return p.iters <= 2 ? launch_evict<2, COMPACT, true>(p, lists, ctas, s)
                         : launch_evict<8, COMPACT, true>(p, lists, ctas, s);
+  if (!COMPACT && p.iters <= 2) return launch_evict<2, COMPACT, false>(p, lists, ctas, s);
   if (p.iters <= 12) return launch_evict<12, COMPACT, false>(p, lists, ctas, s);
   if (p.iters <= kMaxKeys) return launch_evict<kMaxKeys, COMPACT, false>(p, lists, ctas, s);
   return launch_evict<0, COMPACT, false>(p, lists, ctas, s);

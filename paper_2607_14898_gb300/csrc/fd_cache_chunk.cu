@@ -81,53 +81,45 @@ __device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t lead
          (static_cast<uint64_t>(2) << 61);
 }
 
-// The waits of this file. A try suspends the thread for up to kSuspendNs, so that waiting warps
-// leave the issue slots to the others, and kTries of them bound a wait (to seconds; a wait that
-// succeeds takes microseconds). The loops are short on purpose: with the 64-fold unrolled loop of
-// mbar_wait at every wait the attend kernel was 132 KB of code, and a third of its issue slots went
-// to instruction fetches.
-constexpr uint32_t kSuspendNs = 20000;
-constexpr int kTries = 1 << 18;
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(kSuspendNs)
-      : "memory");
-  return ok != 0;
-}
+// The waits of this file, kTries tries at most (a try suspends the thread for a while; a wait that
+// succeeds takes microseconds). One try is inline, the loop in a function of its own: with
+// mbar_wait's 64-fold unrolled loop at every wait the attend kernel was 132 KB of code and a third
+// of its issue slots went to instruction fetches (90 us for the 480p chunk against 66), and short
+// loops inline cost as much in registers spilled around them.
+constexpr int kTries = 1 << 24;
 // Gives up after kTries, or soon after another wait of this launch (or an earlier one on the
-// same status word) has given up (looked up every 64 tries: the word is a trip to L2 away); not so a drain, which waits for the CTA's own copies and
-// products in flight.
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code,
-                                     bool drain = false) {
-  bool ok = try_wait(bar, parity);
+// same status word) has given up (looked up every 64 tries: the word is a trip to L2 away); not so
+// a drain, which waits for the CTA's own copies and products in flight.
+__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, int* err, int code, bool drain) {
 #pragma unroll 1
-  for (int n = 0; !ok; ++n) {
+  for (int n = 0; !mbar_try_wait(bar, parity); ++n) {
     if (n == kTries || (!drain && n % 64 == 63 && *reinterpret_cast<volatile int*>(err) != 0)) {
       atomicOr(err, code);
-      break;
+      return false;
     }
-    ok = try_wait(bar, parity);
   }
-  return ok;
+  return true;
+}
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code,
+                                     bool drain = false) {
+  return mbar_try_wait(bar, parity) || wait_more(bar, parity, err, code, drain);
 }
 // The same for a whole warp that stays together (tcgen05 loads and stores, which follow such
 // waits, have to be executed by all its lanes at once): every decision is the warp's.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, int code) {
-  bool ok = __all_sync(0xffffffffu, try_wait(bar, parity));
+__device__ __noinline__ bool wait_more_warp(uint32_t bar, uint32_t parity, int* err, int code) {
 #pragma unroll 1
-  for (int n = 0; !ok; ++n) {
+  for (int n = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
     if (n == kTries ||
         (n % 64 == 63 && __any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(err) != 0))) {
       atomicOr(err, code);
-      break;
+      return false;
     }
-    ok = __all_sync(0xffffffffu, try_wait(bar, parity));
   }
+  return true;
+}
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, int code) {
+  const bool ok = __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||
+                  wait_more_warp(bar, parity, err, code);
   __syncwarp();
   return ok;
 }
@@ -147,38 +139,40 @@ constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swiz
 // maximum is handed from quarter to quarter, which sets the groups a step apart: the exponentials
 // of one run beside the loads, masks and maxima of the others.
 //   warps 0-15    softmax: warps 4 q .. 4 q + 3 quarter q
-//   warp 16       TMA: Q of the segment, K and V blocks into a ring
+//   warp 16       TMA: Q of the segment, and K by half blocks (128 slots). K and V have a ring each,
+//                 so that a half is fetched as soon as one has been used: two more are there or
+//                 on their way meanwhile (D = 128, where 192 KB of them fit)
 //   warps 17, 18  products: a thread issues one tcgen05.mma per 104 to 158 cycles whatever its
 //                 size, so two of them share the work. D = 64: those of the block's first and
 //                 second half, each half with a running maximum and an O of its own; D = 128: S of
 //                 both halves, and P V into the one O that TMEM has room for.
-//   warp 19       positions of each block, and zeros for the values of empty slots (their
-//                 probability is 0, but 0 times NaN is NaN)
+//   warp 19       positions of each block, a block ahead; V by half blocks, with zeros for the
+//                 values of empty slots (their probability is 0, but 0 times NaN is NaN)
 // TMEM (512 columns): S 2 x 128, P 2 x 64 (two 16-bit values a column), O 2 x 64 or 128. S takes the
 // next scores once the softmax has it in registers.
 template <int D>
 struct AttendCfg {
   static constexpr int kKeys = 256;
   static constexpr int kQBytes = kTile * D * 2;
-  static constexpr int kSub2 = kKeys * 128;        // 64 elements of a block's rows
-  static constexpr int kBlockBytes = kKeys * D * 2;
-  static constexpr int kSlots = D == 128 ? 3 : 6;  // ring of K, V, K, V, ..
+  static constexpr int kHalfBytes = kTile * D * 2;  // K or V of half a block
+  static constexpr int kSlots = D == 128 ? 3 : 6;   // of each ring; half 2 J + h is in slot (2 J + h) % kSlots
   static constexpr bool kTwoO = D == 64;
-  // An odd ring's slots hold K and V in turn, and a slot's full barrier has waiters for every
-  // other phase only. A parity tells a phase from its neighbours and no further: such a waiter first
-  // waits until the slot's use before its own is over (the wait of the loader), or it would
-  // take the phase before that one for its own.
-  static constexpr bool kMixed = kSlots % 2 != 0;
-  static constexpr int kOffRing = kQBytes;
-  static constexpr int kOffPos = kOffRing + kSlots * kBlockBytes;
+  // A parity tells a phase from its neighbours and no further, so whoever waits for a slot's
+  // barrier has to wait for every phase of it: one thread waits for all halves, or (D = 64) one
+  // for each half of the blocks, whose slots differ because the ring's length is even.
+  static_assert(!kTwoO || kSlots % 2 == 0, "waiters");
+  static constexpr int kOffK = kQBytes;
+  static constexpr int kOffV = kOffK + kSlots * kHalfBytes;
+  static constexpr int kOffPos = kOffV + kSlots * kHalfBytes;
   static constexpr int kOffMax = kOffPos + 2 * kKeys * 4;  // two blocks' positions before it
   static constexpr int kOffBar = kOffMax + (kTwoO ? 4 : 1) * kTile * 4;  // D = 64: [half][m, l]
   static constexpr int kSmem = kOffBar + 512;
-  static constexpr int kThreads = 640;
+  static constexpr int kThreads = 640;  // five warps a sub-partition: 96 registers (six: 80)
   static constexpr uint32_t kColS = 0, kColP = 256, kColO = 384;
   // barriers: kSFull, kSRead of the halves, kPFull, kPv, kMax of the quarters, kPos* of the stages
-  static constexpr int kQFull = 0, kQFree = 1, kKvFull = 2, kKvFree = kKvFull + kSlots,
-                       kVReady = kKvFree + kSlots, kSFull = kVReady + 4, kSRead = kSFull + 2,
+  static constexpr int kQFull = 0, kQFree = 1, kKFull = 2, kKFree = kKFull + kSlots,
+                       kVFull = kKFree + kSlots, kVFree = kVFull + kSlots,
+                       kVReady = kVFree + kSlots, kSFull = kVReady + kSlots, kSRead = kSFull + 2,
                        kPFull = kSRead + 2, kPv = kPFull + 4, kMax = kPv + 4, kORead = kMax + 4,
                        kPosFull = kORead + 1, kPosFree = kPosFull + 2, kDone = kPosFree + 2,
                        kBars = kDone + 2;
@@ -254,10 +248,12 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     mbar_init(bar(C::kQFull), 1);
     mbar_init(bar(C::kQFree), C::kTwoO ? 2 : 1);
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(bar(C::kKvFull + i), 1);
-      mbar_init(bar(C::kKvFree + i), C::kTwoO ? 2 : 1);  // warps that read it
+      mbar_init(bar(C::kKFull + i), 1);
+      mbar_init(bar(C::kKFree + i), 1);
+      mbar_init(bar(C::kVFull + i), 1);
+      mbar_init(bar(C::kVFree + i), 1);
+      mbar_init(bar(C::kVReady + i), 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(bar(C::kVReady + i), 1);
     for (int h = 0; h < 2; ++h) {
       mbar_init(bar(C::kSFull + h), 1);
       mbar_init(bar(C::kSRead + h), 256);
@@ -289,8 +285,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     if (lane == 0) {
       prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
-      prefetch_tmap(&tmV);
-      int i = 0, segs = 0;  // i: loads of K and V so far
+      int i = 0, segs = 0;  // i: halves so far
       bool ok = true;
       for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks)) {
         const int lst = w.tile / p.row_tiles;
@@ -304,151 +299,169 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
                         (w.tile - lst * p.row_tiles) * p.tile_tokens, stream);
           segs = w.seg + 1;
         }
-        for (int kv = 0; kv < 2; ++kv, ++i) {
+        for (int h = 0; h < 2; ++h, ++i) {
           const int s = i % C::kSlots;
-          ok = wait(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA);
+          ok = wait(bar(C::kKFree + s), ((i / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA);
           if (!ok) break;
-          mbar_expect_tx(bar(C::kKvFull + s), C::kBlockBytes);
+          mbar_expect_tx(bar(C::kKFull + s), C::kHalfBytes);
           for (int d = 0; d < D / 64; ++d)
-            tma_load_4d(base + C::kOffRing + s * C::kBlockBytes + d * C::kSub2, kv ? &tmV : &tmK,
-                        bar(C::kKvFull + s), 64 * d, w.block * C::kKeys, group, stream);
+            tma_load_4d(base + C::kOffK + s * C::kHalfBytes + d * kSub, &tmK, bar(C::kKFull + s),
+                        64 * d, w.block * C::kKeys + h * kTile, group, stream);
         }
       }
       // nothing may be in flight when the CTA exits
       if (segs > 0) wait(bar(C::kQFull), (segs - 1) & 1, p.err, ERR_WAIT_TMA, true);
       for (int j = i - 1; j >= 0 && j >= i - C::kSlots; --j)
-        wait(bar(C::kKvFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
+        wait(bar(C::kKFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
     }
   } else if (warp == 19) {
-    // ---- positions and empty slots' values
-    int J = 0;
-    bool ok = true;
-    for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks), ++J) {
-      const int lst = w.tile / p.row_tiles;
-      const int32_t* pos = p.pos + static_cast<int64_t>(lst) * p.capacity;
+    // ---- positions, a block ahead, and empty slots' values
+    // publishes block J's positions; bit i of `holes`: the lane's slot 32 i + lane is empty
+    auto publish = [&](int J, const Walk& w, uint32_t& holes) -> bool {
+      const int32_t* pos = p.pos + static_cast<int64_t>(w.tile / p.row_tiles) * p.capacity;
       const int slot0 = w.block * C::kKeys + lane;
       int32_t v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = slot0 + 32 * i < p.used ? __ldg(pos + slot0 + 32 * i) : -1;
       const int st = J & 1;
-      ok = wait_warp(bar(C::kPosFree + st), ((J >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI);
-      if (!ok) break;
+      if (!wait_warp(bar(C::kPosFree + st), ((J >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI)) return false;
       uint32_t top[2] = {0, 0};
-      bool hole = false;
+      holes = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         pos_ring[st * C::kKeys + 32 * i + lane] = v[i];
         top[i / 4] = max(top[i / 4], static_cast<uint32_t>(v[i]));
-        hole |= v[i] < 0 && slot0 + 32 * i < p.used;
+        holes |= v[i] < 0 ? 1u << i : 0u;
       }
       top[0] = __reduce_max_sync(0xffffffffu, top[0]);
       top[1] = __reduce_max_sync(0xffffffffu, top[1]);
       if (lane < 2) pos_top[2 * st + lane] = lane ? top[1] : top[0];
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kPosFull + st));
-      const int i = 2 * J + 1, s = i % C::kSlots;
-      ok = (!C::kMixed || wait_warp(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err,
-                                    ERR_WAIT_MMA)) &&
-           wait_warp(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
-      if (!ok) break;
-      if (__any_sync(0xffffffffu, hole)) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          if (v[r] >= 0) continue;
-          uint4* row = reinterpret_cast<uint4*>(smem + C::kOffRing + s * C::kBlockBytes +
-                                                (32 * r + lane) * 128);
-#pragma unroll
-          for (int d = 0; d < D / 64; ++d)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) row[d * (C::kSub2 / 16) + c] = make_uint4(0, 0, 0, 0);
-        }
-        fence_proxy_async_smem();
+      return true;
+    };
+    // the next half of V into its slot, once the product before last has read that
+    Walk lw(units, blockIdx.x, blocks);
+    int n = 0;
+    auto load = [&]() -> bool {
+      if (!lw.valid()) return true;
+      const int s = n % C::kSlots;
+      if (!wait_warp(bar(C::kVFree + s), ((n / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA))
+        return false;
+      if (lane == 0) {
+        const int lst = lw.tile / p.row_tiles;
+        const int stream = lst / p.groups, group = lst - stream * p.groups;
+        mbar_expect_tx(bar(C::kVFull + s), C::kHalfBytes);
+        for (int d = 0; d < D / 64; ++d)
+          tma_load_4d(base + C::kOffV + s * C::kHalfBytes + d * kSub, &tmV, bar(C::kVFull + s),
+                      64 * d, lw.block * C::kKeys + (n & 1) * kTile, group, stream);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kVReady + (J & 3)));
+      if (n & 1) lw.next(blocks);
+      ++n;
+      return true;
+    };
+    if (lane == 0) prefetch_tmap(&tmV);
+    Walk w(units, blockIdx.x, blocks);
+    uint32_t holes = 0, next_holes = 0;
+    bool ok = !w.valid() || publish(0, w, holes);
+    for (int i = 0; i < C::kSlots - 1 && ok; ++i) ok = load();
+    for (int J = 0; w.valid() && ok; ++J) {
+      w.next(blocks);
+      if (w.valid()) ok = publish(J + 1, w, next_holes);
+#pragma unroll 1
+      for (int h = 0; h < 2 && ok; ++h) {
+        const int i = 2 * J + h, s = i % C::kSlots;
+        ok = wait_warp(bar(C::kVFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
+        if (!ok) break;
+        const uint32_t mine = (holes >> (4 * h)) & 15u;
+        if (__any_sync(0xffffffffu, mine != 0)) {
+#pragma unroll 1
+          for (int r = 0; r < 4; ++r) {
+            if (!((mine >> r) & 1u)) continue;
+            uint4* row = reinterpret_cast<uint4*>(smem + C::kOffV + s * C::kHalfBytes +
+                                                  (32 * r + lane) * 128);
+#pragma unroll
+            for (int d = 0; d < D / 64; ++d)
+#pragma unroll
+              for (int c = 0; c < 8; ++c) row[d * (kSub / 16) + c] = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kVReady + s));
+        ok = load();
+      }
+      holes = next_holes;
     }
-  } else if (warp >= 17) {
+    // nothing may be in flight when the CTA exits
+    if (lane == 0)
+      for (int j = n - 1; j >= 0 && j >= n - C::kSlots; --j)
+        wait(bar(C::kVFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
+  } else if (warp >= 17) {  // 17 and 18
     if (lane == 0) {
       constexpr uint32_t is = Mma<F16, D>::idesc(kTile, false), io = Mma<F16, D>::idesc(D, true);
       const uint32_t s_col = tmem + C::kColS, p_col = tmem + C::kColP, o_col = tmem + C::kColO;
       const uint64_t q0 = sdesc_k_sw128(base);
-      // Q and K of the walk's block, number J, are there
-      auto loaded = [&](int J, const Walk& w) -> bool {
-        const int i = 2 * J, s = i % C::kSlots;
-        return (!w.first || wait(bar(C::kQFull), w.seg & 1, p.err, ERR_WAIT_TMA)) &&
-               (!C::kMixed || wait(bar(C::kKvFree + s), ((i / C::kSlots) & 1) ^ 1, p.err,
-                                   ERR_WAIT_MMA)) &&
-               wait(bar(C::kKvFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
-      };
-      auto scores = [&](int J, int h) {
+      // S of half h of the walk's block, number J, once Q and K are there
+      auto scores = [&](int J, int h, const Walk& w) -> bool {
+        const int i = 2 * J + h, s = i % C::kSlots;
+        if (w.first && (C::kTwoO || h == 0) &&
+            !wait(bar(C::kQFull), w.seg & 1, p.err, ERR_WAIT_TMA))
+          return false;
+        if (!wait(bar(C::kKFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
         tc_fence_after();
-        const uint64_t k0 = sdesc_k_sw128(base + C::kOffRing + (2 * J) % C::kSlots * C::kBlockBytes +
-                                          h * kSub);
+        const uint64_t k0 = sdesc_k_sw128(base + C::kOffK + s * C::kHalfBytes);
 #pragma unroll
         for (int d = 0; d < D / 64; ++d)
           mma4_bf16_ss(s_col + 128u * h, q0 + static_cast<uint64_t>(d * (kSub >> 4)),
-                       k0 + static_cast<uint64_t>(d * (C::kSub2 >> 4)), is, d > 0);
+                       k0 + static_cast<uint64_t>(d * (kSub >> 4)), is, d > 0);
         mma_commit(bar(C::kSFull + h));
+        mma_commit(bar(C::kKFree + s));
+        if (w.last && (C::kTwoO || h == 1)) mma_commit(bar(C::kQFree));
+        return true;
       };
-      // this warp's last scores of the block are issued: K, and Q after a segment, may go
-      auto leave = [&](int J, const Walk& w) {
-        mma_commit(bar(C::kKvFree + (2 * J) % C::kSlots));
-        if (w.last) mma_commit(bar(C::kQFree));
-      };
-      // V of block J has arrived; O of the previous segment has been read
-      auto ready = [&](int J, const Walk& w) -> bool {
-        return wait(bar(C::kVReady + (J & 3)), (J >> 2) & 1, p.err, ERR_WAIT_TMA) &&
-               (!w.first || w.seg == 0 ||
-                wait(bar(C::kORead), (w.seg - 1) & 1, p.err, ERR_WAIT_EPI));
-      };
-      // P V of quarter q of block J into O (the half's own for D = 64)
-      auto values = [&](int J, int q, bool first) -> bool {
-        if (!wait(bar(C::kPFull + q), J & 1, p.err, ERR_WAIT_EPI)) return false;
-        tc_fence_after();
-        const uint64_t v0 = sdesc_mn_sw128(
-            base + C::kOffRing + (2 * J + 1) % C::kSlots * C::kBlockBytes + q * (kSub / 2), C::kSub2);
-        const bool fresh = first && (C::kTwoO ? q % 2 == 0 : q == 0);
-        mma4_ts_mn(o_col + (C::kTwoO ? 64u * (q / 2) : 0u), p_col + 32u * q, v0, io, !fresh);
-        mma_commit(bar(C::kPv + q));
+      // P V of half h of block J into O (the half's own for D = 64), quarter after quarter
+      auto values = [&](int J, int h, const Walk& w) -> bool {
+        const int i = 2 * J + h, s = i % C::kSlots;
+        if (!wait(bar(C::kVReady + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
+        // the previous segment's O has been read
+        if (w.first && w.seg > 0 && (C::kTwoO || h == 0) &&
+            !wait(bar(C::kORead), (w.seg - 1) & 1, p.err, ERR_WAIT_EPI))
+          return false;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int q = 2 * h + x;
+          if (!wait(bar(C::kPFull + q), J & 1, p.err, ERR_WAIT_EPI)) return false;
+          tc_fence_after();
+          const uint64_t v0 =
+              sdesc_mn_sw128(base + C::kOffV + s * C::kHalfBytes + x * (kSub / 2), kSub);
+          const bool fresh = w.first && x == 0 && (C::kTwoO || h == 0);
+          mma4_ts_mn(o_col + (C::kTwoO ? 64u * h : 0u), p_col + 32u * q, v0, io, !fresh);
+          mma_commit(bar(C::kPv + q));
+        }
+        mma_commit(bar(C::kVFree + s));
         return true;
       };
       const int h = warp - 17;
       Walk w(units, blockIdx.x, blocks);
+      bool ok = true;
       if (C::kTwoO) {
-        bool ok = w.valid() && loaded(0, w);
-        if (ok) {
-          scores(0, h);
-          leave(0, w);
-        }
+        ok = w.valid() && scores(0, h, w);
         for (int J = 0; w.valid() && ok; ++J) {
           const Walk here = w;
           w.next(blocks);
-          if (w.valid()) {
-            ok = wait(bar(C::kSRead + h), J & 1, p.err, ERR_WAIT_EPI) && loaded(J + 1, w);
-            if (!ok) break;
-            scores(J + 1, h);
-            leave(J + 1, w);
-          }
-          ok = ready(J, here) && values(J, 2 * h, here.first) && values(J, 2 * h + 1, false);
-          if (ok) mma_commit(bar(C::kKvFree + (2 * J + 1) % C::kSlots));
+          if (w.valid())
+            ok = wait(bar(C::kSRead + h), J & 1, p.err, ERR_WAIT_EPI) && scores(J + 1, h, w);
+          ok = ok && values(J, h, here);
         }
       } else if (h == 0) {
-        bool ok = true;
-        for (int J = 0; w.valid() && ok; w.next(blocks), ++J) {
-          ok = loaded(J, w);
-          for (int x = 0; x < 2 && ok; ++x) {
-            ok = J == 0 || wait(bar(C::kSRead + x), (J - 1) & 1, p.err, ERR_WAIT_EPI);
-            if (ok) scores(J, x);
-          }
-          if (ok) leave(J, w);
-        }
+        for (int J = 0; w.valid() && ok; w.next(blocks), ++J)
+          for (int x = 0; x < 2 && ok; ++x)
+            ok = (J == 0 || wait(bar(C::kSRead + x), (J - 1) & 1, p.err, ERR_WAIT_EPI)) &&
+                 scores(J, x, w);
       } else {
-        bool ok = true;
-        for (int J = 0; w.valid() && ok; w.next(blocks), ++J) {
-          ok = ready(J, w) && values(J, 0, w.first) && values(J, 1, false) &&
-               values(J, 2, false) && values(J, 3, false);
-          if (ok) mma_commit(bar(C::kKvFree + (2 * J + 1) % C::kSlots));
-        }
+        for (int J = 0; w.valid() && ok; w.next(blocks), ++J)
+          ok = values(J, 0, w) && values(J, 1, w);
       }
       mma_commit(bar(C::kDone + h));
       wait(bar(C::kDone + h), 0, p.err, ERR_WAIT_MMA, true);
@@ -467,7 +480,8 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     const bool lead = q % kShare == 0;
     const int prev = lead ? q + kShare - 1 : q - 1;
     volatile float* const my_max = row_max + (C::kTwoO ? 2 * h * kTile : 0) + row;
-    const float c = p.scale_log2;
+    // (a per-thread copy: as a kernel parameter it cost the loops a fifth more instructions)
+    const float c = __shfl_sync(0xffffffffu, p.scale_log2, 0);
     const uint64_t c2 = pack_f32x2(c, c);
     float m = -INFINITY, l = 0.f;
     // the segment's tile and this thread's row in it
@@ -511,7 +525,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           at[i] = static_cast<uint32_t>(pos_ring[st * C::kKeys + 64 * q + 32 * i + lane]);
-#pragma unroll 4
+#pragma unroll 2
         for (int k = 0; k < n_limits; ++k) {
           const uint32_t x = __shfl_sync(0xffffffffu, limits, k);
 #pragma unroll
@@ -925,7 +939,8 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
     const uint32_t col = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * x;
     const uint32_t pos =
         key < p.used ? static_cast<uint32_t>(__ldg(p.pos + list_at + key)) : 0xffffffffu;
-    const float c = p.scale_log2;
+    // (a per-thread copy: as a kernel parameter it cost the loops a fifth more instructions)
+    const float c = __shfl_sync(0xffffffffu, p.scale_log2, 0);
     bool ok = true;
     for (int i = x; i < tiles && ok; i += 2) {
       const int st = i % C::kRowStages;
@@ -1028,14 +1043,12 @@ cudaError_t launch_t(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {
                                 W::kSmem);
   }();
   if (attr != cudaSuccess) return attr;
-  CUtensorMap tq, tk, tv, tk1;
+  CUtensorMap tq, tk, tv;
   if (!make_map(&tq, F16, p.q, D, p.heads, p.n_q, c->streams, p.q_head, p.q_token, p.q_stream,
                 p.per, p.tile_tokens) ||
       !make_map(&tk, F16, p.k, D, p.used, p.groups, c->streams, p.slot_stride, p.group_stride,
-                p.stream_stride, A::kKeys, 1) ||
+                p.stream_stride, kTile, 1) ||
       !make_map(&tv, F16, p.v, D, p.used, p.groups, c->streams, p.slot_stride, p.group_stride,
-                p.stream_stride, A::kKeys, 1) ||
-      !make_map(&tk1, F16, p.k, D, p.used, p.groups, c->streams, p.slot_stride, p.group_stride,
                 p.stream_stride, kTile, 1))
     return cudaErrorInvalidValue;
   cudaError_t e = launch_pdl(attend_kernel<F16, D>, dim3(p.parts), dim3(A::kThreads), A::kSmem, s,
@@ -1045,7 +1058,7 @@ cudaError_t launch_t(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {
                    p);
   if (e != cudaSuccess || p.weight_out == nullptr) return e;
   e = launch_pdl(weigh_kernel<F16, D>, dim3(p.key_tiles, p.row_splits, p.lists), dim3(W::kThreads),
-                 W::kSmem, s, tq, tk1, p);
+                 W::kSmem, s, tq, tk, p);
   if (e != cudaSuccess || p.row_splits == 1) return e;
   const int64_t n = static_cast<int64_t>(p.lists) * p.used;
   return launch_pdl(sum_weights_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0,

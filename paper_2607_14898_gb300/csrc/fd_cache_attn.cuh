@@ -63,6 +63,7 @@ struct Elem<true> {
 
 
 // whether a call runs on the many-rows form: a rule on its sizes, and its plan and workspace
+constexpr int kMaxRows = 32;  // of the few-rows form
 bool chunk_form(int rows, int used);
 struct ChunkPlan {
   int tile_tokens, tile_rows, row_tiles, key_tiles, attend_blocks, parts, row_splits;

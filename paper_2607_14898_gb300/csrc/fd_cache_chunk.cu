@@ -727,18 +727,20 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
   }
 }
 
-// The cut tiles' parts added up: blockIdx.x = tile, blockIdx.y = 4 elements of the head, a thread per
-// row.
+// The cut tiles' parts added up: blockIdx.x + 1 = a CTA of attend, whose first unit may be where a
+// tile was cut (the tile's first cut does the work), blockIdx.y = 4 elements of the head, a thread
+// per row.
 template <bool F16, int D>
 __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant__ CacheAttn p) {
   grid_dep_wait();
   const int blocks = p.attend_blocks;
   const Units units{static_cast<int64_t>(p.lists) * p.row_tiles * blocks, p.parts};
   const int k = blockIdx.y, row = threadIdx.x;
-  const int lst = blockIdx.x / p.row_tiles, tile = blockIdx.x - lst * p.row_tiles;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * blocks;
+  const int gt = static_cast<int>(units.start(blockIdx.x + 1) / blocks);  // tile over all lists
+  const int lst = gt / p.row_tiles, tile = gt - lst * p.row_tiles;
+  const int64_t unit = static_cast<int64_t>(gt) * blocks;
   const int lo = units.owner(unit), hi = units.owner(unit + blocks - 1);
-  if (lo != hi) {
+  if (lo != hi && static_cast<int>(blockIdx.x) == lo) {
     auto part_of = [&](int c) {
       return static_cast<int64_t>(c) * 2 + (units.start(c) > unit ? 0 : 1);
     };
@@ -772,7 +774,7 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
                                                   pack16<F16>(acc.z * inv, acc.w * inv));
     }
     if (k == 0 && row < p.tile_rows)
-      p.lse[static_cast<int64_t>(blockIdx.x) * p.tile_rows + row] =
+      p.lse[static_cast<int64_t>(gt) * p.tile_rows + row] =
           !valid || l == 0.f ? INFINITY : off + log2f(l);
   }
   grid_dep_launch();
@@ -1054,8 +1056,7 @@ cudaError_t launch_t(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {
   cudaError_t e = launch_pdl(attend_kernel<F16, D>, dim3(p.parts), dim3(A::kThreads), A::kSmem, s,
                              tq, tk, tv, p);
   if (e == cudaSuccess && p.parts > 1)
-    e = launch_pdl(join_parts_kernel<F16, D>, dim3(p.lists * p.row_tiles, D / 4), dim3(kTile), 0, s,
-                   p);
+    e = launch_pdl(join_parts_kernel<F16, D>, dim3(p.parts - 1, D / 4), dim3(kTile), 0, s, p);
   if (e != cudaSuccess || p.weight_out == nullptr) return e;
   e = launch_pdl(weigh_kernel<F16, D>, dim3(p.key_tiles, p.row_splits, p.lists), dim3(W::kThreads),
                  W::kSmem, s, tq, tk, p);
@@ -1067,7 +1068,7 @@ cudaError_t launch_t(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {
 
 }  // namespace
 
-bool chunk_form(int rows, int used) { return rows > 32 && used > 0; }
+bool chunk_form(int rows, int used) { return rows > kMaxRows && used > 0; }
 
 ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q) {
   ChunkPlan y{};

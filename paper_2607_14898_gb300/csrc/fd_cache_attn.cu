@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(few::kWarps * 32)
   const int mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
 
   grid_dep_wait();
+  grid_dep_launch();  // the join's blocks may be there, waiting, when the last of these is done
   // tile i of this warp into stage i % kStages
   auto fetch = [&](int i) {
     if (i < mine) {
@@ -288,10 +289,9 @@ __global__ void __launch_bounds__(few::kWarps * 32)
     p.part_o[at * D + d] = acc;
     if (d == 0) p.part_ml[at] = make_float2(top, sum);
   }
-  grid_dep_launch();
 }
 
-// Joins the split parts: a warp per row for the output (the first out_blocks blocks of a list),
+// Joins the split parts: a block per row for the output (the first out_blocks blocks of a list),
 // four slots a thread for the weights (the rest). Every block works out the rows' log2 sums of
 // exponentials for itself: there are kMaxRows rows at most, and a block has 1024 slots to use
 // them on (with 256 the sums took longer than the slots: 23 us for 2 x 65537 slots of 8 groups).
@@ -305,6 +305,7 @@ __global__ void __launch_bounds__(kJoinThreads)
   const int lst = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int stream = lst / p.groups, group = lst - stream * p.groups;
   grid_dep_wait();
+  grid_dep_launch();
   const float2* ml = p.part_ml + static_cast<int64_t>(lst) * p.splits * p.rows;
   // log2 of the row's sum of exponentials (+inf for a row that sees nothing: its weights are 0)
   auto row_lse = [&](int r) {
@@ -323,27 +324,39 @@ __global__ void __launch_bounds__(kJoinThreads)
     return sum == 0.f ? INFINITY : top + log2f(sum);
   };
   if (static_cast<int>(blockIdx.x) < out_blocks) {
-    const int r = blockIdx.x * (kJoinThreads / 32) + warp;
-    if (r < p.rows) {
-      const float lse = row_lse(r);
+    // a block per row: each warp adds up its share of the splits, then the block the warps' sums
+    constexpr int kWarps = kJoinThreads / 32;
+    __shared__ float part[kWarps][D];
+    const int r = blockIdx.x;
+    const float lse = row_lse(r);
+    float acc[D / 32] = {};
+#pragma unroll 4
+    for (int s = warp; s < p.splits; s += kWarps) {
+      const int64_t at = (static_cast<int64_t>(lst) * p.splits + s) * p.rows + r;
+      const float f = ex2_approx(p.part_ml[at].x - lse);
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) {
+        const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + 64 * j + 2 * lane);
+        acc[2 * j] = fmaf(f, x.x, acc[2 * j]);
+        acc[2 * j + 1] = fmaf(f, x.y, acc[2 * j + 1]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+      *reinterpret_cast<float2*>(&part[warp][64 * j + 2 * lane]) =
+          make_float2(acc[2 * j], acc[2 * j + 1]);
+    __syncthreads();
+    if (threadIdx.x < D / 2) {
+      const int d = 2 * threadIdx.x;
+      float a = 0.f, b = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        a += part[w][d];
+        b += part[w][d + 1];
+      }
       const int t = r / p.per, h = group * p.per + r - t * p.per;
       T* out = static_cast<T*>(p.out) + stream * p.out_stream + t * p.out_token + h * p.out_head;
-      float acc[D / 32] = {};
-#pragma unroll 8
-      for (int s = 0; s < p.splits; ++s) {
-        const int64_t at = (static_cast<int64_t>(lst) * p.splits + s) * p.rows + r;
-        const float f = ex2_approx(p.part_ml[at].x - lse);
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-          const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + 64 * j + 2 * lane);
-          acc[2 * j] = fmaf(f, x.x, acc[2 * j]);
-          acc[2 * j + 1] = fmaf(f, x.y, acc[2 * j + 1]);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < D / 64; ++j)
-        *reinterpret_cast<uint32_t*>(out + 64 * j + 2 * lane) =
-            Elem<F16>::pack(acc[2 * j], acc[2 * j + 1]);
+      *reinterpret_cast<uint32_t*>(out + d) = Elem<F16>::pack(a, b);
     }
   } else {
     const int slot = (blockIdx.x - out_blocks) * kJoinSlots + 4 * threadIdx.x;
@@ -374,7 +387,6 @@ __global__ void __launch_bounds__(kJoinThreads)
         if (slot + i < p.used) p.weight_out[at + i] = fmaf(p.decay, old[i], w[i]);
     }
   }
-  grid_dep_launch();
 }
 
 // slots -> (splits, chunk): two CTAs for every SM over all lists and row tiles, at least one
@@ -423,7 +435,7 @@ cudaError_t launch_few(const CacheAttn& p, int lists, cudaStream_t s) {
         launch_pdl(few_rows_kernel<F16, D>, grid, dim3(few::kWarps * 32), few::kSmem, s, p);
     if (e != cudaSuccess) return e;
   }
-  const int out_blocks = (p.rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+  const int out_blocks = p.rows;
   const int slot_blocks = p.weight_out ? (p.used + kJoinSlots - 1) / kJoinSlots : 0;
   return launch_pdl(join_kernel<F16, D>, dim3(out_blocks + slot_blocks, lists), dim3(kJoinThreads),
                     0, s, p, out_blocks);

@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
 
   for (int i = tid; i < kBins0 + kBins1 + kBins2; i += kThreads) sm.hist[i] = 0;
   grid_dep_wait();
+  grid_dep_launch();
   const int64_t protect =
       static_cast<int64_t>(p.newest ? p.newest[static_cast<int64_t>(stream) * p.newest_stride] : 0) -
       p.recent;
@@ -453,7 +454,6 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       p.dst_v[to] = zero;
     }
   }
-  grid_dep_launch();
   if (!ALONE) cluster.sync();  // no CTA leaves while another may still read its shared memory
 }
 

@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(kThreads)
   const int lane = threadIdx.x - local * p.lanes;
   const int64_t slot = static_cast<int64_t>(blockIdx.x) * per_block + local;
   grid_dep_wait();
+  grid_dep_launch();
   if (local < per_block && slot < static_cast<int64_t>(p.tokens) * p.head_slots) {
     const int token = static_cast<int>(slot / p.head_slots);
     const int first = static_cast<int>(slot - static_cast<int64_t>(token) * p.head_slots);
@@ -170,7 +171,6 @@ __global__ void __launch_bounds__(kThreads)
       }
     }
   }
-  grid_dep_launch();
 }
 
 template <typename T, int NV>

@@ -6,23 +6,25 @@
 // and the weight's bits made monotone; the n-th smallest key T is found by radix selection (class
 // with 11 bits, then 11 and 10 bits), and of the slots whose key is T the first e in slot order are
 // given up, so equal weights fall to the lowest index. (The first digit reaches two bits into
-// the mantissa: with the class as bits of the digit it ended at the exponent, most slots fell
-// into some twenty counters, and counting them took longer than all else.) Keys are integers and counts are sums of
-// integers: the choice does not depend on the order in which threads run.
+// the mantissa: with the class as bits of an 11-bit digit it ended at the exponent, most slots fell
+// into some twenty counters, and counting them took longer than all else.) Keys are integers and
+// counts are sums of integers: the choice does not depend on the order in which threads run. A
+// scan of counts then gives every slot that is taken (or kept) its place in slot order, and its
+// position, weight and row move, 16 bytes of a row a thread.
 //
-// One cluster of 1 to 8 CTAs per list. Keys are read once into registers, each warp
-// holding consecutive slots, and histograms are counted in shared memory. Up to kAloneSlots every
-// CTA of the cluster selects from the whole list by itself, and the cluster only shares the
-// writing: more reads from L2, but no exchange, whose steps (a cluster barrier and a round
-// trip through distributed shared memory, three times) took longer than the rest. Longer lists are
-// cut between the CTAs and the histograms summed over the cluster. One scan of counts over
-// warps (and CTAs) gives every slot that is taken (or kept) its place in slot order. Then the
-// cluster writes the list's positions and weights and moves the rows, 16 bytes a thread. For one
-// new token the selection is a minimum over (class, weight, slot) packed into 54 bits, one exchange
-// only, so there the list is always cut.
+// One cluster of 1 to 8 CTAs of 1024 threads per list, in two forms:
+//   short (up to kShortSlots): every CTA selects from the whole list by itself, keys in registers,
+//     and writes its share of the slots. More reads from L2, but no exchange between CTAs,
+//     whose steps (a cluster barrier and a round trip through distributed shared memory, four
+//     times) take longer than all else in a list this size.
+//   long: the list is cut between the CTAs, histograms are summed over the cluster through
+//     distributed shared memory. Up to 24 keys a thread in registers; beyond that (196608 slots in 8
+//     CTAs) they are read again for every digit.
+// For one new token the selection is a minimum over (class, weight, slot) packed into 54 bits: the
+// long form, with one exchange.
 //
-// Bound by memory for long rows (the copied keys and values) and by the latency of the dependent steps for
-// short ones: the positions and weights of a list are 8 bytes a slot.
+// Bound by memory for long rows (the copied keys and values) and by the latency of the dependent
+// steps for short ones: the positions and weights of a list are 8 bytes a slot.
 #include <cooperative_groups.h>
 
 #include "fd_internal.h"
@@ -38,17 +40,15 @@ constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxSlots = 1 << 20;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxKeys = 32;  // keys a thread holds in registers
-constexpr int kAloneSlots = 8 * kThreads;
+constexpr int kShortSlots = 8 * kThreads;
 // Radix digits: class 0 is bin 0 of the first, classes 1 and 2 have 2048 bins each for bits 21..31 (the
 // last of them is never used: the largest key, NaN, is below it); then bits 10..20 and 0..9.
 constexpr int kBins0 = 4096, kBins1 = 2048, kBins2 = 1024;
-constexpr int kHist = kAloneSlots;  // counters; afterwards the list of a CTA that selects alone
-static_assert(kBins0 + kBins1 + kBins2 <= kHist, "counters");
+constexpr int kHist = kBins0 + kBins1 + kBins2;
 
 struct EvictParams {
   int groups, slots, n;      // slots looked at, slots given up, per list
-  int iters;                 // slots a thread has: kThreads * iters (* cluster size) >= slots
+  int iters;                 // slots of a thread (long form)
   int sinks, recent;
   const int32_t* newest;     // per stream, newest_stride apart: the position recency counts from
   int newest_stride;
@@ -68,94 +68,393 @@ struct EvictParams {
   int row16;                 // 16-byte units of a row
 };
 
-// rank key: class in bits 32.., the weight's bits in ascending order below. -0 is +0, NaN is the
-// largest; an empty slot's weight does not count.
-__device__ __forceinline__ uint64_t rank_key(int32_t pos, float w, int sinks, int64_t protect) {
-  if (pos < 0) return 0;
+// A slot's class and its weight's bits in ascending order: -0 is +0, NaN is the largest, an empty
+// slot's weight does not count. protect >= 0.
+struct Rank {
+  uint32_t cls, low;
+};
+__device__ __forceinline__ Rank rank_of(int32_t pos, float w, int sinks, int protect) {
   uint32_t b = __float_as_uint(w);
   if (b == 0x80000000u) b = 0;
   b = w != w ? 0xffc00000u : (b & 0x80000000u ? ~b : b | 0x80000000u);
-  const uint64_t cls = pos < sinks || pos >= protect ? 2 : 1;
-  return (cls << 32) | b;
+  if (pos < 0) return {0, 0};
+  return {pos < sinks || pos >= protect ? 2u : 1u, b};
+}
+// The position from which entries are protected as recent (at least 0: below are empty ones).
+__device__ __forceinline__ int protect_from(const EvictParams& p, int stream) {
+  if (p.newest == nullptr) return 0;
+  const int64_t x = static_cast<int64_t>(p.newest[static_cast<int64_t>(stream) * p.newest_stride]) -
+                    p.recent;
+  return x < 0 ? 0 : static_cast<int>(x);
+}
+// Once the class of the n-th key is known, 32 bits order the slots: classes before it are 0, it has
+// the weight's bits (0 for class 0, never 0 or all ones for the others), classes after it, and
+// places past the list's end (class 3), all ones.
+__device__ __forceinline__ uint32_t order_of(Rank r, uint32_t cls) {
+  return r.cls == cls ? r.low : (r.cls < cls ? 0u : 0xffffffffu);
 }
 
-// The keys of a thread: in registers (KPT > 0), or read again for every use (long lists).
-template <int KPT>
-struct Keys {
-  uint32_t low[KPT];
-  uint64_t cls;  // 2 bits each, 3: past the end of the list
-  __device__ __forceinline__ void load(const EvictParams& p, int64_t at, int slot0, int64_t protect) {
-    cls = ~0ull;
-    int32_t ps[KPT];
-    float ws[KPT];
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      const int slot = slot0 + 32 * i;
-      const bool in = i < p.iters && slot < p.slots;
-      ps[i] = in ? p.pos[at + slot] : 0;
-      ws[i] = in ? p.weight[at + slot] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      const uint64_t key = rank_key(ps[i], ws[i], p.sinks, protect);
-      low[i] = static_cast<uint32_t>(key);
-      if (i < p.iters && slot0 + 32 * i < p.slots)
-        cls ^= (3ull ^ (key >> 32)) << (2 * i);
-    }
+// What has been found: slots with order below `limit` are given up, and of those at it the first
+// `ties` in slot order, or all (then `all`). With n = 0: limit 0, no ties.
+struct Cut {
+  uint32_t cls, limit, ties;
+  bool all;
+  // whatever the other slots: given up, or (compact) kept
+  template <bool COMPACT>
+  __device__ __forceinline__ bool sure(uint32_t x, bool in) const {
+    if (COMPACT) return in && x > limit;
+    return in && (x < limit || (all && x == limit));
   }
-  __device__ __forceinline__ uint64_t get(const EvictParams&, int64_t, int, int64_t, int i) const {
-    return (((cls >> (2 * i)) & 3ull) << 32) | low[i];
+  __device__ __forceinline__ bool tie(uint32_t x, bool in) const { return !all && in && x == limit; }
+  // list entries among slots with na sure ones and nb ties
+  template <bool COMPACT>
+  __device__ __forceinline__ uint32_t place(uint32_t na, uint32_t nb) const {
+    if (COMPACT) return na + (cls >= 1 && nb > ties ? nb - ties : 0u);
+    return na + (nb < ties ? nb : ties);
   }
-};
-template <>
-struct Keys<0> {
-  __device__ __forceinline__ void load(const EvictParams&, int64_t, int, int64_t) {}
-  __device__ __forceinline__ uint64_t get(const EvictParams& p, int64_t at, int slot0,
-                                          int64_t protect, int i) const {
-    const int slot = slot0 + 32 * i;
-    return slot < p.slots ? rank_key(p.pos[at + slot], p.weight[at + slot], p.sinks, protect)
-                          : 3ull << 32;
+  template <bool COMPACT>
+  __device__ __forceinline__ bool tie_in(uint32_t nb) const {  // nb ties before it
+    return COMPACT ? cls >= 1 && nb >= ties : nb < ties;
   }
 };
 
-struct Shared {
-  alignas(16) uint32_t hist[kHist];
-  uint32_t warp_a[kWarps], warp_b[kWarps];
-  uint64_t warp_min[kWarps];
-  uint64_t cta_min;
-  uint32_t cta_a, cta_b;
-  uint32_t digit, rest, found;  // the radix pass's result
+struct Found {
+  uint32_t digit, rest, count;  // the bin, what is left to take in it, what it holds
 };
-
-// exclusive prefix of v over the block's threads (and the total)
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* warp_sums, uint32_t* total) {
+// The bin that holds the rest-th item (1-based); c: counts of this thread's PER consecutive bins.
+template <int PER>
+__device__ __forceinline__ Found find_bin(const uint32_t (&c)[PER], uint32_t rest, uint32_t* sums,
+                                          Found* out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t x = v;
+  uint32_t sum = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) sum += c[j];
+  uint32_t x = sum;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
     if (lane >= d) x += y;
   }
-  if (lane == 31) warp_sums[warp] = x;
+  if (lane == 31) sums[warp] = x;
   __syncthreads();
-  uint32_t s = warp_sums[lane];
+  uint32_t s = sums[lane];
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const uint32_t y = __shfl_up_sync(0xffffffffu, s, d);
     if (lane >= d) s += y;
   }
-  *total = __shfl_sync(0xffffffffu, s, 31);
-  const uint32_t before = __shfl_sync(0xffffffffu, s, warp == 0 ? 0 : warp - 1);
+  const int at = __ffs(__ballot_sync(0xffffffffu, s >= rest)) - 1;  // the warp that has it
+  if (warp == at) {
+    uint32_t before = __shfl_sync(0xffffffffu, s, at) - sums[at] + x - sum;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if (before < rest && rest <= before + c[j])
+        *out = {static_cast<uint32_t>(threadIdx.x * PER + j), rest - before, c[j]};
+      before += c[j];
+    }
+  }
   __syncthreads();
-  return (warp == 0 ? 0 : before) + x - v;
+  return *out;
 }
 
-// COMPACT: the slots that are not given up go to the destination; else the given-up slots are
-// taken by new tokens. ALONE: each CTA selects from the whole list, and writes for its share of
-// the warps.
-template <int KPT, bool COMPACT, bool ALONE>
-__global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constant__ EvictParams p) {
-  __shared__ Shared sm;
+// The three digits. count(pass, high): adds this CTA's slots to the pass's counters; share(): makes all
+// CTAs' counters readable; add(h, c): adds the counters h of every CTA to this thread's c;
+// settle(cls): called once the class is known.
+struct Selector {
+  uint32_t* hist;
+  uint32_t* sums;
+  Found* out;
+  template <class Count, class Share, class Add, class Settle>
+  __device__ __forceinline__ Cut run(uint32_t n, Count count, Share share, Add add, Settle settle) {
+    Cut cut{0, 0, 0, false};
+    if (n == 0) {
+      settle(0u);
+      return cut;
+    }
+    Found f;
+    {
+      uint32_t c[4] = {0, 0, 0, 0};
+      count(0, 0u);
+      share();
+      add(hist, c);
+      f = find_bin<4>(c, n, sums, out);
+    }
+    cut.cls = f.digit == 0 ? 0 : 1 + (f.digit - 1) / 2048;
+    settle(cut.cls);
+    if (cut.cls > 0) {
+      uint32_t high = (f.digit - 1) % 2048;
+      {
+        uint32_t c[2] = {0, 0};
+        count(1, high);
+        share();
+        add(hist + kBins0, c);
+        f = find_bin<2>(c, f.rest, sums, out);
+      }
+      high = (high << 11) | f.digit;
+      {
+        uint32_t c[1] = {0};
+        count(2, high);
+        share();
+        add(hist + kBins0 + kBins1, c);
+        f = find_bin<1>(c, f.rest, sums, out);
+      }
+      cut.limit = (high << 10) | f.digit;
+    }
+    cut.all = f.rest == f.count;
+    cut.ties = cut.all ? 0 : f.rest;
+    // class 0 is all one key; with all of it given up the limit is below every kept slot
+    return cut;
+  }
+};
+__device__ __forceinline__ void count_class(uint32_t* hist, Rank r) {
+  if (r.cls < 3) atomicAdd(hist + (r.cls == 0 ? 0 : 1 + (r.cls - 1) * 2048 + (r.low >> 21)), 1u);
+}
+__device__ __forceinline__ void count_order(uint32_t* hist, int pass, uint32_t high, uint32_t x) {
+  if ((x >> (pass == 1 ? 21 : 10)) == high && x != 0xffffffffu)
+    atomicAdd(hist + (pass == 1 ? kBins0 + ((x >> 10) & 0x7ff) : kBins0 + kBins1 + (x & 0x3ff)), 1u);
+}
+template <int PER>
+__device__ __forceinline__ void add_bins(const uint32_t* h, uint32_t (&c)[PER]) {
+  if constexpr (PER == 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(h + 4 * threadIdx.x);
+    c[0] += x.x, c[1] += x.y, c[2] += x.z, c[3] += x.w;
+  } else if constexpr (PER == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(h + 2 * threadIdx.x);
+    c[0] += x.x, c[1] += x.y;
+  } else {
+    c[0] += h[threadIdx.x];
+  }
+}
+
+// Rows of the list entries [first, first + count): 16 bytes of a key and of a value per thread and
+// step. slot_of(v): entry v's slot.
+template <bool COMPACT, class SlotOf>
+__device__ __forceinline__ void copy_rows(const EvictParams& p, int stream, int group,
+                                          uint32_t first, uint32_t count, SlotOf slot_of) {
+  const int64_t src0 = stream * p.src_stream + group * p.src_group;
+  const int64_t dst0 = stream * p.dst_stream + group * p.dst_group;
+  const int shift = p.row16 == 8 ? 3 : 4;  // 16-byte units of a row: 8 or 16
+  const uint32_t items = count << shift;   // at most 2^24
+  constexpr int kUnroll = 4;
+  for (uint32_t it0 = threadIdx.x; it0 < items; it0 += kUnroll * kThreads) {
+    uint4 xk[kUnroll], xv[kUnroll];
+    int64_t to[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t it = it0 + u * kThreads;
+      if (it >= items) continue;
+      const int64_t v = first + (it >> shift);
+      const int part = static_cast<int>(it & (p.row16 - 1));
+      const int64_t slot = slot_of(static_cast<uint32_t>(v));
+      const int64_t from = src0 + (COMPACT ? slot : v) * p.src_row + part;
+      to[u] = dst0 + (COMPACT ? v : slot) * p.dst_row + part;
+      xk[u] = p.src_k[from];
+      xv[u] = p.src_v[from];
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (it0 + u * kThreads >= items) continue;
+      p.dst_k[to[u]] = xk[u];
+      p.dst_v[to[u]] = xv[u];
+    }
+  }
+}
+// A compacted list's empty end: entries [kept, list_len), shared between the CTAs.
+__device__ __forceinline__ void clear_end(const EvictParams& p, int lst, int stream, int group,
+                                          uint32_t kept, int rank, int ctas) {
+  int32_t* list = p.list + static_cast<int64_t>(lst) * p.list_len;
+  const int64_t out_at = static_cast<int64_t>(lst) * p.out_pitch;
+  const uint32_t first = kept + rank * kThreads + threadIdx.x;
+  for (uint32_t v = first; v < static_cast<uint32_t>(p.list_len); v += ctas * kThreads) {
+    list[v] = -1;
+    p.pos_out[out_at + v] = -1;
+    p.weight_out[out_at + v] = 0.f;
+  }
+  const int64_t dst0 = stream * p.dst_stream + group * p.dst_group;
+  const int64_t end = (static_cast<int64_t>(p.list_len) - kept) * p.row16;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (int64_t it = rank * kThreads + threadIdx.x; it < end; it += static_cast<int64_t>(ctas) * kThreads) {
+    const int64_t to = dst0 + (kept + it / p.row16) * p.dst_row + it % p.row16;
+    p.dst_k[to] = zero;
+    p.dst_v[to] = zero;
+  }
+}
+
+// ---------------------------------------------------------------- short lists
+// Round r is slots 32 r .. 32 r + 31: for the selection warp w has rounds w, w + 32, .. of the whole
+// list, for the writing CTA c of the cluster has an equal run of them, a warp per round.
+template <int KPT, bool COMPACT>
+__global__ void __launch_bounds__(kThreads, 1)
+    evict_short_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kRounds = KPT * kWarps;
+  // counters, then the list of this CTA's share (all slots, where it is alone)
+  constexpr int kShared = KPT * kThreads > kHist ? KPT * kThreads : kHist;
+  __shared__ alignas(16) uint32_t hist[kShared];
+  __shared__ uint32_t sums[kWarps], before_a[kRounds + 1], before_b[kRounds + 1];
+  __shared__ Found found;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = static_cast<int>(cluster.num_blocks());
+  const int rank = static_cast<int>(cluster.block_rank());
+  const int lst = blockIdx.x / ctas;
+  const int stream = lst / p.groups, group = lst - stream * p.groups;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t at = static_cast<int64_t>(lst) * p.pitch;
+  for (int i = tid; i < kHist; i += kThreads) hist[i] = 0;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int protect = protect_from(p, stream);
+  uint32_t low[KPT], cls = 0;
+  {
+    int32_t ps[KPT];
+    float ws[KPT];
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int slot = i * kThreads + tid;
+      ps[i] = slot < p.slots ? p.pos[at + slot] : 0;
+      ws[i] = slot < p.slots ? p.weight[at + slot] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      Rank r = rank_of(ps[i], ws[i], p.sinks, protect);
+      if (i * kThreads + tid >= p.slots) r.cls = 3;
+      low[i] = r.low;
+      cls |= r.cls << (2 * i);
+    }
+  }
+  // positions and weights may be written in place: not before every CTA has read them
+  __syncthreads();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  Selector select{hist, sums, &found};
+  const Cut cut = select.run(
+      static_cast<uint32_t>(p.n),
+      [&](int pass, uint32_t high) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+          if (pass == 0) count_class(hist, {(cls >> (2 * i)) & 3u, low[i]});
+          else count_order(hist, pass, high, low[i]);
+        }
+      },
+      [] { __syncthreads(); }, [](const uint32_t* h, auto& c) { add_bins(h, c); },
+      [&](uint32_t c) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) low[i] = order_of({(cls >> (2 * i)) & 3u, low[i]}, c);
+      });
+  // counts of every round, then of all rounds before it
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) {
+    const bool in = i * kThreads + tid < p.slots;
+    const uint32_t a = __ballot_sync(0xffffffffu, cut.sure<COMPACT>(low[i], in));
+    const uint32_t b = __ballot_sync(0xffffffffu, cut.tie(low[i], in));
+    if (lane == 0) {
+      before_a[i * kWarps + warp] = __popc(a);
+      before_b[i * kWarps + warp] = __popc(b);
+    }
+  }
+  __syncthreads();
+  if (warp == 0) {  // kRounds / 32 entries a lane
+    uint32_t a[KPT], b[KPT], sa = 0, sb = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      a[i] = before_a[lane * KPT + i];
+      b[i] = before_b[lane * KPT + i];
+      sa += a[i];
+      sb += b[i];
+    }
+    uint32_t xa = sa, xb = sb;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t ya = __shfl_up_sync(0xffffffffu, xa, d), yb = __shfl_up_sync(0xffffffffu, xb, d);
+      if (lane >= d) {
+        xa += ya;
+        xb += yb;
+      }
+    }
+    if (lane == 31) {
+      before_a[kRounds] = xa;
+      before_b[kRounds] = xb;
+    }
+    xa -= sa;
+    xb -= sb;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      before_a[lane * KPT + i] = xa;
+      before_b[lane * KPT + i] = xb;
+      xa += a[i];
+      xb += b[i];
+    }
+  }
+  __syncthreads();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+  // ---- this CTA's rounds
+  const int rounds = (p.slots + 31) / 32;
+  const int r0 = rounds * rank / ctas, r1 = rounds * (rank + 1) / ctas;
+  const uint32_t first = cut.place<COMPACT>(before_a[r0], before_b[r0]);
+  const uint32_t count = cut.place<COMPACT>(before_a[r1], before_b[r1]) - first;
+  const uint32_t kept = cut.place<COMPACT>(before_a[kRounds], before_b[kRounds]);
+  const bool copy_pos = p.pos_out != p.pos, copy_weight = p.weight_out != p.weight;
+  const int32_t* np = p.new_pos ? p.new_pos + static_cast<int64_t>(stream) * p.n : nullptr;
+  int32_t* list = p.list + static_cast<int64_t>(lst) * p.list_len;
+  const int64_t out_at = static_cast<int64_t>(lst) * p.out_pitch;
+  constexpr int kGroup = 2;
+  for (int ra = r0 + warp; ra < r1; ra += kGroup * kWarps) {
+    int32_t ps[kGroup];
+    float ws[kGroup];
+#pragma unroll
+    for (int u = 0; u < kGroup; ++u) {
+      const int r = ra + u * kWarps, slot = 32 * r + lane;
+      const bool in = r < r1 && slot < p.slots;
+      ps[u] = in ? p.pos[at + slot] : 0;
+      ws[u] = in ? p.weight[at + slot] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kGroup; ++u) {
+      const int r = ra + u * kWarps, slot = 32 * r + lane;
+      if (r >= r1) break;
+      const bool in = slot < p.slots;
+      const uint32_t x = order_of(rank_of(ps[u], ws[u], p.sinks, protect), cut.cls);
+      const uint32_t a = __ballot_sync(0xffffffffu, cut.sure<COMPACT>(x, in));
+      const uint32_t b = __ballot_sync(0xffffffffu, cut.tie(x, in));
+      const uint32_t below = (1u << lane) - 1;
+      const uint32_t na = before_a[r] + __popc(a & below), nb = before_b[r] + __popc(b & below);
+      const bool take = ((a >> lane) & 1u) || (((b >> lane) & 1u) && cut.tie_in<COMPACT>(nb));
+      const uint32_t v = cut.place<COMPACT>(na, nb);
+      if (take) {
+        list[v] = slot;
+        hist[v - first] = slot;
+      }
+      if (COMPACT) {
+        if (take) {
+          p.pos_out[out_at + v] = ps[u];
+          p.weight_out[out_at + v] = ws[u];
+        }
+      } else if (in) {
+        if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[v] : ps[u];
+        if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : ws[u];
+      }
+    }
+  }
+  __syncthreads();
+  copy_rows<COMPACT>(p, stream, group, first, count,
+                     [&](uint32_t v) { return static_cast<int64_t>(hist[v - first]); });
+  if (COMPACT) clear_end(p, lst, stream, group, kept, rank, ctas);
+}
+
+// ---------------------------------------------------------------- long lists, and one new token
+// The keys of a thread: KPT in registers, or (0) read again for every use. Warps hold consecutive
+// slots: the thread's i-th is slot0 + 32 i.
+struct LongShared {
+  alignas(16) uint32_t hist[kHist];
+  uint32_t sums[kWarps], warp_a[kWarps], warp_b[kWarps];
+  uint64_t warp_min[kWarps], cta_min;
+  uint32_t cta_a, cta_b;
+  Found found;
+};
+
+template <int KPT, bool COMPACT>
+__global__ void __launch_bounds__(kThreads, 1)
+    evict_long_kernel(const __grid_constant__ EvictParams p) {
+  __shared__ LongShared sm;
   cg::cluster_group cluster = cg::this_cluster();
   const int ctas = static_cast<int>(cluster.num_blocks());
   const int rank = static_cast<int>(cluster.block_rank());
@@ -163,33 +462,56 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
   const int stream = lst / p.groups, group = lst - stream * p.groups;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int iters = p.iters;
-  const int slot0 = ((ALONE ? 0 : rank * kWarps) + warp) * 32 * iters + lane;  // i-th: + 32 i
+  const int slot0 = (rank * kWarps + warp) * 32 * iters + lane;
   const int64_t at = static_cast<int64_t>(lst) * p.pitch;
-
-  for (int i = tid; i < kBins0 + kBins1 + kBins2; i += kThreads) sm.hist[i] = 0;
+  for (int i = tid; i < kHist; i += kThreads) sm.hist[i] = 0;
   grid_dep_wait();
   grid_dep_launch();
-  const int64_t protect =
-      static_cast<int64_t>(p.newest ? p.newest[static_cast<int64_t>(stream) * p.newest_stride] : 0) -
-      p.recent;
-  Keys<KPT> keys;
-  keys.load(p, at, slot0, protect);
-  // positions and weights may be written in place: not before every CTA has read them
-  if (ALONE) {
-    __syncthreads();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  const int protect = protect_from(p, stream);
+  constexpr int kRegs = KPT > 0 ? KPT : 1, kGroup = KPT >= 4 || KPT == 0 ? 4 : 2;
+  uint32_t low[kRegs];
+  uint64_t cls = 0;
+  if (KPT > 0) {
+#pragma unroll
+    for (int i0 = 0; i0 < KPT; i0 += kGroup) {
+      int32_t ps[kGroup];
+      float ws[kGroup];
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) {
+        const int slot = slot0 + 32 * (i0 + u);
+        const bool in = i0 + u < iters && slot < p.slots;
+        ps[u] = in ? p.pos[at + slot] : 0;
+        ws[u] = in ? p.weight[at + slot] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) {
+        const int i = i0 + u;
+        Rank r = rank_of(ps[u], ws[u], p.sinks, protect);
+        if (i >= iters || slot0 + 32 * i >= p.slots) r.cls = 3;
+        low[i % kRegs] = r.low;
+        cls |= static_cast<uint64_t>(r.cls) << (2 * i);
+      }
+    }
   }
-  auto key_of = [&](int i) { return keys.get(p, at, slot0, protect, i); };
+  auto rank_at = [&](int i) -> Rank {
+    if (KPT > 0) return {static_cast<uint32_t>(cls >> (2 * i)) & 3u, low[i % kRegs]};
+    const int slot = slot0 + 32 * i;
+    if (slot >= p.slots) return {3, 0};
+    return rank_of(p.pos[at + slot], p.weight[at + slot], p.sinks, protect);
+  };
 #define FOR_KEYS(i) _Pragma("unroll") for (int i = 0; i < (KPT > 0 ? KPT : iters); ++i) if (KPT == 0 || i < iters)
-
-  uint64_t limit = 0;   // T: the n-th smallest key
-  uint32_t ties = 0;    // e: so many of the slots with key T are given up
-  int only = -1;        // the slot, where a minimum tells it
-  if (!COMPACT && !ALONE && p.n == 1) {
+  int32_t* list = p.list + static_cast<int64_t>(lst) * p.list_len;
+  const int64_t out_at = static_cast<int64_t>(lst) * p.out_pitch;
+  const int32_t* np = p.new_pos ? p.new_pos + static_cast<int64_t>(stream) * p.n : nullptr;
+  const bool copy_pos = p.pos_out != p.pos, copy_weight = p.weight_out != p.weight;
+  uint32_t first = 0, count = 0, kept = 0;  // this CTA's list entries; all of the list's
+  if (!COMPACT && p.n == 1) {
     uint64_t best = ~0ull;
     FOR_KEYS(i) {
-      const uint64_t k = (key_of(i) << 20) | static_cast<uint32_t>(slot0 + 32 * i);
-      if (slot0 + 32 * i < p.slots && k < best) best = k;
+      const Rank r = rank_at(i);
+      const uint64_t k = (static_cast<uint64_t>(r.cls) << 52) | (static_cast<uint64_t>(r.low) << 20) |
+                         static_cast<uint32_t>(slot0 + 32 * i);
+      if (r.cls < 3 && k < best) best = k;
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
@@ -215,79 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
         const uint64_t o = *cluster.map_shared_rank(&sm.cta_min, c);
         best = o < best ? o : best;
       }
-    only = static_cast<int>(best & (kMaxSlots - 1));
-  } else if (p.n > 0) {
-    __syncthreads();
-    uint32_t rest = static_cast<uint32_t>(p.n);
-    uint64_t high = 0;  // the digits found so far, in their places
-#pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-      if (pass > 0 && high == 0) break;  // class 0: equal keys
-      uint32_t* hist = sm.hist + (pass == 0 ? 0 : pass == 1 ? kBins0 : kBins0 + kBins1);
-      FOR_KEYS(i) {
-        const uint64_t k = key_of(i);
-        const uint32_t cls = static_cast<uint32_t>(k >> 32), low = static_cast<uint32_t>(k);
-        if (pass == 0 ? cls < 3 : (k >> (pass == 1 ? 21 : 10)) == high)
-          atomicAdd(hist + (pass == 0 ? (cls == 0 ? 0 : 1 + (cls - 1) * 2048 + (low >> 21))
-                                      : pass == 1 ? (low >> 10) & 0x7ff : low & 0x3ff), 1u);
-      }
-      constexpr int kPer[3] = {kBins0 / kThreads, kBins1 / kThreads, kBins2 / kThreads};
-      const int per = kPer[pass];  // 4, 2 or 1 bins a thread
-      uint32_t c[4] = {0, 0, 0, 0}, sum = 0;
-      auto add = [&](const uint32_t* h) {
-        if (per == 4) {
-          const uint4 x = *reinterpret_cast<const uint4*>(h + 4 * tid);
-          c[0] += x.x, c[1] += x.y, c[2] += x.z, c[3] += x.w;
-        } else if (per == 2) {
-          const uint2 x = *reinterpret_cast<const uint2*>(h + 2 * tid);
-          c[0] += x.x, c[1] += x.y;
-        } else {
-          c[0] += h[tid];
-        }
-      };
-      if (ALONE) {
-        __syncthreads();
-        add(hist);
-      } else {
-        cluster.sync();
-#pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r)
-          if (r < ctas) add(cluster.map_shared_rank(hist, r));
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += c[j];
-      uint32_t total;
-      uint32_t before = block_scan(sum, sm.warp_a, &total);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (j < per && before < rest && rest <= before + c[j]) {
-          sm.digit = tid * per + j;
-          sm.rest = rest - before;
-        }
-        before += c[j];
-      }
-      __syncthreads();
-      const uint32_t digit = sm.digit;
-      rest = sm.rest;
-      if (pass == 0)
-        high = digit == 0 ? 0 : (static_cast<uint64_t>(1 + (digit - 1) / 2048) << 11) | ((digit - 1) % 2048);
-      else
-        high = (high << (pass == 1 ? 11 : 10)) | digit;
-      __syncthreads();
-    }
-    limit = high;
-    ties = rest;
-  }
-
-  // slots moved by this CTA: list entries [first, first + count)
-  uint32_t first = 0, count = 0;
-  const int32_t* np = p.new_pos ? p.new_pos + static_cast<int64_t>(stream) * p.n : nullptr;
-  int32_t* list = p.list + static_cast<int64_t>(lst) * p.list_len;
-  const int64_t out_at = static_cast<int64_t>(lst) * p.out_pitch;
-  const bool copy_pos = p.pos_out != p.pos, copy_weight = p.weight_out != p.weight;
-  uint32_t kept = 0;  // entries of the whole list
-  if (ALONE) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  if (only >= 0) {
+    const int only = static_cast<int>(best & (kMaxSlots - 1));
     FOR_KEYS(i) {
       const int slot = slot0 + 32 * i;
       if (slot < p.slots) {
@@ -301,16 +551,37 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
     const int base = rank * kWarps * 32 * iters;
     if (only >= base && only < base + kWarps * 32 * iters) count = 1;
   } else {
-    // counts of this warp: slots that are taken (kept) whatever the ties, and ties
-    const uint32_t tie_cls = static_cast<uint32_t>(limit >> 32);
-    auto sure = [&](uint64_t k) {
-      return COMPACT ? k > limit && (k >> 32) >= 1 && (k >> 32) < 3 : k < limit;
+    __syncthreads();
+    Selector select{sm.hist, sm.sums, &sm.found};
+    uint32_t settled = 0;
+    const Cut cut = select.run(
+        static_cast<uint32_t>(p.n),
+        [&](int pass, uint32_t high) {
+          FOR_KEYS(i) {
+            if (pass == 0) count_class(sm.hist, rank_at(i));
+            else count_order(sm.hist, pass, high, KPT > 0 ? low[i % kRegs] : order_of(rank_at(i), settled));
+          }
+        },
+        [&] { cluster.sync(); },
+        [&](const uint32_t* h, auto& c) {
+#pragma unroll
+          for (int r = 0; r < kMaxCluster; ++r)
+            if (r < ctas) add_bins(cluster.map_shared_rank(h, r), c);
+        },
+        [&](uint32_t c) {
+          settled = c;
+          if (KPT > 0) FOR_KEYS(i) low[i % kRegs] = order_of(rank_at(i), c);
+        });
+    auto order_at = [&](int i) -> uint32_t {
+      return KPT > 0 ? low[i % kRegs] : order_of(rank_at(i), settled);
     };
+    // counts of this warp, of the warps before it, and of the CTAs before this one
     uint32_t a = 0, b = 0;
     FOR_KEYS(i) {
-      const uint64_t k = key_of(i);
-      a += sure(k);
-      b += k == limit;
+      const bool in = slot0 + 32 * i < p.slots;
+      const uint32_t x = order_at(i);
+      a += cut.sure<COMPACT>(x, in);
+      b += cut.tie(x, in);
     }
     a = __reduce_add_sync(0xffffffffu, a);
     b = __reduce_add_sync(0xffffffffu, b);
@@ -319,146 +590,82 @@ __global__ void __launch_bounds__(kThreads, 1) evict_kernel(const __grid_constan
       sm.warp_b[warp] = b;
     }
     __syncthreads();
-    uint32_t wa = sm.warp_a[lane], wb = sm.warp_b[lane];
-    const uint32_t ca = __reduce_add_sync(0xffffffffu, wa), cb = __reduce_add_sync(0xffffffffu, wb);
-    wa = __reduce_add_sync(0xffffffffu, lane < warp ? wa : 0u);
-    wb = __reduce_add_sync(0xffffffffu, lane < warp ? wb : 0u);
-    // before this CTA's slots, and in the whole list
-    uint32_t before_a = 0, before_b = 0, all_a = ca, all_b = cb;
-    if (!ALONE) {
-      if (tid == 0) {
-        sm.cta_a = ca;
-        sm.cta_b = cb;
-      }
-      cluster.sync();
-      all_a = all_b = 0;
+    uint32_t na = sm.warp_a[lane], nb = sm.warp_b[lane];
+    const uint32_t ca = __reduce_add_sync(0xffffffffu, na), cb = __reduce_add_sync(0xffffffffu, nb);
+    na = __reduce_add_sync(0xffffffffu, lane < warp ? na : 0u);
+    nb = __reduce_add_sync(0xffffffffu, lane < warp ? nb : 0u);
+    if (tid == 0) {
+      sm.cta_a = ca;
+      sm.cta_b = cb;
+    }
+    cluster.sync();
+    uint32_t front_a = 0, front_b = 0, all_a = 0, all_b = 0;
 #pragma unroll
-      for (int r = 0; r < kMaxCluster; ++r)
-        if (r < ctas) {
-          const uint32_t ra = *cluster.map_shared_rank(&sm.cta_a, r);
-          const uint32_t rb = *cluster.map_shared_rank(&sm.cta_b, r);
-          before_a += r < rank ? ra : 0;
-          before_b += r < rank ? rb : 0;
-          all_a += ra;
-          all_b += rb;
-        }
-    }
-    // list entries among the slots before a point with na sure ones and nb ties before it
-    auto place = [&](uint32_t na, uint32_t nb) -> uint32_t {
-      if (COMPACT) return na + (tie_cls >= 1 && nb > ties ? nb - ties : 0u);
-      return na + (nb < ties ? nb : ties);
-    };
-    kept = place(all_a, all_b);
-    if (ALONE) {  // an equal share
-      first = static_cast<uint32_t>(static_cast<uint64_t>(kept) * rank / ctas);
-      count = static_cast<uint32_t>(static_cast<uint64_t>(kept) * (rank + 1) / ctas) - first;
-    } else {
-      first = place(before_a, before_b);
-      count = place(before_a + ca, before_b + cb) - first;
-    }
-    uint32_t na = before_a + wa, nb = before_b + wb;
-    if (ALONE) __syncthreads();  // the counters have been read
-    // positions and weights first, so that no load waits for the store before it
-    constexpr int kGroup = 4;
+    for (int r = 0; r < kMaxCluster; ++r)
+      if (r < ctas) {
+        const uint32_t ra = *cluster.map_shared_rank(&sm.cta_a, r);
+        const uint32_t rb = *cluster.map_shared_rank(&sm.cta_b, r);
+        front_a += r < rank ? ra : 0;
+        front_b += r < rank ? rb : 0;
+        all_a += ra;
+        all_b += rb;
+      }
+    first = cut.place<COMPACT>(front_a, front_b);
+    count = cut.place<COMPACT>(front_a + ca, front_b + cb) - first;
+    kept = cut.place<COMPACT>(all_a, all_b);
+    na += front_a;
+    nb += front_b;
+    // positions and weights a group ahead, so that no load waits for the store before it
 #pragma unroll
     for (int i0 = 0; i0 < (KPT > 0 ? KPT : iters); i0 += kGroup) {
       if (i0 >= iters) break;
       int32_t ps[kGroup];
       float ws[kGroup];
+      uint32_t xs[kGroup];
 #pragma unroll
       for (int u = 0; u < kGroup; ++u) {
         const int i = i0 + u, slot = slot0 + 32 * i;
-        // alone: the CTAs write for the warps' rounds in turn
-        const bool mine = i < iters && slot < p.slots && (!ALONE || i % ctas == rank);
-        ps[u] = mine && (COMPACT || copy_pos) ? p.pos[at + slot] : 0;
-        ws[u] = mine && (COMPACT || copy_weight) ? p.weight[at + slot] : 0.f;
+        const bool in = i < iters && slot < p.slots;
+        ps[u] = in && (COMPACT || copy_pos) ? p.pos[at + slot] : 0;
+        ws[u] = in && (COMPACT || copy_weight) ? p.weight[at + slot] : 0.f;
+        xs[u] = i < iters ? order_at(i) : 0xffffffffu;
       }
 #pragma unroll
       for (int u = 0; u < kGroup; ++u) {
         const int i = i0 + u, slot = slot0 + 32 * i;
         if (i >= iters) break;
-        const uint64_t k = key_of(KPT > 0 && i >= KPT ? 0 : i);
-        const bool is_a = sure(k), is_b = k == limit;
-        const uint32_t ma = __ballot_sync(0xffffffffu, is_a), mb = __ballot_sync(0xffffffffu, is_b);
+        const bool in = slot < p.slots;
+        const uint32_t ma = __ballot_sync(0xffffffffu, cut.sure<COMPACT>(xs[u], in));
+        const uint32_t mb = __ballot_sync(0xffffffffu, cut.tie(xs[u], in));
         const uint32_t below = (1u << lane) - 1;
         const uint32_t la = na + __popc(ma & below), lb = nb + __popc(mb & below);
-        const bool tie_in = is_b && (COMPACT ? tie_cls >= 1 && lb >= ties : lb < ties);
-        const bool take = is_a || tie_in;
-        const uint32_t v = place(la, lb);
-        if (slot < p.slots) {
-          if (ALONE && take) sm.hist[v] = slot;
-          if (!ALONE && take) list[v] = slot;
-          if (!ALONE || i % ctas == rank) {
-            if (COMPACT) {
-              if (take) {
-                p.pos_out[out_at + v] = ps[u];
-                p.weight_out[out_at + v] = ws[u];
-              }
-            } else {
-              if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[v] : ps[u];
-              if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : ws[u];
-            }
+        const bool take = ((ma >> lane) & 1u) || (((mb >> lane) & 1u) && cut.tie_in<COMPACT>(lb));
+        const uint32_t v = cut.place<COMPACT>(la, lb);
+        if (take) list[v] = slot;
+        if (COMPACT) {
+          if (take) {
+            p.pos_out[out_at + v] = ps[u];
+            p.weight_out[out_at + v] = ws[u];
           }
+        } else if (in) {
+          if (take || copy_pos) p.pos_out[out_at + slot] = take ? np[v] : ps[u];
+          if (take || copy_weight) p.weight_out[out_at + slot] = take ? 0.f : ws[u];
         }
         na += __popc(ma);
         nb += __popc(mb);
       }
     }
-    if (COMPACT) {  // the destination's empty end
-      for (int v = static_cast<int>(kept) + rank * kThreads + tid; v < p.list_len; v += ctas * kThreads) {
-        list[v] = -1;
-        p.pos_out[out_at + v] = -1;
-        p.weight_out[out_at + v] = 0.f;
-      }
-    }
   }
 #undef FOR_KEYS
-
-  // ---- rows: the entries of this CTA, 16 bytes of a key and of a value per thread and step
   __syncthreads();  // this CTA's part of the list is written
-  if (ALONE)
-    for (uint32_t v = first + tid; v < first + count; v += kThreads) list[v] = sm.hist[v];
-  const int64_t src0 = stream * p.src_stream + group * p.src_group;
-  const int64_t dst0 = stream * p.dst_stream + group * p.dst_group;
-  const int r16 = p.row16;  // 8 or 16
-  const int64_t items = static_cast<int64_t>(count) * r16;
-  constexpr int kUnroll = 4;
-  for (int64_t it0 = tid; it0 < items; it0 += kUnroll * kThreads) {
-    uint4 xk[kUnroll], xv[kUnroll];
-    int64_t to[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t it = it0 + u * kThreads;
-      if (it >= items) continue;
-      const int64_t v = first + it / r16;
-      const int part = static_cast<int>(it % r16);
-      const int64_t slot = ALONE ? static_cast<int64_t>(sm.hist[v]) : list[v];
-      const int64_t from = src0 + (COMPACT ? slot : v) * p.src_row + part;
-      to[u] = dst0 + (COMPACT ? v : slot) * p.dst_row + part;
-      xk[u] = p.src_k[from];
-      xv[u] = p.src_v[from];
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (it0 + u * kThreads >= items) continue;
-      p.dst_k[to[u]] = xk[u];
-      p.dst_v[to[u]] = xv[u];
-    }
-  }
-  if (COMPACT) {
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    const int64_t end = static_cast<int64_t>(p.list_len - static_cast<int>(kept)) * r16;
-    for (int64_t it = rank * kThreads + tid; it < end; it += static_cast<int64_t>(ctas) * kThreads) {
-      const int64_t to = dst0 + (kept + it / r16) * p.dst_row + it % r16;
-      p.dst_k[to] = zero;
-      p.dst_v[to] = zero;
-    }
-  }
-  if (!ALONE) cluster.sync();  // no CTA leaves while another may still read its shared memory
+  copy_rows<COMPACT>(p, stream, group, first, count,
+                     [&](uint32_t v) { return static_cast<int64_t>(list[v]); });
+  if (COMPACT) clear_end(p, lst, stream, group, kept, rank, ctas);
+  cluster.sync();  // no CTA leaves while another may still read its shared memory
 }
 
-template <int KPT, bool COMPACT, bool ALONE>
-cudaError_t launch_evict(const EvictParams& p, int lists, int ctas, cudaStream_t s) {
+cudaError_t launch_cluster(void (*kernel)(EvictParams), const EvictParams& p, int lists, int ctas,
+                           cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(lists) * ctas);
   cfg.blockDim = dim3(kThreads);
@@ -472,7 +679,7 @@ cudaError_t launch_evict(const EvictParams& p, int lists, int ctas, cudaStream_t
   at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, evict_kernel<KPT, COMPACT, ALONE>, p);
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 // CTAs of a cluster: as many as keep the lists' clusters on the GPU at once, but no fewer than
@@ -483,17 +690,18 @@ cudaError_t launch(EvictParams& p, int lists, cudaStream_t s) {
   while (ctas < kMaxCluster && 2 * ctas * static_cast<int64_t>(lists) <= num_sms() &&
          p.slots > 1024 * ctas)
     ctas *= 2;
-  const bool alone = p.slots <= kAloneSlots && (COMPACT || p.n != 1);
-  const int per = alone ? kThreads : kThreads * ctas;
+  if (p.slots <= kShortSlots && (COMPACT || p.n != 1)) {
+    if (p.slots <= 2 * kThreads)
+      return launch_cluster(evict_short_kernel<2, COMPACT>, p, lists, ctas, s);
+    return launch_cluster(evict_short_kernel<8, COMPACT>, p, lists, ctas, s);
+  }
+  const int per = kThreads * ctas;
   p.iters = (p.slots + per - 1) / per;
   if (p.iters < 1) p.iters = 1;
-  if (alone)
-    return p.iters <= 2 ? launch_evict<2, COMPACT, true>(p, lists, ctas, s)
-                        : launch_evict<8, COMPACT, true>(p, lists, ctas, s);
-  if (!COMPACT && p.iters <= 2) return launch_evict<2, COMPACT, false>(p, lists, ctas, s);
-  if (p.iters <= 12) return launch_evict<12, COMPACT, false>(p, lists, ctas, s);
-  if (p.iters <= kMaxKeys) return launch_evict<kMaxKeys, COMPACT, false>(p, lists, ctas, s);
-  return launch_evict<0, COMPACT, false>(p, lists, ctas, s);
+  if (!COMPACT && p.iters <= 2) return launch_cluster(evict_long_kernel<2, COMPACT>, p, lists, ctas, s);
+  if (p.iters <= 12) return launch_cluster(evict_long_kernel<12, COMPACT>, p, lists, ctas, s);
+  if (p.iters <= 24) return launch_cluster(evict_long_kernel<24, COMPACT>, p, lists, ctas, s);
+  return launch_cluster(evict_long_kernel<0, COMPACT>, p, lists, ctas, s);
 }
 
 bool aligned(const void* x, uintptr_t a) { return reinterpret_cast<uintptr_t>(x) % a == 0; }

@@ -332,6 +332,9 @@ INSERTS = [
     (1, 1, 64, 20011, 3001, torch.bfloat16, "dense", 16, 10 ** 6, 0.0),
     (80, 1, 64, 1025, 100, torch.bfloat16, "dense", 0, 300, 0.5),
     (77, 1, 64, 33000, 129, torch.bfloat16, "dense", 2, 5000, 0.01),
+    (77, 1, 64, 30000, 1, torch.bfloat16, "dense", 2, 5000, 0.0),
+    (80, 1, 64, 8192, 8192, torch.bfloat16, "dense", 2, 5000, 0.0),
+    (2, 1, 64, 65537, 20000, torch.float16, "dense", 2, 5000, 0.0),
 ]
 
 
@@ -376,6 +379,9 @@ COMPACTS = [
     (2, 1, 64, 50, 50, 1, torch.bfloat16, "dense", 0, 0, 1.0),
     (1, 2, 128, 20011, 20011, 4099, torch.float16, "dense", 16, 1000, 0.01),
     (80, 1, 64, 33000, 33000, 129, torch.bfloat16, "dense", 2, 50, 0.01),
+    (80, 1, 64, 8192, 8192, 8100, torch.bfloat16, "dense", 2, 50, 0.0),
+    (80, 1, 64, 8193, 8193, 8000, torch.float16, "dense", 2, 50, 0.001),
+    (1, 1, 64, 100000, 100000, 50000, torch.bfloat16, "dense", 2, 50, 0.001),
 ]
 
 

@@ -959,7 +959,16 @@ constexpr int kMaxAttnParts = 4096;  // CTAs of one attention launch (fd_op_atte
 }  // namespace
 
 namespace fd {
-fd_status check_device() { return ::check_device(); }
+// the answer per device is asked for once: it is on the way of every small call
+fd_status check_device() {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FD_ERR_CUDA;
+  if (dev >= 0 && dev < 64 && known[dev].load(std::memory_order_relaxed) == 1) return FD_OK;
+  const fd_status st = ::check_device();
+  if (st == FD_OK && dev >= 0 && dev < 64) known[dev].store(1, std::memory_order_relaxed);
+  return st;
+}
 int num_sms() { return ::num_sms(); }
 bool tmap_16bit_4d(CUtensorMap* m, bool is_f16, const void* base, const uint64_t dims[4],
                    const uint64_t strides[3], uint32_t box1, uint32_t box2) {

@@ -670,12 +670,18 @@ def _dtype_code(dtype) -> int:
     return code
 
 
+_raw_stream = None
+
+
 def _stream_on(device: int, stream) -> int:
     """The stream's handle; of the device's current stream where none is given. (The handle alone:
     a torch.cuda.Stream object takes 3 us to make, half of what a small call takes in all.)"""
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(device)
+        if _raw_stream is None:
+            import torch
+            _raw_stream = torch._C._cuda_getCurrentRawStream
+        return _raw_stream(device)
     return int(getattr(stream, "cuda_stream", stream))
 
 

@@ -389,13 +389,13 @@ __global__ void __launch_bounds__(kJoinThreads)
   }
 }
 
-// slots -> (splits, chunk): two CTAs for every SM over all lists and row tiles, at least one
-// tile for each warp of a CTA
+// slots -> (splits, chunk): two CTAs for every SM over all lists and row tiles, at least a tile for
+// each warp of a CTA, runs of 32 slots so that the last split is not left with a small rest
 void plan_few(int lists, int row_tiles, int used, int* splits, int* chunk) {
   const int64_t want = 2 * kSms / std::max<int64_t>(1, static_cast<int64_t>(lists) * row_tiles);
   int n = static_cast<int>(std::max<int64_t>(1, want));
-  int c = (used + n - 1) / n;
-  c = (c + 127) / 128 * 128;
+  int c = std::max((used + n - 1) / n, 128);
+  c = (c + 31) / 32 * 32;
   *chunk = c;
   *splits = (used + c - 1) / c;
 }

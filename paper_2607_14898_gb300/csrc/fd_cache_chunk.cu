@@ -13,6 +13,7 @@
 // Products: 4 rows used D flops for attend, 2 rows used D for weigh (bf16 or fp16 in, fp32
 // accumulation in TMEM), and two exponentials for each score.
 #include <algorithm>
+#include <type_traits>
 
 #include "fd_cache_attn.cuh"
 
@@ -45,14 +46,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
-      : "memory");
-}
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // 64 steps of K: A from TMEM (16 steps are 8 columns), B MN-major (16 steps are 2048 bytes)
@@ -122,6 +115,18 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* er
                   wait_more_warp(bar, parity, err, code);
   __syncwarp();
   return ok;
+}
+
+// 16 lanes of the warp's quarter and 32 columns in 16 x 8 fragments: of fragment j thread t gets
+// columns 8 j + 2 (t % 4), + 1 of lane t / 4 (r[4 j], r[4 j + 1]) and of lane t / 4 + 8
+__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
 }
 
 constexpr int kTile = 128;      // rows of a tile, slots of a block
@@ -783,9 +788,11 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
 // ------------------------------------------------------------------------------ weigh
 //
 // A CTA has one block of 128 slots of one list and a run of the list's row tiles: S^T = K Q^T, K
-// from shared memory all along, Q tiles through a ring. A thread has one slot (TMEM lane) and
-// adds exp2(c s - lse_r) over the tile's rows; two groups of warps take the tiles in turn, each
-// with its own accumulator in TMEM. Two CTAs fit an SM.
+// from shared memory all along, Q tiles through a ring; two groups of warps take the tiles in turn,
+// each with its own accumulator in TMEM, and add exp2(c s - lse_r) over a tile's rows. Two CTAs
+// fit an SM. Scores come out of TMEM in 16 x 8 fragments: a thread has 4 slots and every fourth
+// pair of rows, so that a row's lse and limit, read from shared memory, serve 4 scores (with a slot
+// a thread and all rows the reads were what bounded the kernel).
 //   warps 0-3 / 4-7  even / odd tiles   warp 8  TMA   warp 9  products   warp 10  lse and limits
 template <int D>
 struct WeighCfg {
@@ -860,8 +867,9 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
+  // this thread's slot in the end
   float total = 0.f;
-  const int key = block * kTile + (warp & 3) * 32 + lane;
+  const int key = block * kTile + (warp & 3) * 32 + (lane & 3) * 8 + (lane >> 2);
   const int64_t list_at = static_cast<int64_t>(lst) * p.capacity;
   if (!aligned) {
   } else if (warp == 8) {
@@ -897,9 +905,9 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
         tc_fence_after();
         const uint64_t q0 = sdesc_k_sw128(base + C::kOffQ + s * C::kTileBytes);
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          const uint64_t at = static_cast<uint64_t>((d / 4) * (kSub >> 4) + (d % 4) * 2);
-          mma_ss(tmem + 128u * x, k0 + at, q0 + at, idesc, d > 0);
+        for (int d = 0; d < D / 64; ++d) {
+          const uint64_t at = static_cast<uint64_t>(d * (kSub >> 4));
+          mma4_bf16_ss(tmem + 128u * x, k0 + at, q0 + at, idesc, d > 0);
         }
         mma_commit(bar(C::kTFull + x));
         mma_commit(bar(C::kQFree + s));
@@ -929,7 +937,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
       if (!ok) break;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        row_lse[st * kTile + 32 * j + lane] = lse[j];
+        row_lse[st * kTile + 32 * j + lane] = -lse[j];
         row_lim[st * kTile + 32 * j + lane] = lim[j];
       }
       if (lane == 0) row_low[st] = low;
@@ -939,10 +947,21 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
   } else if (warp < 8) {
     const int x = warp >> 2;
     const uint32_t col = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * x;
-    const uint32_t pos =
-        key < p.used ? static_cast<uint32_t>(__ldg(p.pos + list_at + key)) : 0xffffffffu;
+    // slot k of the four: lane 8 k + lane / 4 of the warp's quarter; an empty one's sum is not used
+    uint32_t pos[4], top = 0;
+    bool hole[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int slot = block * kTile + (warp & 3) * 32 + 8 * k + (lane >> 2);
+      pos[k] = slot < p.used ? static_cast<uint32_t>(__ldg(p.pos + list_at + slot)) : 0xffffffffu;
+      hole[k] = static_cast<int32_t>(pos[k]) < 0;
+      top = max(top, hole[k] ? 0u : pos[k]);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
     // (a per-thread copy: as a kernel parameter it cost the loops a fifth more instructions)
     const float c = __shfl_sync(0xffffffffu, p.scale_log2, 0);
+    const uint64_t c2 = pack_f32x2(c, c);
+    float totals[4] = {0.f, 0.f, 0.f, 0.f};
     bool ok = true;
     for (int i = x; i < tiles && ok; i += 2) {
       const int st = i % C::kRowStages;
@@ -950,46 +969,61 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
            wait_warp(bar(C::kTFull + x), (i >> 1) & 1, p.err, ERR_WAIT_MMA);
       if (!ok) break;
       tc_fence_after();
-      // an empty slot's sum is not used, so it does not matter here
-      const bool all = __all_sync(0xffffffffu, pos < row_low[st] || static_cast<int32_t>(pos) < 0);
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      uint64_t sum2[4] = {0, 0, 0, 0};  // even and odd rows
+      auto add = [&](auto masked) {
 #pragma unroll
-      for (int d = 0; d < kTile; d += 32) {
-        uint32_t sr[32];
-        tmem_ld_32x32b_x32(col + d, sr);
-        tmem_ld_wait();
-        if (d == kTile - 32) {
-          tc_fence_before();
-          mbar_arrive(bar(C::kTFree + x));
-        }
-        const float4* ls = reinterpret_cast<const float4*>(row_lse + st * kTile + d);
-        if (all) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const float4 v = ls[e / 4];
-            sum[0] += ex2_approx(fmaf(__uint_as_float(sr[e]), c, -v.x));
-            sum[1] += ex2_approx(fmaf(__uint_as_float(sr[e + 1]), c, -v.y));
-            sum[2] += ex2_approx(fmaf(__uint_as_float(sr[e + 2]), c, -v.z));
-            sum[3] += ex2_approx(fmaf(__uint_as_float(sr[e + 3]), c, -v.w));
+        for (int d = 0; d < kTile; d += 32) {
+          uint32_t sr[2][16];  // slots 0 and 1, slots 2 and 3
+          tmem_ld_16x256b_x4(col + d, sr[0]);
+          tmem_ld_16x256b_x4(col + (16u << 16) + d, sr[1]);
+          tmem_ld_wait();
+          if (d == kTile - 32) {
+            tc_fence_before();
+            mbar_arrive(bar(C::kTFree + x));
           }
-        } else {
-          const uint4* lm = reinterpret_cast<const uint4*>(row_lim + st * kTile + d);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const float4 v = ls[e / 4];
-            const uint4 b = lm[e / 4];
-            if (pos < b.x) sum[0] += ex2_approx(fmaf(__uint_as_float(sr[e]), c, -v.x));
-            if (pos < b.y) sum[1] += ex2_approx(fmaf(__uint_as_float(sr[e + 1]), c, -v.y));
-            if (pos < b.z) sum[2] += ex2_approx(fmaf(__uint_as_float(sr[e + 2]), c, -v.z));
-            if (pos < b.w) sum[3] += ex2_approx(fmaf(__uint_as_float(sr[e + 3]), c, -v.w));
+          for (int j = 0; j < 4; ++j) {
+            const int at = st * kTile + d + 8 * j + 2 * (lane & 3);
+            const uint64_t lse2 = *reinterpret_cast<const uint64_t*>(row_lse + at);  // negated
+            uint2 lim;
+            if constexpr (decltype(masked)::value) lim = *reinterpret_cast<const uint2*>(row_lim + at);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint64_t v;
+              asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(sr[k / 2][4 * j + 2 * (k % 2)]),
+                  "r"(sr[k / 2][4 * j + 2 * (k % 2) + 1]));
+              asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(v), "l"(c2), "l"(lse2));
+              float e0, e1;
+              asm("mov.b64 {%0, %1}, %2;" : "=f"(e0), "=f"(e1) : "l"(v));
+              e0 = ex2_approx(e0);
+              e1 = ex2_approx(e1);
+              if constexpr (decltype(masked)::value) {
+                e0 = pos[k] < lim.x ? e0 : 0.f;
+                e1 = pos[k] < lim.y ? e1 : 0.f;
+              }
+              asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[k]) : "l"(pack_f32x2(e0, e1)));
+            }
           }
         }
+      };
+      if (top < row_low[st]) add(std::false_type{});
+      else add(std::true_type{});
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float s0, s1;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum2[k]));
+        totals[k] += s0 + s1;
       }
-      total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kRowFree + st));
     }
-    if (static_cast<int32_t>(pos) < 0) total = 0.f;
+    // the four threads of a slot have shared out the rows; thread t keeps slot t % 4
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      totals[k] += __shfl_xor_sync(0xffffffffu, totals[k], 1);
+      totals[k] += __shfl_xor_sync(0xffffffffu, totals[k], 2);
+      if ((lane & 3) == k) total = hole[k] ? 0.f : totals[k];
+    }
   }
   float* sums = reinterpret_cast<float*>(smem + C::kOffSum);
   if (warp >= 4 && warp < 8) sums[(warp & 3) * 32 + lane] = total;

@@ -291,11 +291,13 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
       int i = 0, segs = 0;  // i: halves so far
+      int stream = 0, group = 0;
       bool ok = true;
       for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks)) {
-        const int lst = w.tile / p.row_tiles;
-        const int stream = lst / p.groups, group = lst - stream * p.groups;
         if (w.first) {
+          const int lst = w.tile / p.row_tiles;
+          stream = lst / p.groups;
+          group = lst - stream * p.groups;
           ok = w.seg == 0 || wait(bar(C::kQFree), (w.seg - 1) & 1, p.err, ERR_WAIT_MMA);
           if (!ok) break;
           mbar_expect_tx(bar(C::kQFull), p.tile_rows * D * 2);
@@ -322,8 +324,9 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
   } else if (warp == 19) {
     // ---- positions, a block ahead, and empty slots' values
     // publishes block J's positions; bit i of `holes`: the lane's slot 32 i + lane is empty
+    const int32_t* pos = p.pos;
     auto publish = [&](int J, const Walk& w, uint32_t& holes) -> bool {
-      const int32_t* pos = p.pos + static_cast<int64_t>(w.tile / p.row_tiles) * p.capacity;
+      if (w.first) pos = p.pos + static_cast<int64_t>(w.tile / p.row_tiles) * p.capacity;
       const int slot0 = w.block * C::kKeys + lane;
       int32_t v[8];
 #pragma unroll
@@ -347,15 +350,18 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     };
     // the next half of V into its slot, once the product before last has read that
     Walk lw(units, blockIdx.x, blocks);
-    int n = 0;
+    int n = 0, stream = 0, group = 0;
     auto load = [&]() -> bool {
       if (!lw.valid()) return true;
       const int s = n % C::kSlots;
       if (!wait_warp(bar(C::kVFree + s), ((n / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA))
         return false;
-      if (lane == 0) {
+      if (lw.first && (n & 1) == 0) {
         const int lst = lw.tile / p.row_tiles;
-        const int stream = lst / p.groups, group = lst - stream * p.groups;
+        stream = lst / p.groups;
+        group = lst - stream * p.groups;
+      }
+      if (lane == 0) {
         mbar_expect_tx(bar(C::kVFull + s), C::kHalfBytes);
         for (int d = 0; d < D / 64; ++d)
           tma_load_4d(base + C::kOffV + s * C::kHalfBytes + d * kSub, &tmV, bar(C::kVFull + s),
@@ -917,6 +923,10 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
     }
   } else if (warp == 10) {
     bool ok = true;
+    int token_of[4];  // within the tile
+#pragma unroll
+    for (int j = 0; j < 4; ++j) token_of[j] = (32 * j + lane) / p.per;
+    const int32_t* q_pos = p.q_pos + static_cast<int64_t>(stream) * p.n_q;
     for (int i = 0; i < tiles && ok; ++i) {
       const int st = i % C::kRowStages;
       const int64_t at = (static_cast<int64_t>(lst) * p.row_tiles + first + i) * p.tile_rows;
@@ -925,10 +935,10 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = 32 * j + lane;
-        const int token = (first + i) * p.tile_tokens + r / p.per;
+        const int token = (first + i) * p.tile_tokens + token_of[j];
         const bool in = r < p.tile_rows && token < p.n_q;
         lse[j] = in ? __ldcg(p.lse + at + r) : INFINITY;
-        const int qp = in ? __ldg(p.q_pos + static_cast<int64_t>(stream) * p.n_q + token) : -1;
+        const int qp = in ? __ldg(q_pos + token) : -1;
         lim[j] = qp < 0 ? 0u : static_cast<uint32_t>(qp) + 1u;
         if (in) low = min(low, lim[j]);
       }

@@ -1,0 +1,94 @@
+"""One attention layer's cache of bounded size for streams that never end.
+
+The decoder's own caches keep the last W chunks. A BoundedStream keeps, in the same memory for
+any length of stream, the entries that attention has used most: each step turns the new queries
+and keys by their positions, puts the new keys and values into the slots of the entries with the
+least accumulated weight, and attends over the slots, adding to their weights. A step is three
+library calls (fd_op_rotary, fd_op_cache_insert, fd_op_cache_attention) on buffers that are
+allocated once for each step size, so that once the cache is full steps can be captured in a CUDA
+graph.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import flashdec as fdp
+
+
+class BoundedStream:
+    """Caches of `streams` streams with `capacity` slots for each KV group.
+
+    plan: the Rotary that turns queries and keys (None: they come turned). sinks, recent: entries at
+    positions below `sinks` or among the last `recent` before the step's first token are given up last.
+    decay: the weights gathered so far are multiplied by it before a step's are added."""
+
+    def __init__(self, streams, heads, groups, head_dim, capacity, dtype=torch.bfloat16, plan=None,
+                 sinks=4, recent=0, decay=1.0, device="cuda"):
+        self.heads, self.plan = heads, plan
+        self.sinks, self.recent, self.decay = sinks, recent, decay
+        shape = (streams, groups, capacity)
+        k = torch.zeros(*shape, head_dim, dtype=dtype, device=device)
+        self.cache = fdp.Cache(k, torch.zeros_like(k),
+                               torch.full(shape, -1, dtype=torch.int32, device=device),
+                               torch.zeros(shape, device=device))
+        self.filled = 0  # slots that may hold something: new tokens take empty slots in order
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self._buffers: dict = {}
+
+    def _buffer(self, name, shape, dtype):
+        """A buffer of the step, allocated when its size first comes up."""
+        key = (name, tuple(shape))
+        t = self._buffers.get(key)
+        if t is None:
+            t = self._buffers[key] = torch.empty(shape, dtype=dtype, device=self.err.device)
+        return t
+
+    def step(self, q, k, v, pos, axes_pos=None, whole_chunk=False, stream=None):
+        """Attention of q [streams][n][heads][head_dim] over the cache with the new k, v
+        [streams][n][groups][head_dim] in it; returns out like q (a buffer that the next step of
+        n tokens overwrites). pos int32 [streams][n]: ascending positions, those of the rotary
+        embedding too unless axes_pos int32 [streams][n][axes] gives its own. whole_chunk: every
+        token sees all n new tokens, as in the decoder's chunks; else a token sees no later one."""
+        S, n, H, D = q.shape
+        c = self.cache
+        G = c.groups
+        if self.plan is not None:
+            turn = (pos if axes_pos is None else axes_pos).reshape(S * n, -1)
+            q_t, k_t = (self._buffer("q", q.shape, q.dtype), self._buffer("k", k.shape, k.dtype))
+            fdp.op_rotary(self.plan, turn, q.reshape(S * n, H, D), q_t.view(S * n, H, D),
+                          k.reshape(S * n, G, D), k_t.view(S * n, G, D), stream=stream)
+            q, k = q_t, k_t
+        slots = self._buffer("slots", (S, G, n), torch.int32)
+        fdp.op_cache_insert(c, k, v, pos, slots, sinks=self.sinks, recent=self.recent,
+                            stream=stream)
+        self.filled = min(c.capacity, self.filled + n)
+        out = self._buffer("out", (S, n, H, D), c.dtype)
+        # what a call needs does not only grow with the slots: take the larger of now and full
+        need = max(fdp.cache_attention_workspace_bytes(c, H, n, u)
+                   for u in (self.filled, c.capacity))
+        work = self._buffer("work", (need,), torch.uint8)
+        q_pos = pos[:, -1:].expand(S, n).contiguous() if whole_chunk else pos
+        fdp.op_cache_attention(c, q, q_pos, out, weight_out=c.weight, used=self.filled,
+                               decay=self.decay, workspace=work, err=self.err, stream=stream)
+        return out
+
+    def compact(self, capacity, now, stream=None):
+        """A BoundedStream of fewer slots that holds this one's most used entries; now int32
+        [streams]: the next token's position (recency counts from it)."""
+        c = self.cache
+        used = self.filled
+        new = BoundedStream(c.streams, self.heads, c.groups, c.head_dim, capacity, c.dtype,
+                            self.plan, self.sinks, self.recent, self.decay, self.err.device)
+        came = torch.empty(c.streams, c.groups, capacity, dtype=torch.int32,
+                           device=self.err.device)
+        # slots past the filled ones are empty, so they may count where they are needed
+        fdp.op_cache_compact(c, new.cache, now, came, used=max(used, capacity), sinks=self.sinks,
+                             recent=self.recent, stream=stream)
+        new.filled = min(capacity, used)
+        return new
+
+    def check(self) -> None:
+        """Raises if a kernel of an earlier step gave up a wait (synchronises)."""
+        code = int(self.err)
+        if code:
+            raise RuntimeError(f"bounded cache: status word {code}")

@@ -98,7 +98,9 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, in
   return mbar_try_wait(bar, parity) || wait_more(bar, parity, err, code, drain);
 }
 // The same for a whole warp that stays together (tcgen05 loads and stores, which follow such
-// waits, have to be executed by all its lanes at once): every decision is the warp's.
+// waits, have to be executed by all its lanes at once): every decision is the warp's, so that its
+// lanes never part. (Each instruction that only brings lanes together, or waits for a barrier that
+// is through already, took 100 to 200 cycles of the attend kernel's softmax.)
 __device__ __noinline__ bool wait_more_warp(uint32_t bar, uint32_t parity, int* err, int code) {
 #pragma unroll 1
   for (int n = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
@@ -111,10 +113,8 @@ __device__ __noinline__ bool wait_more_warp(uint32_t bar, uint32_t parity, int* 
   return true;
 }
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, int code) {
-  const bool ok = __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||
-                  wait_more_warp(bar, parity, err, code);
-  __syncwarp();
-  return ok;
+  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||
+         wait_more_warp(bar, parity, err, code);
 }
 
 // 16 lanes of the warp's quarter and 32 columns in 16 x 8 fragments: of fragment j thread t gets
@@ -151,8 +151,8 @@ constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swiz
 //                 size, so two of them share the work. D = 64: those of the block's first and
 //                 second half, each half with a running maximum and an O of its own; D = 128: S of
 //                 both halves, and P V into the one O that TMEM has room for.
-//   warp 19       positions of each block, a block ahead; V by half blocks, with zeros for the
-//                 values of empty slots (their probability is 0, but 0 times NaN is NaN)
+//   warp 19       positions of each block, on the barrier of its scores; V by half blocks, with
+//                 zeros for the values of empty slots (their probability is 0, but 0 times NaN is NaN)
 // TMEM (512 columns): S 2 x 128, P 2 x 64 (two 16-bit values a column), O 2 x 64 or 128. S takes the
 // next scores once the softmax has it in registers.
 template <int D>
@@ -169,19 +169,18 @@ struct AttendCfg {
   static constexpr int kOffK = kQBytes;
   static constexpr int kOffV = kOffK + kSlots * kHalfBytes;
   static constexpr int kOffPos = kOffV + kSlots * kHalfBytes;
-  static constexpr int kOffMax = kOffPos + 2 * kKeys * 4;  // two blocks' positions before it
+  static constexpr int kOffMax = kOffPos + kKeys * 4;
   static constexpr int kOffBar = kOffMax + (kTwoO ? 4 : 1) * kTile * 4;  // D = 64: [half][m, l]
-  static constexpr int kSmem = kOffBar + 512;
   static constexpr int kThreads = 640;  // five warps a sub-partition: 96 registers (six: 80)
   static constexpr uint32_t kColS = 0, kColP = 256, kColO = 384;
-  // barriers: kSFull, kSRead of the halves, kPFull, kPv, kMax of the quarters, kPos* of the stages
+  // barriers: kSFull, kSRead of the halves, kPFull, kPv of the quarters, kMax of each of their
+  // warps
   static constexpr int kQFull = 0, kQFree = 1, kKFull = 2, kKFree = kKFull + kSlots,
                        kVFull = kKFree + kSlots, kVFree = kVFull + kSlots,
                        kVReady = kVFree + kSlots, kSFull = kVReady + kSlots, kSRead = kSFull + 2,
-                       kPFull = kSRead + 2, kPv = kPFull + 4, kMax = kPv + 4, kORead = kMax + 4,
-                       kPosFull = kORead + 1, kPosFree = kPosFull + 2, kDone = kPosFree + 2,
-                       kBars = kDone + 2;
-  static_assert(kBars * 8 + 24 <= 512, "barriers, TMEM slot, largest positions");
+                       kPFull = kSRead + 2, kPv = kPFull + 4, kMax = kPv + 4, kORead = kMax + 16,
+                       kDone = kORead + 1, kBars = kDone + 2;
+  static constexpr int kSmem = kOffBar + (kBars * 8 + 24 + 127) / 128 * 128;  // TMEM slot, largest positions
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -237,8 +236,8 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
-  volatile uint32_t* pos_top = tmem_slot + 1;  // largest position, [stage][half]
-  int32_t* pos_ring = reinterpret_cast<int32_t*>(smem + C::kOffPos);  // [stage][256]
+  volatile uint32_t* pos_top = tmem_slot + 1;  // largest position of each half
+  int32_t* pos_ring = reinterpret_cast<int32_t*>(smem + C::kOffPos);  // [256]
   // the rows' running maximum (D = 64: of each half); at a segment's end their sums
   volatile float* row_max = reinterpret_cast<volatile float*>(smem + C::kOffMax);
   const int blocks = p.attend_blocks;
@@ -260,16 +259,14 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       mbar_init(bar(C::kVReady + i), 1);
     }
     for (int h = 0; h < 2; ++h) {
-      mbar_init(bar(C::kSFull + h), 1);
+      mbar_init(bar(C::kSFull + h), 2);  // scores, positions
       mbar_init(bar(C::kSRead + h), 256);
-      mbar_init(bar(C::kPosFull + h), 1);
-      mbar_init(bar(C::kPosFree + h), 16);
       mbar_init(bar(C::kDone + h), 1);
     }
     for (int q = 0; q < 4; ++q) {
       mbar_init(bar(C::kPFull + q), 128);
       mbar_init(bar(C::kPv + q), 1);
-      mbar_init(bar(C::kMax + q), 128);
+      for (int i = 0; i < 4; ++i) mbar_init(bar(C::kMax + 4 * q + i), 32);
     }
     mbar_init(bar(C::kORead), 512);
     fence_barrier_init();
@@ -322,30 +319,35 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         wait(bar(C::kKFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
     }
   } else if (warp == 19) {
-    // ---- positions, a block ahead, and empty slots' values
-    // publishes block J's positions; bit i of `holes`: the lane's slot 32 i + lane is empty
+    // ---- positions, fetched a block ahead, and empty slots' values
     const int32_t* pos = p.pos;
-    auto publish = [&](int J, const Walk& w, uint32_t& holes) -> bool {
+    int32_t v[8];
+    auto fetch = [&](const Walk& w) {
+      if (!w.valid()) return;
       if (w.first) pos = p.pos + static_cast<int64_t>(w.tile / p.row_tiles) * p.capacity;
       const int slot0 = w.block * C::kKeys + lane;
-      int32_t v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = slot0 + 32 * i < p.used ? __ldg(pos + slot0 + 32 * i) : -1;
-      const int st = J & 1;
-      if (!wait_warp(bar(C::kPosFree + st), ((J >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI)) return false;
+    };
+    // publishes those fetched as block J's, once the softmax is through with the block before; bit
+    // i of `holes`: the lane's slot 32 i + lane is empty
+    auto publish = [&](int J, uint32_t& holes) -> bool {
+      if (J > 0)
+        for (int h = 0; h < 2; ++h)
+          if (!wait_warp(bar(C::kSRead + h), (J - 1) & 1, p.err, ERR_WAIT_EPI)) return false;
       uint32_t top[2] = {0, 0};
       holes = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        pos_ring[st * C::kKeys + 32 * i + lane] = v[i];
+        pos_ring[32 * i + lane] = v[i];
         top[i / 4] = max(top[i / 4], static_cast<uint32_t>(v[i]));
         holes |= v[i] < 0 ? 1u << i : 0u;
       }
       top[0] = __reduce_max_sync(0xffffffffu, top[0]);
       top[1] = __reduce_max_sync(0xffffffffu, top[1]);
-      if (lane < 2) pos_top[2 * st + lane] = lane ? top[1] : top[0];
+      if (lane < 2) pos_top[lane] = lane ? top[1] : top[0];
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kPosFull + st));
+      if (lane < 2) mbar_arrive(bar(C::kSFull + lane));
       return true;
     };
     // the next half of V into its slot, once the product before last has read that
@@ -374,11 +376,22 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     if (lane == 0) prefetch_tmap(&tmV);
     Walk w(units, blockIdx.x, blocks);
     uint32_t holes = 0, next_holes = 0;
-    bool ok = !w.valid() || publish(0, w, holes);
+    Walk pw(units, blockIdx.x, blocks);  // of the positions to fetch next
+    bool ok = true;
+    if (w.valid()) {
+      fetch(pw);
+      ok = publish(0, holes);
+      pw.next(blocks);
+      fetch(pw);
+    }
     for (int i = 0; i < C::kSlots - 1 && ok; ++i) ok = load();
     for (int J = 0; w.valid() && ok; ++J) {
       w.next(blocks);
-      if (w.valid()) ok = publish(J + 1, w, next_holes);
+      if (w.valid()) {
+        ok = publish(J + 1, next_holes);
+        pw.next(blocks);
+        fetch(pw);
+      }
 #pragma unroll 1
       for (int h = 0; h < 2 && ok; ++h) {
         const int i = 2 * J + h, s = i % C::kSlots;
@@ -494,157 +507,147 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     // (a per-thread copy: as a kernel parameter it cost the loops a fifth more instructions)
     const float c = __shfl_sync(0xffffffffu, p.scale_log2, 0);
     const uint64_t c2 = pack_f32x2(c, c);
-    float m = -INFINITY, l = 0.f;
-    // the segment's tile and this thread's row in it
-    int lst = 0, stream = 0, group = 0, token = 0;
-    bool valid = false;
-    uint32_t limit = 0;  // a slot is visible if its position, unsigned, is below this
-    // the warp's different limits: lane i has the i-th of n_limits, which is this row's if my_limit = i
-    uint32_t limits = 0;
-    int n_limits = 0, my_limit = 0;
     // A wait that gives up has set the status word, and every wait after it returns at once: the
-    // warps walk on to the end, since they have to meet at the segments' barriers.
+    // warps go on to the end, since they have to meet at the segments' barriers.
     int J = 0;
-    for (Walk w(units, blockIdx.x, blocks); w.valid(); w.next(blocks), ++J) {
-      if (w.first) {
-        lst = w.tile / p.row_tiles;
-        stream = lst / p.groups;
-        group = lst - stream * p.groups;
-        token = (w.tile - lst * p.row_tiles) * p.tile_tokens + row / p.per;
-        valid = row < p.tile_rows && token < p.n_q;
-        m = -INFINITY;
-        l = 0.f;
-        // (rows that are none see every entry: their results go nowhere, and they do not send the
-        // warp through the masked path)
-        const int qp = valid ? __ldg(p.q_pos + static_cast<int64_t>(stream) * p.n_q + token)
-                             : 0x7fffffff;
-        limit = qp < 0 ? 0u : static_cast<uint32_t>(qp) + 1u;
-        n_limits = 0;
-        for (uint32_t todo = 0xffffffffu; todo != 0; ++n_limits) {
-          const uint32_t x = __shfl_sync(0xffffffffu, limit, __ffs(todo) - 1);
-          todo &= ~__ballot_sync(0xffffffffu, limit == x);
-          if (limit == x) my_limit = n_limits;
-          if (lane == n_limits) limits = x;
-        }
-      }
-      const int st = J & 1;
-      wait_warp(bar(C::kPosFull + st), (J >> 1) & 1, p.err, ERR_WAIT_EPI);
-      const bool all_seen = __all_sync(0xffffffffu, pos_top[2 * st + h] < limit);
-      uint32_t seen[2] = {0, 0};
-      if (!all_seen) {
-        uint32_t at[2];
+    Walk w(units, blockIdx.x, blocks);  // at the segments' first blocks
+    while (w.valid()) {
+      // the segment's tile and this thread's row in it
+      const int lst = w.tile / p.row_tiles, stream = lst / p.groups, group = lst - stream * p.groups;
+      const int token = (w.tile - lst * p.row_tiles) * p.tile_tokens + row / p.per;
+      const bool valid = row < p.tile_rows && token < p.n_q;
+      const int qp = valid ? __ldg(p.q_pos + static_cast<int64_t>(stream) * p.n_q + token) : -1;
+      // a slot is visible if its position, unsigned, is below this
+      const uint32_t limit = qp < 0 ? 0u : static_cast<uint32_t>(qp) + 1u;
+      // of the warp's rows (those that are none do not count: their results go nowhere)
+      const uint32_t least = __reduce_min_sync(0xffffffffu, valid ? limit : 0x80000000u);
+      const uint32_t most = __reduce_max_sync(0xffffffffu, limit);
+      float m = -INFINITY, l = 0.f;
+      const int count = min(blocks - w.block, w.left + 1), end = J + count;
+      bool first = true;
+#pragma unroll 1
+      for (; J < end; ++J, first = false) {
+        wait_warp(bar(C::kSFull + h), J & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+        uint32_t sr[2][32];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          at[i] = static_cast<uint32_t>(pos_ring[st * C::kKeys + 64 * q + 32 * i + lane]);
-#pragma unroll 2
-        for (int k = 0; k < n_limits; ++k) {
-          const uint32_t x = __shfl_sync(0xffffffffu, limits, k);
+        for (int i = 0; i < 2; ++i) tmem_ld_32x32b_x32(s_col + 32 * i, sr[i]);
+        // The slots that this row sees. The rows of a warp differ in slots whose position is between
+        // their limits, which are few: a warp's rows are a handful of tokens, next to each other as
+        // a rule. Bit i of some_hidden: some row does not see all of slots 8 i to 8 i + 7.
+        uint32_t seen[2] = {0xffffffffu, 0xffffffffu}, some_hidden = 0;
+        if (pos_top[h] >= least) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint32_t b = __ballot_sync(0xffffffffu, at[i] < x);
-            if (my_limit == k) seen[i] = b;
+            const uint32_t at =
+                static_cast<uint32_t>(pos_ring[64 * q + 32 * i + lane]);
+            seen[i] = __ballot_sync(0xffffffffu, at < least);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if ((~seen[i] & (255u << 8 * e)) != 0) some_hidden |= 1u << (4 * i + e);
+            uint32_t todo = __ballot_sync(0xffffffffu, at < most) & ~seen[i];
+#pragma unroll 1
+            for (; todo != 0; todo &= todo - 1) {
+              const int e = __ffs(todo) - 1;
+              if (__shfl_sync(0xffffffffu, at, e) < limit) seen[i] |= 1u << e;
+            }
           }
         }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kPosFree + st));
-      wait_warp(bar(C::kSFull + h), J & 1, p.err, ERR_WAIT_MMA);
-      tc_fence_after();
-      uint32_t sr[2][32];
+        tmem_ld_wait();
+        tc_fence_before();
+        mbar_arrive(bar(C::kSRead + h));
+        if (some_hidden != 0) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) tmem_ld_32x32b_x32(s_col + 32 * i, sr[i]);
-      tmem_ld_wait();
-      tc_fence_before();
-      mbar_arrive(bar(C::kSRead + h));
-      if (!all_seen) {
+          for (int g = 0; g < 8; ++g)
+            if (some_hidden & (1u << g)) {
+#pragma unroll
+              for (int e = 8 * (g % 4); e < 8 * (g % 4) + 8; ++e)
+                if (!(seen[g / 4] & (1u << e))) sr[g / 4][e] = 0xff800000u;
+            }
+        }
+        float mx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t* x = sr[i / 2] + 16 * (i % 2);
+          mx[i] = __uint_as_float(x[0]);
+#pragma unroll
+          for (int e = 1; e < 15; e += 2)
+            mx[i] = fmax3(mx[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+          mx[i] = fmaxf(mx[i], __uint_as_float(x[15]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        // the maximum that O stands for now
+        const bool fresh = first && lead;  // O holds nothing yet
+        float before = -INFINITY;
+        if (!lead || J > 0) {
+          wait_warp(bar(C::kMax + 4 * prev + lanes), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_EPI);
+          if (!fresh) before = *my_max;
+        }
+        const bool grow = top > before + kSlack;
+        const float now = grow ? top : before;
+        const float off = now == -INFINITY ? 0.f : now;
+        *my_max = now;
+        mbar_arrive(bar(C::kMax + 4 * q + lanes));
+        const float f = grow ? ex2_approx(before - off) : 1.f;  // of O
+        l *= m == now ? 1.f : ex2_approx(m - off);
+        m = now;
+        const uint64_t off2 = pack_f32x2(-off, -off);
+        uint64_t sum2[2] = {0, 0};
+        uint32_t pk[2][16];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (!(seen[i] & (1u << e))) sr[i][e] = 0xff800000u;
-      }
-      float mx[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t* x = sr[i / 2] + 16 * (i % 2);
-        mx[i] = __uint_as_float(x[0]);
-#pragma unroll
-        for (int e = 1; e < 15; e += 2)
-          mx[i] = fmax3(mx[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-        mx[i] = fmaxf(mx[i], __uint_as_float(x[15]));
-      }
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-      // the maximum that O stands for now
-      const bool fresh = w.first && lead;  // O holds nothing yet
-      float before = -INFINITY;
-      if (!lead || J > 0) {
-        wait_warp(bar(C::kMax + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_EPI);
-        if (!fresh) before = *my_max;
-      }
-      const bool grow = top > before + kSlack;
-      const float now = grow ? top : before;
-      const float off = now == -INFINITY ? 0.f : now;
-      *my_max = now;
-      mbar_arrive(bar(C::kMax + q));
-      const float f = grow ? ex2_approx(before - off) : 1.f;  // of O
-      l *= m == now ? 1.f : ex2_approx(m - off);
-      m = now;
-      const uint64_t off2 = pack_f32x2(-off, -off);
-      uint64_t sum2[2] = {0, 0};
-      uint32_t pk[2][16];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          uint64_t x;
-          asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(sr[i][e]), "r"(sr[i][e + 1]));
-          asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(x), "l"(c2), "l"(off2));
-          float a, b;
-          asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
-          a = ex2_approx(a);
-          b = ex2_approx(b);
-          asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[e / 2 % 2]) : "l"(pack_f32x2(a, b)));
-          pk[i][e / 2] = pack16<F16>(a, b);
-        }
-      // the previous block's product has read this quarter's P
-      if (!w.first) wait_warp(bar(C::kPv + q), (J - 1) & 1, p.err, ERR_WAIT_MMA);
-      if (!fresh && __any_sync(0xffffffffu, grow)) {
-        // O as the products of all quarters before left it
-        wait_warp(bar(C::kPv + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_MMA);
-        tc_fence_after();
+          for (int e = 0; e < 32; e += 2) {
+            uint64_t x;
+            asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(sr[i][e]), "r"(sr[i][e + 1]));
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(x), "l"(c2), "l"(off2));
+            float a, b;
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+            a = ex2_approx(a);
+            b = ex2_approx(b);
+            asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[e / 2 % 2]) : "l"(pack_f32x2(a, b)));
+            pk[i][e / 2] = pack16<F16>(a, b);
+          }
+        // the previous block's product has read this quarter's P
+        if (!first) wait_warp(bar(C::kPv + q), (J - 1) & 1, p.err, ERR_WAIT_MMA);
+        if (!fresh && __any_sync(0xffffffffu, grow)) {
+          // O as the products of all quarters before left it
+          wait_warp(bar(C::kPv + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_MMA);
+          tc_fence_after();
 #pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
-          uint32_t o[16];
-          const uint32_t at = o_col + (C::kTwoO ? 64u * h : 0u) + d;
-          tmem_ld_32x32b_x16(at, o);
-          tmem_ld_wait();
+          for (int d = 0; d < D; d += 16) {
+            uint32_t o[16];
+            const uint32_t at = o_col + (C::kTwoO ? 64u * h : 0u) + d;
+            tmem_ld_32x32b_x16(at, o);
+            tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-          tmem_st_32x32b_x16(at, o);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st_32x32b_x16(at, o);
+          }
         }
-      }
-      tc_fence_after();
-      __syncwarp();
+        tc_fence_after();
+        __syncwarp();
 #pragma unroll
-      for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(p_col + 16 * i, pk[i]);
-      {
-        float a0, b0, a1, b1;
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(b0) : "l"(sum2[0]));
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(a1), "=f"(b1) : "l"(sum2[1]));
-        l += (a0 + b0) + (a1 + b1);
+        for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(p_col + 16 * i, pk[i]);
+        {
+          float a0, b0, a1, b1;
+          asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(b0) : "l"(sum2[0]));
+          asm("mov.b64 {%0, %1}, %2;" : "=f"(a1), "=f"(b1) : "l"(sum2[1]));
+          l += (a0 + b0) + (a1 + b1);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(bar(C::kPFull + q));
       }
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(bar(C::kPFull + q));
-      if (!w.last) continue;
 
       // ---- the segment's result: this thread's quarter of the row's elements
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wait_warp(bar(C::kPv + i), J & 1, p.err, ERR_WAIT_MMA);
+      for (int i = 0; i < 4; ++i) wait_warp(bar(C::kPv + i), (J - 1) & 1, p.err, ERR_WAIT_MMA);
       tc_fence_after();
       // the sums on the last maximum, added up in the order of the quarters (named barriers of
       // the row's four warps between the steps)
-      wait_warp(bar(C::kMax + q / kShare * kShare + kShare - 1), J & 1, p.err, ERR_WAIT_EPI);
+      wait_warp(bar(C::kMax + 4 * (q / kShare * kShare + kShare - 1) + lanes), (J - 1) & 1, p.err,
+                ERR_WAIT_EPI);
       const float last = *my_max;
       l *= m == last ? 1.f : ex2_approx(m - last);
       m = last;
@@ -727,6 +730,9 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
           p.lse[static_cast<int64_t>(w.tile) * p.tile_rows + row] =
               !valid || all == 0.f ? INFINITY : m + log2f(all);
       }
+      w.left -= count;
+      ++w.tile;
+      w.block = 0;
     }
   }
   grid_dep_launch();

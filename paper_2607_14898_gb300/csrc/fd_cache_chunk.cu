@@ -97,7 +97,15 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, in
                                      bool drain = false) {
   return mbar_try_wait(bar, parity) || wait_more(bar, parity, err, code, drain);
 }
-// The same for a whole warp that stays together (tcgen05 loads and stores, which follow such
+// For loops over several barriers that take whichever is through: whether to go on after a round
+// that found none (kTries rounds at most; the status word is looked up every 1024).
+__device__ __forceinline__ bool poll_again(int& rounds, int* err, int code) {
+  if (++rounds % 1024 != 0) return true;
+  if (rounds < kTries && *reinterpret_cast<volatile int*>(err) == 0) return true;
+  atomicOr(err, code);
+  return false;
+}
+// The waits for a whole warp that stays together (tcgen05 loads and stores, which follow such
 // waits, have to be executed by all its lanes at once): every decision is the warp's, so that its
 // lanes never part. (Each instruction that only brings lanes together, or waits for a barrier that
 // is through already, took 100 to 200 cycles of the attend kernel's softmax.)
@@ -144,15 +152,15 @@ constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swiz
 // maximum is handed from quarter to quarter, which sets the groups a step apart: the exponentials
 // of one run beside the loads, masks and maxima of the others.
 //   warps 0-15    softmax: warps 4 q .. 4 q + 3 quarter q
-//   warp 16       TMA: Q of the segment, and K by half blocks (128 slots). K and V have a ring each,
-//                 so that a half is fetched as soon as one has been used: two more are there or
-//                 on their way meanwhile (D = 128, where 192 KB of them fit)
+//   warp 16       TMA: Q of the segment, K and V by half blocks (128 slots). K and V have a ring
+//                 each, so that a half is fetched as soon as one has been used: two more are there
+//                 or on their way meanwhile (D = 128, where 192 KB of them fit)
 //   warps 17, 18  products: a thread issues one tcgen05.mma per 104 to 158 cycles whatever its
 //                 size, so two of them share the work. D = 64: those of the block's first and
 //                 second half, each half with a running maximum and an O of its own; D = 128: S of
 //                 both halves, and P V into the one O that TMEM has room for.
-//   warp 19       positions of each block, on the barrier of its scores; V by half blocks, with
-//                 zeros for the values of empty slots (their probability is 0, but 0 times NaN is NaN)
+//   warp 19       positions of each block, on the barrier of its scores; zeros for the values of
+//                 empty slots (their probability is 0, but 0 times NaN is NaN)
 // TMEM (512 columns): S 2 x 128, P 2 x 64 (two 16-bit values a column), O 2 x 64 or 128. S takes the
 // next scores once the softmax has it in registers.
 template <int D>
@@ -287,122 +295,123 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     if (lane == 0) {
       prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
-      int i = 0, segs = 0;  // i: halves so far
-      int stream = 0, group = 0;
-      bool ok = true;
-      for (Walk w(units, blockIdx.x, blocks); w.valid() && ok; w.next(blocks)) {
-        if (w.first) {
-          const int lst = w.tile / p.row_tiles;
-          stream = lst / p.groups;
-          group = lst - stream * p.groups;
-          ok = w.seg == 0 || wait(bar(C::kQFree), (w.seg - 1) & 1, p.err, ERR_WAIT_MMA);
-          if (!ok) break;
-          mbar_expect_tx(bar(C::kQFull), p.tile_rows * D * 2);
-          for (int d = 0; d < D / 64; ++d)
-            tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.per,
-                        (w.tile - lst * p.row_tiles) * p.tile_tokens, stream);
-          segs = w.seg + 1;
+      prefetch_tmap(&tmV);
+      // the next half of K, or of V, as soon as its slot is free
+      struct Next {
+        Walk w;
+        int half, slot;  // half: halves so far
+        uint32_t phase;
+        int stream, group;
+      };
+      const Walk w0(units, blockIdx.x, blocks);
+      Next k{w0, 0, 0, 0, 0, 0}, v{w0, 0, 0, 0, 0, 0};
+      auto load = [&](Next& n, const CUtensorMap* map, uint32_t to, int full) {
+        const uint32_t b = bar(full + n.slot);
+        mbar_expect_tx(b, C::kHalfBytes);
+        for (int d = 0; d < D / 64; ++d)
+          tma_load_4d(to + n.slot * C::kHalfBytes + d * kSub, map, b, 64 * d,
+                      n.w.block * C::kKeys + (n.half & 1) * kTile, n.group, n.stream);
+        if (++n.slot == C::kSlots) {
+          n.slot = 0;
+          n.phase ^= 1;
         }
-        for (int h = 0; h < 2; ++h, ++i) {
-          const int s = i % C::kSlots;
-          ok = wait(bar(C::kKFree + s), ((i / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA);
-          if (!ok) break;
-          mbar_expect_tx(bar(C::kKFull + s), C::kHalfBytes);
-          for (int d = 0; d < D / 64; ++d)
-            tma_load_4d(base + C::kOffK + s * C::kHalfBytes + d * kSub, &tmK, bar(C::kKFull + s),
-                        64 * d, w.block * C::kKeys + h * kTile, group, stream);
+        if (n.half++ & 1) n.w.next(blocks);
+      };
+      auto begins = [&](const Next& n) { return n.w.first && (n.half & 1) == 0; };
+      auto locate = [&](Next& n) {
+        const int lst = n.w.tile / p.row_tiles;
+        n.stream = lst / p.groups;
+        n.group = lst - n.stream * p.groups;
+        return lst;
+      };
+      int segs = 0, idle = 0;
+      while (k.w.valid() || v.w.valid()) {
+        bool moved = false;
+        if (k.w.valid() && mbar_test_wait(bar(C::kKFree + k.slot), k.phase ^ 1) &&
+            (!begins(k) || k.w.seg == 0 || mbar_test_wait(bar(C::kQFree), (k.w.seg - 1) & 1))) {
+          if (begins(k)) {
+            const int lst = locate(k);
+            mbar_expect_tx(bar(C::kQFull), p.tile_rows * D * 2);
+            for (int d = 0; d < D / 64; ++d)
+              tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, k.group * p.per,
+                          (k.w.tile - lst * p.row_tiles) * p.tile_tokens, k.stream);
+            segs = k.w.seg + 1;
+          }
+          load(k, &tmK, base + C::kOffK, C::kKFull);
+          moved = true;
         }
+        if (v.w.valid() && mbar_test_wait(bar(C::kVFree + v.slot), v.phase ^ 1)) {
+          if (begins(v)) locate(v);
+          load(v, &tmV, base + C::kOffV, C::kVFull);
+          moved = true;
+        }
+        if (moved)
+          idle = 0;
+        else if (!poll_again(idle, p.err, ERR_WAIT_MMA))
+          break;
       }
       // nothing may be in flight when the CTA exits
       if (segs > 0) wait(bar(C::kQFull), (segs - 1) & 1, p.err, ERR_WAIT_TMA, true);
-      for (int j = i - 1; j >= 0 && j >= i - C::kSlots; --j)
+      for (int j = k.half - 1; j >= 0 && j >= k.half - C::kSlots; --j)
         wait(bar(C::kKFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = v.half - 1; j >= 0 && j >= v.half - C::kSlots; --j)
+        wait(bar(C::kVFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
     }
   } else if (warp == 19) {
     // ---- positions, fetched a block ahead, and empty slots' values
+    Walk w(units, blockIdx.x, blocks);  // at the block whose positions are fetched next
+    const int count = w.left + 1;
     const int32_t* pos = p.pos;
-    int32_t v[8];
-    auto fetch = [&](const Walk& w) {
+    int32_t at[8];
+    auto fetch = [&]() {
       if (!w.valid()) return;
       if (w.first) pos = p.pos + static_cast<int64_t>(w.tile / p.row_tiles) * p.capacity;
       const int slot0 = w.block * C::kKeys + lane;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = slot0 + 32 * i < p.used ? __ldg(pos + slot0 + 32 * i) : -1;
-    };
-    // publishes those fetched as block J's, once the softmax is through with the block before; bit
-    // i of `holes`: the lane's slot 32 i + lane is empty
-    auto publish = [&](int J, uint32_t& holes) -> bool {
-      if (J > 0)
-        for (int h = 0; h < 2; ++h)
-          if (!wait_warp(bar(C::kSRead + h), (J - 1) & 1, p.err, ERR_WAIT_EPI)) return false;
-      uint32_t top[2] = {0, 0};
-      holes = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        pos_ring[32 * i + lane] = v[i];
-        top[i / 4] = max(top[i / 4], static_cast<uint32_t>(v[i]));
-        holes |= v[i] < 0 ? 1u << i : 0u;
-      }
-      top[0] = __reduce_max_sync(0xffffffffu, top[0]);
-      top[1] = __reduce_max_sync(0xffffffffu, top[1]);
-      if (lane < 2) pos_top[lane] = lane ? top[1] : top[0];
-      __syncwarp();
-      if (lane < 2) mbar_arrive(bar(C::kSFull + lane));
-      return true;
-    };
-    // the next half of V into its slot, once the product before last has read that
-    Walk lw(units, blockIdx.x, blocks);
-    int n = 0, stream = 0, group = 0;
-    auto load = [&]() -> bool {
-      if (!lw.valid()) return true;
-      const int s = n % C::kSlots;
-      if (!wait_warp(bar(C::kVFree + s), ((n / C::kSlots) & 1) ^ 1, p.err, ERR_WAIT_MMA))
-        return false;
-      if (lw.first && (n & 1) == 0) {
-        const int lst = lw.tile / p.row_tiles;
-        stream = lst / p.groups;
-        group = lst - stream * p.groups;
-      }
-      if (lane == 0) {
-        mbar_expect_tx(bar(C::kVFull + s), C::kHalfBytes);
-        for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(base + C::kOffV + s * C::kHalfBytes + d * kSub, &tmV, bar(C::kVFull + s),
-                      64 * d, lw.block * C::kKeys + (n & 1) * kTile, group, stream);
-      }
-      if (n & 1) lw.next(blocks);
-      ++n;
-      return true;
-    };
-    if (lane == 0) prefetch_tmap(&tmV);
-    Walk w(units, blockIdx.x, blocks);
-    uint32_t holes = 0, next_holes = 0;
-    Walk pw(units, blockIdx.x, blocks);  // of the positions to fetch next
-    bool ok = true;
-    if (w.valid()) {
-      fetch(pw);
-      ok = publish(0, holes);
-      pw.next(blocks);
-      fetch(pw);
-    }
-    for (int i = 0; i < C::kSlots - 1 && ok; ++i) ok = load();
-    for (int J = 0; w.valid() && ok; ++J) {
+      for (int i = 0; i < 8; ++i)
+        at[i] = slot0 + 32 * i < p.used ? __ldg(pos + slot0 + 32 * i) : -1;
       w.next(blocks);
-      if (w.valid()) {
-        ok = publish(J + 1, next_holes);
-        pw.next(blocks);
-        fetch(pw);
+    };
+    auto through = [&](int b, uint32_t parity) {
+      return __all_sync(0xffffffffu, mbar_test_wait(bar(b), parity)) != 0;
+    };
+    fetch();
+    // blocks published and halves of V made ready so far
+    int J = 0, n = 0, slot = 0, idle = 0;
+    uint32_t phase = 0;
+    // Bit i: this lane's slot 32 i + lane of the block published last is empty; above, those of the
+    // blocks before it. (The softmax reads a block's scores after its part of the product before
+    // last, so V is at most two blocks behind.)
+    uint32_t holes = 0;
+    while (n < 2 * count) {
+      bool moved = false;
+      // once the softmax is through with the positions and scores of the block before
+      if (J < count && (J == 0 || (through(C::kSRead, (J - 1) & 1) &&
+                                   through(C::kSRead + 1, (J - 1) & 1)))) {
+        uint32_t top[2] = {0, 0};
+        holes <<= 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          pos_ring[32 * i + lane] = at[i];
+          top[i / 4] = max(top[i / 4], static_cast<uint32_t>(at[i]));
+          holes |= at[i] < 0 ? 1u << i : 0u;
+        }
+        top[0] = __reduce_max_sync(0xffffffffu, top[0]);
+        top[1] = __reduce_max_sync(0xffffffffu, top[1]);
+        if (lane < 2) pos_top[lane] = lane ? top[1] : top[0];
+        __syncwarp();
+        if (lane < 2) mbar_arrive(bar(C::kSFull + lane));
+        ++J;
+        fetch();
+        moved = true;
       }
-#pragma unroll 1
-      for (int h = 0; h < 2 && ok; ++h) {
-        const int i = 2 * J + h, s = i % C::kSlots;
-        ok = wait_warp(bar(C::kVFull + s), (i / C::kSlots) & 1, p.err, ERR_WAIT_TMA);
-        if (!ok) break;
-        const uint32_t mine = (holes >> (4 * h)) & 15u;
+      if (n < 2 * J && through(C::kVFull + slot, phase)) {
+        const uint32_t mine = (holes >> (8 * (J - 1 - n / 2) + 4 * (n & 1))) & 15u;
         if (__any_sync(0xffffffffu, mine != 0)) {
 #pragma unroll 1
           for (int r = 0; r < 4; ++r) {
             if (!((mine >> r) & 1u)) continue;
-            uint4* row = reinterpret_cast<uint4*>(smem + C::kOffV + s * C::kHalfBytes +
+            uint4* row = reinterpret_cast<uint4*>(smem + C::kOffV + slot * C::kHalfBytes +
                                                   (32 * r + lane) * 128);
 #pragma unroll
             for (int d = 0; d < D / 64; ++d)
@@ -412,15 +421,19 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
           fence_proxy_async_smem();
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::kVReady + s));
-        ok = load();
+        if (lane == 0) mbar_arrive(bar(C::kVReady + slot));
+        ++n;
+        if (++slot == C::kSlots) {
+          slot = 0;
+          phase ^= 1;
+        }
+        moved = true;
       }
-      holes = next_holes;
+      if (moved)
+        idle = 0;
+      else if (!__all_sync(0xffffffffu, poll_again(idle, p.err, ERR_WAIT_TMA)))
+        break;
     }
-    // nothing may be in flight when the CTA exits
-    if (lane == 0)
-      for (int j = n - 1; j >= 0 && j >= n - C::kSlots; --j)
-        wait(bar(C::kVFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
   } else if (warp >= 17) {  // 17 and 18
     if (lane == 0) {
       constexpr uint32_t is = Mma<F16, D>::idesc(kTile, false), io = Mma<F16, D>::idesc(D, true);

@@ -125,15 +125,13 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* er
          wait_more_warp(bar, parity, err, code);
 }
 
-// 16 lanes of the warp's quarter and 32 columns in 16 x 8 fragments: of fragment j thread t gets
+// 16 lanes of the warp's quarter and 16 columns in 16 x 8 fragments: of fragment j thread t gets
 // columns 8 j + 2 (t % 4), + 1 of lane t / 4 (r[4 j], r[4 j + 1]) and of lane t / 4 + 8
-__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t (&r)[8]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
+        "=r"(r[7])
       : "r"(taddr));
 }
 
@@ -548,16 +546,13 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         // The slots that this row sees. The rows of a warp differ in slots whose position is between
         // their limits, which are few: a warp's rows are a handful of tokens, next to each other as
         // a rule. Bit i of some_hidden: some row does not see all of slots 8 i to 8 i + 7.
-        uint32_t seen[2] = {0xffffffffu, 0xffffffffu}, some_hidden = 0;
+        uint32_t seen[2] = {0xffffffffu, 0xffffffffu}, all[2] = {0xffffffffu, 0xffffffffu};
         if (pos_top[h] >= least) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint32_t at =
                 static_cast<uint32_t>(pos_ring[64 * q + 32 * i + lane]);
-            seen[i] = __ballot_sync(0xffffffffu, at < least);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if ((~seen[i] & (255u << 8 * e)) != 0) some_hidden |= 1u << (4 * i + e);
+            all[i] = seen[i] = __ballot_sync(0xffffffffu, at < least);
             uint32_t todo = __ballot_sync(0xffffffffu, at < most) & ~seen[i];
 #pragma unroll 1
             for (; todo != 0; todo &= todo - 1) {
@@ -569,15 +564,13 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         tmem_ld_wait();
         tc_fence_before();
         mbar_arrive(bar(C::kSRead + h));
-        if (some_hidden != 0) {
 #pragma unroll
-          for (int g = 0; g < 8; ++g)
-            if (some_hidden & (1u << g)) {
+        for (int i = 0; i < 2; ++i)
+          if (all[i] != 0xffffffffu) {
 #pragma unroll
-              for (int e = 8 * (g % 4); e < 8 * (g % 4) + 8; ++e)
-                if (!(seen[g / 4] & (1u << e))) sr[g / 4][e] = 0xff800000u;
-            }
-        }
+            for (int e = 0; e < 32; ++e)
+              if (!(seen[i] & (1u << e))) sr[i][e] = 0xff800000u;
+          }
         float mx[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -762,7 +755,6 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
 // per row.
 template <bool F16, int D>
 __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant__ CacheAttn p) {
-  grid_dep_wait();
   const int blocks = p.attend_blocks;
   const Units units{static_cast<int64_t>(p.lists) * p.row_tiles * blocks, p.parts};
   const int k = blockIdx.y, row = threadIdx.x;
@@ -770,10 +762,10 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
   const int lst = gt / p.row_tiles, tile = gt - lst * p.row_tiles;
   const int64_t unit = static_cast<int64_t>(gt) * blocks;
   const int lo = units.owner(unit), hi = units.owner(unit + blocks - 1);
+  grid_dep_wait();  // (the divisions above are done while attend's last CTAs run)
   if (lo != hi && static_cast<int>(blockIdx.x) == lo) {
-    auto part_of = [&](int c) {
-      return static_cast<int64_t>(c) * 2 + (units.start(c) > unit ? 0 : 1);
-    };
+    // the tile is the last segment of its first CTA and the first of the others
+    auto part_of = [&](int c) { return static_cast<int64_t>(c) * 2 + (c == lo ? 1 : 0); };
     float top = -INFINITY;
     for (int c = lo; c <= hi; ++c) top = fmaxf(top, __ldcg(p.part_ml + part_of(c) * kTile + row).x);
     const float off = top == -INFINITY ? 0.f : top;
@@ -823,7 +815,7 @@ template <int D>
 struct WeighCfg {
   static constexpr int kTileBytes = kTile * D * 2;
   static constexpr int kStages = D == 128 ? 2 : 4;
-  static constexpr int kRowStages = 4;
+  static constexpr int kRowStages = 4;  // two for each of the accumulators
   static constexpr int kOffQ = kTileBytes;
   static constexpr int kOffRows = kOffQ + kStages * kTileBytes;    // lse, then limits, per stage
   static constexpr int kOffLow = kOffRows + kRowStages * kTile * 8;  // smallest limit per stage
@@ -832,8 +824,7 @@ struct WeighCfg {
   static constexpr int kSmem = kOffBar + 256;
   static constexpr int kThreads = 352;
   static constexpr int kKFull = 0, kQFull = 1, kQFree = kQFull + kStages,
-                       kTFull = kQFree + kStages, kTFree = kTFull + 2, kRowFull = kTFree + 2,
-                       kRowFree = kRowFull + kRowStages, kDone = kRowFree + kRowStages,
+                       kTFull = kQFree + kStages, kTFree = kTFull + 2, kDone = kTFree + 2,
                        kBars = kDone + 1;
   static_assert(kBars * 8 + 8 <= 256, "barriers");
   static_assert(2 * (kSmem + 1024) <= 227 * 1024, "two CTAs");
@@ -872,12 +863,8 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
       mbar_init(bar(C::kQFree + i), 1);
     }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(bar(C::kTFull + x), 1);
+      mbar_init(bar(C::kTFull + x), 2);  // scores, rows
       mbar_init(bar(C::kTFree + x), 128);
-    }
-    for (int i = 0; i < C::kRowStages; ++i) {
-      mbar_init(bar(C::kRowFull + i), 1);
-      mbar_init(bar(C::kRowFree + i), 4);
     }
     mbar_init(bar(C::kDone), 1);
     fence_barrier_init();
@@ -962,7 +949,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
         if (in) low = min(low, lim[j]);
       }
       low = __reduce_min_sync(0xffffffffu, low);
-      ok = wait_warp(bar(C::kRowFree + st), ((i / C::kRowStages) & 1) ^ 1, p.err, ERR_WAIT_EPI);
+      ok = wait_warp(bar(C::kTFree + (i & 1)), ((i >> 1) & 1) ^ 1, p.err, ERR_WAIT_EPI);
       if (!ok) break;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -971,7 +958,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
       }
       if (lane == 0) row_low[st] = low;
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kRowFull + st));
+      if (lane == 0) mbar_arrive(bar(C::kTFull + (i & 1)));
     }
   } else if (warp < 8) {
     const int x = warp >> 2;
@@ -994,24 +981,27 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
     bool ok = true;
     for (int i = x; i < tiles && ok; i += 2) {
       const int st = i % C::kRowStages;
-      ok = wait_warp(bar(C::kRowFull + st), (i / C::kRowStages) & 1, p.err, ERR_WAIT_EPI) &&
-           wait_warp(bar(C::kTFull + x), (i >> 1) & 1, p.err, ERR_WAIT_MMA);
+      ok = wait_warp(bar(C::kTFull + x), (i >> 1) & 1, p.err, ERR_WAIT_MMA);
       if (!ok) break;
       tc_fence_after();
+      uint32_t buf[2][2][8];  // a step of 16 rows ahead
+      tmem_ld_16x256b_x2(col, buf[0][0]);
+      tmem_ld_16x256b_x2(col + (16u << 16), buf[0][1]);
       uint64_t sum2[4] = {0, 0, 0, 0};  // even and odd rows
       auto add = [&](auto masked) {
 #pragma unroll
-        for (int d = 0; d < kTile; d += 32) {
-          uint32_t sr[2][16];  // slots 0 and 1, slots 2 and 3
-          tmem_ld_16x256b_x4(col + d, sr[0]);
-          tmem_ld_16x256b_x4(col + (16u << 16) + d, sr[1]);
+        for (int d = 0; d < kTile; d += 16) {
+          uint32_t(&sr)[2][8] = buf[d / 16 % 2];  // slots 0 and 1, slots 2 and 3
           tmem_ld_wait();
-          if (d == kTile - 32) {
+          if (d + 16 < kTile) {
+            tmem_ld_16x256b_x2(col + d + 16, buf[d / 16 % 2 ^ 1][0]);
+            tmem_ld_16x256b_x2(col + (16u << 16) + d + 16, buf[d / 16 % 2 ^ 1][1]);
+          } else {
             tc_fence_before();
             mbar_arrive(bar(C::kTFree + x));
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 2; ++j) {
             const int at = st * kTile + d + 8 * j + 2 * (lane & 3);
             const uint64_t lse2 = *reinterpret_cast<const uint64_t*>(row_lse + at);  // negated
             uint2 lim;
@@ -1043,8 +1033,6 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
         asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum2[k]));
         totals[k] += s0 + s1;
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kRowFree + st));
     }
     // the four threads of a slot have shared out the rows; thread t keeps slot t % 4
 #pragma unroll
@@ -1074,11 +1062,11 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
 
 // the row splits' sums, in their order
 __global__ void __launch_bounds__(256) sum_weights_kernel(const __grid_constant__ CacheAttn p) {
-  grid_dep_wait();
   const int64_t n = static_cast<int64_t>(p.lists) * p.used;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t lst = i / p.used, at = lst * p.capacity + (i - lst * p.used);
+  grid_dep_wait();
   if (i < n) {
-    const int64_t lst = i / p.used, at = lst * p.capacity + (i - lst * p.used);
     float w = 0.f;
     for (int s = 0; s < p.row_splits; ++s) w += __ldcg(p.part_w + s * n + i);
     p.weight_out[at] = fmaf(p.decay, p.weight[at], w);

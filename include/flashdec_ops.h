@@ -283,8 +283,8 @@ typedef struct {
   int32_t reserved;                   /* 0                                                  */
   void* k;                            /* element i of slot j: k[stream stream_stride + group */
   void* v;                            /*   group_stride + j slot_stride + i]; v the same     */
-  int64_t stream_stride, group_stride, slot_stride; /* elements, multiples of 8, >= 0; slot_stride >=
-                                         head_dim; k and v 16-byte aligned                  */
+  int64_t stream_stride, group_stride, slot_stride; /* elements, multiples of 8, >= head_dim (>= 0
+                                         of one stream or group); k and v 16-byte aligned   */
   int32_t* pos;                       /* [streams][groups][capacity]                        */
   float* weight;                      /* [streams][groups][capacity]                        */
 } fd_cache;
@@ -298,7 +298,7 @@ typedef struct {
  * chunk lets each see the whole chunk). A query that sees no slot gives zeros and adds nothing.
  * q, out of the cache's type: element (stream, t, h, i) of q at q[stream q_stream_stride + t
  * q_token_stride + h q_head_stride + i], of out with the out strides (elements; 16-byte
- * aligned, strides multiples of 8). q_pos int32 [streams][n_q]. scale > 0, finite; decay finite;
+ * aligned; strides multiples of 8, and >= head_dim where there is more than one entry). q_pos int32 [streams][n_q]. scale > 0, finite; decay finite;
  * heads / groups <= 128. weight_out fp32
  * [streams][groups][capacity], entries past `used` are not written; it may be cache->weight;
  * NULL: the weights are not gathered. Softmax, sums and weights are in fp32, P is rounded to the

@@ -504,8 +504,13 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
     if (!fd::ok_ptr(q, 16) || !fd::ok_ptr(out, 16) || !fd::ok_ptr(q_pos, 4) ||
         !fd::ok_ptr(err_dev, 4) || (used > 0 && !fd::ok_ptr(workspace, 16)))
       return FD_ERR_INVALID_ARG;
-    if ((q_stream_stride | q_token_stride | q_head_stride | out_stream_stride | out_token_stride |
-         out_head_stride) % 8)
+    // (rows that share elements would be written by several threads in out, and have no use in q)
+    auto steps = [&](int64_t entries, int64_t stride) {
+      return stride % 8 == 0 && (entries == 1 || stride >= cache->head_dim);
+    };
+    if (!steps(cache->streams, q_stream_stride) || !steps(n_q, q_token_stride) ||
+        !steps(heads, q_head_stride) || !steps(cache->streams, out_stream_stride) ||
+        !steps(n_q, out_token_stride) || !steps(heads, out_head_stride))
       return FD_ERR_INVALID_ARG;
   }
   const fd_status st = fd::check_device();

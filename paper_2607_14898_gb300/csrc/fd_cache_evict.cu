@@ -716,8 +716,10 @@ bool valid_cache(const fd_cache* c) {
     return false;
   if (c->head_dim != 64 && c->head_dim != 128) return false;
   if (c->dtype != FD_DTYPE_BF16 && c->dtype != FD_DTYPE_F16) return false;
-  if (c->stream_stride < 0 || c->group_stride < 0 || c->slot_stride < c->head_dim ||
-      c->stream_stride % 8 || c->group_stride % 8 || c->slot_stride % 8)
+  // (lists that share rows have no meaning: an insert would write them twice)
+  if (c->slot_stride < c->head_dim || (c->streams > 1 && c->stream_stride < c->head_dim) ||
+      (c->groups > 1 && c->group_stride < c->head_dim) || c->stream_stride < 0 ||
+      c->group_stride < 0 || c->stream_stride % 8 || c->group_stride % 8 || c->slot_stride % 8)
     return false;
   if (c->streams == 0 || c->capacity == 0) return true;
   return c->k && c->v && c->pos && c->weight && aligned(c->k, 16) && aligned(c->v, 16) &&

@@ -123,6 +123,16 @@ def test_attention_arguments():
     assert L.fd_cache_attention_workspace_bytes(ctypes.byref(c), 100, 16, 1) > 0
 
 
+def test_rows_that_share_elements_are_refused():
+    L, c = fdp.lib(), cache()
+    for bad in (dict(qs=0), dict(qs=-1024), dict(qt=0, n_q=2), dict(qh=0), dict(qh=56),
+                dict(os=0), dict(ot=0, n_q=2), dict(ot=-1024, n_q=2), dict(oh=32)):
+        assert attend(c, L, **bad) == INVALID, bad
+    for bad in (dict(stream_stride=0), dict(group_stride=0), dict(group_stride=56)):
+        assert attend(cache(**bad), L) == INVALID, bad
+        assert insert(cache(**bad), L) == INVALID, bad
+
+
 def test_insert_arguments():
     L, c = fdp.lib(), cache()
     for bad in (dict(n=-1), dict(n=101), dict(k=None), dict(v=None), dict(k=P + 8), dict(v=P + 2),

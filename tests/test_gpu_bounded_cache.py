@@ -223,6 +223,23 @@ def test_strided_queries_and_outputs(n):
     assert bool((buf[..., 64:] == 3.0).all())
 
 
+@pytest.mark.parametrize("heads", [1, 3, 16])
+@pytest.mark.parametrize("order", ["ascending", "descending", "mixed", "steps"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_masks_over_a_cache_in_order(heads, order, D):
+    """Rows of one tile that see different parts of it: entries in the order of their positions,
+    queries at positions in the cache, before it and after it."""
+    n, C = 150, 500
+    gen = torch.Generator(device="cuda").manual_seed(heads)
+    cache = make_cache(2, 1, C, D, torch.bfloat16, gen, empty=0.02)
+    cache.pos.copy_(torch.where(cache.pos < 0, -1, torch.arange(C, device="cuda").int()))
+    t = torch.arange(C - 100, C - 100 + n, device="cuda").int()
+    t = {"ascending": t, "descending": t.flip(0), "steps": t // 7 * 7,
+         "mixed": torch.randint(-4, C + 4, (n,), generator=gen, device="cuda").int()}[order]
+    q = torch.randn(2, n, heads, D, generator=gen, device="cuda").bfloat16()
+    check(cache, q, torch.stack([t, t - 250]).contiguous())
+
+
 def test_no_queries_no_slots():
     gen = torch.Generator(device="cuda").manual_seed(9)
     cache = make_cache(2, 2, 300, 64, torch.bfloat16, gen)

@@ -15,8 +15,8 @@
 // computed once for them; the lanes of a head are neighbours, so accesses are whole lines. Up
 // to kHeadsPerThread heads a thread once the launch fills the GPU, fewer for few tokens, where
 // latency counts and a thread per (token, head, chunk) is the shortest chain. 40001 tokens of 40
-// heads of 128 elements, 64 of them turned in halves (819 MB read and written): 147 us, 5.6
-// TB/s, with 20 heads a thread and 128 threads a block (8 heads and 256 threads: 189 us).
+// heads of 128 elements, 64 of them turned in halves (819 MB read and written): 155 us, 5.3 TB/s.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -182,10 +182,15 @@ template <typename T, int NV>
 cudaError_t launch_nv(RotaryParams& p, int num_sms, cudaStream_t s) {
   p.rot_lanes = p.rot_dim / 2 / (p.half ? Chunk<NV, true>::kPairs : Chunk<NV, false>::kPairs);
   p.lanes = p.rot_lanes + (p.head_dim - p.rot_dim) / NV;
-  // heads a thread walks over: enough threads for 4 blocks on every SM come first
+  // Heads a thread walks over: threads for 12 blocks on every SM come first, but 3 heads do while
+  // there are 4 blocks. In us, with threads for 4 / 8 / 12 / 16 blocks: 4000 tokens of 40 heads
+  // of 128 bf16 25 / 22 / 21 / 22; 24960 of 20 heads of 64 28 / 28 / 25 / 25; 1560 of them 3.6 (3
+  // heads) / 5.0 / 5.0 / 5.0 (1 head). More than 20 heads: 40001 tokens of 40 heads 163, with 20 155,
+  // with 8 164, with 1 353.
   const int64_t all = static_cast<int64_t>(p.tokens) * p.heads * p.lanes;
-  int64_t per = all / (static_cast<int64_t>(num_sms) * 4 * kThreads);
-  per = per < 1 ? 1 : (per > kHeadsPerThread ? kHeadsPerThread : per);
+  const int64_t fill = static_cast<int64_t>(num_sms) * 4 * kThreads;
+  const int64_t per = std::min<int64_t>(
+      std::max<int64_t>({1, all / (3 * fill), std::min<int64_t>(3, all / fill)}), kHeadsPerThread);
   p.head_slots = (p.heads + static_cast<int>(per) - 1) / static_cast<int>(per);
   const int threads = p.lanes > kThreads ? kMaxThreads : kThreads;
   const int per_block = threads / p.lanes;

@@ -682,15 +682,23 @@ cudaError_t launch_cluster(void (*kernel)(EvictParams), const EvictParams& p, in
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-// CTAs of a cluster: as many as keep the lists' clusters on the GPU at once, but no fewer than
-// 1024 slots each (below that the cluster's barriers cost more than the shorter loops save).
+// CTAs of a cluster: as many as keep the lists' clusters on the GPU at once, but no fewer than 512
+// (short form) or 1024 slots each: below that the cluster's barriers cost more than the shorter loops
+// save. Device times in us at 512 / 1024 / 2048 slots each: compact of 4 lists of 2000 slots to 500
+// 6.1 / 7.0 / 8.7, of 6240 to 1560 9.0 / 9.0 / 10.4; insert of one into 32 lists of 1500 slots
+// 4.9 / 4.2 / 4.8.
+// Short form or long, same cases: compact of 2000 7.0 / 14.5, of 6240 9.0 / 21.2, insert of 1560 into 32
+// lists of 6240 11.9 / 16.4. Insert of one in the short form: 9.0 for 32 lists of 6240, 5.4 in the
+// long one. Keys of a thread: 2 against 8 (short, 2000 slots) 7.0 / 9.2, 2 against 12 (long, insert of
+// one into 32 x 6240) 5.4 / 8.5, 12 / 24 / read again (compact of 32 lists of 32771) 42 / 49 / 57.
 template <bool COMPACT>
 cudaError_t launch(EvictParams& p, int lists, cudaStream_t s) {
+  const bool is_short = p.slots <= kShortSlots && (COMPACT || p.n != 1);
   int ctas = 1;
   while (ctas < kMaxCluster && 2 * ctas * static_cast<int64_t>(lists) <= num_sms() &&
-         p.slots > 1024 * ctas)
+         p.slots > (is_short ? 512 : 1024) * ctas)
     ctas *= 2;
-  if (p.slots <= kShortSlots && (COMPACT || p.n != 1)) {
+  if (is_short) {
     if (p.slots <= 2 * kThreads)
       return launch_cluster(evict_short_kernel<2, COMPACT>, p, lists, ctas, s);
     return launch_cluster(evict_short_kernel<8, COMPACT>, p, lists, ctas, s);

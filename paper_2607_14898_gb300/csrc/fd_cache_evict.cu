@@ -24,7 +24,9 @@
 // long form, with one exchange.
 //
 // Bound by memory for long rows (the copied keys and values) and by the latency of the dependent
-// steps for short ones: the positions and weights of a list are 8 bytes a slot.
+// steps for short ones: the positions and weights of a list are 8 bytes a slot. Insert of one token
+// into 32 lists of 6240 slots (3.2 MB): 5.4 us; of 1560 tokens (29 MB): 11.9 us, 2.4 TB/s; compact of 32
+// lists of 32771 slots of 128 elements to 4099 (144 MB): 42 us, 3.4 TB/s, half of it the selection.
 #include <cooperative_groups.h>
 
 #include "fd_internal.h"

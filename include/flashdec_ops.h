@@ -299,7 +299,7 @@ typedef struct {
  * q, out of the cache's type: element (stream, t, h, i) of q at q[stream q_stream_stride + t
  * q_token_stride + h q_head_stride + i], of out with the out strides (elements; 16-byte
  * aligned; strides multiples of 8, and >= head_dim where there is more than one entry). q_pos int32 [streams][n_q]. scale > 0, finite; decay finite;
- * heads / groups <= 128. weight_out fp32
+ * heads / groups <= 128, streams groups <= 65,535, n_q heads / groups <= 1,048,560. weight_out fp32
  * [streams][groups][capacity], entries past `used` are not written; it may be cache->weight;
  * NULL: the weights are not gathered. Softmax, sums and weights are in fp32, P is rounded to the
  * cache's type for its product with V. The order of every sum is fixed: equal calls give equal

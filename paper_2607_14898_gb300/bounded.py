@@ -20,7 +20,9 @@ class BoundedStream:
 
     plan: the Rotary that turns queries and keys (None: they come turned). sinks, recent: entries at
     positions below `sinks` or among the last `recent` before the step's first token are given up last.
-    decay: the weights gathered so far are multiplied by it before a step's are added."""
+    decay: the weights gathered so far are multiplied by it before a step's are added.
+
+    The calls run on the current stream; the tensors that they are given have to be ready on it."""
 
     def __init__(self, streams, heads, groups, head_dim, capacity, dtype=torch.bfloat16, plan=None,
                  sinks=4, recent=0, decay=1.0, device="cuda"):
@@ -34,6 +36,7 @@ class BoundedStream:
         self.filled = 0  # slots that may hold something: new tokens take empty slots in order
         self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self._buffers: dict = {}
+        self._work = torch.empty(0, dtype=torch.uint8, device=device)
 
     def _buffer(self, name, shape, dtype):
         """A buffer of the step, allocated when its size first comes up."""
@@ -43,36 +46,39 @@ class BoundedStream:
             t = self._buffers[key] = torch.empty(shape, dtype=dtype, device=self.err.device)
         return t
 
-    def step(self, q, k, v, pos, axes_pos=None, whole_chunk=False, stream=None):
+    def step(self, q, k, v, pos, axes_pos=None, whole_chunk=False):
         """Attention of q [streams][n][heads][head_dim] over the cache with the new k, v
         [streams][n][groups][head_dim] in it; returns out like q (a buffer that the next step of
         n tokens overwrites). pos int32 [streams][n]: ascending positions, those of the rotary
         embedding too unless axes_pos int32 [streams][n][axes] gives its own. whole_chunk: every
         token sees all n new tokens, as in the decoder's chunks; else a token sees no later one."""
         S, n, H, D = q.shape
+        if n == 0:
+            return torch.empty_like(q)
         c = self.cache
         G = c.groups
         if self.plan is not None:
             turn = (pos if axes_pos is None else axes_pos).reshape(S * n, -1)
             q_t, k_t = (self._buffer("q", q.shape, q.dtype), self._buffer("k", k.shape, k.dtype))
             fdp.op_rotary(self.plan, turn, q.reshape(S * n, H, D), q_t.view(S * n, H, D),
-                          k.reshape(S * n, G, D), k_t.view(S * n, G, D), stream=stream)
+                          k.reshape(S * n, G, D), k_t.view(S * n, G, D))
             q, k = q_t, k_t
         slots = self._buffer("slots", (S, G, n), torch.int32)
-        fdp.op_cache_insert(c, k, v, pos, slots, sinks=self.sinks, recent=self.recent,
-                            stream=stream)
+        fdp.op_cache_insert(c, k, v, pos, slots, sinks=self.sinks, recent=self.recent)
         self.filled = min(c.capacity, self.filled + n)
         out = self._buffer("out", (S, n, H, D), c.dtype)
         # what a call needs does not only grow with the slots: take the larger of now and full
         need = max(fdp.cache_attention_workspace_bytes(c, H, n, u)
                    for u in (self.filled, c.capacity))
-        work = self._buffer("work", (need,), torch.uint8)
+        if self._work.numel() < need:
+            self._work = torch.empty(need, dtype=torch.uint8, device=self.err.device)
         q_pos = pos[:, -1:].expand(S, n).contiguous() if whole_chunk else pos
         fdp.op_cache_attention(c, q, q_pos, out, weight_out=c.weight, used=self.filled,
-                               decay=self.decay, workspace=work, err=self.err, stream=stream)
+                               decay=self.decay, workspace=self._work,
+                               err=self.err)
         return out
 
-    def compact(self, capacity, now, stream=None):
+    def compact(self, capacity, now):
         """A BoundedStream of fewer slots that holds this one's most used entries; now int32
         [streams]: the next token's position (recency counts from it)."""
         c = self.cache
@@ -83,7 +89,7 @@ class BoundedStream:
                            device=self.err.device)
         # slots past the filled ones are empty, so they may count where they are needed
         fdp.op_cache_compact(c, new.cache, now, came, used=max(used, capacity), sinks=self.sinks,
-                             recent=self.recent, stream=stream)
+                             recent=self.recent)
         new.filled = min(capacity, used)
         return new
 

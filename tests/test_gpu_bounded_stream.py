@@ -153,3 +153,29 @@ def test_example_runs():
     assert r.returncode == 0, r.stderr[-2000:]
     window, used = (float(line.split(": ")[1].split()[0]) for line in r.stdout.strip().splitlines())
     assert used < 0.5 * window
+
+
+def test_steps_on_another_stream_and_of_no_tokens():
+    """Everything runs on the current stream, a chunk's common position too."""
+    S, H, G, D, C = 2, 8, 2, 64, 64
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x = [[torch.randn(S, n, h, D, generator=gen, device="cuda").bfloat16() for h in (H, G, G)]
+         for n in (48, 16, 0, 40)]
+    pos, start = [], 0
+    for q, _, _ in x:
+        pos.append((start + torch.arange(q.shape[1], device="cuda").int()).expand(S, -1).contiguous())
+        start += q.shape[1]
+
+    def run():
+        b = BoundedStream(S, H, G, D, C, plan=fdp.Rotary(D), sinks=1, recent=8)
+        return [b.step(*t, p, whole_chunk=True).clone() for t, p in zip(x, pos)], b
+    want, a = run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(5_000_000)  # the current stream of the calls is behind the default one
+        got, b = run()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(s, t) for s, t in zip(got, want)) and want[2].shape[1] == 0
+    assert torch.equal(a.cache.weight, b.cache.weight) and torch.equal(a.cache.pos, b.cache.pos)
+    a.check(), b.check()

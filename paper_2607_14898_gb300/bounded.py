@@ -36,7 +36,6 @@ class BoundedStream:
         self.filled = 0  # slots that may hold something: new tokens take empty slots in order
         self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self._buffers: dict = {}
-        self._work = torch.empty(0, dtype=torch.uint8, device=device)
 
     def _buffer(self, name, shape, dtype):
         """A buffer of the step, allocated when its size first comes up."""
@@ -67,15 +66,17 @@ class BoundedStream:
         fdp.op_cache_insert(c, k, v, pos, slots, sinks=self.sinks, recent=self.recent)
         self.filled = min(c.capacity, self.filled + n)
         out = self._buffer("out", (S, n, H, D), c.dtype)
-        # what a call needs does not only grow with the slots: take the larger of now and full
+        # What a call needs does not only grow with the slots: take the larger of now and full. (One
+        # workspace for each step size: a captured step keeps its own.)
         need = max(fdp.cache_attention_workspace_bytes(c, H, n, u)
                    for u in (self.filled, c.capacity))
-        if self._work.numel() < need:
-            self._work = torch.empty(need, dtype=torch.uint8, device=self.err.device)
+        work = self._buffers.get(("work", n))
+        if work is None or work.numel() < need:
+            work = self._buffers[("work", n)] = torch.empty(need, dtype=torch.uint8,
+                                                            device=self.err.device)
         q_pos = pos[:, -1:].expand(S, n).contiguous() if whole_chunk else pos
         fdp.op_cache_attention(c, q, q_pos, out, weight_out=c.weight, used=self.filled,
-                               decay=self.decay, workspace=self._work,
-                               err=self.err)
+                               decay=self.decay, workspace=work, err=self.err)
         return out
 
     def compact(self, capacity, now):

@@ -135,6 +135,13 @@ __device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t (&r)
       : "r"(taddr));
 }
 
+// sum += x where a < b
+__device__ __forceinline__ void add_if_less(float& sum, float x, uint32_t a, uint32_t b) {
+  asm("{\n\t.reg .pred p;\n\tsetp.lt.u32 p, %2, %3;\n\t@p add.rn.f32 %0, %0, %1;\n\t}"
+      : "+f"(sum)
+      : "f"(x), "r"(a), "r"(b));
+}
+
 constexpr int kTile = 128;      // rows of a tile, slots of a block
 constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swizzled sub-tile
 
@@ -816,7 +823,7 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
 // a thread and all rows the reads were what bounded the kernel).
 // Bound by the exponentials and the wait for the next scores: an accumulator is free when its group
 // has read the last of it, and the other group's is all that runs meanwhile (TMEM holds two for
-// each of the SM's two CTAs). 2 x 2001 queries of 32 heads of 128 over 8191 slots: 250 us, 1073
+// each of the SM's two CTAs). 2 x 2001 queries of 32 heads of 128 over 8191 slots: 240 us, 1119
 // TFLOP/s; 1560 of 16 heads of 64 over 6240: 34 us, 586 TFLOP/s.
 //   warps 0-3 / 4-7  even / odd tiles   warp 8  TMA   warp 9  products   warp 10  lse and limits
 template <int D>
@@ -996,6 +1003,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
       tmem_ld_16x256b_x2(col, buf[0][0]);
       tmem_ld_16x256b_x2(col + (16u << 16), buf[0][1]);
       uint64_t sum2[4] = {0, 0, 0, 0};  // even and odd rows
+      float sum[4][2] = {};
       auto add = [&](auto masked) {
 #pragma unroll
         for (int d = 0; d < kTile; d += 16) {
@@ -1025,10 +1033,12 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
               e0 = ex2_approx(e0);
               e1 = ex2_approx(e1);
               if constexpr (decltype(masked)::value) {
-                e0 = pos[k] < lim.x ? e0 : 0.f;
-                e1 = pos[k] < lim.y ? e1 : 0.f;
+                // (as predicated sums: with selects the integer pipe was the busiest)
+                add_if_less(sum[k][0], e0, pos[k], lim.x);
+                add_if_less(sum[k][1], e1, pos[k], lim.y);
+              } else {
+                asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[k]) : "l"(pack_f32x2(e0, e1)));
               }
-              asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[k]) : "l"(pack_f32x2(e0, e1)));
             }
           }
         }
@@ -1039,7 +1049,7 @@ __global__ void __launch_bounds__(WeighCfg<D>::kThreads, 2)
       for (int k = 0; k < 4; ++k) {
         float s0, s1;
         asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(sum2[k]));
-        totals[k] += s0 + s1;
+        totals[k] += (s0 + sum[k][0]) + (s1 + sum[k][1]);
       }
     }
     // the four threads of a slot have shared out the rows; thread t keeps slot t % 4

@@ -1154,7 +1154,7 @@ ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q) {
   // CTAs of 2 blocks at least 16, of 8 at least 27)
   y.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kSms, units)));
   // row splits: the fewest waves of two CTAs an SM, counted in tiles one after the other (480p
-  // chunk: 3 splits 95 us, none 103; prompt of 2 x 2001 queries over 8191 slots: 2 splits 658, none 667)
+  // chunk: 3 splits 95 us, none 103; prompt of 2 x 2001 queries over 8191 slots: 2 or none the same)
   const int64_t ctas = lists * y.key_tiles;
   int64_t best = INT64_MAX;
   for (int r = 1; r <= 8 && r <= y.row_tiles; ++r) {

@@ -823,7 +823,9 @@ __global__ void __launch_bounds__(kTile) join_parts_kernel(const __grid_constant
 // a thread and all rows the reads were what bounded the kernel).
 // Bound by the exponentials and the wait for the next scores: an accumulator is free when its group
 // has read the last of it, and the other group's is all that runs meanwhile (TMEM holds two for
-// each of the SM's two CTAs). 2 x 2001 queries of 32 heads of 128 over 8191 slots: 240 us, 1119
+// each of the SM's two CTAs). Freeing them by halves of 64 rows with a product thread for each group was
+// slower all the same (275 us for the prompt below, then at 249), and so was that thread alone (264).
+// 2 x 2001 queries of 32 heads of 128 over 8191 slots: 240 us, 1119
 // TFLOP/s; 1560 of 16 heads of 64 over 6240: 34 us, 586 TFLOP/s.
 //   warps 0-3 / 4-7  even / odd tiles   warp 8  TMA   warp 9  products   warp 10  lse and limits
 template <int D>

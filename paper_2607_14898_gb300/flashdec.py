@@ -763,6 +763,8 @@ def op_rotary(plan: Rotary, positions, q, q_out, k=None, k_out=None, backward=Fa
     """Turns q [T][heads][head_dim] (and k) by positions int32 [T][axes] ([T] for one axis) into
     q_out (k_out), which may be q (k) itself; with backward=True the gradient (fd_op_rotary)."""
     shape, dtype, dev = q.shape, q.dtype, q.get_device()
+    if dev < 0:  # (the other tensors are compared with q)
+        raise TypeError("q: a CUDA tensor is required")
     if len(shape) != 3 or shape[2] != plan.head_dim:
         raise ValueError(f"q: shape {tuple(shape)}, [tokens][heads][{plan.head_dim}] is required")
     T = shape[0]

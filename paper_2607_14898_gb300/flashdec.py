@@ -670,13 +670,21 @@ def _dtype_code(dtype) -> int:
     return code
 
 
-_raw_stream = None
+_raw_stream = _cuda = None
 
 
 def _stream_on(device: int, stream) -> int:
     """The stream's handle; of the device's current stream where none is given. (The handle alone:
-    a torch.cuda.Stream object takes 3 us to make, half of what a small call takes in all.)"""
-    global _raw_stream
+    a torch.cuda.Stream object takes 3 us to make, half of what a small call takes in all.) The
+    library launches on the current device: tensors of another one are refused."""
+    global _raw_stream, _cuda
+    if _cuda is None:
+        import torch
+        _cuda = torch.cuda
+    current = _cuda.current_device()
+    if device != current:
+        raise ValueError(f"tensors on cuda:{device}: the library works on the current device, "
+                         f"which is cuda:{current}")
     if stream is None:
         if _raw_stream is None:
             import torch

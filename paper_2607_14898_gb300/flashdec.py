@@ -733,6 +733,20 @@ def _rows(t, what: str, shape, dtype, device: int):
     _refuse(t, what, shape, dtype, device, False)
 
 
+def _status_word(err, dtype, device: int) -> int:
+    """Address of the int32 that a call's kernels report a wait in that gave up (0 for None, which the
+    library refuses where it needs one)."""
+    if err is None:
+        return 0
+    try:
+        if (err.dtype is dtype and err.get_device() == device and err.shape.numel() > 0
+                and err.is_contiguous()):
+            return err.data_ptr()
+    except AttributeError:
+        pass
+    raise TypeError(f"err: a contiguous int32 tensor on cuda:{device} is required")
+
+
 class Rotary:
     """Frequencies of a rotary embedding (fd_rotary_create): the leading rot_dim elements of a
     head (all by default) in pairs of the given layout, split over the position axes by axis_dims."""
@@ -862,7 +876,8 @@ def op_cache_attention(cache: Cache, q, q_pos, out, weight_out=None, used=None, 
         raise ValueError(f"workspace: {need} bytes of contiguous memory on cuda:{dev} are required")
     code = lib().fd_op_cache_attention(
         cache.ref, used, H, n, qp, qs[0], qs[1], qs[2], pos, D ** -0.5 if scale is None else scale,
-        decay, op, os_[0], os_[1], os_[2], wp, _ptr(workspace), _ptr(err), _stream_on(dev, stream))
+        decay, op, os_[0], os_[1], os_[2], wp, _ptr(workspace), _status_word(err, cache.int32, dev),
+        _stream_on(dev, stream))
     if code:
         raise FdError(code, "fd_op_cache_attention")
 

@@ -5,8 +5,8 @@ any length of stream, the entries that attention has used most: each step turns 
 and keys by their positions, puts the new keys and values into the slots of the entries with the
 least accumulated weight, and attends over the slots, adding to their weights. A step is three
 library calls (fd_op_rotary, fd_op_cache_insert, fd_op_cache_attention) on buffers that are
-allocated once for each step size, so that once the cache is full steps can be captured in a CUDA
-graph.
+allocated when a step size first comes up, so that once the cache is full steps can be captured in
+a CUDA graph. The buffers of the last few step sizes are kept, and those of captured steps.
 """
 from __future__ import annotations
 
@@ -24,6 +24,8 @@ class BoundedStream:
 
     The calls run on the current stream; the tensors that they are given have to be ready on it."""
 
+    KEPT_SIZES = 4  # step sizes whose buffers are kept, besides those of captured steps
+
     def __init__(self, streams, heads, groups, head_dim, capacity, dtype=torch.bfloat16, plan=None,
                  sinks=4, recent=0, decay=1.0, device="cuda"):
         self.heads, self.plan = heads, plan
@@ -36,14 +38,43 @@ class BoundedStream:
         self.filled = 0  # slots that may hold something: new tokens take empty slots in order
         self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self._buffers: dict = {}
+        self._streams: dict = {}      # the streams that have used each buffer
+        self._sizes: dict = {}        # the buffers of each step size, the one used last at the end
+        self._captured: set = set()   # step sizes that graphs hold
+
+    def _begin(self, n):
+        """A step of n tokens begins: lets go of the buffers of the size that was used least recently
+        when there are more than KEPT_SIZES. A captured step's stay: its graph holds their addresses."""
+        self._here = fdp._stream_on(self.cache.device, None)
+        self._capturing = torch.cuda.is_current_stream_capturing()
+        if self._capturing:
+            self._captured.add(n)
+        self._size = self._sizes[n] = self._sizes.pop(n, set())
+        if len(self._sizes) > self.KEPT_SIZES:
+            for m in [m for m in self._sizes if m not in self._captured][:-self.KEPT_SIZES]:
+                for key in self._sizes.pop(m):
+                    del self._buffers[key], self._streams[key]
+
+    def _find(self, key):
+        """The buffer of this key, or None. Its memory is not given to anyone else, once it is let go of,
+        before the current stream is through with it."""
+        t = self._buffers.get(key)
+        if t is not None and self._here not in self._streams[key] and not self._capturing:
+            t.record_stream(torch.cuda.current_stream(t.device))
+            self._streams[key].add(self._here)
+        return t
+
+    def _new(self, key, shape, dtype):
+        self._size.add(key)
+        self._streams[key] = {self._here}
+        t = self._buffers[key] = torch.empty(shape, dtype=dtype, device=self.err.device)
+        return t
 
     def _buffer(self, name, shape, dtype):
         """A buffer of the step, allocated when its size first comes up."""
         key = (name, tuple(shape))
-        t = self._buffers.get(key)
-        if t is None:
-            t = self._buffers[key] = torch.empty(shape, dtype=dtype, device=self.err.device)
-        return t
+        t = self._find(key)
+        return self._new(key, shape, dtype) if t is None else t
 
     def step(self, q, k, v, pos, axes_pos=None, whole_chunk=False):
         """Attention of q [streams][n][heads][head_dim] over the cache with the new k, v
@@ -56,6 +87,7 @@ class BoundedStream:
             return torch.empty_like(q)
         c = self.cache
         G = c.groups
+        self._begin(n)
         if self.plan is not None:
             turn = (pos if axes_pos is None else axes_pos).reshape(S * n, -1)
             q_t, k_t = (self._buffer("q", q.shape, q.dtype), self._buffer("k", k.shape, k.dtype))
@@ -76,10 +108,9 @@ class BoundedStream:
         # workspace for each step size: a captured step keeps its own.)
         need = max(fdp.cache_attention_workspace_bytes(c, H, n, u)
                    for u in (self.filled, c.capacity))
-        work = self._buffers.get(("work", n))
+        work = self._find(("work", n))
         if work is None or work.numel() < need:
-            work = self._buffers[("work", n)] = torch.empty(need, dtype=torch.uint8,
-                                                            device=self.err.device)
+            work = self._new(("work", n), (need,), torch.uint8)
         q_pos = pos[:, -1:].expand(S, n).contiguous() if whole_chunk else pos
         fdp.op_cache_attention(c, q, q_pos, out, weight_out=c.weight, used=self.filled,
                                decay=self.decay, workspace=work, err=self.err)

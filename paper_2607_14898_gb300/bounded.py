@@ -19,7 +19,9 @@ class BoundedStream:
     """Caches of `streams` streams with `capacity` slots for each KV group.
 
     plan: the Rotary that turns queries and keys (None: they come turned). sinks, recent: entries at
-    positions below `sinks` or among the last `recent` before the step's first token are given up last.
+    positions below `sinks` or among the last `recent` before the step's first token are given up last;
+    recent is half of the capacity by default. (With none of the newest protected, totals that only
+    grow give up the entries that came last first, and the cache stays as it was when it filled up.)
     decay: the weights gathered so far are multiplied by it before a step's are added.
 
     The calls run on the current stream; the tensors that they are given have to be ready on it."""
@@ -27,9 +29,11 @@ class BoundedStream:
     KEPT_SIZES = 4  # step sizes whose buffers are kept, besides those of captured steps
 
     def __init__(self, streams, heads, groups, head_dim, capacity, dtype=torch.bfloat16, plan=None,
-                 sinks=4, recent=0, decay=1.0, device="cuda"):
+                 sinks=4, recent=None, decay=1.0, device="cuda"):
         self.heads, self.plan = heads, plan
-        self.sinks, self.recent, self.decay = sinks, recent, decay
+        self._recent_given = recent is not None
+        self.recent = recent if self._recent_given else capacity // 2
+        self.sinks, self.decay = sinks, decay
         shape = (streams, groups, capacity)
         k = torch.zeros(*shape, head_dim, dtype=dtype, device=device)
         self.cache = fdp.Cache(k, torch.zeros_like(k),
@@ -118,16 +122,18 @@ class BoundedStream:
 
     def compact(self, capacity, now):
         """A BoundedStream of fewer slots that holds this one's most used entries; now int32
-        [streams]: the next token's position (recency counts from it)."""
+        [streams]: the next token's position (recency counts from it, and is the new stream's: half of
+        its capacity unless this stream was given another)."""
         c = self.cache
         used = self.filled
         new = BoundedStream(c.streams, self.heads, c.groups, c.head_dim, capacity, c.dtype,
-                            self.plan, self.sinks, self.recent, self.decay, self.err.device)
+                            self.plan, self.sinks, self.recent if self._recent_given else None,
+                            self.decay, self.err.device)
         came = torch.empty(c.streams, c.groups, capacity, dtype=torch.int32,
                            device=self.err.device)
         # slots past the filled ones are empty, so they may count where they are needed
         fdp.op_cache_compact(c, new.cache, now, came, used=max(used, capacity), sinks=self.sinks,
-                             recent=self.recent)
+                             recent=new.recent)
         new.filled = min(capacity, used)
         return new
 

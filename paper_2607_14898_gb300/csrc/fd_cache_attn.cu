@@ -431,8 +431,13 @@ Layout layout_of(const fd_cache* c, int used, int heads, int n_q) {
 
 template <bool F16, int D>
 cudaError_t launch_few(const CacheAttn& p, int lists, cudaStream_t s) {
-  static const cudaError_t attr = cudaFuncSetAttribute(
-      few_rows_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, few::kSmem);
+  int device = -1;
+  if (const cudaError_t e = cudaGetDevice(&device); e != cudaSuccess) return e;
+  static OncePerDevice smem;
+  const cudaError_t attr = smem.run(device, [] {
+    return cudaFuncSetAttribute(few_rows_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                few::kSmem);
+  });
   if (attr != cudaSuccess) return attr;
   if (p.rows > 0) {
     const dim3 grid(p.splits, (p.rows + few::kRows - 1) / few::kRows, lists);

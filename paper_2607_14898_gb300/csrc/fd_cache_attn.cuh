@@ -2,6 +2,7 @@
 // fd_cache_chunk.cu (many rows).
 #pragma once
 #include "fd_internal.h"
+#include "fd_once.h"
 #include "fd_ptx.cuh"
 #include "flashdec_ops.h"
 

@@ -1110,13 +1110,16 @@ template <bool F16, int D>
 cudaError_t launch_t(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {
   using A = AttendCfg<D>;
   using W = WeighCfg<D>;
-  static const cudaError_t attr = [] {
+  int device = -1;
+  if (const cudaError_t e = cudaGetDevice(&device); e != cudaSuccess) return e;
+  static OncePerDevice smem;
+  const cudaError_t attr = smem.run(device, [] {
     const cudaError_t e = cudaFuncSetAttribute(
         attend_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, A::kSmem);
     if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(weigh_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 W::kSmem);
-  }();
+  });
   if (attr != cudaSuccess) return attr;
   CUtensorMap tq, tk, tv;
   if (!make_map(&tq, F16, p.q, D, p.heads, p.n_q, c->streams, p.q_head, p.q_token, p.q_stream,

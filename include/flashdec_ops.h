@@ -314,6 +314,12 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
                                 int64_t out_token_stride, int64_t out_head_stride,
                                 float* weight_out, void* workspace, int* err_dev, void* stream);
 
+/* Failure-path check: the waits of the attention's kernels for many rows give up after 2 s; here one of
+ * them (0 a thread's, 1 a thread's for copies in flight, 2 a warp's, 3 a polling loop) waits on a
+ * barrier that nothing arrives at, with a limit of 1 ms, and sets bit 32 of *err_dev when it gives up.
+ * (All but 1 give up early where *err_dev is not 0 already.) The kernel ends by itself. */
+fd_status fd_debug_cache_wait_timeout(int which, int* err_dev, void* stream);
+
 /* New tokens into the cache, evicting what they displace. For each (stream, group), the slots
  * are ranked by (class, weight, slot index): class 0 empty slots (weights ignored), class 1
  * entries that nothing protects, class 2 protected ones (pos < sinks, or pos >= new_pos[0] -

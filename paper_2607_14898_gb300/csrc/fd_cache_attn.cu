@@ -590,4 +590,13 @@ fd_status fd_op_cache_attention(const fd_cache* cache, int used, int heads, int 
   return e == cudaSuccess ? FD_OK : FD_ERR_CUDA;
 }
 
+fd_status fd_debug_cache_wait_timeout(int which, int* err_dev, void* stream) {
+  if (which < 0 || which > 3 || !fd::ok_ptr(err_dev, 4)) return FD_ERR_INVALID_ARG;
+  const fd_status st = fd::check_device();
+  if (st != FD_OK) return st;
+  return fd::launch_chunk_wait_check(which, err_dev, static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? FD_OK
+             : FD_ERR_CUDA;
+}
+
 }  // extern "C"

@@ -76,5 +76,7 @@ struct ChunkPlan {
 };
 ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q);
 cudaError_t launch_chunk(const CacheAttn& p, const fd_cache* c, cudaStream_t s);
+// one of the many-rows form's waits (0 to 3) on a barrier that nothing arrives at
+cudaError_t launch_chunk_wait_check(int which, int* err, cudaStream_t s);
 
 }  // namespace fd

@@ -74,34 +74,46 @@ __device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t lead
          (static_cast<uint64_t>(2) << 61);
 }
 
-// The waits of this file, kTries tries at most (a try suspends the thread for a while; a wait that
+// The waits of this file: at most kWaitLimitNs, like those of the library's other kernels (a wait that
 // succeeds takes microseconds). One try is inline, the loop in a function of its own: with
 // mbar_wait's 64-fold unrolled loop at every wait the attend kernel was 132 KB of code and a third
 // of its issue slots went to instruction fetches (a third slower over the 480p chunk), and short
-// loops inline cost as much in registers spilled around them.
-constexpr int kTries = 1 << 24;
-// Gives up after kTries, or soon after another wait of this launch (or an earlier one on the
+// loops inline cost as much in registers spilled around them. LIMIT is another only in the check of
+// the waits themselves.
+//
+// Gives up after LIMIT, or soon after another wait of this launch (or an earlier one on the
 // same status word) has given up (looked up every 64 tries: the word is a trip to L2 away); not so
 // a drain, which waits for the CTA's own copies and products in flight.
+template <unsigned long long LIMIT>
 __device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, int* err, int code, bool drain) {
+  unsigned long long start = 0;
 #pragma unroll 1
-  for (int n = 0; !mbar_try_wait(bar, parity); ++n) {
-    if (n == kTries || (!drain && n % 64 == 63 && *reinterpret_cast<volatile int*>(err) != 0)) {
+  for (unsigned n = 0; !mbar_try_wait(bar, parity); ++n) {
+    if (n % 64 != 63) continue;
+    const unsigned long long now = globaltimer();
+    if (n == 63) start = now;
+    if (now - start > LIMIT || (!drain && *reinterpret_cast<volatile int*>(err) != 0)) {
       atomicOr(err, code);
       return false;
     }
   }
   return true;
 }
+template <unsigned long long LIMIT = kWaitLimitNs>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int* err, int code,
                                      bool drain = false) {
-  return mbar_try_wait(bar, parity) || wait_more(bar, parity, err, code, drain);
+  return mbar_try_wait(bar, parity) || wait_more<LIMIT>(bar, parity, err, code, drain);
 }
 // For loops over several barriers that take whichever is through: whether to go on after a round
-// that found none (kTries rounds at most; the status word is looked up every 1024).
-__device__ __forceinline__ bool poll_again(int& rounds, int* err, int code) {
+// that found none. rounds is 0 after one that did; every 1024 the time and the status word are looked at
+// (32 bits of nanoseconds: they wrap after more than twice the limit).
+template <unsigned long long LIMIT = kWaitLimitNs>
+__device__ __forceinline__ bool poll_again(int& rounds, uint32_t& start, int* err, int code) {
+  static_assert(LIMIT < 1ull << 31, "start wraps");
   if (++rounds % 1024 != 0) return true;
-  if (rounds < kTries && *reinterpret_cast<volatile int*>(err) == 0) return true;
+  const uint32_t now = static_cast<uint32_t>(globaltimer());
+  if (rounds == 1024) start = now;
+  if (now - start <= LIMIT && *reinterpret_cast<volatile int*>(err) == 0) return true;
   atomicOr(err, code);
   return false;
 }
@@ -109,20 +121,52 @@ __device__ __forceinline__ bool poll_again(int& rounds, int* err, int code) {
 // waits, have to be executed by all its lanes at once): every decision is the warp's, so that its
 // lanes never part. (Each instruction that only brings lanes together, or waits for a barrier that
 // is through already, took 100 to 200 cycles of the attend kernel's softmax.)
+template <unsigned long long LIMIT>
 __device__ __noinline__ bool wait_more_warp(uint32_t bar, uint32_t parity, int* err, int code) {
+  unsigned long long start = 0;
 #pragma unroll 1
-  for (int n = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
-    if (n == kTries ||
-        (n % 64 == 63 && __any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(err) != 0))) {
+  for (unsigned n = 0; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
+    if (n % 64 != 63) continue;
+    const unsigned long long now = globaltimer();
+    if (n == 63) start = now;
+    if (__any_sync(0xffffffffu,
+                   now - start > LIMIT || *reinterpret_cast<volatile int*>(err) != 0)) {
       atomicOr(err, code);
       return false;
     }
   }
   return true;
 }
+template <unsigned long long LIMIT = kWaitLimitNs>
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, int code) {
   return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) ||
-         wait_more_warp(bar, parity, err, code);
+         wait_more_warp<LIMIT>(bar, parity, err, code);
+}
+
+// The waits above on a barrier that nothing arrives at, a warp: the word gets ERR_WAIT_CHECK when
+// they give up, after a millisecond.
+constexpr unsigned long long kCheckLimitNs = 1000000ull;
+__global__ void __launch_bounds__(32) wait_check_kernel(int which, int* err) {
+  __shared__ uint64_t never;
+  const uint32_t bar = smem_u32(&never);
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    fence_barrier_init();
+  }
+  __syncthreads();
+  if (which == 0) {
+    if (threadIdx.x == 0) wait<kCheckLimitNs>(bar, 0, err, ERR_WAIT_CHECK);
+  } else if (which == 1) {
+    if (threadIdx.x == 0) wait<kCheckLimitNs>(bar, 0, err, ERR_WAIT_CHECK, true);
+  } else if (which == 2) {
+    wait_warp<kCheckLimitNs>(bar, 0, err, ERR_WAIT_CHECK);
+  } else if (threadIdx.x == 0) {
+    int rounds = 0;
+    uint32_t start = 0;
+    while (!mbar_test_wait(bar, 0) &&
+           poll_again<kCheckLimitNs>(rounds, start, err, ERR_WAIT_CHECK)) {
+    }
+  }
 }
 
 // 16 lanes of the warp's quarter and 16 columns in 16 x 8 fragments: of fragment j thread t gets
@@ -334,6 +378,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         return lst;
       };
       int segs = 0, idle = 0;
+      uint32_t idle_since = 0;
       while (k.w.valid() || v.w.valid()) {
         bool moved = false;
         if (k.w.valid() && mbar_test_wait(bar(C::kKFree + k.slot), k.phase ^ 1) &&
@@ -356,7 +401,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         }
         if (moved)
           idle = 0;
-        else if (!poll_again(idle, p.err, ERR_WAIT_MMA))
+        else if (!poll_again(idle, idle_since, p.err, ERR_WAIT_MMA))
           break;
       }
       // nothing may be in flight when the CTA exits
@@ -387,7 +432,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
     fetch();
     // blocks published and halves of V made ready so far
     int J = 0, n = 0, slot = 0, idle = 0;
-    uint32_t phase = 0;
+    uint32_t phase = 0, idle_since = 0;
     // Bit i: this lane's slot 32 i + lane of the block published last is empty; above, those of the
     // blocks before it. (The softmax reads a block's scores after its part of the product before
     // last, so V is at most two blocks behind.)
@@ -440,7 +485,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
       }
       if (moved)
         idle = 0;
-      else if (!__all_sync(0xffffffffu, poll_again(idle, p.err, ERR_WAIT_TMA)))
+      else if (!__all_sync(0xffffffffu, poll_again(idle, idle_since, p.err, ERR_WAIT_TMA)))
         break;
     }
   } else if (warp >= 17) {  // 17 and 18
@@ -1182,6 +1227,11 @@ ChunkPlan chunk_plan(const fd_cache* c, int used, int per, int n_q) {
   if (y.row_splits > 1) at += up(static_cast<size_t>(y.row_splits) * lists * used * 4);
   y.total = at;
   return y;
+}
+
+cudaError_t launch_chunk_wait_check(int which, int* err, cudaStream_t s) {
+  wait_check_kernel<<<1, 32, 0, s>>>(which, err);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_chunk(const CacheAttn& p, const fd_cache* c, cudaStream_t s) {

@@ -137,6 +137,7 @@ _SIGS = {
                                                              _I]),
     "fd_op_cache_attention": (_I, [ctypes.POINTER(fd_cache), _I, _I, _I, _P, _L, _L, _L, _P, _F,
                                    _F, _P, _L, _L, _L, _P, _P, _P, _P]),
+    "fd_debug_cache_wait_timeout": (_I, [_I, _P, _P]),
     "fd_op_cache_insert": (_I, [ctypes.POINTER(fd_cache), _I, _P, _P, _L, _L, _L, _P, _I, _I, _P,
                                 _P, _P, _P]),
     "fd_op_cache_compact": (_I, [ctypes.POINTER(fd_cache), _I, ctypes.POINTER(fd_cache), _P, _I,
@@ -885,6 +886,17 @@ def op_cache_attention(cache: Cache, q, q_pos, out, weight_out=None, used=None, 
         _stream_on(dev, stream))
     if code:
         raise FdError(code, "fd_op_cache_attention")
+
+
+def debug_cache_wait_timeout(which: int, err, stream=None) -> None:
+    """One of the attention's bounded waits on a barrier that nothing arrives at, with a limit of 1 ms:
+    sets bit 32 of err (fd_debug_cache_wait_timeout)."""
+    import torch
+    dev = err.get_device()
+    code = lib().fd_debug_cache_wait_timeout(which, _status_word(err, torch.int32, dev),
+                                             _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_debug_cache_wait_timeout")
 
 
 def op_cache_insert(cache: Cache, k_new, v_new, new_pos, slots, pos_out=None, weight_out=None,

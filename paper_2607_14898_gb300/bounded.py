@@ -44,41 +44,50 @@ class BoundedStream:
         self._buffers: dict = {}
         self._streams: dict = {}      # the streams that have used each buffer
         self._sizes: dict = {}        # the buffers of each step size, the one used last at the end
+        self._latest = self._marked = None
         self._captured: set = set()   # step sizes that graphs hold
 
     def _begin(self, n):
         """A step of n tokens begins: lets go of the buffers of the size that was used least recently
         when there are more than KEPT_SIZES. A captured step's stay: its graph holds their addresses."""
-        self._here = fdp._stream_on(self.cache.device, None)
-        self._capturing = torch.cuda.is_current_stream_capturing()
-        if self._capturing:
+        self._here = here = fdp._stream_on(self.cache.device, None)
+        capturing = torch.cuda.is_current_stream_capturing()
+        if capturing:
             self._captured.add(n)
-        self._size = self._sizes[n] = self._sizes.pop(n, set())
+        # the buffers of the last step that came to its end know the stream that it ran on
+        self._moved = self._marked != (n, here) and not capturing
+        self._marked = None
+        if n == self._latest:
+            return
+        self._latest = n
+        self._sizes[n] = self._sizes.pop(n, set())
         if len(self._sizes) > self.KEPT_SIZES:
             for m in [m for m in self._sizes if m not in self._captured][:-self.KEPT_SIZES]:
                 for key in self._sizes.pop(m):
                     del self._buffers[key], self._streams[key]
 
-    def _find(self, key):
-        """The buffer of this key, or None. Its memory is not given to anyone else, once it is let go of,
-        before the current stream is through with it."""
-        t = self._buffers.get(key)
-        if t is not None and self._here not in self._streams[key] and not self._capturing:
-            t.record_stream(torch.cuda.current_stream(t.device))
-            self._streams[key].add(self._here)
-        return t
-
     def _new(self, key, shape, dtype):
-        self._size.add(key)
+        self._sizes[self._latest].add(key)
         self._streams[key] = {self._here}
         t = self._buffers[key] = torch.empty(shape, dtype=dtype, device=self.err.device)
         return t
 
+    def _mark(self, key, t):
+        """The current stream uses the buffer: its memory, once it is let go of, is not given to anyone
+        else before the stream is through with it."""
+        if self._here not in self._streams[key]:
+            t.record_stream(torch.cuda.current_stream(t.device))
+            self._streams[key].add(self._here)
+
     def _buffer(self, name, shape, dtype):
         """A buffer of the step, allocated when its size first comes up."""
         key = (name, tuple(shape))
-        t = self._find(key)
-        return self._new(key, shape, dtype) if t is None else t
+        t = self._buffers.get(key)
+        if t is None:
+            return self._new(key, shape, dtype)
+        if self._moved:
+            self._mark(key, t)
+        return t
 
     def step(self, q, k, v, pos, axes_pos=None, whole_chunk=False):
         """Attention of q [streams][n][heads][head_dim] over the cache with the new k, v
@@ -110,14 +119,18 @@ class BoundedStream:
         out = self._buffer("out", (S, n, H, D), c.dtype)
         # What a call needs does not only grow with the slots: take the larger of now and full. (One
         # workspace for each step size: a captured step keeps its own.)
-        need = max(fdp.cache_attention_workspace_bytes(c, H, n, u)
-                   for u in (self.filled, c.capacity))
-        work = self._find(("work", n))
+        need = c.workspace_bytes(self.filled, H, n)
+        if self.filled < c.capacity:
+            need = max(need, c.workspace_bytes(c.capacity, H, n))
+        work = self._buffers.get(("work", n))
         if work is None or work.numel() < need:
             work = self._new(("work", n), (need,), torch.uint8)
+        elif self._moved:
+            self._mark(("work", n), work)
         q_pos = pos[:, -1:].expand(S, n).contiguous() if whole_chunk else pos
         fdp.op_cache_attention(c, q, q_pos, out, weight_out=c.weight, used=self.filled,
                                decay=self.decay, workspace=work, err=self.err)
+        self._marked = None if n in self._captured else (n, self._here)
         return out
 
     def compact(self, capacity, now):

@@ -671,18 +671,18 @@ def _dtype_code(dtype) -> int:
     return code
 
 
-_raw_stream = _cuda = None
+_raw_stream = _get_device = None
 
 
 def _stream_on(device: int, stream) -> int:
     """The stream's handle; of the device's current stream where none is given. (The handle alone:
     a torch.cuda.Stream object takes 3 us to make, half of what a small call takes in all.) The
     library launches on the current device: tensors of another one are refused."""
-    global _raw_stream, _cuda
-    if _cuda is None:
+    global _raw_stream, _get_device
+    if _get_device is None:
         import torch
-        _cuda = torch.cuda
-    current = _cuda.current_device()
+        _get_device = torch._C._cuda_getDevice  # torch.cuda.current_device once CUDA is up
+    current = _get_device()
     if device != current:
         raise ValueError(f"tensors on cuda:{device}: the library works on the current device, "
                          f"which is cuda:{current}")
@@ -745,7 +745,7 @@ def _status_word(err, dtype, device: int) -> int:
     if err is None:
         return 0
     try:
-        if (err.dtype is dtype and err.get_device() == device and err.shape.numel() > 0
+        if (err.dtype is dtype and err.get_device() == device and err.numel()
                 and err.is_contiguous()):
             return err.data_ptr()
     except AttributeError:

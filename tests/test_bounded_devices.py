@@ -27,6 +27,9 @@ class OnDevice:
     def dim(self):
         return len(self.shape)
 
+    def numel(self):
+        return self.shape.numel()
+
     def stride(self):
         return self.steps
 
@@ -83,7 +86,7 @@ def library(monkeypatch):
     lib = Lib()
     monkeypatch.setattr(fdp, "lib", lambda: lib)
     monkeypatch.setattr(fdp, "_raw_stream", lambda device: 0)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(fdp, "_get_device", lambda: 0)  # the current device
     return lib
 
 

@@ -708,7 +708,9 @@ cudaError_t launch(EvictParams& p, int lists, cudaStream_t s) {
   const int per = kThreads * ctas;
   p.iters = (p.slots + per - 1) / per;
   if (p.iters < 1) p.iters = 1;
-  if (!COMPACT && p.iters <= 2) return launch_cluster(evict_long_kernel<2, COMPACT>, p, lists, ctas, s);
+  // (one token's insert as a rule; other lists come here from 8193 slots on, 2 a thread in 8 CTAs)
+  if constexpr (!COMPACT)
+    if (p.iters <= 2) return launch_cluster(evict_long_kernel<2, false>, p, lists, ctas, s);
   if (p.iters <= 12) return launch_cluster(evict_long_kernel<12, COMPACT>, p, lists, ctas, s);
   if (p.iters <= 24) return launch_cluster(evict_long_kernel<24, COMPACT>, p, lists, ctas, s);
   return launch_cluster(evict_long_kernel<0, COMPACT>, p, lists, ctas, s);

@@ -107,7 +107,7 @@ class BoundedStream:
             fdp.op_rotary(self.plan, turn, q.reshape(S * n, H, D), q_t.view(S * n, H, D),
                           k.reshape(S * n, G, D), k_t.view(S * n, G, D))
             q, k = q_t, k_t
-        if not fdp._same_steps(k.stride(), v.stride(), k.shape):
+        if k.stride() != v.stride() and not fdp._same_steps(k.stride(), v.stride(), k.shape):
             # (the insert takes one set of strides: what comes out of the rotation is contiguous, values
             # that are a part of a fused projection are not)
             k, v = (self._buffer(name, x.shape, x.dtype).copy_(x)

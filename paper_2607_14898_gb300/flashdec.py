@@ -736,7 +736,7 @@ def _rows(t, what: str, shape, dtype, device: int):
 
 def _same_steps(a, b, shape) -> bool:
     """Whether strides a and b lead to the same elements: a dimension of one entry never steps."""
-    return a == b or all(x == y or n < 2 for x, y, n in zip(a, b, shape))
+    return all(x == y or n < 2 for x, y, n in zip(a, b, shape))
 
 
 def _status_word(err, dtype, device: int) -> int:
@@ -834,7 +834,7 @@ class Cache:
         vp, vst = _rows(v, "v", k.shape, k.dtype, dev)
         if dev < 0:
             raise TypeError("k: a CUDA tensor is required")
-        if not _same_steps(st, vst, k.shape):
+        if vst != st and not _same_steps(st, vst, k.shape):
             raise ValueError("v: the strides of k are required")
         self.k, self.v, self.pos, self.weight = k, v, pos, weight
         self.streams, self.groups, self.capacity, self.head_dim = S, G, C, D
@@ -912,7 +912,7 @@ def op_cache_insert(cache: Cache, k_new, v_new, new_pos, slots, pos_out=None, we
     n = shape[1]
     kp, st = _rows(k_new, "k_new", shape, cache.dtype, dev)
     vp, vst = _rows(v_new, "v_new", shape, cache.dtype, dev)
-    if not _same_steps(st, vst, shape):
+    if vst != st and not _same_steps(st, vst, shape):
         raise ValueError("v_new: the strides of k_new are required")
     code = lib().fd_op_cache_insert(
         cache.ref, n, kp, vp, st[0], st[1], st[2],

@@ -298,7 +298,9 @@ typedef struct {
  * chunk lets each see the whole chunk). A query that sees no slot gives zeros and adds nothing.
  * q, out of the cache's type: element (stream, t, h, i) of q at q[stream q_stream_stride + t
  * q_token_stride + h q_head_stride + i], of out with the out strides (elements; 16-byte
- * aligned; strides multiples of 8, and >= head_dim where there is more than one entry). q_pos int32 [streams][n_q]. scale > 0, finite; decay finite;
+ * aligned; strides multiples of 8, and >= head_dim where there is more than one entry). out
+ * shares no memory with q, which is read again for the weights, or with the cache. q_pos int32
+ * [streams][n_q]. scale > 0, finite; decay finite;
  * heads / groups <= 128, streams groups <= 65,535, n_q heads / groups <= 1,048,560. weight_out fp32
  * [streams][groups][capacity], entries past `used` are not written; it may be cache->weight;
  * NULL: the weights are not gathered. Softmax, sums and weights are in fp32, P is rounded to the

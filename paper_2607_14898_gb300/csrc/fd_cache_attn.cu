@@ -232,6 +232,9 @@ __global__ void __launch_bounds__(few::kWarps * 32)
         s[n][e] = ex2_approx(s[n][e] - base[e >> 1]);
         l[e >> 1] += s[n][e];
       }
+    // P goes to the cache's type for its product with V, since the tensor cores take 16-bit operands (sums are
+    // fp32): every p is off by 2^-9 (bf16) or 2^-12 (fp16) of itself at most, the output by that share of
+    // sum p |v|, beside its own rounding of the same size. l and the weights come from P unrounded.
 #pragma unroll
     for (int kk = 0; kk < KT / 16; ++kk) {
       const uint32_t a[4] = {Elem<F16>::pack(s[2 * kk][0], s[2 * kk][1]),

@@ -655,6 +655,9 @@ __global__ void __launch_bounds__(AttendCfg<D>::kThreads, 1)
         m = now;
         const uint64_t off2 = pack_f32x2(-off, -off);
         uint64_t sum2[2] = {0, 0};
+        // P in the cache's type, which the product with V takes (fp32 sums): 2^-9 (bf16) or 2^-12 (fp16) of
+        // each p at most, the output by that share of sum p |v|, beside its own rounding of the same
+        // size. The sums are of P unrounded, and weigh works its scores out for itself.
         uint32_t pk[2][16];
 #pragma unroll
         for (int i = 0; i < 2; ++i)

@@ -7,7 +7,10 @@
 // F in units of 2^-64 turns; pos F in wrapping 64-bit arithmetic is then the phase modulo one
 // turn, exact in the product: what is left is the rounding of F (f as a double), |pos| f 2^-53, below
 // 3e-7 rad for any int32 position, where fp32 pos * f is already 0.03 rad off at position 10^6.
-// Its upper 32 bits, as a signed fraction of half a turn, go to sincospif.
+// Its upper 32 bits, as a signed fraction of half a turn, go to sincospif where the outputs are fp32. For
+// 16-bit outputs the hardware's sine and cosine do: at most 4.2e-7 off on [-pi, pi], 3e-7 more
+// from the rounding of the angle and 1.8e-7 from the products, 9e-7 m (|a| + |b|) together, where the
+// output's own rounding is 2^-9 (bf16) or 2^-12 of it (40001 x 40 heads below: 181 us with sincospif).
 //
 // Bound by memory: every element is read and written once. A thread owns one chunk (16 bytes
 // of elements, with their 16 bytes of partners in the half layout) of one token and

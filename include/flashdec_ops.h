@@ -351,6 +351,81 @@ fd_status fd_op_cache_compact(const fd_cache* src, int used, const fd_cache* dst
                               const int32_t* now, int sinks, int recent, int32_t* src_slots,
                               void* stream);
 
+/* ---- checkpoints: activations kept in 8 bits for the backward pass ----
+ *
+ * Blocks of 32 neighbouring elements of a row share a power of two 2^E, the smallest with E >= -126
+ * that lets the block's largest magnitude fit into 127 steps; an element is the code
+ * rint(x 2^-E), ties to even, and stands for code 2^E: at most half a step, 2^(E - 1), off, which is
+ * at most 1/127 of the block's largest magnitude. codes int8 [rows][width], exps uint8
+ * [rows][ceil(width / 32)] holding E + 127. A block that holds an infinity or a NaN has the byte 255 and
+ * codes 0, and is restored as NaN. (What rounds past the largest finite number of the type stays
+ * at the last step, or at the largest fp16 number, before it.) */
+
+/* x of dtype FD_DTYPE_F32 / BF16 / F16, element (row, i) at x[row x_stride + i], into codes and exps.
+ * width % 8 == 0, 8..1,048,576; x 16-byte aligned, x_stride % 8 == 0; codes 8-byte aligned. rows may
+ * be 0. */
+fd_status fd_op_checkpoint_save(int dtype, int rows, int width, const void* x, int64_t x_stride,
+                                int8_t* codes, uint8_t* exps, void* stream);
+
+/* The values back, rounded to dtype (exact in fp32 and bf16). transposed = 0: element (row, i) at
+ * x[row x_stride + i], x 16-byte aligned, x_stride % 8 == 0 and >= width. transposed = 1, the operand of a
+ * weight gradient: element (row, i) at x[i x_stride + row], x_stride >= rows, any alignment of whole
+ * elements. */
+fd_status fd_op_checkpoint_load(int dtype, int transposed, int rows, int width,
+                                const int8_t* codes, const uint8_t* exps, void* x,
+                                int64_t x_stride, void* stream);
+
+/* ---- the join between two residual blocks ----
+ *
+ * The norm after a block, its gate and residual scale, the residual sum and the norm before the
+ * next block, for `rows` tokens of `width` elements in one pass:
+ *   n = b r_post,  r_post = (mean(b^2) + eps)^(-1/2)      (post_gain NULL: n = b, a gain of ones)
+ *   y = h + scale gate n post_gain                        (gate NULL: ones)
+ *   u = y r_pre pre_gain,  r_pre = (mean(y^2) + eps)^(-1/2)   (pre_gain NULL: no u)
+ * in fp32; the norm before is that of y before it is rounded. */
+typedef struct {
+  int32_t rows, width;      /* rows >= 0; width % 8 == 0, 8..8192                             */
+  int32_t dtype;            /* of b, u, du and db: FD_DTYPE_BF16 or FD_DTYPE_F16              */
+  int32_t stream_dtype;     /* of h, y, dy and dh: FD_DTYPE_F32 or dtype                      */
+  const float* post_gain;   /* [width] or NULL                                                */
+  const float* pre_gain;    /* [width] or NULL                                                */
+  const float* gate;        /* [ceil(rows / gate_rows)][width] or NULL; token t has the gate of row
+                               t / gate_rows (one gate for all: gate_rows >= rows; a token's own: 1) */
+  int32_t gate_rows;        /* >= 1 with a gate                                               */
+  float scale;              /* finite                                                         */
+} fd_block_join;
+
+/* Forward. Rows of h, b, y, u are their strides apart (elements, multiples of 8, >= width where there
+ * is more than one row); pointers 16-byte aligned. y may be h and u may be b (same pointer and strides), no other
+ * overlap is allowed. u is NULL without a pre_gain. r_post, r_pre [rows] receive the norms' factors,
+ * which the gradient needs (NULL: not wanted). h_codes, h_exps and b_codes, b_exps (both NULL: not
+ * wanted) receive h and b as fd_op_checkpoint_save gives them. eps >= 0. */
+fd_status fd_op_block_join(const fd_block_join* join, const void* h, int64_t h_stride,
+                           const void* b, int64_t b_stride, float eps, void* y, int64_t y_stride,
+                           void* u, int64_t u_stride, float* r_post, float* r_pre,
+                           int8_t* h_codes, uint8_t* h_exps, int8_t* b_codes, uint8_t* b_exps,
+                           void* stream);
+
+/* Gradient, from those of y (dy; NULL: zero, with a pre_gain only) and u (du; NULL without a pre_gain):
+ * with m = y r_pre, g = du pre_gain and y = h + scale gate n post_gain computed again,
+ *   d = dy + r_pre (g - m mean(g m));  dh = d;  w = scale d
+ *   d_gate = sum w n post_gain;  d_post = sum w gate n;  d_pre = sum du m
+ *   e = w gate post_gain;  db = r_post (e - n mean(e n))
+ * (without the norms: d = dy, db = w gate). h_exps not NULL: h points to codes of rows of `width` (h_stride =
+ * width), their exponents at h_exps; b the same. h is not read without a pre_gain. dh may be dy, db may
+ * be du or a b that is not in codes (same pointer and strides); dh, db, d_post, d_pre, d_gate may be NULL: not wanted. Sums over tokens are in a fixed
+ * order: equal calls give equal bits. workspace: fd_block_join_bwd_workspace_bytes(...) bytes of device
+ * memory (16-byte aligned) that the call overwrites; calls that may overlap need one each. With rows
+ * = 0 d_post and d_pre are zeros. */
+size_t fd_block_join_bwd_workspace_bytes(int rows, int width);
+fd_status fd_op_block_join_bwd(const fd_block_join* join, const void* dy, int64_t dy_stride,
+                               const void* du, int64_t du_stride, const void* h, int64_t h_stride,
+                               const uint8_t* h_exps, const void* b, int64_t b_stride,
+                               const uint8_t* b_exps, const float* r_post, const float* r_pre,
+                               void* dh, int64_t dh_stride, void* db, int64_t db_stride,
+                               float* d_post, float* d_pre, float* d_gate, void* workspace,
+                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

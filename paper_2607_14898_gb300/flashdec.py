@@ -65,6 +65,12 @@ class fd_cache(ctypes.Structure):
         ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
 
 
+class fd_block_join(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "width", "dtype", "stream_dtype")] + [
+        (n, ctypes.c_void_p) for n in ("post_gain", "pre_gain", "gate")] + [
+        ("gate_rows", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
@@ -142,6 +148,13 @@ _SIGS = {
                                 _P, _P, _P]),
     "fd_op_cache_compact": (_I, [ctypes.POINTER(fd_cache), _I, ctypes.POINTER(fd_cache), _P, _I,
                                  _I, _P, _P]),
+    "fd_op_checkpoint_save": (_I, [_I, _I, _I, _P, _L, _P, _P, _P]),
+    "fd_op_checkpoint_load": (_I, [_I, _I, _I, _I, _P, _P, _P, _L, _P]),
+    "fd_op_block_join": (_I, [ctypes.POINTER(fd_block_join), _P, _L, _P, _L, _F, _P, _L, _P, _L,
+                              _P, _P, _P, _P, _P, _P, _P]),
+    "fd_block_join_bwd_workspace_bytes": (ctypes.c_size_t, [_I, _I]),
+    "fd_op_block_join_bwd": (_I, [ctypes.POINTER(fd_block_join), _P, _L, _P, _L, _P, _L, _P, _P, _L,
+                                  _P, _P, _P, _P, _L, _P, _L, _P, _P, _P, _P, _P]),
 }
 
 
@@ -940,3 +953,172 @@ def op_cache_compact(src: Cache, dst: Cache, now, src_slots, used=None, sinks=0,
         _stream_on(dev, stream))
     if code:
         raise FdError(code, "fd_op_cache_compact")
+
+
+# --------------------------------------- a residual block in training: checkpoints and the join
+KEPT_BLOCK = 32  # elements of a row that share a checkpoint's exponent
+
+_types = None
+
+
+def _torch_types():
+    """(int8, uint8, float32, int32), looked up once."""
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.int8, torch.uint8, torch.float32, torch.int32)
+    return _types
+
+
+class Checkpoint8:
+    """Rows of activations kept in 8 bits (fd_op_checkpoint_save): codes int8 [rows][width] and the
+    exponents of their blocks of 32, uint8 [rows][ceil(width / 32)], in the caller's tensors."""
+
+    def __init__(self, codes, exps):
+        int8, uint8, _, _ = _torch_types()
+        if getattr(codes, "ndim", 0) != 2 or not codes.is_cuda:
+            raise TypeError("codes: a CUDA tensor [rows][width] is required")
+        self.device, self.shape = codes.get_device(), codes.shape
+        rows, width = codes.shape
+        self.codes, self.exps = codes, exps
+        self.codes_ptr = _dense(codes, "codes", codes.shape, int8, self.device)
+        self.exps_ptr = _dense(exps, "exps", (rows, -(-width // KEPT_BLOCK)), uint8, self.device)
+
+    @classmethod
+    def empty(cls, rows, width, device="cuda"):
+        import torch
+        return cls(torch.empty(rows, width, dtype=torch.int8, device=device),
+                   torch.empty(rows, -(-width // KEPT_BLOCK), dtype=torch.uint8, device=device))
+
+
+def op_checkpoint_save(x, kept: Checkpoint8, stream=None) -> None:
+    """x [rows][width] (float32, bfloat16 or float16) into kept (fd_op_checkpoint_save)."""
+    xp, st = _rows(x, "x", kept.shape, x.dtype, kept.device)
+    code = lib().fd_op_checkpoint_save(_dtype_code(x.dtype), kept.shape[0], kept.shape[1], xp, st[0],
+                                       kept.codes_ptr, kept.exps_ptr,
+                                       _stream_on(kept.device, stream))
+    if code:
+        raise FdError(code, "fd_op_checkpoint_save")
+
+
+def op_checkpoint_load(kept: Checkpoint8, x, transposed=False, stream=None) -> None:
+    """What kept stands for into x [rows][width], or transposed into x [width][rows]
+    (fd_op_checkpoint_load)."""
+    rows, width = kept.shape
+    xp, st = _rows(x, "x", (width, rows) if transposed else kept.shape, x.dtype, kept.device)
+    code = lib().fd_op_checkpoint_load(_dtype_code(x.dtype), 1 if transposed else 0, rows, width,
+                                       kept.codes_ptr, kept.exps_ptr, xp, st[0],
+                                       _stream_on(kept.device, stream))
+    if code:
+        raise FdError(code, "fd_op_checkpoint_load")
+
+
+def _join_view(rows, width, dtype, stream_dtype, dev, post_gain, pre_gain, gate, gate_tokens, scale):
+    """(fd_block_join, addresses of its gains and gate) of a join's arguments."""
+    f32 = _torch_types()[2]
+    pp = 0 if post_gain is None else _dense(post_gain, "post_gain", (width,), f32, dev)
+    qp = 0 if pre_gain is None else _dense(pre_gain, "pre_gain", (width,), f32, dev)
+    gp = 0
+    if gate is not None:
+        if gate_tokens < 1:
+            raise ValueError("gate_tokens: the number of tokens that share a gate is required")
+        gp = _dense(gate, "gate", (-(-rows // gate_tokens), width), f32, dev)
+        gate_tokens = min(gate_tokens, max(rows, 1))
+    return fd_block_join(rows, width, _dtype_code(dtype), _dtype_code(stream_dtype), pp, qp, gp,
+                         gate_tokens, scale)
+
+
+def _row_or_null(t, what, rows, dev):
+    return 0 if t is None else _dense(t, what, (rows,), _torch_types()[2], dev)
+
+
+def op_block_join(h, b, y, u=None, post_gain=None, pre_gain=None, gate=None, gate_tokens=0,
+                  scale=1.0, eps=1e-6, r_post=None, r_pre=None, h_kept=None, b_kept=None,
+                  stream=None) -> None:
+    """The join between two blocks for residual h [tokens][width] (float32, or b's type) and the block's
+    output b (bfloat16 or float16): y = h + scale gate norm(b) post_gain, and with a pre_gain
+    u = norm(y) pre_gain. gate float32 [ceil(tokens / gate_tokens)][width]; r_post, r_pre float32
+    [tokens] receive the norms' factors, h_kept and b_kept (Checkpoint8) the inputs in 8 bits
+    (fd_op_block_join)."""
+    shape, dev = b.shape, b.get_device()
+    if dev < 0 or len(shape) != 2:
+        raise TypeError("b: a CUDA tensor [tokens][width] is required")
+    rows, width = shape
+    hp, hs = _rows(h, "h", shape, h.dtype, dev)
+    bp, bs = _rows(b, "b", shape, b.dtype, dev)
+    yp, ys = _rows(y, "y", shape, h.dtype, dev)
+    if (u is None) != (pre_gain is None):
+        raise ValueError("u and pre_gain come together")
+    up, us = (0, (0, 0)) if u is None else _rows(u, "u", shape, b.dtype, dev)
+    kept = [0, 0, 0, 0]
+    for i, k in enumerate((h_kept, b_kept)):
+        if k is not None:
+            if k.shape != shape or k.device != dev:
+                raise ValueError(f"a checkpoint of {tuple(shape)} on cuda:{dev} is required")
+            kept[2 * i:2 * i + 2] = k.codes_ptr, k.exps_ptr
+    j = _join_view(rows, width, b.dtype, h.dtype, dev, post_gain, pre_gain, gate, gate_tokens, scale)
+    code = lib().fd_op_block_join(ctypes.byref(j), hp, hs[0], bp, bs[0], eps, yp, ys[0], up, us[0],
+                                  _row_or_null(r_post, "r_post", rows, dev),
+                                  _row_or_null(r_pre, "r_pre", rows, dev), *kept,
+                                  _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_block_join")
+
+
+def block_join_bwd_workspace_bytes(tokens, width) -> int:
+    return lib().fd_block_join_bwd_workspace_bytes(tokens, width)
+
+
+_join_workspace: dict = {}
+
+
+def _input_rows(x, what, shape, dtype, dev):
+    """(address, row stride, exponents' address) of a tensor or of a checkpoint."""
+    if isinstance(x, Checkpoint8):
+        if x.shape != shape or x.device != dev:
+            raise ValueError(f"{what}: a checkpoint of {tuple(shape)} on cuda:{dev} is required")
+        return x.codes_ptr, shape[1], x.exps_ptr
+    p, st = _rows(x, what, shape, dtype, dev)
+    return p, st[0], 0
+
+
+def op_block_join_bwd(dy, du, h, b, dh, db, post_gain=None, pre_gain=None, gate=None,
+                      gate_tokens=0, scale=1.0, r_post=None, r_pre=None, d_post=None, d_pre=None,
+                      d_gate=None, workspace=None, stream=None) -> None:
+    """The gradient of op_block_join from dy (None: zero) and du (None without a pre_gain): dh (may be
+    None), db, and d_post, d_pre float32 [width], d_gate like gate (None: not wanted). h and b: the inputs of
+    the forward call, or the Checkpoint8 that hold them; r_post, r_pre as that call left them
+    (fd_op_block_join_bwd)."""
+    shape, dev = db.shape, db.get_device()
+    if dev < 0 or len(shape) != 2:
+        raise TypeError("db: a CUDA tensor [tokens][width] is required")
+    rows, width = shape
+    stream_dtype = dh.dtype if dh is not None else dy.dtype if dy is not None else h.dtype
+    bp, bs = _rows(db, "db", shape, db.dtype, dev)
+    yp, ys = (0, (0, 0)) if dy is None else _rows(dy, "dy", shape, stream_dtype, dev)
+    hp, hs = (0, (0, 0)) if dh is None else _rows(dh, "dh", shape, stream_dtype, dev)
+    if (du is None) != (pre_gain is None):
+        raise ValueError("du and pre_gain come together")
+    up, us = (0, (0, 0)) if du is None else _rows(du, "du", shape, db.dtype, dev)
+    h_in = (0, 0, 0) if pre_gain is None else _input_rows(h, "h", shape, stream_dtype, dev)
+    b_in = _input_rows(b, "b", shape, db.dtype, dev)
+    f32 = _torch_types()[2]
+    sums = [0 if t is None else _dense(t, n, s, f32, dev) for t, n, s in (
+        (d_post, "d_post", (width,)), (d_pre, "d_pre", (width,)),
+        (d_gate, "d_gate", () if gate is None else gate.shape))]
+    j = _join_view(rows, width, db.dtype, stream_dtype, dev, post_gain, pre_gain, gate, gate_tokens,
+                   scale)
+    need = _join_workspace.get((rows, width))
+    if need is None:
+        if len(_join_workspace) > 1000:
+            _join_workspace.clear()
+        need = _join_workspace[rows, width] = block_join_bwd_workspace_bytes(rows, width)
+    if need and (workspace is None or workspace.get_device() != dev
+                 or not workspace.is_contiguous() or workspace.nbytes < need):
+        raise ValueError(f"workspace: {need} bytes of contiguous memory on cuda:{dev} are required")
+    code = lib().fd_op_block_join_bwd(
+        ctypes.byref(j), yp, ys[0], up, us[0], *h_in, *b_in,
+        _row_or_null(r_post, "r_post", rows, dev), _row_or_null(r_pre, "r_pre", rows, dev), hp, hs[0],
+        bp, bs[0], *sums, _ptr(workspace), _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_block_join_bwd")

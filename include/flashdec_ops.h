@@ -351,6 +351,41 @@ fd_status fd_op_cache_compact(const fd_cache* src, int used, const fd_cache* dst
                               const int32_t* now, int sinks, int recent, int32_t* src_slots,
                               void* stream);
 
+/* ---- attention in which every query sees a span of keys, and its gradient ----
+ *
+ * n_q queries of `heads` heads and n_k keys of `groups` KV heads (head h reads group h / (heads /
+ * groups)); query t sees the keys j with spans[t][0] <= j < spans[t][1] (spans int32 [n_q][2], 8-byte
+ * aligned; bounds outside of [0, n_k) are cut off, an empty span sees nothing). Sequences packed one
+ * behind another, causal masks, the decoder's chunks with their window and new tokens after a past
+ * are all such spans.
+ * Element (token, head, i) of a matrix is at its token_stride token + head_stride head + i (elements;
+ * multiples of 8, >= head_dim where there is more than one; 16-byte aligned pointers).
+ * What no query sees, and the rows of queries that see nothing, have no effect whatever they hold
+ * (NaN too). Keys and values that some query sees, and the queries (and their gradients) that see some,
+ * are finite. */
+typedef struct {
+  int32_t n_q, n_k;         /* 0..16,777,216                                                  */
+  int32_t heads, groups;    /* heads % groups == 0, heads / groups <= 128, heads <= 65,535    */
+  int32_t head_dim;         /* 64 or 128                                                      */
+  int32_t dtype;            /* FD_DTYPE_BF16 or FD_DTYPE_F16                                  */
+  float scale;              /* of the scores, > 0, finite                                     */
+} fd_span_attention;
+
+/* Workspace of the call below (backward = 0) or of its gradient (1), bytes of device memory, 16-byte
+ * aligned, that a call overwrites; calls that may overlap need one each. */
+size_t fd_span_attention_workspace_bytes(const fd_span_attention* attn, int backward);
+
+/* out[t][h] = sum_j exp(s_j - lse) v_j,  s_j = scale q[t][h] . k_j,  lse[h][t] = log sum_j exp(s_j)
+ * (fp32, natural logarithm). A query that sees nothing gets zeros and -inf. Softmax and sums are in fp32, the
+ * probabilities are rounded to dtype for their product with V. The order of every sum is fixed: equal
+ * calls give equal bits. out shares no memory with the inputs. err_dev as for fd_op_linear. */
+fd_status fd_op_span_attention(const fd_span_attention* attn, const void* q, int64_t q_token_stride,
+                               int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                               int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                               int64_t v_head_stride, const int32_t* spans, void* out,
+                               int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                               void* workspace, int* err_dev, void* stream);
+
 /* ---- checkpoints: activations kept in 8 bits for the backward pass ----
  *
  * Blocks of 32 neighbouring elements of a row share a power of two 2^E, the smallest with E >= -126

@@ -71,6 +71,11 @@ class fd_block_join(ctypes.Structure):
         ("gate_rows", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class fd_span_attention(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_q", "n_k", "heads", "groups", "head_dim",
+                                              "dtype")] + [("scale", ctypes.c_float)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
@@ -148,6 +153,9 @@ _SIGS = {
                                 _P, _P, _P]),
     "fd_op_cache_compact": (_I, [ctypes.POINTER(fd_cache), _I, ctypes.POINTER(fd_cache), _P, _I,
                                  _I, _P, _P]),
+    "fd_span_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(fd_span_attention), _I]),
+    "fd_op_span_attention": (_I, [ctypes.POINTER(fd_span_attention)] + [_P, _L, _L] * 3 + [
+        _P, _P, _L, _L, _P, _P, _P, _P]),
     "fd_op_checkpoint_save": (_I, [_I, _I, _I, _P, _L, _P, _P, _P]),
     "fd_op_checkpoint_load": (_I, [_I, _I, _I, _I, _P, _P, _P, _L, _P]),
     "fd_op_block_join": (_I, [ctypes.POINTER(fd_block_join), _P, _L, _P, _L, _F, _P, _L, _P, _L,
@@ -955,9 +963,7 @@ def op_cache_compact(src: Cache, dst: Cache, now, src_slots, used=None, sinks=0,
         raise FdError(code, "fd_op_cache_compact")
 
 
-# --------------------------------------- a residual block in training: checkpoints and the join
-KEPT_BLOCK = 32  # elements of a row that share a checkpoint's exponent
-
+# --------------------------------------------------- attention in spans of keys, and its gradient
 _types = None
 
 
@@ -969,6 +975,62 @@ def _torch_types():
         _types = (torch.int8, torch.uint8, torch.float32, torch.int32)
     return _types
 
+
+_span_workspace: dict = {}
+
+
+def span_attention_workspace_bytes(n_q, n_k, heads, groups, head_dim, backward=False) -> int:
+    """Workspace of op_span_attention, or of op_span_attention_bwd."""
+    key = (n_q, n_k, heads, groups, head_dim, bool(backward))
+    need = _span_workspace.get(key)
+    if need is None:
+        if len(_span_workspace) > 1000:
+            _span_workspace.clear()
+        view = fd_span_attention(n_q, n_k, heads, groups, head_dim, DTYPE_BF16, 1.0)
+        need = _span_workspace[key] = lib().fd_span_attention_workspace_bytes(
+            ctypes.byref(view), 1 if backward else 0)
+    return need
+
+
+def _span_view(q, k, v, spans, scale, workspace, backward):
+    """(fd_span_attention, device, the arguments up to the spans) of a span attention's inputs."""
+    shape, kv, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
+    if dev < 0 or len(shape) != 3:
+        raise TypeError("q: a CUDA tensor [queries][heads][head_dim] is required")
+    if len(kv) != 3 or kv[2] != shape[2]:
+        raise ValueError(f"k: shape {tuple(kv)}, [keys][groups][{shape[2]}] is required")
+    qp, qs = _rows(q, "q", shape, dtype, dev)
+    kp, ks = _rows(k, "k", kv, dtype, dev)
+    vp, vs = _rows(v, "v", kv, dtype, dev)
+    sp = _dense(spans, "spans", (shape[0], 2), _torch_types()[3], dev)
+    need = span_attention_workspace_bytes(shape[0], kv[0], shape[1], kv[1], shape[2], backward)
+    if need and (workspace is None or workspace.get_device() != dev
+                 or not workspace.is_contiguous() or workspace.nbytes < need):
+        raise ValueError(f"workspace: {need} bytes of contiguous memory on cuda:{dev} are required")
+    view = fd_span_attention(shape[0], kv[0], shape[1], kv[1], shape[2], _dtype_code(dtype),
+                             shape[2] ** -0.5 if scale is None else scale)
+    return view, dev, (qp, qs[0], qs[1], kp, ks[0], ks[1], vp, vs[0], vs[1], sp)
+
+
+def op_span_attention(q, k, v, spans, out, lse, scale=None, workspace=None, err=None,
+                      stream=None) -> None:
+    """Attention of q [queries][heads][head_dim] over k, v [keys][groups][head_dim] into out like q, query
+    t seeing keys spans[t][0] <= j < spans[t][1] (int32 [queries][2]); lse float32 [heads][queries]
+    receives the logarithm of the rows' sums of exponentials, which the gradient needs. scale: 1 /
+    sqrt(head_dim) by default (fd_op_span_attention)."""
+    view, dev, args = _span_view(q, k, v, spans, scale, workspace, False)
+    _, _, float32, int32 = _torch_types()
+    op, os_ = _rows(out, "out", q.shape, q.dtype, dev)
+    code = lib().fd_op_span_attention(
+        ctypes.byref(view), *args, op, os_[0], os_[1],
+        _dense(lse, "lse", (view.heads, view.n_q), float32, dev), _ptr(workspace),
+        _status_word(err, int32, dev), _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_span_attention")
+
+
+# --------------------------------------- a residual block in training: checkpoints and the join
+KEPT_BLOCK = 32  # elements of a row that share a checkpoint's exponent
 
 class Checkpoint8:
     """Rows of activations kept in 8 bits (fd_op_checkpoint_save): codes int8 [rows][width] and the

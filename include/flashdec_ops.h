@@ -386,6 +386,24 @@ fd_status fd_op_span_attention(const fd_span_attention* attn, const void* q, int
                                int64_t out_token_stride, int64_t out_head_stride, float* lse,
                                void* workspace, int* err_dev, void* stream);
 
+/* The gradient, from dout like out, with out and lse as the forward call left them:
+ *   P = exp(s - lse),  dS = P (dout . v_j - dout . out)
+ *   dq[t][h] = scale sum_j dS k_j;  dk[j] = scale sum dS q[t][h];  dv[j] = sum P dout[t][h]
+ * (dk, dv over the queries and the group's heads). The probabilities are computed again and never
+ * stored. Sums are in fp32 and a fixed order: equal calls give equal bits; P and dS are rounded to dtype for
+ * their products (fp16: scaled by powers of two, dS by that of the largest |dout|). Queries that see
+ * nothing and keys that nothing sees get zeros. dq like q, dk and dv like k, each with strides of its own;
+ * they share no memory with the inputs or each other. spans, err_dev as above; workspace of
+ * fd_span_attention_workspace_bytes(attn, 1). */
+fd_status fd_op_span_attention_bwd(
+    const fd_span_attention* attn, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+    const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+    int64_t v_token_stride, int64_t v_head_stride, const int32_t* spans, const void* out,
+    int64_t out_token_stride, int64_t out_head_stride, const float* lse, const void* dout,
+    int64_t dout_token_stride, int64_t dout_head_stride, void* dq, int64_t dq_token_stride,
+    int64_t dq_head_stride, void* dk, int64_t dk_token_stride, int64_t dk_head_stride, void* dv,
+    int64_t dv_token_stride, int64_t dv_head_stride, void* workspace, int* err_dev, void* stream);
+
 /* ---- checkpoints: activations kept in 8 bits for the backward pass ----
  *
  * Blocks of 32 neighbouring elements of a row share a power of two 2^E, the smallest with E >= -126

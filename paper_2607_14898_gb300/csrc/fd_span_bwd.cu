@@ -1,4 +1,1025 @@
+// Gradient of the attention in spans of keys (fd_op_span_attention_bwd). The probabilities are
+// computed again from the log-sum-exp, tile by tile, and never stored:
+//   P = exp(scale q k^T - lse),  delta = rowsum(dout o out),  dS = P (dout v^T - delta)
+//   dv = P^T dout,  dk = scale dS^T q  (over the rows of a group's heads),  dq = scale dS k
+//
+//   span_rows   each row's lse and delta, each row tile's limits
+//   span_keys   dk and dv: a block has 128 keys and walks over the row tiles that see some of them
+//   span_query  dq: a block has a row tile and walks over its key blocks
+// Scores and dout v^T are computed twice, 7 products for the 5 that are needed, so that every sum stays
+// in one block's TMEM: no atomics, the same bits every time.
+#include <algorithm>
+#include <cmath>
+
 #include "fd_span.cuh"
+
 namespace fd {
-size_t span_bwd_workspace_bytes(int, int, int, int, int) { return 0; }
+namespace {
+
+struct SpanBwd {
+  SpanShape y;
+  int q_parts, k_parts;
+  const int32_t* spans;
+  float scale, scale_log2;
+  SpanRows out, dout, dq, dk, dv;
+  const float* lse;
+  float* stat;    // [group][row tile][4][128]: -lse log2(e), -delta, the span's ends (int)
+  int4* limits;   // of each row tile: first and last key seen, the keys that all see; see below
+  float* most;    // [group][row tile]: the largest |dout| (fp16)
+  float* part_q;  // [group][row tile][part][128][D]
+  float* part_k;  // [group][key block][part][dk, dv][128][D]
+  int* err;
+};
+
+// fp16 has few exponents: P goes into its product times 2^14, and dS divided by the power of two in the
+// largest |dout|, so that small gradients keep their digits. bf16 has fp32's range.
+constexpr float kPUp = 16384.f;
+constexpr float kPUpLog2 = 14.f;
+
+// ------------------------------------------------------------------------------ rows
+// D / 8 lanes a row. A row that sees nothing, or is none, gets P = 0 by an infinite lse.
+template <bool F16, int D>
+__global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ SpanBwd p) {
+  constexpr int kLanes = D / 8;
+  __shared__ float top[8];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int tile = blockIdx.x, group = blockIdx.y;
+  const int token0 = tile * p.y.tile_tokens;
+  const int lane = threadIdx.x % kLanes;
+  float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * 4 * kTile;
+  float most = 0.f;
+#pragma unroll
+  for (int row = threadIdx.x / kLanes; row < kTile; row += 256 / kLanes) {
+    const int token = token0 + row / p.y.per, head = group * p.y.per + row % p.y.per;
+    const bool valid = row < p.y.tile_rows && token < p.y.n_q;
+    const int2 span = valid ? span_of(p.spans, token, p.y.n_k) : make_int2(0, 0);
+    const bool sees = span.x < span.y;
+    float sum = 0.f;
+    if (sees) {
+      const uint4 a = __ldg(reinterpret_cast<const uint4*>(
+          static_cast<const uint16_t*>(p.out.p) + token * p.out.token + head * p.out.head + lane * 8));
+      const uint4 b = __ldg(reinterpret_cast<const uint4*>(
+          static_cast<const uint16_t*>(p.dout.p) + token * p.dout.token + head * p.dout.head + lane * 8));
+      const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float2 u, v;
+        if (F16) {
+          u = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
+          v = __half22float2(*reinterpret_cast<const __half2*>(&y[i]));
+          most = fmaxf(most, fmaxf(fabsf(v.x), fabsf(v.y)));
+        } else {
+          u = make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
+          v = make_float2(__uint_as_float(y[i] << 16), __uint_as_float(y[i] & 0xffff0000u));
+        }
+        sum = fmaf(u.x, v.x, fmaf(u.y, v.y, sum));
+      }
+    }
+#pragma unroll
+    for (int i = kLanes / 2; i; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
+    if (lane == 0) {
+      const float l = sees ? __ldg(p.lse + static_cast<int64_t>(head) * p.y.n_q + token) : 0.f;
+      stat[row] = sees ? fmaf(-l, kLog2e, F16 ? kPUpLog2 : 0.f) : -INFINITY;
+      stat[kTile + row] = sees ? -sum : 0.f;
+      reinterpret_cast<int*>(stat)[2 * kTile + row] = span.x;
+      reinterpret_cast<int*>(stat)[3 * kTile + row] = span.y;
+    }
+  }
+  if (F16) {
+#pragma unroll
+    for (int i = 16; i; i >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, i));
+    if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int i = 1; i < 8; ++i) most = fmaxf(most, top[i]);
+      p.most[group * p.y.row_tiles + tile] = most;
+    }
+  }
+  if (group == 0 && threadIdx.x < 32) {
+    // {first key, end of the keys} that some query sees, {first, end} of those that all queries see which see
+    // any; the third is negative (~) where some query sees none
+    int4 m = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
+    bool none = false;
+    for (int i = threadIdx.x; i < p.y.tile_tokens && token0 + i < p.y.n_q; i += 32) {
+      const int2 s = span_of(p.spans, token0 + i, p.y.n_k);
+      if (s.x < s.y) {
+        m.x = min(m.x, s.x);
+        m.y = max(m.y, s.y);
+        m.z = max(m.z, s.x);
+        m.w = min(m.w, s.y);
+      } else {
+        none = true;
+      }
+    }
+    m.x = __reduce_min_sync(0xffffffffu, m.x);
+    m.y = __reduce_max_sync(0xffffffffu, m.y);
+    m.z = __reduce_max_sync(0xffffffffu, m.z);
+    m.w = __reduce_min_sync(0xffffffffu, m.w);
+    if (__any_sync(0xffffffffu, none)) m.z = ~m.z;
+    if (threadIdx.x == 0) p.limits[tile] = m;
+  }
 }
+
+// 2^-E of the largest |dout| = f 2^E, 1 <= f < 2, over all tiles, by one warp (fp16)
+__device__ __forceinline__ float down_scale(const float* most, int n) {
+  float m = 0.f;
+  for (int i = threadIdx.x & 31; i < n; i += 32) m = fmaxf(m, __ldcg(most + i));
+#pragma unroll
+  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+  const uint32_t e = __float_as_uint(m) >> 23;  // (fp16: e is 103 at least unless m is zero)
+  return m > 0.f && e < 255u ? __uint_as_float((254u - e) << 23) : 1.f;
+}
+
+// ------------------------------------------------------------------------------ keys: dk and dv
+// Lanes are keys and columns rows of the tile: X = K Q^T and Y = V dout^T into TMEM, P^T and dS^T
+// from there back into TMEM as the first operands of dv += P^T dout and dk += dS^T q.
+//   warps 0-15   P and dS: four groups of 128 threads (a key each), a quarter of a step's rows each
+//   warp 16      TMA: K and V, then q, dout and the rows' numbers by tiles
+//   warps 17-20  products: X, Y, dv, dk (a warp issues one per 104 to 158 cycles)
+// A step is a tile, or (D = 128, where TMEM has no room for more) half of one.
+template <int D>
+struct KeyCfg {
+  static constexpr int kThreads = 21 * 32;
+  static constexpr int kStep = D == 64 ? 128 : 64;  // rows of a step
+  static constexpr int kSteps = kTile / kStep;      // of a tile
+  static constexpr int kCols = kStep / 4;           // of a thread
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int kStages = D == 64 ? 4 : 2;
+  static constexpr int kStat = 4 * kTile * 4;
+  static constexpr int kOffV = kTileBytes;
+  static constexpr int kOffRing = 2 * kTileBytes;  // q, dout of each stage
+  static constexpr int kOffStat = kOffRing + kStages * 2 * kTileBytes;
+  static constexpr int kOffBar = kOffStat + kStages * kStat;
+  static constexpr int kKV = 0, kFull = 1, kFree = kFull + kStages, kReady = kFree + kStages,
+                       kXFull = kReady + kStages, kYFull = kXFull + 1, kXRead = kYFull + 1,
+                       kYRead = kXRead + 1, kPFull = kYRead + 1, kDsFull = kPFull + 1,
+                       kPDone = kDsFull + 1, kDsDone = kPDone + 1, kBars = kDsDone + 1;
+  static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
+  static constexpr uint32_t kColX = 0, kColY = kStep, kColP = 2 * kStep, kColDs = kColP + kStep / 2,
+                            kColDv = 512 - 2 * D, kColDk = 512 - D;
+  static_assert(kSmem <= 227 * 1024 && kColDs + kStep / 2 <= kColDv, "room");
+};
+
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[N]) {
+  if constexpr (N == 32)
+    tmem_ld_32x32b_x32(at, r);
+  else
+    tmem_ld_32x32b_x16(at, r);
+}
+template <int N>
+__device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
+  if constexpr (N == 16)
+    tmem_st_32x32b_x16(at, r);
+  else
+    tmem_st_32x32b_x8(at, r);
+}
+
+// 16 (or 32) columns of an accumulator times f to a row of a matrix of 16-bit elements or of floats
+template <bool F16>
+__device__ __forceinline__ void leave16(uint32_t at, float f, uint16_t* to, float* part, bool here) {
+  uint32_t a[16];
+  tmem_ld_32x32b_x16(at, a);
+  tmem_ld_wait();
+  if (!here) return;
+  float o[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(a[e]) * f;
+  if (part == nullptr) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 8)
+      *reinterpret_cast<uint4*>(to + e) =
+          make_uint4(pack16<F16>(o[e], o[e + 1]), pack16<F16>(o[e + 2], o[e + 3]),
+                     pack16<F16>(o[e + 4], o[e + 5]), pack16<F16>(o[e + 6], o[e + 7]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<float4*>(part + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+  }
+}
+
+template <bool F16, int D>
+__global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
+    span_keys_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
+                     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ SpanBwd p) {
+  using C = KeyCfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem);
+  const bool aligned = (base & 1023u) == 0;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kOffBar);
+  const uint32_t bar0 = smem_u32(bars);
+  auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
+  int* range = reinterpret_cast<int*>(tmem_slot + 1);  // first row tile, the one past the last
+  volatile float* down = reinterpret_cast<volatile float*>(tmem_slot + 3);
+
+  const int part = blockIdx.x % p.k_parts, kb = static_cast<int>(blockIdx.x) / p.k_parts;
+  const int group = blockIdx.y;
+  const int key0 = kb * kTile;
+
+  // rows past tile_rows are never loaded
+  for (int i = threadIdx.x; i < C::kStages * 2 * C::kTileBytes / 16; i += C::kThreads)
+    reinterpret_cast<uint4*>(smem + C::kOffRing)[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async_smem();
+  if (threadIdx.x == 0) {
+    if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
+    mbar_init(bar(C::kKV), 1);
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(bar(C::kFull + i), 1);
+      mbar_init(bar(C::kFree + i), 2);
+      mbar_init(bar(C::kReady + i), 1);
+    }
+    mbar_init(bar(C::kXFull), 1);
+    mbar_init(bar(C::kYFull), 1);
+    mbar_init(bar(C::kXRead), 16);
+    mbar_init(bar(C::kYRead), 16);
+    mbar_init(bar(C::kPFull), 16);
+    mbar_init(bar(C::kDsFull), 16);
+    mbar_init(bar(C::kPDone), 1);
+    mbar_init(bar(C::kDsDone), 1);
+    fence_barrier_init();
+    range[0] = 0x7fffffff;
+    range[1] = 0;
+  }
+  grid_dep_wait();
+  grid_dep_launch();
+  if (warp == 0) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  __syncthreads();
+  {
+    // the row tiles that see some of the keys: from the first to the last
+    int first = 0x7fffffff, end = 0;
+    for (int i = threadIdx.x; i < p.y.row_tiles; i += C::kThreads) {
+      const int4 m = __ldcg(p.limits + i);
+      if (m.x < key0 + kTile && m.y > key0) {
+        first = min(first, i);
+        end = max(end, i + 1);
+      }
+    }
+    first = __reduce_min_sync(0xffffffffu, first);
+    end = __reduce_max_sync(0xffffffffu, end);
+    if (lane == 0 && end > 0) {
+      atomicMin(range, first);
+      atomicMax(range + 1, end);
+    }
+    if (F16 && warp == 0) {
+      const float f = down_scale(p.most, p.y.groups * p.y.row_tiles);
+      if (lane == 0) *down = f;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int n = aligned && range[1] > 0 ? range[1] - range[0] : 0;
+  const int tile0 = range[0] + static_cast<int>(static_cast<int64_t>(n) * part / p.k_parts);
+  const int count = static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.k_parts) -
+                    static_cast<int>(static_cast<int64_t>(n) * part / p.k_parts);
+  const float ds_down = F16 ? *down : 1.f;  // dS is kept times this
+
+  if (count == 0) {
+    // no row sees any of the keys
+  } else if (warp == 16) {
+    if (lane == 0) {
+      prefetch_tmap(&tmQ);
+      prefetch_tmap(&tmDo);
+      mbar_expect_tx(bar(C::kKV), 2 * C::kTileBytes);
+      for (int d = 0; d < D / 64; ++d) {
+        tma_load_4d(base + d * kSub, &tmK, bar(C::kKV), 64 * d, group, key0, 0);
+        tma_load_4d(base + C::kOffV + d * kSub, &tmV, bar(C::kKV), 64 * d, group, key0, 0);
+      }
+      int i = 0;
+      for (; i < count; ++i) {
+        const int st = i % C::kStages;
+        if (i >= C::kStages &&
+            !wait(bar(C::kFree + st), (i / C::kStages - 1) & 1, p.err, ERR_WAIT_MMA))
+          break;
+        const uint32_t b = bar(C::kFull + st), q = base + C::kOffRing + st * 2 * C::kTileBytes;
+        mbar_expect_tx(b, 2 * p.y.tile_rows * D * 2 + C::kStat);
+        const int token = (tile0 + i) * p.y.tile_tokens;
+        for (int d = 0; d < D / 64; ++d) {
+          tma_load_4d(q + d * kSub, &tmQ, b, 64 * d, group * p.y.per, token, 0);
+          tma_load_4d(q + C::kTileBytes + d * kSub, &tmDo, b, 64 * d, group * p.y.per, token, 0);
+        }
+        bulk_load(base + C::kOffStat + st * C::kStat,
+                  p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile0 + i) * 4 * kTile,
+                  C::kStat, b);
+      }
+      // nothing may be in flight when the block exits
+      wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, i - C::kStages); j < i; ++j)
+        wait(bar(C::kFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA, true);
+    }
+  } else if (warp == 17 || warp == 18) {
+    // ---- X = K Q^T (17), Y = V dout^T (18), and zeros for the rows of queries that see nothing:
+    // their P and dS are 0, but 0 times NaN is NaN
+    const bool y = warp == 18;
+    constexpr uint32_t idesc = Mma<F16, D>::idesc(C::kStep, false);
+    const uint64_t a0 = sdesc_k_sw128(base + (y ? C::kOffV : 0));
+    const uint32_t col = tmem + (y ? C::kColY : C::kColX);
+    bool ok = wait_warp(bar(C::kKV), 0, p.err, ERR_WAIT_TMA);
+    for (int i = 0; i < count && ok; ++i) {
+      const int st = i % C::kStages;
+      const bool some_none = __ldcg(&p.limits[tile0 + i].z) < 0;
+      ok = wait_warp(bar(C::kFull + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
+      if (!ok) break;
+      const int off = C::kOffRing + st * 2 * C::kTileBytes + (y ? C::kTileBytes : 0);
+      if (some_none) {
+        const int* ends = reinterpret_cast<const int*>(smem + C::kOffStat + st * C::kStat) + 2 * kTile;
+#pragma unroll 1
+        for (int r = lane; r < p.y.tile_rows; r += 32) {
+          if (ends[r] < ends[kTile + r]) continue;
+          uint4* row = reinterpret_cast<uint4*>(smem + off + r * 128);
+#pragma unroll
+          for (int d = 0; d < D / 64; ++d)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) row[d * (kSub / 16) + c] = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      if (y && lane == 0) mbar_arrive(bar(C::kReady + st));
+#pragma unroll
+      for (int s = 0; s < C::kSteps; ++s) {
+        const int k = i * C::kSteps + s;
+        if (k > 0)
+          ok = ok && wait_warp(bar(y ? C::kYRead : C::kXRead), (k - 1) & 1, p.err, ERR_WAIT_EPI);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t b0 = sdesc_k_sw128(base + off + s * C::kStep * 128);
+#pragma unroll
+        for (int d = 0; d < D / 64; ++d)
+          mma4_bf16_ss_w(col, a0 + static_cast<uint64_t>(d * (kSub >> 4)),
+                         b0 + static_cast<uint64_t>(d * (kSub >> 4)), idesc, d > 0);
+        mma_commit_w(bar(y ? C::kYFull : C::kXFull));
+      }
+    }
+  } else if (warp == 19 || warp == 20) {
+    // ---- dv += P^T dout (19), dk += dS^T q (20)
+    const bool dk = warp == 20;
+    constexpr uint32_t idesc = Mma<F16, D>::idesc(D, true);
+    const uint32_t a = tmem + (dk ? C::kColDs : C::kColP), acc = tmem + (dk ? C::kColDk : C::kColDv);
+    bool ok = true;
+    for (int i = 0; i < count && ok; ++i) {
+      const int st = i % C::kStages;
+      // (dv does not depend on Y, which waits for dout; dk on both)
+      ok = wait_warp(bar(C::kReady + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
+      const uint32_t b = base + C::kOffRing + st * 2 * C::kTileBytes + (dk ? 0 : C::kTileBytes);
+#pragma unroll
+      for (int s = 0; s < C::kSteps; ++s) {
+        const int k = i * C::kSteps + s;
+        ok = ok && wait_warp(bar(dk ? C::kDsFull : C::kPFull), k & 1, p.err, ERR_WAIT_EPI);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int x = 0; x < C::kStep / 64; ++x)
+          mma4_ts_mn_w(acc, a + 32u * x, sdesc_mn_sw128(b + (s * C::kStep + x * 64) * 128, kSub), idesc,
+                       k > 0 || x > 0);
+        mma_commit_w(bar(dk ? C::kDsDone : C::kPDone));
+      }
+      if (ok) mma_commit_w(bar(C::kFree + st));
+    }
+  }
+  if (warp < 16) {
+    // ---- P^T and dS^T of a quarter of each step's rows
+    const int q = warp >> 2, key = key0 + (warp & 3) * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t x_col = tmem + lane_off + C::kColX + C::kCols * q;
+    const uint32_t y_col = tmem + lane_off + C::kColY + C::kCols * q;
+    const uint32_t p_col = tmem + lane_off + C::kColP + C::kCols / 2 * q;
+    const uint32_t ds_col = tmem + lane_off + C::kColDs + C::kCols / 2 * q;
+    const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2);
+    const float dn = F16 ? ds_down / kPUp : 1.f;
+    const uint64_t down2 = pack_f32x2(dn, dn);
+    int k = 0;
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      const int4 m = __ldcg(p.limits + tile0 + i);
+      // (a tile between others may see nothing of the block, or nothing at all)
+      const bool masked = m.x > key0 || (m.z < 0 ? ~m.z : m.z) > key0 || m.w < key0 + kTile;
+      const int st = i % C::kStages;
+#pragma unroll 1
+      for (int s = 0; s < C::kSteps; ++s, ++k) {
+        const uint8_t* stat = smem + C::kOffStat + st * C::kStat + (s * C::kStep + q * C::kCols) * 4;
+        wait_warp(bar(C::kXFull), k & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+        uint32_t x[C::kCols];
+        tmem_ld(x_col, x);
+        uint32_t seen = 0xffffffffu;  // bit c: the key is seen by row c of the quarter
+        if (masked) {
+          seen = 0;
+#pragma unroll
+          for (int c = 0; c < C::kCols; c += 4) {
+            const int4 lo = *reinterpret_cast<const int4*>(stat + 2 * kTile * 4 + c * 4);
+            const int4 hi = *reinterpret_cast<const int4*>(stat + 3 * kTile * 4 + c * 4);
+            seen |= (lo.x <= key && key < hi.x ? 1u << c : 0u) |
+                    (lo.y <= key && key < hi.y ? 2u << c : 0u) |
+                    (lo.z <= key && key < hi.z ? 4u << c : 0u) |
+                    (lo.w <= key && key < hi.w ? 8u << c : 0u);
+          }
+        }
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kXRead));
+        uint32_t pk[C::kCols / 2];
+#pragma unroll
+        for (int c = 0; c < C::kCols; c += 4) {
+          const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(stat + c * 4);
+          const float2 a = halves_of(fma2(pair_of(x[c], x[c + 1]), c2, l.x));
+          const float2 b = halves_of(fma2(pair_of(x[c + 2], x[c + 3]), c2, l.y));
+          x[c] = __float_as_uint(ex2_approx(a.x));
+          x[c + 1] = __float_as_uint(ex2_approx(a.y));
+          x[c + 2] = __float_as_uint(ex2_approx(b.x));
+          x[c + 3] = __float_as_uint(ex2_approx(b.y));
+        }
+        if (masked) {
+#pragma unroll
+          for (int c = 0; c < C::kCols; ++c)
+            if (!(seen & (1u << c))) x[c] = 0;
+        }
+        // P and dS in the inputs' type, which the products take: half a step each, 2^-9 or 2^-12 of
+        // their size; sums in fp32
+#pragma unroll
+        for (int c = 0; c < C::kCols; c += 2)
+          pk[c / 2] = pack16<F16>(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+        if (k > 0) wait_warp(bar(C::kPDone), (k - 1) & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+        tmem_st(p_col, pk);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kPFull));
+
+        wait_warp(bar(C::kYFull), k & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+        uint32_t y[C::kCols];
+        tmem_ld(y_col, y);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kYRead));
+#pragma unroll
+        for (int c = 0; c < C::kCols; c += 4) {
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(stat + kTile * 4 + c * 4);
+          uint64_t a = pair_of(x[c], x[c + 1]), b = pair_of(x[c + 2], x[c + 3]);
+          if (F16) {
+            a = mul2(a, down2);
+            b = mul2(b, down2);
+          }
+          const float2 u = halves_of(mul2(a, add2(pair_of(y[c], y[c + 1]), d.x)));
+          const float2 v = halves_of(mul2(b, add2(pair_of(y[c + 2], y[c + 3]), d.y)));
+          y[c] = __float_as_uint(u.x);
+          y[c + 1] = __float_as_uint(u.y);
+          y[c + 2] = __float_as_uint(v.x);
+          y[c + 3] = __float_as_uint(v.y);
+        }
+        if (masked) {
+#pragma unroll
+          for (int c = 0; c < C::kCols; ++c)
+            if (!(seen & (1u << c))) y[c] = 0;
+        }
+#pragma unroll
+        for (int c = 0; c < C::kCols; c += 2)
+          pk[c / 2] = pack16<F16>(__uint_as_float(y[c]), __uint_as_float(y[c + 1]));
+        if (k > 0) wait_warp(bar(C::kDsDone), (k - 1) & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+        tmem_st(ds_col, pk);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(C::kDsFull));
+      }
+    }
+    if (count > 0) {
+      wait_warp(bar(C::kPDone), (k - 1) & 1, p.err, ERR_WAIT_MMA);
+      wait_warp(bar(C::kDsDone), (k - 1) & 1, p.err, ERR_WAIT_MMA);
+    }
+    tc_fence_after();
+    const bool here = key < p.y.n_k;
+    const int64_t slot =
+        ((static_cast<int64_t>(group) * p.y.key_blocks + kb) * p.k_parts + part) * 2 * kTile +
+        (warp & 3) * 32 + lane;
+    const float fk = p.scale / ds_down, fv = F16 ? 1.f / kPUp : 1.f;
+#pragma unroll 1
+    for (int d = q * (D / 4); d < (q + 1) * (D / 4); d += 16) {
+      uint16_t* dk = static_cast<uint16_t*>(p.dk.p) + key * p.dk.token + group * p.dk.head + d;
+      uint16_t* dv = static_cast<uint16_t*>(p.dv.p) + key * p.dv.token + group * p.dv.head + d;
+      float* part_k = p.k_parts > 1 ? p.part_k + slot * D + d : nullptr;
+      float* part_v = p.k_parts > 1 ? p.part_k + (slot + kTile) * D + d : nullptr;
+      if (count > 0) {
+        leave16<F16>(tmem + lane_off + C::kColDk + d, fk, dk, part_k, here);
+        leave16<F16>(tmem + lane_off + C::kColDv + d, fv, dv, part_v, here);
+      } else if (here) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+          const uint4 z = make_uint4(0, 0, 0, 0);
+          if (part_k == nullptr) {
+            *reinterpret_cast<uint4*>(dk + e) = z;
+            *reinterpret_cast<uint4*>(dv + e) = z;
+          } else {
+            *reinterpret_cast<uint4*>(part_k + e) = *reinterpret_cast<uint4*>(part_k + e + 4) = z;
+            *reinterpret_cast<uint4*>(part_v + e) = *reinterpret_cast<uint4*>(part_v + e + 4) = z;
+          }
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------------------ queries: dq
+// Lanes are rows of the tile and columns keys: X = q k^T, Y = dout v^T, dS back into TMEM as the first
+// operand of dq += dS k.
+//   warps 0-15   dS: four groups of 128 threads (a row each), a quarter of a block's keys each
+//   warp 16      TMA: q and dout, then K and V by blocks
+//   warps 17-19  products: X (and zeros for the keys that no query of the tile sees), Y, dq
+template <int D>
+struct QueryCfg {
+  static constexpr int kThreads = 20 * 32;
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int kStages = D == 64 ? 5 : 2;
+  static constexpr int kOffDo = kTileBytes;
+  static constexpr int kOffRing = 2 * kTileBytes;  // K, V of each stage
+  static constexpr int kOffBar = kOffRing + kStages * 2 * kTileBytes;
+  static constexpr int kQ = 0, kFull = 1, kFree = kFull + kStages, kXFull = kFree + kStages,
+                       kYFull = kXFull + 1, kXRead = kYFull + 1, kYRead = kXRead + 1,
+                       kDsFull = kYRead + 1, kDsDone = kDsFull + 1, kBars = kDsDone + 1;
+  static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
+  static constexpr uint32_t kColX = 0, kColY = 128, kColDs = 256, kColDq = 384;
+  static_assert(kSmem <= 227 * 1024, "shared memory");
+};
+
+template <bool F16, int D>
+__global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
+    span_query_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
+                      const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                      const __grid_constant__ SpanBwd p) {
+  using C = QueryCfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem);
+  const bool aligned = (base & 1023u) == 0;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::kOffBar);
+  const uint32_t bar0 = smem_u32(bars);
+  auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
+  volatile float* down = reinterpret_cast<volatile float*>(tmem_slot + 1);
+
+  const int part = blockIdx.x % p.q_parts;
+  const int tile = p.y.row_tiles - 1 - static_cast<int>(blockIdx.x) / p.q_parts;
+  const int group = blockIdx.y;
+  const int token0 = tile * p.y.tile_tokens;
+
+  // rows past tile_rows are never loaded
+  for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += C::kThreads)
+    reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+  fence_proxy_async_smem();
+  if (threadIdx.x == 0) {
+    if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
+    mbar_init(bar(C::kQ), 1);
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(bar(C::kFull + i), 1);
+      mbar_init(bar(C::kFree + i), 1);
+    }
+    mbar_init(bar(C::kXFull), 1);
+    mbar_init(bar(C::kYFull), 1);
+    mbar_init(bar(C::kXRead), 16);
+    mbar_init(bar(C::kYRead), 16);
+    mbar_init(bar(C::kDsFull), 16);
+    mbar_init(bar(C::kDsDone), 1);
+    fence_barrier_init();
+  }
+  grid_dep_wait();
+  grid_dep_launch();
+  if (warp == 0) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  } else if (F16 && warp == 1) {
+    const float f = down_scale(p.most, p.y.groups * p.y.row_tiles);
+    if (lane == 0) *down = f;
+  }
+  const int4 m = __ldcg(p.limits + tile);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int b0 = m.y > 0 ? m.x / kTile : 0;
+  const int n = aligned && m.y > 0 ? (m.y + kTile - 1) / kTile - b0 : 0;
+  const int block0 = b0 + static_cast<int>(static_cast<int64_t>(n) * part / p.q_parts);
+  const int count = b0 + static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.q_parts) - block0;
+  const float ds_down = F16 ? *down : 1.f;
+
+  if (count == 0) {
+    // no row sees any key
+  } else if (warp == 16) {
+    if (lane == 0) {
+      prefetch_tmap(&tmK);
+      prefetch_tmap(&tmV);
+      mbar_expect_tx(bar(C::kQ), 2 * p.y.tile_rows * D * 2);
+      for (int d = 0; d < D / 64; ++d) {
+        tma_load_4d(base + d * kSub, &tmQ, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
+        tma_load_4d(base + C::kOffDo + d * kSub, &tmDo, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
+      }
+      int i = 0;
+      for (; i < count; ++i) {
+        const int st = i % C::kStages;
+        if (i >= C::kStages &&
+            !wait(bar(C::kFree + st), (i / C::kStages - 1) & 1, p.err, ERR_WAIT_MMA))
+          break;
+        const uint32_t b = bar(C::kFull + st), k = base + C::kOffRing + st * 2 * C::kTileBytes;
+        mbar_expect_tx(b, 2 * C::kTileBytes);
+        for (int d = 0; d < D / 64; ++d) {
+          tma_load_4d(k + d * kSub, &tmK, b, 64 * d, group, (block0 + i) * kTile, 0);
+          tma_load_4d(k + C::kTileBytes + d * kSub, &tmV, b, 64 * d, group, (block0 + i) * kTile, 0);
+        }
+      }
+      // nothing may be in flight when the block exits
+      wait(bar(C::kQ), 0, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, i - C::kStages); j < i; ++j)
+        wait(bar(C::kFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA, true);
+    }
+  } else if (warp == 17 || warp == 18) {
+    // ---- X = q k^T (17), Y = dout v^T (18)
+    const bool y = warp == 18;
+    constexpr uint32_t idesc = Mma<F16, D>::idesc(kTile, false);
+    const uint64_t a0 = sdesc_k_sw128(base + (y ? C::kOffDo : 0));
+    const uint32_t col = tmem + (y ? C::kColY : C::kColX);
+    int2 span[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = lane + 32 * i;
+      span[i] = t < p.y.tile_tokens && token0 + t < p.y.n_q ? span_of(p.spans, token0 + t, p.y.n_k)
+                                                           : make_int2(0, 0);
+    }
+    bool ok = wait_warp(bar(C::kQ), 0, p.err, ERR_WAIT_TMA);
+    for (int i = 0; i < count && ok; ++i) {
+      const int st = i % C::kStages, key0 = (block0 + i) * kTile;
+      ok = wait_warp(bar(C::kFull + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
+      const int off = C::kOffRing + st * 2 * C::kTileBytes + (y ? C::kTileBytes : 0);
+      if (!y) {
+        // zeros for K of keys that no query of the tile sees: their dS is 0, but 0 times NaN is NaN
+        bool whole = false;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) whole |= span[s].x <= key0 && span[s].y >= key0 + kTile;
+        if (!__any_sync(0xffffffffu, whole)) {
+          bool some = false;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t mine = 0;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) mine |= seen_word(span[s], key0 + 32 * w);
+            const uint32_t seen = __reduce_or_sync(0xffffffffu, mine);
+            some |= seen != 0xffffffffu;
+            if ((seen >> lane) & 1u) continue;
+            uint4* row = reinterpret_cast<uint4*>(smem + off + (32 * w + lane) * 128);
+#pragma unroll
+            for (int d = 0; d < D / 64; ++d)
+#pragma unroll
+              for (int c = 0; c < 8; ++c) row[d * (kSub / 16) + c] = make_uint4(0, 0, 0, 0);
+          }
+          if (some) fence_proxy_async_smem();
+          __syncwarp();
+        }
+      }
+      if (i > 0)
+        ok = ok && wait_warp(bar(y ? C::kYRead : C::kXRead), (i - 1) & 1, p.err, ERR_WAIT_EPI);
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t k0 = sdesc_k_sw128(base + off);
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d)
+        mma4_bf16_ss_w(col, a0 + static_cast<uint64_t>(d * (kSub >> 4)),
+                       k0 + static_cast<uint64_t>(d * (kSub >> 4)), idesc, d > 0);
+      mma_commit_w(bar(y ? C::kYFull : C::kXFull));
+    }
+  } else if (warp == 19) {
+    // ---- dq += dS k
+    constexpr uint32_t idesc = Mma<F16, D>::idesc(D, true);
+    bool ok = true;
+    for (int i = 0; i < count && ok; ++i) {
+      const int st = i % C::kStages;
+      ok = wait_warp(bar(C::kFull + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA) &&
+           wait_warp(bar(C::kDsFull), i & 1, p.err, ERR_WAIT_EPI);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t k = base + C::kOffRing + st * 2 * C::kTileBytes;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        mma4_ts_mn_w(tmem + C::kColDq, tmem + C::kColDs + 32u * x, sdesc_mn_sw128(k + x * 64 * 128, kSub),
+                     idesc, i > 0 || x > 0);
+      mma_commit_w(bar(C::kDsDone));
+      mma_commit_w(bar(C::kFree + st));
+    }
+  }
+  if (warp < 16) {
+    // ---- dS of a quarter of each block's keys
+    const int q = warp >> 2, row = (warp & 3) * 32 + lane;
+    const int token = token0 + row / p.y.per, head = group * p.y.per + row % p.y.per;
+    const bool valid = row < p.y.tile_rows && token < p.y.n_q;
+    const float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * 4 * kTile + row;
+    const float neg_lse = __ldcg(stat), neg_delta = __ldcg(stat + kTile);
+    const int2 span = make_int2(__ldcg(reinterpret_cast<const int*>(stat) + 2 * kTile),
+                                __ldcg(reinterpret_cast<const int*>(stat) + 3 * kTile));
+    const bool sees = span.x < span.y;
+    const int all_from = __reduce_max_sync(0xffffffffu, sees ? span.x : 0);
+    const int all_to = __reduce_min_sync(0xffffffffu, sees ? span.y : 0x7fffffff);
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t x_col = tmem + lane_off + C::kColX + 32u * q;
+    const uint32_t y_col = tmem + lane_off + C::kColY + 32u * q;
+    const uint32_t ds_col = tmem + lane_off + C::kColDs + 16u * q;
+    const uint64_t c2 = pack_f32x2(p.scale_log2, p.scale_log2), l2 = pack_f32x2(neg_lse, neg_lse),
+                   d2 = pack_f32x2(neg_delta, neg_delta);
+    const float dn = F16 ? ds_down / kPUp : 1.f;
+    const uint64_t down2 = pack_f32x2(dn, dn);
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      const int key0 = (block0 + i) * kTile + 32 * q;
+      const bool masked = key0 < all_from || key0 + 32 > all_to;
+      wait_warp(bar(C::kXFull), i & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      uint32_t x[32], y[32];
+      tmem_ld_32x32b_x32(x_col, x);
+      tmem_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::kXRead));
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) {
+        const float2 a = halves_of(fma2(pair_of(x[c], x[c + 1]), c2, l2));
+        x[c] = __float_as_uint(ex2_approx(a.x));
+        x[c + 1] = __float_as_uint(ex2_approx(a.y));
+      }
+      wait_warp(bar(C::kYFull), i & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      tmem_ld_32x32b_x32(y_col, y);
+      tmem_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::kYRead));
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) {
+        uint64_t a = pair_of(x[c], x[c + 1]);
+        if (F16) a = mul2(a, down2);
+        const float2 u = halves_of(mul2(a, add2(pair_of(y[c], y[c + 1]), d2)));
+        y[c] = __float_as_uint(u.x);
+        y[c + 1] = __float_as_uint(u.y);
+      }
+      if (masked) {
+        const uint32_t seen = seen_word(span, key0);
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+          if (!(seen & (1u << c))) y[c] = 0;
+      }
+      uint32_t pk[16];
+#pragma unroll
+      for (int c = 0; c < 32; c += 2)
+        pk[c / 2] = pack16<F16>(__uint_as_float(y[c]), __uint_as_float(y[c + 1]));
+      if (i > 0) wait_warp(bar(C::kDsDone), (i - 1) & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      tmem_st_32x32b_x16(ds_col, pk);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::kDsFull));
+    }
+    if (count > 0) wait_warp(bar(C::kDsDone), (count - 1) & 1, p.err, ERR_WAIT_MMA);
+    tc_fence_after();
+    const int64_t slot =
+        ((static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.q_parts + part) * kTile + row;
+    const float f = p.scale / ds_down;
+#pragma unroll 1
+    for (int d = q * (D / 4); d < (q + 1) * (D / 4); d += 16) {
+      uint16_t* dq = static_cast<uint16_t*>(p.dq.p) + token * p.dq.token + head * p.dq.head + d;
+      float* part_q = p.q_parts > 1 ? p.part_q + slot * D + d : nullptr;
+      if (count > 0) leave16<F16>(tmem + lane_off + C::kColDq + d, f, dq, part_q, valid && sees);
+      if (valid && (!sees || count == 0)) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+          const uint4 z = make_uint4(0, 0, 0, 0);
+          if (part_q == nullptr)
+            *reinterpret_cast<uint4*>(dq + e) = z;
+          else
+            *reinterpret_cast<uint4*>(part_q + e) = *reinterpret_cast<uint4*>(part_q + e + 4) = z;
+        }
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ------------------------------------------------------------------------------ parts added up
+// in their order: a thread per eight elements
+template <bool F16, int D>
+__global__ void __launch_bounds__(256) span_sums_kernel(const __grid_constant__ SpanBwd p) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 * 8 / D) + threadIdx.x / (D / 8);
+  const int d = threadIdx.x % (D / 8) * 8;
+  const float* from;
+  uint16_t* to;
+  int parts;
+  int64_t step;
+  if (blockIdx.y == 0) {
+    if (p.q_parts == 1 || i >= static_cast<int64_t>(p.y.n_q) * p.y.heads) return;
+    const int token = static_cast<int>(i / p.y.heads), head = static_cast<int>(i % p.y.heads);
+    const int tile = token / p.y.tile_tokens;
+    const int row = (token - tile * p.y.tile_tokens) * p.y.per + head % p.y.per;
+    parts = p.q_parts;
+    step = kTile * D;
+    from = p.part_q + ((static_cast<int64_t>(head / p.y.per) * p.y.row_tiles + tile) * parts * kTile + row) * D + d;
+    to = static_cast<uint16_t*>(p.dq.p) + token * p.dq.token + head * p.dq.head + d;
+  } else {
+    if (p.k_parts == 1 || i >= static_cast<int64_t>(p.y.n_k) * p.y.groups) return;
+    const bool v = blockIdx.y == 2;
+    const int key = static_cast<int>(i / p.y.groups), group = static_cast<int>(i % p.y.groups);
+    parts = p.k_parts;
+    step = 2 * kTile * D;
+    from = p.part_k +
+           ((static_cast<int64_t>(group) * p.y.key_blocks + key / kTile) * parts * 2 * kTile +
+            (v ? kTile : 0) + key % kTile) * D + d;
+    const SpanRows& r = v ? p.dv : p.dk;
+    to = static_cast<uint16_t*>(r.p) + key * r.token + group * r.head + d;
+  }
+  float sum[8] = {};
+#pragma unroll 4
+  for (int c = 0; c < parts; ++c) {
+    const float4 a = __ldcg(reinterpret_cast<const float4*>(from + c * step));
+    const float4 b = __ldcg(reinterpret_cast<const float4*>(from + c * step + 4));
+    sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w;
+    sum[4] += b.x, sum[5] += b.y, sum[6] += b.z, sum[7] += b.w;
+  }
+  *reinterpret_cast<uint4*>(to) =
+      make_uint4(pack16<F16>(sum[0], sum[1]), pack16<F16>(sum[2], sum[3]),
+                 pack16<F16>(sum[4], sum[5]), pack16<F16>(sum[6], sum[7]));
+}
+
+// no keys, or no queries: what there is gets zeros
+__global__ void span_zeros_kernel(SpanRows r, int tokens, int heads, int head_dim) {
+  grid_dep_wait();
+  const int64_t rows = static_cast<int64_t>(tokens) * heads;
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x)
+    static_cast<uint16_t*>(r.p)[i / heads * r.token + i % heads * r.head + threadIdx.x] = 0;
+  grid_dep_launch();
+}
+
+// Parts where there are few units: as many as fill the GPU.
+int parts_for(int64_t units, int most) {
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, num_sms() / units)));
+}
+
+struct BwdPlan {
+  int q_parts, k_parts;
+  size_t stat, limits, most, part_q, part_k, total;  // byte offsets
+};
+BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
+  BwdPlan b{};
+  b.q_parts = parts_for(static_cast<int64_t>(y.groups) * y.row_tiles, y.key_blocks);
+  b.k_parts = parts_for(static_cast<int64_t>(y.groups) * y.key_blocks, y.row_tiles);
+  const size_t tiles = static_cast<size_t>(y.groups) * y.row_tiles;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  b.stat = 0;
+  b.limits = b.stat + tiles * 4 * kTile * sizeof(float);
+  b.most = b.limits + up(static_cast<size_t>(y.row_tiles) * sizeof(int4));
+  b.part_q = b.most + up(tiles * sizeof(float));
+  b.part_k = b.part_q + (b.q_parts > 1 ? tiles * b.q_parts * kTile * head_dim * sizeof(float) : 0);
+  b.total = b.part_k + (b.k_parts > 1 ? static_cast<size_t>(y.groups) * y.key_blocks * b.k_parts * 2 *
+                                            kTile * head_dim * sizeof(float)
+                                      : 0);
+  return b;
+}
+
+template <bool F16, int D>
+cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, const SpanRows& v,
+                       cudaStream_t s) {
+  CUtensorMap tmQ, tmDo, tmK, tmV;
+  if (!make_map(&tmQ, F16, q.p, D, p.y.heads, p.y.n_q, 1, q.head, q.token, 0, p.y.per, p.y.tile_tokens) ||
+      !make_map(&tmDo, F16, p.dout.p, D, p.y.heads, p.y.n_q, 1, p.dout.head, p.dout.token, 0, p.y.per,
+                p.y.tile_tokens) ||
+      !make_map(&tmK, F16, k.p, D, p.y.groups, p.y.n_k, 1, k.head, k.token, 0, 1, kTile) ||
+      !make_map(&tmV, F16, v.p, D, p.y.groups, p.y.n_k, 1, v.head, v.token, 0, 1, kTile))
+    return cudaErrorInvalidValue;
+  static OncePerDevice once;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess)
+    e = once.run(dev, [&] {
+      const cudaError_t a = cudaFuncSetAttribute(
+          span_keys_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, KeyCfg<D>::kSmem);
+      return a != cudaSuccess ? a
+                              : cudaFuncSetAttribute(span_query_kernel<F16, D>,
+                                                     cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     QueryCfg<D>::kSmem);
+    });
+  if (e == cudaSuccess)
+    e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles, p.y.groups), dim3(256), 0, s, p);
+  if (e == cudaSuccess)
+    e = launch_pdl(span_keys_kernel<F16, D>, dim3(p.y.key_blocks * p.k_parts, p.y.groups),
+                   dim3(KeyCfg<D>::kThreads), KeyCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, p);
+  if (e == cudaSuccess)
+    e = launch_pdl(span_query_kernel<F16, D>, dim3(p.y.row_tiles * p.q_parts, p.y.groups),
+                   dim3(QueryCfg<D>::kThreads), QueryCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, p);
+  if (e != cudaSuccess || (p.q_parts == 1 && p.k_parts == 1)) return e;
+  const int64_t rows = std::max(p.q_parts > 1 ? static_cast<int64_t>(p.y.n_q) * p.y.heads : 0,
+                                p.k_parts > 1 ? static_cast<int64_t>(p.y.n_k) * p.y.groups : 0);
+  constexpr int kRows = 256 * 8 / D;
+  return launch_pdl(span_sums_kernel<F16, D>, dim3(static_cast<unsigned>((rows + kRows - 1) / kRows), 3),
+                    dim3(256), 0, s, p);
+}
+
+}  // namespace
+
+size_t span_bwd_workspace_bytes(int n_q, int n_k, int heads, int groups, int head_dim) {
+  if (n_q == 0 || n_k == 0) return 0;
+  return bwd_plan(span_shape(n_q, n_k, heads, groups), head_dim).total;
+}
+
+}  // namespace fd
+
+extern "C" {
+
+fd_status fd_op_span_attention_bwd(
+    const fd_span_attention* a, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+    const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+    int64_t v_token_stride, int64_t v_head_stride, const int32_t* spans, const void* out,
+    int64_t out_token_stride, int64_t out_head_stride, const float* lse, const void* dout,
+    int64_t dout_token_stride, int64_t dout_head_stride, void* dq, int64_t dq_token_stride,
+    int64_t dq_head_stride, void* dk, int64_t dk_token_stride, int64_t dk_head_stride, void* dv,
+    int64_t dv_token_stride, int64_t dv_head_stride, void* workspace, int* err_dev, void* stream) {
+  if (!fd::span_valid(a)) return FD_ERR_INVALID_ARG;
+  if (a->n_q == 0 && a->n_k == 0) return FD_OK;
+  const fd::SpanRows qr{const_cast<void*>(q), q_token_stride, q_head_stride},
+      kr{const_cast<void*>(k), k_token_stride, k_head_stride},
+      vr{const_cast<void*>(v), v_token_stride, v_head_stride};
+  fd::SpanBwd p{};
+  p.out = {const_cast<void*>(out), out_token_stride, out_head_stride};
+  p.dout = {const_cast<void*>(dout), dout_token_stride, dout_head_stride};
+  p.dq = {dq, dq_token_stride, dq_head_stride};
+  p.dk = {dk, dk_token_stride, dk_head_stride};
+  p.dv = {dv, dv_token_stride, dv_head_stride};
+  auto queries = [&](const fd::SpanRows& r) {
+    return a->n_q == 0 || fd::span_rows_ok(r, a->n_q, a->heads, a->head_dim);
+  };
+  auto keys = [&](const fd::SpanRows& r) {
+    return a->n_k == 0 || fd::span_rows_ok(r, a->n_k, a->groups, a->head_dim);
+  };
+  if (!queries(qr) || !queries(p.out) || !queries(p.dout) || !queries(p.dq) || !keys(kr) ||
+      !keys(vr) || !keys(p.dk) || !keys(p.dv) || !fd::span_ptr(err_dev, 4))
+    return FD_ERR_INVALID_ARG;
+  if (a->n_q > 0 && a->n_k > 0 &&
+      (!fd::span_ptr(spans, 8) || !fd::span_ptr(lse, 4) || !fd::span_ptr(workspace, 16)))
+    return FD_ERR_INVALID_ARG;
+  const fd_status st = fd::check_device();
+  if (st != FD_OK) return st;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a->n_q == 0 || a->n_k == 0) {
+    cudaError_t e = cudaSuccess;
+    auto zeros = [&](const fd::SpanRows& r, int tokens, int heads) {
+      if (tokens > 0 && e == cudaSuccess)
+        e = fd::launch_pdl(fd::span_zeros_kernel, dim3(fd::num_sms()), dim3(a->head_dim), 0, s, r, tokens,
+                           heads, a->head_dim);
+    };
+    zeros(p.dq, a->n_q, a->heads);
+    zeros(p.dk, a->n_k, a->groups);
+    zeros(p.dv, a->n_k, a->groups);
+    return e == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+  }
+  p.y = fd::span_shape(a->n_q, a->n_k, a->heads, a->groups);
+  const fd::BwdPlan b = fd::bwd_plan(p.y, a->head_dim);
+  p.q_parts = b.q_parts;
+  p.k_parts = b.k_parts;
+  p.spans = spans;
+  p.scale = a->scale;
+  p.scale_log2 = a->scale * fd::kLog2e;
+  p.lse = lse;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.stat = reinterpret_cast<float*>(ws + b.stat);
+  p.limits = reinterpret_cast<int4*>(ws + b.limits);
+  p.most = reinterpret_cast<float*>(ws + b.most);
+  p.part_q = reinterpret_cast<float*>(ws + b.part_q);
+  p.part_k = reinterpret_cast<float*>(ws + b.part_k);
+  p.err = err_dev;
+  const bool f16 = a->dtype == FD_DTYPE_F16;
+  const cudaError_t e = a->head_dim == 64 ? (f16 ? fd::launch_bwd<true, 64>(p, qr, kr, vr, s)
+                                                 : fd::launch_bwd<false, 64>(p, qr, kr, vr, s))
+                                          : (f16 ? fd::launch_bwd<true, 128>(p, qr, kr, vr, s)
+                                                 : fd::launch_bwd<false, 128>(p, qr, kr, vr, s));
+  return e == cudaSuccess ? FD_OK : FD_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -156,6 +156,8 @@ _SIGS = {
     "fd_span_attention_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(fd_span_attention), _I]),
     "fd_op_span_attention": (_I, [ctypes.POINTER(fd_span_attention)] + [_P, _L, _L] * 3 + [
         _P, _P, _L, _L, _P, _P, _P, _P]),
+    "fd_op_span_attention_bwd": (_I, [ctypes.POINTER(fd_span_attention)] + [_P, _L, _L] * 3 + [
+        _P, _P, _L, _L, _P] + [_P, _L, _L] * 4 + [_P, _P, _P]),
     "fd_op_checkpoint_save": (_I, [_I, _I, _I, _P, _L, _P, _P, _P]),
     "fd_op_checkpoint_load": (_I, [_I, _I, _I, _I, _P, _P, _P, _L, _P]),
     "fd_op_block_join": (_I, [ctypes.POINTER(fd_block_join), _P, _L, _P, _L, _F, _P, _L, _P, _L,
@@ -1027,6 +1029,24 @@ def op_span_attention(q, k, v, spans, out, lse, scale=None, workspace=None, err=
         _status_word(err, int32, dev), _stream_on(dev, stream))
     if code:
         raise FdError(code, "fd_op_span_attention")
+
+
+def op_span_attention_bwd(q, k, v, spans, out, lse, dout, dq, dk, dv, scale=None, workspace=None,
+                          err=None, stream=None) -> None:
+    """The gradient of op_span_attention from dout like out: dq like q, dk and dv like k, from the forward
+    call's inputs and what it left in out and lse (fd_op_span_attention_bwd)."""
+    view, dev, args = _span_view(q, k, v, spans, scale, workspace, True)
+    _, _, float32, int32 = _torch_types()
+    rows = []
+    for t, what, like in ((out, "out", q), (dout, "dout", q), (dq, "dq", q), (dk, "dk", k),
+                          (dv, "dv", k)):
+        p, st = _rows(t, what, like.shape, q.dtype, dev)
+        rows += [p, st[0], st[1]]
+    code = lib().fd_op_span_attention_bwd(
+        ctypes.byref(view), *args, *rows[:3], _dense(lse, "lse", (view.heads, view.n_q), float32, dev),
+        *rows[3:], _ptr(workspace), _status_word(err, int32, dev), _stream_on(dev, stream))
+    if code:
+        raise FdError(code, "fd_op_span_attention_bwd")
 
 
 # --------------------------------------- a residual block in training: checkpoints and the join

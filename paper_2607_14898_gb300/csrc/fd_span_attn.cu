@@ -11,48 +11,60 @@ namespace {
 
 struct SpanFwd {
   SpanShape y;
-  int pairs, parts;
+  int parts;
   const int32_t* spans;
   float scale_log2;
   SpanRows out;
   float* lse;      // [heads][n_q]
-  float* part_o;   // [group][pair][part][tile][128][D]
+  float* part_o;   // [group][row tile][part][128][D]
   float2* part_ml; // the same rows: running maximum (log2) and sum
   int* err;
 };
 
 constexpr float kSlack = 8.f;  // log2 by which a row's maximum may grow before O is rescaled
 
-// A block has two row tiles of a group (a pair) and a run of the key blocks that any of their
-// queries see.
-//   warps 0 ..     softmax: D = 128: four warps a tile, a thread per row; D = 64: eight, half of a
-//                  block's keys each, with a running maximum, a sum and an O of its own
-//   next           TMA: Q of both tiles, then K and V by blocks through one ring
-//   next           zeros for the values of keys that no query of the pair sees (their probability is
-//                  0, but 0 times NaN is NaN)
-//   last two       products of a tile each: S = Q K^T, O += P V
-// TMEM: S of both tiles (P takes the first columns of what it was made of), then O.
+// A block has a row tile of a group and a run of the key blocks, of 256 keys, that any of its queries
+// see.
+//
+// The softmax is the longest chain of a key block (scores out of TMEM, maximum, exponentials, P into
+// TMEM), so sixteen warps share it, four on every SM sub-partition: each of four groups of 128
+// threads has a quarter of the keys, a row (TMEM lane) per thread. The row's running maximum is
+// handed from quarter to quarter, which sets the groups a step apart: the exponentials of one run
+// beside the loads, masks and maxima of the others.
+//   warps 0-15    softmax: warps 4 q .. 4 q + 3 quarter q
+//   warp 16       TMA: Q, then K and V by half blocks (128 keys), through a ring each, so that a half
+//                 is fetched as soon as one has been used
+//   warps 17, 18  products (a thread issues one per 104 to 158 cycles whatever its size). D = 64:
+//                 those of the block's first and second half, each half with a running maximum and an
+//                 O of its own; D = 128: S of both halves, and P V into the one O that TMEM has
+//                 room for
+//   warp 19       zeros for the values of keys that no query of the tile sees (their probability is 0,
+//                 but 0 times NaN is NaN)
+// TMEM (512 columns): S 2 x 128, P 2 x 64 (two 16-bit values a column), O 2 x 64 or 128. S takes the
+// next scores once the softmax has it in registers.
 template <int D>
 struct FwdCfg {
-  static constexpr int kHalves = D == 64 ? 2 : 1;
-  static constexpr int kKeys = kTile / kHalves;  // of a softmax thread
-  static constexpr int kSoftmax = 8 * kHalves;   // warps
-  static constexpr int kThreads = (kSoftmax + 4) * 32;
-  static constexpr int kTileBytes = kTile * D * 2;
-  static constexpr int kSlots = D == 128 ? 5 : 10;
-  static constexpr int kOffRing = 2 * kTileBytes;
-  static constexpr int kOffMl = kOffRing + kSlots * kTileBytes;
-  static constexpr int kOffBar = kOffMl + (kHalves == 2 ? 4 * kTile * 8 : 0);
-  static constexpr int kQFull = 0, kFull = 1, kFree = kFull + kSlots, kReady = kFree + kSlots,
-                       kSFull = kReady + kSlots, kPFull = kSFull + 2, kOFull = kPFull + 4,
-                       kBars = kOFull + 2;
+  static constexpr int kKeys = 256;
+  static constexpr int kThreads = 640;  // five warps a sub-partition: 96 registers
+  static constexpr int kTileBytes = kTile * D * 2;  // Q, and K or V of half a block
+  static constexpr int kSlots = D == 128 ? 3 : 6;   // of each ring; half 2 J + h is in slot (2 J + h) % kSlots
+  static constexpr bool kTwoO = D == 64;
+  // A parity tells a phase from its neighbours and no further, so whoever waits for a slot's
+  // barrier has to wait for every phase of it: one thread waits for all halves, or (D = 64) one
+  // for each half of the blocks, whose slots differ because the ring's length is even.
+  static_assert(!kTwoO || kSlots % 2 == 0, "waiters");
+  static constexpr int kOffK = kTileBytes;
+  static constexpr int kOffV = kOffK + kSlots * kTileBytes;
+  static constexpr int kOffMax = kOffV + kSlots * kTileBytes;
+  static constexpr int kOffBar = kOffMax + (kTwoO ? 4 : 1) * kTile * 4;  // D = 64: [half][m, l]
+  static constexpr uint32_t kColS = 0, kColP = 256, kColO = 384;
+  // barriers: kSFull, kSRead of the halves, kPFull, kPv of the quarters, kMax of each of their warps
+  static constexpr int kQFull = 0, kKFull = 1, kKFree = kKFull + kSlots, kVFull = kKFree + kSlots,
+                       kVFree = kVFull + kSlots, kVReady = kVFree + kSlots,
+                       kSFull = kVReady + kSlots, kSRead = kSFull + 2, kPFull = kSRead + 2,
+                       kPv = kPFull + 4, kMax = kPv + 4, kDone = kMax + 16, kBars = kDone + 2;
   static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
-  static constexpr uint32_t kColS = 0, kColO = 256;  // S of tile t at 128 t, O at 128 t (+ 64 half)
   static_assert(kSmem <= 227 * 1024, "shared memory");
-  // the phase of kReady for item i of the ring: a slot has a V every kSlots items, or every second time
-  static __device__ uint32_t ready_phase(int i) {
-    return (kSlots % 2 ? i / (2 * kSlots) : i / kSlots) & 1;
-  }
 };
 
 template <bool F16, int D>
@@ -68,31 +80,40 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
-  volatile int* range = reinterpret_cast<volatile int*>(tmem_slot + 1);  // first block, blocks
-  float2* ml = reinterpret_cast<float2*>(smem + C::kOffMl);              // [tile][half][row]
+  volatile int* range = reinterpret_cast<volatile int*>(tmem_slot + 1);  // first key, blocks
+  // the rows' running maximum (D = 64: of each half); at the end their sums
+  volatile float* row_max = reinterpret_cast<volatile float*>(smem + C::kOffMax);
 
   // (later tokens first: under a causal mask they see most)
   const int part = blockIdx.x % p.parts;
-  const int pair = p.pairs - 1 - static_cast<int>(blockIdx.x) / p.parts;
+  const int tile = p.y.row_tiles - 1 - static_cast<int>(blockIdx.x) / p.parts;
   const int group = blockIdx.y;
-  const int token0 = pair * 2 * p.y.tile_tokens;
-  const int tokens = min(2 * p.y.tile_tokens, p.y.n_q - token0);
+  const int token0 = tile * p.y.tile_tokens;
+  const int tokens = min(p.y.tile_tokens, p.y.n_q - token0);
 
-  for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += C::kThreads)
+  // rows past tile_rows are never loaded
+  for (int i = threadIdx.x; i < C::kTileBytes / 16; i += C::kThreads)
     reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   fence_proxy_async_smem();
   if (threadIdx.x == 0) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
     mbar_init(bar(C::kQFull), 1);
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(bar(C::kFull + i), 1);
-      mbar_init(bar(C::kFree + i), 2);
-      mbar_init(bar(C::kReady + i), 1);
+      mbar_init(bar(C::kKFull + i), 1);
+      mbar_init(bar(C::kKFree + i), 1);
+      mbar_init(bar(C::kVFull + i), 1);
+      mbar_init(bar(C::kVFree + i), 1);
+      mbar_init(bar(C::kVReady + i), 1);
     }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(bar(C::kSFull + t), 1);
-      mbar_init(bar(C::kOFull + t), 1);
-      for (int h = 0; h < 2; ++h) mbar_init(bar(C::kPFull + 2 * t + h), 4);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(bar(C::kSFull + h), 1);
+      mbar_init(bar(C::kSRead + h), 8);
+      mbar_init(bar(C::kDone + h), 1);
+    }
+    for (int q = 0; q < 4; ++q) {
+      mbar_init(bar(C::kPFull + q), 4);
+      mbar_init(bar(C::kPv + q), 1);
+      for (int i = 0; i < 4; ++i) mbar_init(bar(C::kMax + 4 * q + i), 32);
     }
     fence_barrier_init();
   }
@@ -102,7 +123,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   } else if (warp == 1) {
-    // the key blocks that any query of the pair sees, and this block's part of them
+    // the keys that any query of the tile sees, and this block's part of them
     int lo = 0x7fffffff, hi = 0;
     for (int i = lane; i < tokens; i += 32) {
       const int2 s = span_of(p.spans, token0 + i, p.y.n_k);
@@ -113,11 +134,12 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
     }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
-    const int b0 = hi > 0 ? lo / kTile : 0, n = hi > 0 ? (hi + kTile - 1) / kTile - b0 : 0;
+    const int key = hi > 0 ? lo / kTile * kTile : 0;
+    const int n = (hi - key + C::kKeys - 1) / C::kKeys;
     const int first = static_cast<int>(static_cast<int64_t>(n) * part / p.parts);
     const int end = static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.parts);
     if (lane == 0) {
-      range[0] = b0 + first;
+      range[0] = key + first * C::kKeys;
       range[1] = aligned ? end - first : 0;
     }
   }
@@ -125,69 +147,82 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int block0 = range[0], count = range[1];
+  const int key_start = range[0], count = range[1];
 
   if (count == 0) {
     // nothing is seen: the softmax warps write that below
-  } else if (warp == C::kSoftmax) {
+  } else if (warp == 16) {
     if (lane == 0) {
-      prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
       prefetch_tmap(&tmV);
-      mbar_expect_tx(bar(C::kQFull), 2 * p.y.tile_rows * D * 2);
-      for (int t = 0; t < 2; ++t)
+      mbar_expect_tx(bar(C::kQFull), p.y.tile_rows * D * 2);
+      for (int d = 0; d < D / 64; ++d)
+        tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.y.per, token0, 0);
+      // the next half of K, or of V, as soon as its slot is free
+      int k = 0, v = 0, idle = 0;  // halves so far
+      uint32_t idle_since = 0;
+      auto room = [&](int n, int free) {
+        return n < 2 * count && (n < C::kSlots ||
+                                 mbar_test_wait(bar(free + n % C::kSlots), (n / C::kSlots - 1) & 1));
+      };
+      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int full) {
+        const int slot = n % C::kSlots;
+        mbar_expect_tx(bar(full + slot), C::kTileBytes);
         for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(base + t * C::kTileBytes + d * kSub, &tmQ, bar(C::kQFull), 64 * d,
-                      group * p.y.per, token0 + t * p.y.tile_tokens, 0);
-      int i = 0;  // K of block j is item 2 j of the ring, V item 2 j + 1
-      for (; i < 2 * count; ++i) {
-        const int slot = i % C::kSlots;
-        if (i >= C::kSlots &&
-            !wait(bar(C::kFree + slot), (i / C::kSlots - 1) & 1, p.err, ERR_WAIT_MMA))
+          tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
+                      key_start + n * kTile, 0);
+      };
+      while (k < 2 * count || v < 2 * count) {
+        bool moved = false;
+        if (room(k, C::kKFree)) {
+          load(k++, &tmK, base + C::kOffK, C::kKFull);
+          moved = true;
+        }
+        if (room(v, C::kVFree)) {
+          load(v++, &tmV, base + C::kOffV, C::kVFull);
+          moved = true;
+        }
+        if (moved)
+          idle = 0;
+        else if (!poll_again(idle, idle_since, p.err, ERR_WAIT_MMA))
           break;
-        mbar_expect_tx(bar(C::kFull + slot), C::kTileBytes);
-        for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(base + C::kOffRing + slot * C::kTileBytes + d * kSub, i & 1 ? &tmV : &tmK,
-                      bar(C::kFull + slot), 64 * d, group, (block0 + i / 2) * kTile, 0);
       }
       // nothing may be in flight when the block exits
       wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA, true);
-      for (int j = max(0, i - C::kSlots); j < i; ++j)
-        wait(bar(C::kFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, k - C::kSlots); j < k; ++j)
+        wait(bar(C::kKFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, v - C::kSlots); j < v; ++j)
+        wait(bar(C::kVFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
     }
-  } else if (warp == C::kSoftmax + 1) {
+  } else if (warp == 19) {
     // ---- values of keys that nothing sees
-    int2 span[8];
+    int2 span[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
       span[i] = lane + 32 * i < tokens ? span_of(p.spans, token0 + lane + 32 * i, p.y.n_k)
                                        : make_int2(0, 0);
-    for (int j = 0; j < count; ++j) {
-      const int key0 = (block0 + j) * kTile, item = 2 * j + 1, slot = item % C::kSlots;
+    for (int n = 0; n < 2 * count; ++n) {
+      const int key0 = key_start + n * kTile, slot = n % C::kSlots;
       bool whole = false;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) whole |= span[i].x <= key0 && span[i].y >= key0 + kTile;
+      for (int i = 0; i < 4; ++i) whole |= span[i].x <= key0 && span[i].y >= key0 + kTile;
       uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
       if (!__any_sync(0xffffffffu, whole)) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           uint32_t mine = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) mine |= seen_word(span[i], key0 + 32 * w);
+          for (int i = 0; i < 4; ++i) mine |= seen_word(span[i], key0 + 32 * w);
           seen[w] = __reduce_or_sync(0xffffffffu, mine);
         }
       }
-      // (K too: a parity tells a phase from its neighbours only, so none may be left out)
-      const int before = item - 1;
-      if (!wait_warp(bar(C::kFull + before % C::kSlots), (before / C::kSlots) & 1, p.err,
-                     ERR_WAIT_TMA) ||
-          !wait_warp(bar(C::kFull + slot), (item / C::kSlots) & 1, p.err, ERR_WAIT_TMA))
-        break;
+      if (!wait_warp(bar(C::kVFull + slot), (n / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) break;
       if ((seen[0] & seen[1] & seen[2] & seen[3]) != 0xffffffffu) {
-#pragma unroll
+#pragma unroll 1
         for (int w = 0; w < 4; ++w) {
-          if ((seen[w] >> lane) & 1u) continue;
-          uint4* row = reinterpret_cast<uint4*>(smem + C::kOffRing + slot * C::kTileBytes +
+          const uint32_t there = w == 0 ? seen[0] : w == 1 ? seen[1] : w == 2 ? seen[2] : seen[3];
+          if ((there >> lane) & 1u) continue;
+          uint4* row = reinterpret_cast<uint4*>(smem + C::kOffV + slot * C::kTileBytes +
                                                 (32 * w + lane) * 128);
 #pragma unroll
           for (int d = 0; d < D / 64; ++d)
@@ -197,220 +232,278 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
         fence_proxy_async_smem();
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kReady + slot));
+      if (lane == 0) mbar_arrive(bar(C::kVReady + slot));
     }
-  } else if (warp > C::kSoftmax + 1) {
-    // ---- products of tile t. S of the next block goes where P of this one is: it is issued after
-    // the product that reads P, by the same thread, and products run in their order.
-    const int t = warp - C::kSoftmax - 2;
+  } else if (warp >= 17) {  // 17 and 18
     if (lane == 0) {
       constexpr uint32_t is = Mma<F16, D>::idesc(kTile, false), io = Mma<F16, D>::idesc(D, true);
-      const uint32_t s_col = tmem + C::kColS + 128u * t, o_col = tmem + C::kColO + 128u * t;
-      const uint64_t q0 = sdesc_k_sw128(base + t * C::kTileBytes);
-      auto scores = [&](int j) -> bool {
-        const int item = 2 * j, slot = item % C::kSlots;
-        if (!wait(bar(C::kFull + slot), (item / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
+      const uint32_t s_col = tmem + C::kColS, p_col = tmem + C::kColP, o_col = tmem + C::kColO;
+      const uint64_t q0 = sdesc_k_sw128(base);
+      // S of half h of block J, once K is there
+      auto scores = [&](int J, int h) -> bool {
+        const int n = 2 * J + h, slot = n % C::kSlots;
+        if (!wait(bar(C::kKFull + slot), (n / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
         tc_fence_after();
-        const uint64_t k0 = sdesc_k_sw128(base + C::kOffRing + slot * C::kTileBytes);
+        const uint64_t k0 = sdesc_k_sw128(base + C::kOffK + slot * C::kTileBytes);
 #pragma unroll
         for (int d = 0; d < D / 64; ++d)
-          mma4_bf16_ss(s_col, q0 + static_cast<uint64_t>(d * (kSub >> 4)),
+          mma4_bf16_ss(s_col + 128u * h, q0 + static_cast<uint64_t>(d * (kSub >> 4)),
                        k0 + static_cast<uint64_t>(d * (kSub >> 4)), is, d > 0);
-        mma_commit(bar(C::kSFull + t));
-        mma_commit(bar(C::kFree + slot));
+        mma_commit(bar(C::kSFull + h));
+        mma_commit(bar(C::kKFree + slot));
         return true;
       };
-      bool ok = wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA) && scores(0);
-      for (int j = 0; j < count && ok; ++j) {
-        const int item = 2 * j + 1, slot = item % C::kSlots;
-        ok = wait(bar(C::kReady + slot), C::ready_phase(item), p.err, ERR_WAIT_TMA);
-        const uint32_t v = base + C::kOffRing + slot * C::kTileBytes;
+      // P V of half h of block J into O (the half's own for D = 64), quarter after quarter
+      auto values = [&](int J, int h) -> bool {
+        const int n = 2 * J + h, slot = n % C::kSlots;
+        if (!wait(bar(C::kVReady + slot), (n / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
 #pragma unroll
-        for (int h = 0; h < C::kHalves; ++h) {
-          ok = ok && wait(bar(C::kPFull + 2 * t + h), j & 1, p.err, ERR_WAIT_EPI);
-          if (!ok) break;
+        for (int x = 0; x < 2; ++x) {
+          const int q = 2 * h + x;
+          if (!wait(bar(C::kPFull + q), J & 1, p.err, ERR_WAIT_EPI)) return false;
           tc_fence_after();
-#pragma unroll
-          for (int x = 0; x < C::kKeys / 64; ++x)
-            mma4_ts_mn(o_col + 64u * h, s_col + 64u * h + 32u * x,
-                       sdesc_mn_sw128(v + (h * C::kKeys + x * 64) * 128, kSub), io, j > 0 || x > 0);
+          const uint64_t v0 =
+              sdesc_mn_sw128(base + C::kOffV + slot * C::kTileBytes + x * (kSub / 2), kSub);
+          const bool fresh = J == 0 && x == 0 && (C::kTwoO || h == 0);
+          mma4_ts_mn(o_col + (C::kTwoO ? 64u * h : 0u), p_col + 32u * q, v0, io, !fresh);
+          mma_commit(bar(C::kPv + q));
         }
-        if (!ok) break;
-        mma_commit(bar(C::kFree + slot));
-        if (j + 1 < count) ok = scores(j + 1);
+        mma_commit(bar(C::kVFree + slot));
+        return true;
+      };
+      const int h = warp - 17;
+      bool ok = true;
+      if (C::kTwoO) {
+        ok = wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA) && scores(0, h);
+        for (int J = 0; J < count && ok; ++J) {
+          if (J + 1 < count)
+            ok = wait(bar(C::kSRead + h), J & 1, p.err, ERR_WAIT_EPI) && scores(J + 1, h);
+          ok = ok && values(J, h);
+        }
+      } else if (h == 0) {
+        ok = wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA);
+        for (int J = 0; J < count && ok; ++J)
+          for (int x = 0; x < 2 && ok; ++x)
+            ok = (J == 0 || wait(bar(C::kSRead + x), (J - 1) & 1, p.err, ERR_WAIT_EPI)) && scores(J, x);
+      } else {
+        for (int J = 0; J < count && ok; ++J) ok = values(J, 0) && values(J, 1);
       }
-      mma_commit(bar(C::kOFull + t));
-      wait(bar(C::kOFull + t), 0, p.err, ERR_WAIT_MMA, true);
+      mma_commit(bar(C::kDone + h));
+      wait(bar(C::kDone + h), 0, p.err, ERR_WAIT_MMA, true);
     }
   }
-  if (warp < C::kSoftmax) {
-    // ---- softmax of half h of tile t
-    const int t = warp / (4 * C::kHalves), h = (warp >> 2) % C::kHalves;
-    const int row = (warp & 3) * 32 + lane;
-    const int token = token0 + t * p.y.tile_tokens + row / p.y.per;
+  if (warp < 16) {
+    // ---- softmax of quarter q of the blocks
+    const int q = warp >> 2, h = q >> 1, lanes = warp & 3;
+    const int row = lanes * 32 + lane;
+    const int token = token0 + row / p.y.per;
     const bool valid = row < p.y.tile_rows && token < p.y.n_q;
     const int2 span = valid ? span_of(p.spans, token, p.y.n_k) : make_int2(0, 0);
     const bool sees = span.x < span.y;
     // keys that all of the warp's rows see (rows that see none, or are none, are set right at the end)
     const int all_from = __reduce_max_sync(0xffffffffu, sees ? span.x : 0);
     const int all_to = __reduce_min_sync(0xffffffffu, sees ? span.y : 0x7fffffff);
-    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_col = tmem + lane_off + C::kColS + 128u * t + 64u * h;
-    const uint32_t o_col = tmem + lane_off + C::kColO + 128u * t + 64u * h;
-    const float c = p.scale_log2;
+    const uint32_t lane_off = static_cast<uint32_t>(lanes * 32) << 16;
+    const uint32_t s_col = tmem + lane_off + C::kColS + 64u * q;
+    const uint32_t p_col = tmem + lane_off + C::kColP + 32u * q;
+    const uint32_t o_col = tmem + lane_off + C::kColO + (C::kTwoO ? 64u * h : 0u);
+    // the quarters that share an O and a running maximum: the one before this, in the same block
+    // or (the first one) the last in the block before
+    constexpr int kShare = C::kTwoO ? 2 : 4;
+    const bool lead = q % kShare == 0;
+    const int prev = lead ? q + kShare - 1 : q - 1;
+    volatile float* const my_max = row_max + (C::kTwoO ? 2 * h * kTile : 0) + row;
+    // (a per-thread copy: a kernel parameter costs the loop more instructions)
+    const float c = __shfl_sync(0xffffffffu, p.scale_log2, 0);
     const uint64_t c2 = pack_f32x2(c, c);
     float m = -INFINITY, l = 0.f;
+    // A wait that gives up has set the status word, and every wait after it returns at once: the warps
+    // go on to the end.
 #pragma unroll 1
-    for (int j = 0; j < count; ++j) {
-      const int key0 = (block0 + j) * kTile + h * C::kKeys;
-      wait_warp(bar(C::kSFull + t), j & 1, p.err, ERR_WAIT_MMA);
+    for (int J = 0; J < count; ++J) {
+      const int key0 = key_start + J * C::kKeys + 64 * q;
+      wait_warp(bar(C::kSFull + h), J & 1, p.err, ERR_WAIT_MMA);
       tc_fence_after();
-      const bool masked = key0 < all_from || key0 + C::kKeys > all_to;
-      // 64 scores at a time; those of 128 are fetched again for their exponentials
       uint32_t sr[2][32];
-      auto fetch = [&](int x) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) tmem_ld_32x32b_x32(s_col + 64 * x + 32 * i, sr[i]);
-        tmem_ld_wait();
-        if (masked) {
+      for (int i = 0; i < 2; ++i) tmem_ld_32x32b_x32(s_col + 32 * i, sr[i]);
+      tmem_ld_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::kSRead + h));
+      if (key0 < all_from || key0 + 64 > all_to) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t seen = seen_word(span, key0 + 64 * x + 32 * i);
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t seen = seen_word(span, key0 + 32 * i);
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!(seen & (1u << e))) sr[i][e] = 0xff800000u;
-          }
+          for (int e = 0; e < 32; ++e)
+            if (!(seen & (1u << e))) sr[i][e] = 0xff800000u;
         }
-      };
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+      float mx[4];
 #pragma unroll
-      for (int x = 0; x < C::kKeys / 64; ++x) {
-        fetch(x);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t* x = sr[i / 2] + 16 * (i % 2);
+        mx[i] = __uint_as_float(x[0]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; e += 2)
-            mx[i] = fmax3(mx[i], __uint_as_float(sr[i / 2][16 * (i % 2) + e]),
-                          __uint_as_float(sr[i / 2][16 * (i % 2) + e + 1]));
+        for (int e = 1; e < 15; e += 2)
+          mx[i] = fmax3(mx[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+        mx[i] = fmaxf(mx[i], __uint_as_float(x[15]));
       }
       const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-      const bool grow = top > m + kSlack;
-      if (j > 0 && __any_sync(0xffffffffu, grow)) {
-        // O as the products of the blocks before left it: they came before these scores
-        const float f = grow ? ex2_approx(m - top) : 1.f;
-        l *= f;
-#pragma unroll 1
-        for (int d = 0; d < D; d += 32) {
-          uint32_t o[32];
-          tmem_ld_32x32b_x32(o_col + d, o);
-          tmem_ld_wait();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-          tmem_st_32x32b_x32(o_col + d, o);
-        }
+      // the maximum that O stands for now
+      const bool fresh = J == 0 && lead;  // O holds nothing yet
+      float before = -INFINITY;
+      if (!fresh) {
+        wait_warp(bar(C::kMax + 4 * prev + lanes), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_EPI);
+        before = *my_max;
       }
-      if (grow) m = top;
-      const float off = m == -INFINITY ? 0.f : m;
+      const bool grow = top > before + kSlack;
+      const float now = grow ? top : before;
+      const float off = now == -INFINITY ? 0.f : now;
+      *my_max = now;
+      mbar_arrive(bar(C::kMax + 4 * q + lanes));
+      const float f = grow ? ex2_approx(before - off) : 1.f;  // of O
+      l *= m == now ? 1.f : ex2_approx(m - off);
+      m = now;
       const uint64_t off2 = pack_f32x2(-off, -off);
       uint64_t sum2[2] = {0, 0};
       // P in the inputs' type, which the product with V takes: 2^-9 (bf16) or 2^-12 (fp16) of each p at
       // most. The sums are of P unrounded.
+      uint32_t pk[2][16];
 #pragma unroll
-      for (int x = 0; x < C::kKeys / 64; ++x) {
-        if (C::kKeys > 64) fetch(x);
-        uint32_t pk[2][16];
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < 32; e += 2) {
+          const float2 x = halves_of(fma2(pair_of(sr[i][e], sr[i][e + 1]), c2, off2));
+          const float a = ex2_approx(x.x), b = ex2_approx(x.y);
+          sum2[e / 2 % 2] = add2(sum2[e / 2 % 2], pack_f32x2(a, b));
+          pk[i][e / 2] = pack16<F16>(a, b);
+        }
+      // the previous block's product has read this quarter's P
+      if (J > 0) wait_warp(bar(C::kPv + q), (J - 1) & 1, p.err, ERR_WAIT_MMA);
+      if (!fresh && __any_sync(0xffffffffu, grow)) {
+        // O as the products of all quarters before left it
+        wait_warp(bar(C::kPv + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_MMA);
+        tc_fence_after();
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          uint32_t o[16];
+          tmem_ld_32x32b_x16(o_col + d, o);
+          tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            uint64_t v;
-            asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(sr[i][e]), "r"(sr[i][e + 1]));
-            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(v), "l"(c2), "l"(off2));
-            float a, b;
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-            a = ex2_approx(a);
-            b = ex2_approx(b);
-            asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum2[e / 2 % 2]) : "l"(pack_f32x2(a, b)));
-            pk[i][e / 2] = pack16<F16>(a, b);
-          }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(s_col + 32 * x + 16 * i, pk[i]);
+          for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+          tmem_st_32x32b_x16(o_col + d, o);
+        }
       }
+      tc_fence_after();
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(p_col + 16 * i, pk[i]);
       {
-        float a0, b0, a1, b1;
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(b0) : "l"(sum2[0]));
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(a1), "=f"(b1) : "l"(sum2[1]));
-        l += (a0 + b0) + (a1 + b1);
+        const float2 x = halves_of(sum2[0]), y = halves_of(sum2[1]);
+        l += (x.x + x.y) + (y.x + y.y);
       }
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kPFull + 2 * t + h));
+      if (lane == 0) mbar_arrive(bar(C::kPFull + q));
     }
-    if (count > 0) wait_warp(bar(C::kOFull + t), 0, p.err, ERR_WAIT_MMA);
-    tc_fence_after();
-    // the halves on the larger maximum
-    float f0 = 1.f, f1 = 0.f;
-    if (C::kHalves == 2) {
-      ml[(2 * t + h) * kTile + row] = make_float2(m, l);
-      named_barrier(1 + t, 256);
-      const float2 a = ml[2 * t * kTile + row], b = ml[(2 * t + 1) * kTile + row];
-      m = fmaxf(a.x, b.x);
-      const float at = m == -INFINITY ? 0.f : m;
-      f0 = ex2_approx(a.x - at);
-      f1 = ex2_approx(b.x - at);
-      l = fmaf(f0, a.y, f1 * b.y);
+
+    // ---- the result: this thread's quarter of the row's elements
+    float all = 0.f, f0 = 1.f, f1 = 1.f;
+    if (count > 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wait_warp(bar(C::kPv + i), (count - 1) & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      // the sums on the last maximum, added up in the order of the quarters (named barriers of the
+      // row's four warps between the steps)
+      wait_warp(bar(C::kMax + 4 * (q / kShare * kShare + kShare - 1) + lanes), (count - 1) & 1, p.err,
+                ERR_WAIT_EPI);
+      const float last = *my_max;
+      l *= m == last ? 1.f : ex2_approx(m - last);
+      m = last;
+      // (the warp together at each of them)
+      auto meet = [&]() {
+        __syncwarp();
+        named_barrier(1 + lanes, 128);
+      };
+      meet();
+      if (C::kTwoO) {  // [half][m, l]: the halves on the larger maximum
+        volatile float* const my_sum = my_max + kTile;
+        if (lead) *my_sum = l;
+        meet();
+        if (!lead) *my_sum = *my_sum + l;
+        meet();
+        const float m0 = row_max[row], l0 = row_max[kTile + row];
+        const float m1 = row_max[2 * kTile + row], l1 = row_max[3 * kTile + row];
+        m = fmaxf(m0, m1);
+        const float at = m == -INFINITY ? 0.f : m;
+        f0 = ex2_approx(m0 - at);
+        f1 = ex2_approx(m1 - at);
+        all = fmaf(f0, l0, f1 * l1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (q == i) *my_max = i == 0 ? l : *my_max + l;
+          meet();
+        }
+        all = *my_max;
+      }
     }
-    if (!sees || count == 0) l = 0.f, m = -INFINITY;
+    if (!sees) all = 0.f;
+    if (all == 0.f) m = -INFINITY;
     const bool whole = p.parts == 1;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = all == 0.f ? 0.f : 1.f / all;
     const int head = group * p.y.per + row % p.y.per;
     uint16_t* out = static_cast<uint16_t*>(p.out.p) + static_cast<int64_t>(token) * p.out.token +
                     static_cast<int64_t>(head) * p.out.head;
     const int64_t slot =
-        ((static_cast<int64_t>(group) * p.pairs + pair) * p.parts + part) * 2 * kTile + t * kTile + row;
-    float* part_o = whole ? nullptr : p.part_o + slot * D;
+        ((static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.parts + part) * kTile + row;
 #pragma unroll 1
-    for (int d = h * (D / C::kHalves); d < (h + 1) * (D / C::kHalves); d += 32) {
-      float o[32];
+    for (int d = q * (D / 4); d < (q + 1) * (D / 4); d += 16) {
+      uint32_t o[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] = 0;
       if (count > 0) {
-        uint32_t a[32];
-        tmem_ld_32x32b_x32(tmem + lane_off + C::kColO + 128u * t + d, a);
-        if (C::kHalves == 2) {
-          uint32_t b[32];
-          tmem_ld_32x32b_x32(tmem + lane_off + C::kColO + 128u * t + 64u + d, b);
+        __syncwarp();
+        tmem_ld_32x32b_x16(tmem + lane_off + C::kColO + d, o);
+        if (C::kTwoO) {
+          uint32_t o2[16];
+          tmem_ld_32x32b_x16(tmem + lane_off + C::kColO + 64 + d, o2);
           tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; ++e)
-            o[e] = fmaf(f0, __uint_as_float(a[e]), f1 * __uint_as_float(b[e]));
+          for (int e = 0; e < 16; ++e)
+            o[e] = __float_as_uint(fmaf(f0, __uint_as_float(o[e]), f1 * __uint_as_float(o2[e])));
         } else {
           tmem_ld_wait();
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(a[e]);
         }
       }
       if (!valid) continue;
       if (whole) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
+        for (int e = 0; e < 16; e += 8) {
           uint32_t v[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            v[i] = l == 0.f ? 0u : pack16<F16>(o[e + 2 * i] * inv, o[e + 2 * i + 1] * inv);
+            v[i] = all == 0.f ? 0u
+                              : pack16<F16>(__uint_as_float(o[e + 2 * i]) * inv,
+                                            __uint_as_float(o[e + 2 * i + 1]) * inv);
           *reinterpret_cast<uint4*>(out + d + e) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-      } else if (l != 0.f) {
+      } else if (all != 0.f) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *reinterpret_cast<float4*>(part_o + d + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<uint4*>(p.part_o + slot * D + d + e) =
+              make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
       }
     }
-    if (h == 0 && valid) {
+    if (q == 0 && valid) {
       if (whole)
         p.lse[static_cast<int64_t>(head) * p.y.n_q + token] =
-            l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+            all == 0.f ? -INFINITY : (m + log2f(all)) * kLn2;
       else
-        p.part_ml[slot] = make_float2(m, l);
+        p.part_ml[slot] = make_float2(m, all);
     }
     tc_fence_before();
   }
@@ -432,14 +525,13 @@ __global__ void __launch_bounds__(256) span_join_kernel(const __grid_constant__ 
   const int token = static_cast<int>(i / p.y.heads), head = static_cast<int>(i % p.y.heads);
   const int group = head / p.y.per, tile = token / p.y.tile_tokens;
   const int row = (token - tile * p.y.tile_tokens) * p.y.per + head % p.y.per;
-  const int64_t first = (static_cast<int64_t>(group) * p.pairs + tile / 2) * p.parts * 2 * kTile +
-                        tile % 2 * kTile + row;
+  const int64_t first = (static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.parts * kTile + row;
   float m = -INFINITY;
-  for (int c = 0; c < p.parts; ++c) m = fmaxf(m, __ldcg(&p.part_ml[first + c * 2 * kTile].x));
+  for (int c = 0; c < p.parts; ++c) m = fmaxf(m, __ldcg(&p.part_ml[first + c * kTile].x));
   float l = 0.f, o = 0.f;
 #pragma unroll 4
   for (int c = 0; c < p.parts; ++c) {
-    const int64_t at = first + c * 2 * kTile;
+    const int64_t at = first + c * kTile;
     const float2 x = __ldcg(p.part_ml + at);
     if (x.y == 0.f) continue;
     const float f = ex2_approx(x.x - m);
@@ -454,10 +546,11 @@ __global__ void __launch_bounds__(256) span_join_kernel(const __grid_constant__ 
         l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Parts of every pair's key blocks: as many as fill the GPU where there are few pairs.
+// Parts of every tile's key blocks: as many as fill the GPU where there are few tiles.
 int fwd_parts(const SpanShape& y) {
-  const int64_t units = static_cast<int64_t>(y.groups) * ((y.row_tiles + 1) / 2);
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(y.key_blocks, num_sms() / units)));
+  const int64_t units = static_cast<int64_t>(y.groups) * y.row_tiles;
+  return static_cast<int>(
+      std::max<int64_t>(1, std::min<int64_t>((y.key_blocks + 1) / 2, num_sms() / units)));
 }
 
 template <bool F16, int D>
@@ -478,7 +571,7 @@ cudaError_t launch_fwd(const SpanFwd& p, const SpanRows& q, const SpanRows& k, c
                                   cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     });
   if (e != cudaSuccess) return e;
-  e = launch_pdl(span_fwd_kernel<F16, D>, dim3(p.pairs * p.parts, p.y.groups), dim3(C::kThreads),
+  e = launch_pdl(span_fwd_kernel<F16, D>, dim3(p.y.row_tiles * p.parts, p.y.groups), dim3(C::kThreads),
                  C::kSmem, s, tmQ, tmK, tmV, p);
   if (e != cudaSuccess || p.parts == 1) return e;
   const int64_t rows = static_cast<int64_t>(p.y.n_q) * p.y.heads;
@@ -514,7 +607,7 @@ size_t span_fwd_workspace_bytes(int n_q, int n_k, int heads, int groups, int hea
   const SpanShape y = span_shape(n_q, n_k, heads, groups);
   const int parts = fwd_parts(y);
   if (parts == 1) return 0;
-  return static_cast<size_t>(groups) * ((y.row_tiles + 1) / 2) * parts * 2 * kTile *
+  return static_cast<size_t>(groups) * y.row_tiles * parts * kTile *
          (head_dim * sizeof(float) + sizeof(float2));
 }
 
@@ -553,13 +646,12 @@ fd_status fd_op_span_attention(const fd_span_attention* a, const void* q, int64_
   if (st != FD_OK) return st;
   fd::SpanFwd p{};
   p.y = fd::span_shape(a->n_q, a->n_k, a->heads, a->groups);
-  p.pairs = (p.y.row_tiles + 1) / 2;
   p.parts = a->n_k > 0 ? fd::fwd_parts(p.y) : 1;
   p.spans = spans;
   p.scale_log2 = a->scale * fd::kLog2e;
   p.out = outr;
   p.lse = lse;
-  const int64_t rows = static_cast<int64_t>(p.y.groups) * p.pairs * p.parts * 2 * fd::kTile;
+  const int64_t rows = static_cast<int64_t>(p.y.groups) * p.y.row_tiles * p.parts * fd::kTile;
   p.part_o = static_cast<float*>(workspace);
   p.part_ml = need > 0 ? reinterpret_cast<float2*>(p.part_o + rows * a->head_dim) : nullptr;
   p.err = err_dev;

@@ -209,6 +209,7 @@ __host__ __device__ inline int block_of(int rows, int grid, int row) {
   return static_cast<int>(((static_cast<int64_t>(row) + 1) * grid - 1) / rows);
 }
 
+// A thread's eight columns of a row as they lie in memory, fetched a row ahead.
 template <typename B, typename H>
 struct Inputs {
   Raw8<H> dy, h;
@@ -216,9 +217,13 @@ struct Inputs {
   uint32_t h_byte, b_byte;
 };
 
+// Bound by its instructions (pairs of fp32 throughout, gains and gate in registers while they stay the
+// same): copies ahead into a ring in shared memory, three or four rows deep, made it slower (480p chunk 24.7 to 35
+// us), fewer instructions faster.
 template <typename B, typename H, int NT, int NV>
 __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ JoinBwd p) {
   constexpr int NW = NT / 32;
+  constexpr bool kKeep = NV == 1;  // gains stay in registers
   __shared__ float4 part[2][NW];
   grid_dep_wait();
   grid_dep_launch();
@@ -226,178 +231,202 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
   const int row0 = first_row(p.rows, p.grid, blockIdx.x);
   const int row1 = first_row(p.rows, p.grid, blockIdx.x + 1);
   const float inv_width = 1.f / static_cast<float>(p.width);
+  const int lane = threadIdx.x & 31;
+  const bool pre = p.pre != nullptr, post = p.post != nullptr;
   Inputs<B, H> in[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) in[v] = Inputs<B, H>{};
   float next_post = 1.f, next_pre = 0.f;
   auto fetch = [&](int row) {
-    if (p.post != nullptr) next_post = p.r_post[row];
-    if (p.pre != nullptr) next_pre = p.r_pre[row];
+    if (post) next_post = p.r_post[row];
+    if (pre) next_pre = p.r_pre[row];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int unit = threadIdx.x + v * NT;
       Inputs<B, H>& x = in[v];
-      if (unit < units) {
-        const int64_t at = unit * 8;
-        if (p.dy != nullptr) x.dy = load_raw(static_cast<const H*>(p.dy) + row * p.dy_stride + at);
-        if (p.pre != nullptr) {
-          x.du = load_raw(static_cast<const B*>(p.du) + row * p.du_stride + at);
-          if (p.h_exps != nullptr) {
-            const uint2 c =
-                *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(p.h) + row * p.h_stride + at);
-            x.h.a.x = c.x;
-            x.h.a.y = c.y;
-            x.h_byte = p.h_exps[static_cast<int64_t>(row) * blocks + unit / 4];
-          } else {
-            x.h = load_raw(static_cast<const H*>(p.h) + row * p.h_stride + at);
-          }
-        }
-        if (p.b_exps != nullptr) {
-          const uint2 c =
-              *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(p.b) + row * p.b_stride + at);
-          x.b.a.x = c.x;
-          x.b.a.y = c.y;
-          x.b_byte = p.b_exps[static_cast<int64_t>(row) * blocks + unit / 4];
+      if (unit >= units) continue;
+      auto codes = [&](const void* from, int64_t stride) {
+        return *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(from) + row * stride + unit * 8);
+      };
+      if (p.dy != nullptr) x.dy = load_raw(static_cast<const H*>(p.dy) + row * p.dy_stride + unit * 8);
+      if (pre) {
+        x.du = load_raw(static_cast<const B*>(p.du) + row * p.du_stride + unit * 8);
+        if (p.h_exps != nullptr) {
+          const uint2 c = codes(p.h, p.h_stride);
+          x.h.a.x = c.x;
+          x.h.a.y = c.y;
+          x.h_byte = p.h_exps[static_cast<int64_t>(row) * blocks + unit / 4];
         } else {
-          x.b = load_raw(static_cast<const B*>(p.b) + row * p.b_stride + at);
+          x.h = load_raw(static_cast<const H*>(p.h) + row * p.h_stride + unit * 8);
         }
+      }
+      if (p.b_exps != nullptr) {
+        const uint2 c = codes(p.b, p.b_stride);
+        x.b.a.x = c.x;
+        x.b.a.y = c.y;
+        x.b_byte = p.b_exps[static_cast<int64_t>(row) * blocks + unit / 4];
+      } else {
+        x.b = load_raw(static_cast<const B*>(p.b) + row * p.b_stride + unit * 8);
       }
     }
   };
+  int gate_at = p.gate != nullptr ? row0 / p.gate_rows : 0;
+  int64_t gate_end = p.gate != nullptr ? (static_cast<int64_t>(gate_at) + 1) * p.gate_rows : p.rows;
+  // scale gate post of the present gate
+  auto factors = [&](int unit) {
+    Pairs q;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) in[v] = Inputs<B, H>{};
-  float s_post[NV][8], s_pre[NV][8], s_gate[NV][8];
+    for (int i = 0; i < 4; ++i) q.v[i] = pack_f32x2(p.scale, p.scale);
+    if (p.gate != nullptr) {
+      const Pairs g = load8_2(p.gate + static_cast<int64_t>(gate_at) * p.width + unit * 8);
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
+      for (int i = 0; i < 4; ++i) q.v[i] = mul2(q.v[i], g.v[i]);
+    }
+    if (post) {
+      const Pairs g = load8_2(p.post + unit * 8);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s_post[v][i] = s_pre[v][i] = s_gate[v][i] = 0.f;
+      for (int i = 0; i < 4; ++i) q.v[i] = mul2(q.v[i], g.v[i]);
+    }
+    return q;
+  };
+  // sums over rows: du m; d n of the present gate; gate d n (times scale when they leave)
+  Pairs s_pre[NV], s_gate[NV], s_post[NV], q_kept[NV], pre_kept[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int unit = threadIdx.x + v * NT;
+    s_pre[v] = s_gate[v] = s_post[v] = q_kept[v] = pre_kept[v] = Pairs{};
+    if (kKeep && unit < units) {
+      q_kept[v] = factors(unit);
+      if (pre) pre_kept[v] = load8_2(p.pre + unit * 8);
+    }
+  }
   const int64_t plane = static_cast<int64_t>(p.grid) * p.width;
   float* mine = p.part + static_cast<int64_t>(blockIdx.x) * p.width;
-  int gate_at = p.gate != nullptr ? row0 / p.gate_rows : 0;
-  // dgate's sum of the present gate leaves: with the gain where it is complete (the only gate's is
-  // left to join_sums, which makes dpost of it too)
+  // The present gate's sum leaves: into dpost's, and with the gain to dgate where it is complete (the
+  // only gate's is left to join_sums, which makes dpost of it too).
   auto leave = [&]() {
-    const int64_t first = static_cast<int64_t>(gate_at) * p.gate_rows;
-    const int64_t end = first + p.gate_rows;
-    const bool whole = !p.one_gate && first >= row0 && (end < p.rows ? end : p.rows) <= row1;
+    const int64_t first = gate_end - p.gate_rows;
+    const bool whole = !p.one_gate && first >= row0 && (gate_end < p.rows ? gate_end : p.rows) <= row1;
     float* to = whole ? p.d_gate + static_cast<int64_t>(gate_at) * p.width
                       : mine + (first < row0 ? 2 : 3) * plane;
-    if (whole && p.d_gate == nullptr) return;
+    if (whole && p.d_gate == nullptr) to = nullptr;
+    const uint64_t scale2 = pack_f32x2(p.scale, p.scale);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int unit = threadIdx.x + v * NT;
       if (unit >= units) continue;
-      if (whole && p.post != nullptr) {
-        float g[8];
-        load8(p.post + unit * 8, g);
+      const Pairs g = load8_2(p.gate + static_cast<int64_t>(gate_at) * p.width + unit * 8);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s_gate[v][i] *= g[i];
+      for (int i = 0; i < 4; ++i) {
+        s_gate[v].v[i] = mul2(s_gate[v].v[i], scale2);
+        s_post[v].v[i] = fma2(s_gate[v].v[i], g.v[i], s_post[v].v[i]);
       }
-      store8(to + unit * 8, s_gate[v]);
+      if (whole && post) {
+        const Pairs gain = load8_2(p.post + unit * 8);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s_gate[v][i] = 0.f;
+        for (int i = 0; i < 4; ++i) s_gate[v].v[i] = mul2(s_gate[v].v[i], gain.v[i]);
+      }
+      if (to != nullptr) store8(to + unit * 8, s_gate[v]);
+      s_gate[v] = Pairs{};
     }
   };
   if (row0 < row1) fetch(row0);
+#pragma unroll 1
   for (int row = row0; row < row1; ++row) {
-    if (p.gate != nullptr && row / p.gate_rows != gate_at) {
+    if (row >= gate_end) {
       leave();
       gate_at = row / p.gate_rows;
+      gate_end = (static_cast<int64_t>(gate_at) + 1) * p.gate_rows;
+      if (kKeep && threadIdx.x < units) q_kept[0] = factors(threadIdx.x);
     }
-    // into floats, and the next row's inputs on their way
-    float n[NV][8], d[NV][8], m[NV][8], q[NV][8];
+    // into pairs, and the next row's inputs on their way
+    Pairs n[NV], d[NV], m[NV];
     const float r_post = next_post, r_pre = next_pre;
-    float3 sum = make_float3(0.f, 0.f, 0.f);
+    const uint64_t rpost2 = pack_f32x2(r_post, r_post), rpre2 = pack_f32x2(r_pre, r_pre);
+    uint64_t sum_gm = 0, sum_dq = 0, sum_mq = 0;
+    Pairs du[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const Inputs<B, H>& x = in[v];
-      const int unit = threadIdx.x + v * NT;
-      const bool here = unit < units;
-      if (p.b_exps != nullptr)
-        kept_values(make_uint2(x.b.a.x, x.b.a.y), x.b_byte, n[v]);
-      else
-        widen(x.b, n[v]);
-      widen(x.dy, d[v]);
-      float post[8], g[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        n[v][i] *= r_post;
-        q[v][i] = p.scale;
-        post[i] = 1.f;
+      n[v] = p.b_exps != nullptr ? kept_values2(make_uint2(x.b.a.x, x.b.a.y), x.b_byte) : widen2(x.b);
+      d[v] = widen2(x.dy);
+      if (pre) {
+        m[v] = p.h_exps != nullptr ? kept_values2(make_uint2(x.h.a.x, x.h.a.y), x.h_byte) : widen2(x.h);
+        du[v] = widen2(x.du);
+      } else {
+        m[v] = du[v] = Pairs{};
       }
-      if (p.gate != nullptr && here) {
-        load8(p.gate + static_cast<int64_t>(gate_at) * p.width + unit * 8, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[v][i] *= g[i];
-      }
-      if (p.post != nullptr && here) load8(p.post + unit * 8, post);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[v][i] *= post[i];  // e = q d
-      if (p.pre != nullptr) {
-        float du[8], pre[8];
-        if (p.h_exps != nullptr)
-          kept_values(make_uint2(x.h.a.x, x.h.a.y), x.h_byte, m[v]);
-        else
-          widen(x.h, m[v]);
-        widen(x.du, du);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pre[i] = 0.f;
-        if (here) load8(p.pre + unit * 8, pre);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          m[v][i] = fmaf(q[v][i], n[v][i], m[v][i]) * r_pre;  // y r_pre
-          s_pre[v][i] = fmaf(du[i], m[v][i], s_pre[v][i]);
-          g[i] = du[i] * pre[i];
-          sum.x = fmaf(g[i], m[v][i], sum.x);
-          d[v][i] = fmaf(r_pre, g[i], d[v][i]);
-          sum.z = fmaf(m[v][i], q[v][i] * n[v][i], sum.z);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum.y = fmaf(d[v][i], q[v][i] * n[v][i], sum.y);
     }
     if (row + 1 < row1) fetch(row + 1);
-    sum.x = warp_sum(sum.x);
-    sum.y = warp_sum(sum.y);
-    sum.z = warp_sum(sum.z);
-    if constexpr (NW > 1) {
-      float4* to = part[row & 1];
-      if ((threadIdx.x & 31) == 0) to[threadIdx.x >> 5] = make_float4(sum.x, sum.y, sum.z, 0.f);
-      __syncthreads();
-      sum = make_float3(0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        const float4 x = to[i];
-        sum.x += x.x;
-        sum.y += x.y;
-        sum.z += x.z;
-      }
-    }
-    const float mean_gm = r_pre * sum.x * inv_width;  // r_pre mean(g m)
-    const float mean_en = p.post != nullptr ? (sum.y - mean_gm * sum.z) * inv_width : 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int unit = threadIdx.x + v * NT;
       if (unit >= units) continue;
-      if (p.pre != nullptr) {
+      const Pairs q = kKeep ? q_kept[v] : factors(unit);
+      Pairs qn;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[v][i] = fmaf(-mean_gm, m[v][i], d[v][i]);
+      for (int i = 0; i < 4; ++i) {
+        n[v].v[i] = mul2(n[v].v[i], rpost2);
+        qn.v[i] = mul2(q.v[i], n[v].v[i]);
+      }
+      if (pre) {
+        const Pairs gain = kKeep ? pre_kept[v] : load8_2(p.pre + unit * 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          m[v].v[i] = mul2(add2(m[v].v[i], qn.v[i]), rpre2);  // y r_pre
+          s_pre[v].v[i] = fma2(du[v].v[i], m[v].v[i], s_pre[v].v[i]);
+          const uint64_t g = mul2(du[v].v[i], gain.v[i]);
+          sum_gm = fma2(g, m[v].v[i], sum_gm);
+          d[v].v[i] = fma2(rpre2, g, d[v].v[i]);
+          sum_mq = fma2(m[v].v[i], qn.v[i], sum_mq);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum_dq = fma2(d[v].v[i], qn.v[i], sum_dq);
+    }
+    const float2 a = halves_of(sum_gm), b = halves_of(sum_dq), c = halves_of(sum_mq);
+    float3 sum = make_float3(warp_sum(a.x + a.y), warp_sum(b.x + b.y), warp_sum(c.x + c.y));
+    if constexpr (NW > 1) {
+      float4* to = part[row & 1];
+      if (lane == 0) to[threadIdx.x >> 5] = make_float4(sum.x, sum.y, sum.z, 0.f);
+      __syncthreads();
+      if constexpr (NW <= 4) {
+        sum = make_float3(0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+          const float4 x = to[i];
+          sum.x += x.x;
+          sum.y += x.y;
+          sum.z += x.z;
+        }
+      } else {
+        const float4 x = to[lane % NW];
+        sum = make_float3(x.x, x.y, x.z);
+#pragma unroll
+        for (int i = NW / 2; i; i >>= 1) {
+          sum.x += __shfl_xor_sync(0xffffffffu, sum.x, i);
+          sum.y += __shfl_xor_sync(0xffffffffu, sum.y, i);
+          sum.z += __shfl_xor_sync(0xffffffffu, sum.z, i);
+        }
+      }
+    }
+    const float mean_gm = r_pre * sum.x * inv_width;  // r_pre mean(g m)
+    const float mean_en = post ? (sum.y - mean_gm * sum.z) * inv_width : 0.f;
+    const float en = -r_post * mean_en;
+    const uint64_t gm2 = pack_f32x2(-mean_gm, -mean_gm), en2 = pack_f32x2(en, en);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int unit = threadIdx.x + v * NT;
+      if (unit >= units) continue;
+      const Pairs q = kKeep ? q_kept[v] : factors(unit);
+      Pairs db;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (pre) d[v].v[i] = fma2(gm2, m[v].v[i], d[v].v[i]);
+        s_gate[v].v[i] = fma2(d[v].v[i], n[v].v[i], s_gate[v].v[i]);
+        db.v[i] = fma2(mul2(q.v[i], d[v].v[i]), rpost2, mul2(en2, n[v].v[i]));
       }
       if (p.dh != nullptr) store8(static_cast<H*>(p.dh) + row * p.dh_stride + unit * 8, d[v]);
-      float db[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float wn = p.scale * d[v][i] * n[v][i];
-        s_gate[v][i] += wn;
-        db[i] = r_post * fmaf(-mean_en, n[v][i], q[v][i] * d[v][i]);
-      }
-      if (p.post != nullptr && !p.one_gate) {
-        float g[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = 1.f;
-        if (p.gate != nullptr) load8(p.gate + static_cast<int64_t>(gate_at) * p.width + unit * 8, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          s_post[v][i] = fmaf(p.scale * d[v][i] * n[v][i], g[i], s_post[v][i]);
-      }
       if (p.db != nullptr) store8(static_cast<B*>(p.db) + row * p.db_stride + unit * 8, db);
     }
   }
@@ -406,69 +435,78 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
   for (int v = 0; v < NV; ++v) {
     const int unit = threadIdx.x + v * NT;
     if (unit >= units) continue;
-    if (p.post != nullptr && !p.one_gate) store8(mine + unit * 8, s_post[v]);
-    if (p.pre != nullptr) store8(mine + plane + unit * 8, s_pre[v]);
+    if (p.gate == nullptr) {  // no gate: dpost is the sum itself
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_post[v].v[i] = mul2(s_gate[v].v[i], pack_f32x2(p.scale, p.scale));
+    }
+    if (post && !p.one_gate) store8(mine + unit * 8, s_post[v]);
+    if (pre) store8(mine + plane + unit * 8, s_pre[v]);
   }
 }
 
-// The blocks' partial rows added up in their order. Grid: (32 columns, what): 0 dpost, 1 dpre, then
-// the gates that several blocks share, by the border between blocks c and c + 1 that is their first.
-constexpr int kSumThreads = 512, kSumSlices = kSumThreads / 32;
+// The blocks' partial rows added up in their order, 32 columns a block and an item for blockIdx.y:
+// dpost, dpre, then the gates that several blocks share: each of them in turn where there are fewer gates
+// than blocks, else (a gate then spans two or three blocks) 32 of the borders between blocks, a warp each.
+constexpr int kSumThreads = 1024, kSumSlices = kSumThreads / 32;
 __global__ void __launch_bounds__(kSumThreads) join_sums_kernel(const __grid_constant__ JoinBwd p) {
-  __shared__ float part[kSumSlices][32];
+  __shared__ float part[kSumSlices][33];
   grid_dep_wait();
   grid_dep_launch();
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
   const int col = blockIdx.x * 32 + lane;
+  const bool there = col < p.width;
   const int64_t plane = static_cast<int64_t>(p.grid) * p.width;
-  // rows [c0, c1) of a plane; row c0 is another plane's where it is said to be
-  auto total = [&](int which, int c0, int c1, int first_which) {
-    float sum = 0.f;
-    const int n = c1 - c0;
-    const int a = c0 + n * slice / kSumSlices, e = c0 + n * (slice + 1) / kSumSlices;
-    if (col < p.width) {
-#pragma unroll 8
-      for (int c = a; c < e; ++c)
-        sum += p.part[(c == c0 ? first_which : which) * plane + static_cast<int64_t>(c) * p.width + col];
-    }
-    __syncthreads();
-    part[slice][lane] = sum;
-    __syncthreads();
-    sum = 0.f;
-    if (slice == 0) {
-#pragma unroll
-      for (int i = 0; i < kSumSlices; ++i) sum += part[i][lane];
-    }
-    return sum;
-  };
-  const bool out = slice == 0 && col < p.width;
-  if (blockIdx.y == 0) {
-    if (p.post == nullptr || p.one_gate || p.d_post == nullptr) return;
-    const float sum = total(0, 0, p.grid, 0);
-    if (out) p.d_post[col] = sum;
-  } else if (blockIdx.y == 1) {
-    if (p.pre == nullptr || p.d_pre == nullptr) return;
-    const float sum = total(1, 0, p.grid, 1);
-    if (out) p.d_pre[col] = sum;
-  } else if (p.one_gate) {
-    // the only gate: began in block 0
-    const float sum = total(2, 0, p.grid, 3);
-    if (!out) return;
-    if (p.d_gate != nullptr) p.d_gate[col] = p.post != nullptr ? sum * p.post[col] : sum;
-    if (p.post != nullptr && p.d_post != nullptr) p.d_post[col] = sum * p.gate[col];
+  const float* from = p.part + col;
+  const int item = static_cast<int>(blockIdx.y) - 2;
+  const int gates = p.gate == nullptr ? 0 : (p.rows + p.gate_rows - 1) / p.gate_rows;
+  const float gain = there && p.post != nullptr ? p.post[col] : 1.f;
+  if (item >= 0 && gates > p.grid) {
+    // the gate across the border between blocks c and c + 1, if it begins in block c
+    const int c = item * kSumSlices + slice;
+    if (c + 1 >= p.grid || !there || p.d_gate == nullptr) return;
+    const int row = first_row(p.rows, p.grid, c + 1);
+    const int at = row / p.gate_rows, begin = at * p.gate_rows;
+    if (begin == row || block_of(p.rows, p.grid, begin) != c) return;
+    const int64_t end = static_cast<int64_t>(begin) + p.gate_rows;
+    const int last = block_of(p.rows, p.grid, static_cast<int>(end < p.rows ? end : p.rows) - 1);
+    float sum = from[3 * plane + static_cast<int64_t>(c) * p.width];
+    for (int i = c + 1; i <= last; ++i) sum += from[2 * plane + static_cast<int64_t>(i) * p.width];
+    p.d_gate[static_cast<int64_t>(at) * p.width + col] = sum * gain;
+    return;
+  }
+  // blocks [c0, c1) of a plane, but block c0 of another where it is a gate's first
+  int which = 0, first = 0, c0 = 0, c1 = p.grid;
+  float* to = p.d_post;
+  if (item < 0) {
+    which = first = blockIdx.y;
+    if (item == -1) to = p.d_pre;
+    if (to == nullptr || (item == -2 && p.one_gate)) return;
   } else {
-    if (p.d_gate == nullptr) return;
-    for (int border = blockIdx.y - 2; border + 1 < p.grid; border += gridDim.y - 2) {
-      const int row = first_row(p.rows, p.grid, border + 1);
-      const int at = row / p.gate_rows, begin = at * p.gate_rows;
-      if (begin == row || block_of(p.rows, p.grid, begin) != border) continue;
-      const int64_t end = static_cast<int64_t>(begin) + p.gate_rows;
-      const int last = static_cast<int>(end < p.rows ? end : p.rows) - 1;
-      const float sum = total(2, border, block_of(p.rows, p.grid, last) + 1, 3);
-      if (out)
-        p.d_gate[static_cast<int64_t>(at) * p.width + col] =
-            p.post != nullptr ? sum * p.post[col] : sum;
-    }
+    const int64_t begin = static_cast<int64_t>(item) * p.gate_rows, end = begin + p.gate_rows;
+    c0 = block_of(p.rows, p.grid, static_cast<int>(begin));
+    c1 = block_of(p.rows, p.grid, static_cast<int>(end < p.rows ? end : p.rows) - 1) + 1;
+    to = p.d_gate == nullptr ? nullptr : p.d_gate + begin / p.gate_rows * p.width;
+    which = 2;
+    first = 3;
+    if (!p.one_gate && (c1 == c0 + 1 || to == nullptr)) return;
+  }
+  float sum = 0.f;
+  if (there) {
+#pragma unroll 8
+    for (int c = c0 + slice; c < c1; c += kSumSlices)
+      sum += __ldcg(from + (c == c0 ? first : which) * plane + static_cast<int64_t>(c) * p.width);
+  }
+  part[slice][lane] = sum;
+  __syncthreads();
+  // a warp of 32 slices for every column
+  sum = warp_sum(part[lane][slice]);
+  if (lane == 0 && blockIdx.x * 32 + slice < p.width) {
+    const int64_t at = blockIdx.x * 32 + slice;
+    const float g = item >= 0 && p.post != nullptr ? p.post[at] : 1.f;
+    if (to != nullptr) to[at] = sum * g;
+    // one gate: dpost is the gate times the sum without the gain
+    if (item >= 0 && p.one_gate && p.post != nullptr && p.d_post != nullptr)
+      p.d_post[at] = sum * p.gate[at];
   }
 }
 
@@ -489,17 +527,19 @@ template <typename B, typename H>
 cudaError_t launch_join_bwd(const JoinBwd& p, cudaStream_t s) {
   const int t = bwd_threads(p.width);
   auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(p.grid), dim3(t), 0, s, p); };
-  cudaError_t e = p.width > 4096 ? go(join_bwd_kernel<B, H, 512, 2>)
-                  : t == 32      ? go(join_bwd_kernel<B, H, 32, 1>)
-                  : t == 64      ? go(join_bwd_kernel<B, H, 64, 1>)
-                  : t == 128     ? go(join_bwd_kernel<B, H, 128, 1>)
-                  : t == 256     ? go(join_bwd_kernel<B, H, 256, 1>)
-                                 : go(join_bwd_kernel<B, H, 512, 1>);
+  const cudaError_t e = p.width > 4096 ? go(join_bwd_kernel<B, H, 512, 2>)
+                        : t == 32      ? go(join_bwd_kernel<B, H, 32, 1>)
+                        : t == 64      ? go(join_bwd_kernel<B, H, 64, 1>)
+                        : t == 128     ? go(join_bwd_kernel<B, H, 128, 1>)
+                        : t == 256     ? go(join_bwd_kernel<B, H, 256, 1>)
+                                       : go(join_bwd_kernel<B, H, 512, 1>);
   if (e != cudaSuccess) return e;
-  // (one gate's sum is one item; of several gates at most one begins before every border)
-  const int gates = p.gate == nullptr ? 0 : p.one_gate ? 1 : std::min(p.grid - 1, 64);
-  if (p.post == nullptr && p.pre == nullptr && gates == 0) return cudaSuccess;
-  return launch_pdl(join_sums_kernel, dim3((p.width + 31) / 32, 2 + gates), dim3(kSumThreads), 0, s, p);
+  const int64_t gates =
+      p.gate == nullptr ? 0 : (static_cast<int64_t>(p.rows) + p.gate_rows - 1) / p.gate_rows;
+  const int items = static_cast<int>(
+      gates <= p.grid ? gates : (p.grid - 1 + kSumSlices - 1) / kSumSlices);
+  if (p.post == nullptr && p.pre == nullptr && items == 0) return cudaSuccess;
+  return launch_pdl(join_sums_kernel, dim3((p.width + 31) / 32, 2 + items), dim3(kSumThreads), 0, s, p);
 }
 
 bool ok_ptr(const void* p, uintptr_t align) {

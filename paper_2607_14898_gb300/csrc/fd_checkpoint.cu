@@ -101,17 +101,20 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// Transposed: x[column][row]. A block turns kTileRows rows by kTileCols columns over in shared
-// memory: codes are read by whole sectors of a row, and every column's values leave as 16-byte
-// stores from the first aligned address on, wherever the column starts (rows may be odd).
-constexpr int kTileRows = 128, kTileCols = 128;
+// Transposed: x[column][row]. A block turns 256 rows by 64 columns over in shared memory: codes are
+// read by whole sectors of a row, and a column's values leave as aligned 16-byte stores. Columns begin
+// at any address (rows may be odd), so a vector may reach over the tile's end: it is the tile's that has
+// its first element, which has the next rows too for that. Only a column's own two ends are stored by
+// elements. (Tiles of 128 x 128 that stored their ends by elements took 74 us for 16001 x 4096.)
+constexpr int kTileRows = 256, kTileCols = 64;
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
     load_transposed_kernel(int rows, int width, const int8_t* codes, const uint8_t* exps, T* x,
                            int64_t stride) {
   constexpr int kVec = 16 / sizeof(T);
-  constexpr int kPitch = kTileRows + 4 / sizeof(T);  // an odd number of 32-bit words
+  constexpr int kAll = kTileRows + 8;             // with the next tile's first rows
+  constexpr int kPitch = kAll + 4 / sizeof(T);    // an odd number of 32-bit words
   extern __shared__ __align__(16) uint8_t smem[];
   T* tile = reinterpret_cast<T*>(smem);  // [column][row]
   grid_dep_wait();
@@ -122,25 +125,27 @@ __global__ void __launch_bounds__(kThreads)
   // lanes: 4 groups of eight columns (a sector) by 8 rows
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r_in = lane >> 2, u_in = lane & 3;
-  constexpr int kSteps = kTileRows * (kTileCols / 8) / kThreads;  // 8
+  constexpr int kRuns = kAll / 8 * (kTileCols / 32);  // 33 runs of 8 rows by 2 of 32 columns
+  constexpr int kSteps = (kRuns + kThreads / 32 - 1) / (kThreads / 32);
   uint2 raw[kSteps];
   uint32_t byte[kSteps];
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {
-    const int step = j * (kThreads / 32) + warp;  // 16 runs of 8 rows by 4 runs of 32 columns
-    const int64_t row = row0 + (step >> 2) * 8 + r_in;
-    const int col = col0 + (step & 3) * 32 + u_in * 8;
+    const int step = j * (kThreads / 32) + warp;
+    const int64_t row = row0 + (step >> 1) * 8 + r_in;
+    const int col = col0 + (step & 1) * 32 + u_in * 8;
     raw[j] = make_uint2(0u, 0u);
     byte[j] = 1u;
-    if (row < rows && col < width) {
-      raw[j] = *reinterpret_cast<const uint2*>(codes + row * width + col);
-      byte[j] = exps[row * blocks + col / kKeptBlock];
+    if (step < kRuns && row < rows && col < width) {
+      raw[j] = __ldg(reinterpret_cast<const uint2*>(codes + row * width + col));
+      byte[j] = __ldg(exps + row * blocks + col / kKeptBlock);
     }
   }
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {
     const int step = j * (kThreads / 32) + warp;
-    const int r = (step >> 2) * 8 + r_in, c = (step & 3) * 32 + u_in * 8;
+    if (step >= kRuns) break;
+    const int r = (step >> 1) * 8 + r_in, c = (step & 1) * 32 + u_in * 8;
     float v[8];
     kept_values(raw[j], byte[j], v);
     into_range<T>(v);
@@ -148,16 +153,24 @@ __global__ void __launch_bounds__(kThreads)
     for (int i = 0; i < 8; ++i) tile[(c + i) * kPitch + r] = T(v[i]);
   }
   __syncthreads();
-  const int count = static_cast<int>(min(static_cast<int64_t>(kTileRows), rows - row0));
+  // elements there are from row0 on, with those of the next tile that a vector may need
+  const int count = static_cast<int>(min(static_cast<int64_t>(kAll), rows - row0));
+  const int mine = min(kTileRows, count);
+  const bool starts = blockIdx.x == 0;
   const int cols = min(kTileCols, width - col0);
-  constexpr int kChunks = kTileRows / kVec + 1;
+  constexpr int kChunks = kTileRows / kVec;
+  // lanes are neighbouring vectors of a column
   for (int it = threadIdx.x; it < cols * kChunks; it += kThreads) {
-    const int c = it / kChunks, chunk = it - c * kChunks;
+    const int c = it / kChunks, chunk = it % kChunks;
     T* column = x + static_cast<int64_t>(col0 + c) * stride + row0;
-    const int off = static_cast<int>((reinterpret_cast<uintptr_t>(column) / sizeof(T)) % kVec);
-    const int first = chunk * kVec - off;  // element of the tile's column
+    const int lead =  // elements up to the first aligned address
+        static_cast<int>((0 - reinterpret_cast<uintptr_t>(column) / sizeof(T)) % kVec);
+    const int first = lead + chunk * kVec;
     const T* from = tile + c * kPitch;
-    if (first >= 0 && first + kVec <= count) {
+    if (starts && chunk == 0)
+      for (int e = 0; e < min(lead, count); ++e) column[e] = from[e];
+    if (first >= mine) continue;
+    if (first + kVec <= count) {
       uint4 v;
       if constexpr (sizeof(T) == 2) {
         const uint32_t* w = reinterpret_cast<const uint32_t*>(from) + (first >> 1);
@@ -174,8 +187,8 @@ __global__ void __launch_bounds__(kThreads)
         v = make_uint4(w[0], w[1], w[2], w[3]);
       }
       *reinterpret_cast<uint4*>(column + first) = v;
-    } else {
-      for (int e = max(0, first); e < min(count, first + kVec); ++e) column[e] = from[e];
+    } else {  // the column's end
+      for (int e = first; e < count; ++e) column[e] = from[e];
     }
   }
 }
@@ -196,7 +209,7 @@ cudaError_t load_type(bool transposed, int rows, int width, const int8_t* codes,
     return launch_pdl(load_kernel<T>, grid_of(p), dim3(kThreads), 0, s, p, codes, exps,
                       static_cast<T*>(x), stride);
   }
-  constexpr size_t kSmem = kTileCols * (kTileRows + 4 / sizeof(T)) * sizeof(T);
+  constexpr size_t kSmem = kTileCols * (kTileRows + 8 + 4 / sizeof(T)) * sizeof(T);
   static OncePerDevice once;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -69,6 +69,38 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   }
 }
 
+// as four pairs
+struct Pairs {
+  uint64_t v[4];
+};
+__device__ __forceinline__ Pairs pairs_of(const float (&x)[8]) {
+  Pairs r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = pack_f32x2(x[2 * i], x[2 * i + 1]);
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ Pairs widen2(const Raw8<T>& r) {
+  float x[8];
+  widen(r, x);
+  return pairs_of(x);
+}
+template <typename T>
+__device__ __forceinline__ Pairs load8_2(const T* p) {
+  return widen2(load_raw(p));
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const Pairs& x) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 h = halves_of(x.v[i]);
+    f[2 * i] = h.x;
+    f[2 * i + 1] = h.y;
+  }
+  store8(p, f);
+}
+
 // ---- the 8-bit form: blocks of 32 neighbours of a row share a power of two, 2^E; E the smallest
 // (-126 at least) that lets the largest magnitude fit into 127 steps, stored as E + 127, 255 for a
 // block that holds an infinity or a NaN. The step being a power of two, codes are the same in
@@ -83,16 +115,19 @@ __device__ __forceinline__ uint32_t kept_exponent(uint32_t top_bits) {
   const int byte = static_cast<int>(e) - 6 + ((top_bits & 0x7fffffu) > 0x7e0000u);
   return static_cast<uint32_t>(byte < 1 ? 1 : byte);
 }
-// the codes of eight elements of the block, low byte first
+// The codes of eight elements of the block, low byte first. x 2^-E + 1.5 2^23 is rounded to a whole
+// number by the addition itself, ties to even, and its low byte is the code: no conversions, which
+// run at a quarter of the additions' rate.
 __device__ __forceinline__ uint2 kept_codes(const float (&x)[8], uint32_t byte) {
   if (byte == 255u) return make_uint2(0u, 0u);
   const float per_step = __uint_as_float((254u - byte) << 23);  // 2^-E
-  int c[8];
+  uint32_t c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    c[i] = __float2int_rn(x[i] * per_step);
+    float v = x[i];
     // 64 steps of 2^122 are 2^128: the largest floats stay finite
-    if (byte >= 249u) c[i] = min(63, max(-63, c[i]));
+    if (byte >= 249u) v = fminf(fmaxf(v, -63.f * 0x1p122f), 63.f * 0x1p122f);
+    c[i] = __float_as_uint(fmaf(v, per_step, 12582912.f));
   }
   auto four = [&](int i) {
     return __byte_perm(__byte_perm(c[i], c[i + 1], 0x0040), __byte_perm(c[i + 2], c[i + 3], 0x0040),
@@ -100,14 +135,27 @@ __device__ __forceinline__ uint2 kept_codes(const float (&x)[8], uint32_t byte) 
   };
   return make_uint2(four(0), four(4));
 }
-// what eight codes stand for (a byte of 255 makes the step infinite and the block NaN: 0 times it)
+// What eight codes stand for: code + 128 goes into the last bits of 2^23, which is taken off again. (A
+// byte of 255 makes the step infinite and the block NaN: 0 times it.)
 __device__ __forceinline__ void kept_values(uint2 codes, uint32_t byte, float (&x)[8]) {
   const float step = __uint_as_float(byte << 23);
+  const uint32_t w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = static_cast<float>(static_cast<int8_t>(codes.x >> (8 * i))) * step;
-    x[4 + i] = static_cast<float>(static_cast<int8_t>(codes.y >> (8 * i))) * step;
-  }
+  for (int i = 0; i < 8; ++i)
+    x[i] = (__uint_as_float(__byte_perm(w[i / 4], 0x4b000000u, 0x7650 + i % 4)) - 8388736.f) * step;
+}
+__device__ __forceinline__ Pairs kept_values2(uint2 codes, uint32_t byte) {
+  const float step = __uint_as_float(byte << 23);
+  const uint64_t step2 = pack_f32x2(step, step), base2 = pack_f32x2(-8388736.f, -8388736.f);
+  const uint32_t w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
+  Pairs r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r.v[i] = mul2(add2(pair_of(__byte_perm(w[i / 2], 0x4b000000u, 0x7650 + 2 * (i % 2)),
+                               __byte_perm(w[i / 2], 0x4b000000u, 0x7651 + 2 * (i % 2))),
+                       base2),
+                  step2);
+  return r;
 }
 // the largest magnitude's bits over the four neighbouring lanes that hold a block (NaN above all)
 __device__ __forceinline__ uint32_t block_top(const float (&x)[8]) {

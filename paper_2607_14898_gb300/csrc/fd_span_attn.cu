@@ -573,11 +573,12 @@ __global__ void __launch_bounds__(256) span_join_kernel(const __grid_constant__ 
         l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Parts of every tile's key blocks: as many as fill the GPU where there are few tiles.
+// Parts of every tile's key blocks: as many as fill the GPU where there are few tiles, but 512 keys (2 us)
+// each at least, since joining the parts takes 3 us.
 int fwd_parts(const SpanShape& y) {
   const int64_t units = static_cast<int64_t>(y.groups) * y.row_tiles;
   return static_cast<int>(
-      std::max<int64_t>(1, std::min<int64_t>((y.key_blocks + 1) / 2, num_sms() / units)));
+      std::max<int64_t>(1, std::min<int64_t>(y.key_blocks / 4, num_sms() / units)));
 }
 
 template <bool F16, int D>

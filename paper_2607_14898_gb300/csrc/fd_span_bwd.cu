@@ -548,13 +548,17 @@ template <int D>
 struct QueryCfg {
   static constexpr int kThreads = 20 * 32;
   static constexpr int kTileBytes = kTile * D * 2;
-  static constexpr int kStages = D == 64 ? 5 : 2;
+  // V is through with when Y is, K when dq is: a ring each. (With one slot of both each, two of them for
+  // D = 128, the loads were what a step waited for: 650 us for 8191 causal tokens of 32 heads.)
+  static constexpr int kSlotsK = D == 64 ? 6 : 3, kSlotsV = D == 64 ? 5 : 2;
   static constexpr int kOffDo = kTileBytes;
-  static constexpr int kOffRing = 2 * kTileBytes;  // K, V of each stage
-  static constexpr int kOffBar = kOffRing + kStages * 2 * kTileBytes;
-  static constexpr int kQ = 0, kFull = 1, kFree = kFull + kStages, kXFull = kFree + kStages,
-                       kYFull = kXFull + 1, kXRead = kYFull + 1, kYRead = kXRead + 1,
-                       kDsFull = kYRead + 1, kDsDone = kDsFull + 1, kBars = kDsDone + 1;
+  static constexpr int kOffK = 2 * kTileBytes;
+  static constexpr int kOffV = kOffK + kSlotsK * kTileBytes;
+  static constexpr int kOffBar = kOffV + kSlotsV * kTileBytes;
+  static constexpr int kQ = 0, kKFull = 1, kKFree = kKFull + kSlotsK, kVFull = kKFree + kSlotsK,
+                       kVFree = kVFull + kSlotsV, kXFull = kVFree + kSlotsV, kYFull = kXFull + 1,
+                       kXRead = kYFull + 1, kYRead = kXRead + 1, kDsFull = kYRead + 1,
+                       kDsDone = kDsFull + 1, kBars = kDsDone + 1;
   static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
   static constexpr uint32_t kColX = 0, kColY = 128, kColDs = 256, kColDq = 384;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -588,9 +592,13 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
   if (threadIdx.x == 0) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
     mbar_init(bar(C::kQ), 1);
-    for (int i = 0; i < C::kStages; ++i) {
-      mbar_init(bar(C::kFull + i), 1);
-      mbar_init(bar(C::kFree + i), 1);
+    for (int i = 0; i < C::kSlotsK; ++i) {
+      mbar_init(bar(C::kKFull + i), 1);
+      mbar_init(bar(C::kKFree + i), 1);
+    }
+    for (int i = 0; i < C::kSlotsV; ++i) {
+      mbar_init(bar(C::kVFull + i), 1);
+      mbar_init(bar(C::kVFree + i), 1);
     }
     mbar_init(bar(C::kXFull), 1);
     mbar_init(bar(C::kYFull), 1);
@@ -631,23 +639,41 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
         tma_load_4d(base + d * kSub, &tmQ, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
         tma_load_4d(base + C::kOffDo + d * kSub, &tmDo, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
       }
-      int i = 0;
-      for (; i < count; ++i) {
-        const int st = i % C::kStages;
-        if (i >= C::kStages &&
-            !wait(bar(C::kFree + st), (i / C::kStages - 1) & 1, p.err, ERR_WAIT_MMA))
-          break;
-        const uint32_t b = bar(C::kFull + st), k = base + C::kOffRing + st * 2 * C::kTileBytes;
-        mbar_expect_tx(b, 2 * C::kTileBytes);
-        for (int d = 0; d < D / 64; ++d) {
-          tma_load_4d(k + d * kSub, &tmK, b, 64 * d, group, (block0 + i) * kTile, 0);
-          tma_load_4d(k + C::kTileBytes + d * kSub, &tmV, b, 64 * d, group, (block0 + i) * kTile, 0);
+      // the next K, or V, as soon as its slot is free
+      int k = 0, v = 0, idle = 0;
+      uint32_t idle_since = 0;
+      auto room = [&](int n, int slots, int free) {
+        return n < count &&
+               (n < slots || mbar_test_wait(bar(free + n % slots), (n / slots - 1) & 1));
+      };
+      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full) {
+        const uint32_t b = bar(full + n % slots);
+        mbar_expect_tx(b, C::kTileBytes);
+        for (int d = 0; d < D / 64; ++d)
+          tma_load_4d(to + n % slots * C::kTileBytes + d * kSub, map, b, 64 * d, group,
+                      (block0 + n) * kTile, 0);
+      };
+      while (k < count || v < count) {
+        bool moved = false;
+        if (room(k, C::kSlotsK, C::kKFree)) {
+          load(k++, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull);
+          moved = true;
         }
+        if (room(v, C::kSlotsV, C::kVFree)) {
+          load(v++, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull);
+          moved = true;
+        }
+        if (moved)
+          idle = 0;
+        else if (!poll_again(idle, idle_since, p.err, ERR_WAIT_MMA))
+          break;
       }
       // nothing may be in flight when the block exits
       wait(bar(C::kQ), 0, p.err, ERR_WAIT_TMA, true);
-      for (int j = max(0, i - C::kStages); j < i; ++j)
-        wait(bar(C::kFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, k - C::kSlotsK); j < k; ++j)
+        wait(bar(C::kKFull + j % C::kSlotsK), (j / C::kSlotsK) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, v - C::kSlotsV); j < v; ++j)
+        wait(bar(C::kVFull + j % C::kSlotsV), (j / C::kSlotsV) & 1, p.err, ERR_WAIT_TMA, true);
     }
   } else if (warp == 17 || warp == 18) {
     // ---- X = q k^T (17), Y = dout v^T (18)
@@ -664,9 +690,9 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
     }
     bool ok = wait_warp(bar(C::kQ), 0, p.err, ERR_WAIT_TMA);
     for (int i = 0; i < count && ok; ++i) {
-      const int st = i % C::kStages, key0 = (block0 + i) * kTile;
-      ok = wait_warp(bar(C::kFull + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
-      const int off = C::kOffRing + st * 2 * C::kTileBytes + (y ? C::kTileBytes : 0);
+      const int slots = y ? C::kSlotsV : C::kSlotsK, st = i % slots, key0 = (block0 + i) * kTile;
+      ok = wait_warp(bar((y ? C::kVFull : C::kKFull) + st), (i / slots) & 1, p.err, ERR_WAIT_TMA);
+      const int off = (y ? C::kOffV : C::kOffK) + st * C::kTileBytes;
       if (!y) {
         // zeros for K of keys that no query of the tile sees: their dS is 0, but 0 times NaN is NaN
         bool whole = false;
@@ -702,24 +728,25 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
         mma4_bf16_ss_w(col, a0 + static_cast<uint64_t>(d * (kSub >> 4)),
                        k0 + static_cast<uint64_t>(d * (kSub >> 4)), idesc, d > 0);
       mma_commit_w(bar(y ? C::kYFull : C::kXFull));
+      if (y) mma_commit_w(bar(C::kVFree + st));
     }
   } else if (warp == 19) {
     // ---- dq += dS k
     constexpr uint32_t idesc = Mma<F16, D>::idesc(D, true);
     bool ok = true;
     for (int i = 0; i < count && ok; ++i) {
-      const int st = i % C::kStages;
-      ok = wait_warp(bar(C::kFull + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA) &&
+      const int st = i % C::kSlotsK;
+      ok = wait_warp(bar(C::kKFull + st), (i / C::kSlotsK) & 1, p.err, ERR_WAIT_TMA) &&
            wait_warp(bar(C::kDsFull), i & 1, p.err, ERR_WAIT_EPI);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t k = base + C::kOffRing + st * 2 * C::kTileBytes;
+      const uint32_t k = base + C::kOffK + st * C::kTileBytes;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
         mma4_ts_mn_w(tmem + C::kColDq, tmem + C::kColDs + 32u * x, sdesc_mn_sw128(k + x * 64 * 128, kSub),
                      idesc, i > 0 || x > 0);
       mma_commit_w(bar(C::kDsDone));
-      mma_commit_w(bar(C::kFree + st));
+      mma_commit_w(bar(C::kKFree + st));
     }
   }
   if (warp < 16) {
@@ -878,9 +905,11 @@ __global__ void span_zeros_kernel(SpanRows r, int tokens, int heads, int head_di
   grid_dep_launch();
 }
 
-// Parts where there are few units: as many as fill the GPU.
-int parts_for(int64_t units, int most) {
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(most, num_sms() / units)));
+// Parts of a unit's walk over `steps` tiles: as many as give every SM `rounds` units to take, but four tiles
+// (4 us) each at least, since the sums of the parts take 3 us.
+int parts_for(int64_t units, int steps, int rounds) {
+  const int64_t want = (static_cast<int64_t>(rounds) * num_sms() + units - 1) / units;
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(steps / 4, want)));
 }
 
 struct BwdPlan {
@@ -889,8 +918,8 @@ struct BwdPlan {
 };
 BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   BwdPlan b{};
-  b.q_parts = parts_for(static_cast<int64_t>(y.groups) * y.row_tiles, y.key_blocks);
-  b.k_parts = parts_for(static_cast<int64_t>(y.groups) * y.key_blocks, y.row_tiles);
+  b.q_parts = parts_for(static_cast<int64_t>(y.groups) * y.row_tiles, y.key_blocks, 1);
+  b.k_parts = parts_for(static_cast<int64_t>(y.groups) * y.key_blocks, y.row_tiles, 4);
   const size_t tiles = static_cast<size_t>(y.groups) * y.row_tiles;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   b.stat = 0;

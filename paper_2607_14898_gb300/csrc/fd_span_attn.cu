@@ -332,6 +332,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kSRead + h));
       if (key0 < all_from || key0 + 64 > all_to) {
+        __syncwarp();  // (not predicated: else the selections are made for every block)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const uint32_t seen = seen_word(span, key0 + 32 * i);

@@ -23,8 +23,8 @@ struct SpanBwd {
   float scale, scale_log2;
   SpanRows out, dout, dq, dk, dv;
   const float* lse;
-  float* stat;    // [group][row tile][4][128]: -lse log2(e), -delta, the span's ends (int)
-  int4* limits;   // of each row tile: first and last key seen, the keys that all see; see below
+  float* stat;    // [group][row tile] records of kRecord: see below
+  int4* limits;   // of each row tile, those of its records
   float* most;    // [group][row tile]: the largest |dout| (fp16)
   float* part_q;  // [group][row tile][part][128][D]
   float* part_k;  // [group][key block][part][dk, dv][128][D]
@@ -35,6 +35,11 @@ struct SpanBwd {
 // largest |dout|, so that small gradients keep their digits. bf16 has fp32's range.
 constexpr float kPUp = 16384.f;
 constexpr float kPUpLog2 = 14.f;
+
+// What a row tile's record holds, 16 bytes in line: -lse log2(e), -delta and the ends of the span (int) of
+// each row, [4][128], then the tile's limits: {first key, end of the keys} that some query sees, {first, end}
+// of those that all queries see which see any; the third is negative (~) where some query sees none.
+constexpr int kRecord = 4 * kTile + 4;
 
 // ------------------------------------------------------------------------------ rows
 // D / 8 lanes a row. A row that sees nothing, or is none, gets P = 0 by an infinite lse.
@@ -47,7 +52,7 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
   const int tile = blockIdx.x, group = blockIdx.y;
   const int token0 = tile * p.y.tile_tokens;
   const int lane = threadIdx.x % kLanes;
-  float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * 4 * kTile;
+  float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord;
   float most = 0.f;
 #pragma unroll
   for (int row = threadIdx.x / kLanes; row < kTile; row += 256 / kLanes) {
@@ -96,9 +101,7 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
       p.most[group * p.y.row_tiles + tile] = most;
     }
   }
-  if (group == 0 && threadIdx.x < 32) {
-    // {first key, end of the keys} that some query sees, {first, end} of those that all queries see which see
-    // any; the third is negative (~) where some query sees none
+  if (threadIdx.x < 32) {
     int4 m = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
     bool none = false;
     for (int i = threadIdx.x; i < p.y.tile_tokens && token0 + i < p.y.n_q; i += 32) {
@@ -117,7 +120,10 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
     m.z = __reduce_max_sync(0xffffffffu, m.z);
     m.w = __reduce_min_sync(0xffffffffu, m.w);
     if (__any_sync(0xffffffffu, none)) m.z = ~m.z;
-    if (threadIdx.x == 0) p.limits[tile] = m;
+    if (threadIdx.x == 0) {
+      *reinterpret_cast<int4*>(stat + 4 * kTile) = m;
+      if (group == 0) p.limits[tile] = m;
+    }
   }
 }
 
@@ -146,7 +152,7 @@ struct KeyCfg {
   static constexpr int kCols = kStep / 4;           // of a thread
   static constexpr int kTileBytes = kTile * D * 2;
   static constexpr int kStages = D == 64 ? 4 : 2;
-  static constexpr int kStat = 4 * kTile * 4;
+  static constexpr int kStat = kRecord * 4;
   static constexpr int kOffV = kTileBytes;
   static constexpr int kOffRing = 2 * kTileBytes;  // q, dout of each stage
   static constexpr int kOffStat = kOffRing + kStages * 2 * kTileBytes;
@@ -307,7 +313,7 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
           tma_load_4d(q + C::kTileBytes + d * kSub, &tmDo, b, 64 * d, group * p.y.per, token, 0);
         }
         bulk_load(base + C::kOffStat + st * C::kStat,
-                  p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile0 + i) * 4 * kTile,
+                  p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile0 + i) * kRecord,
                   C::kStat, b);
       }
       // nothing may be in flight when the block exits
@@ -325,11 +331,11 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
     bool ok = wait_warp(bar(C::kKV), 0, p.err, ERR_WAIT_TMA);
     for (int i = 0; i < count && ok; ++i) {
       const int st = i % C::kStages;
-      const bool some_none = __ldcg(&p.limits[tile0 + i].z) < 0;
       ok = wait_warp(bar(C::kFull + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
       if (!ok) break;
       const int off = C::kOffRing + st * 2 * C::kTileBytes + (y ? C::kTileBytes : 0);
-      if (some_none) {
+      const int4 m = *reinterpret_cast<const int4*>(smem + C::kOffStat + st * C::kStat + 16 * kTile);
+      if (m.z < 0) {  // some query sees nothing
         const int* ends = reinterpret_cast<const int*>(smem + C::kOffStat + st * C::kStat) + 2 * kTile;
 #pragma unroll 1
         for (int r = lane; r < p.y.tile_rows; r += 32) {
@@ -399,10 +405,8 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
     int k = 0;
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
-      const int4 m = __ldcg(p.limits + tile0 + i);
-      // (a tile between others may see nothing of the block, or nothing at all)
-      const bool masked = m.x > key0 || (m.z < 0 ? ~m.z : m.z) > key0 || m.w < key0 + kTile;
       const int st = i % C::kStages;
+      bool masked = false;
 #pragma unroll 1
       for (int s = 0; s < C::kSteps; ++s, ++k) {
         const uint8_t* stat = smem + C::kOffStat + st * C::kStat + (s * C::kStep + q * C::kCols) * 4;
@@ -410,8 +414,16 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
         tc_fence_after();
         uint32_t x[C::kCols];
         tmem_ld(x_col, x);
+        if (s == 0) {
+          // (a tile between others may see nothing of the block, or nothing at all)
+          const int4 m = *reinterpret_cast<const int4*>(smem + C::kOffStat + st * C::kStat + 16 * kTile);
+          masked = m.x > key0 || (m.z < 0 ? ~m.z : m.z) > key0 || m.w < key0 + kTile;
+        }
         uint32_t seen = 0xffffffffu;  // bit c: the key is seen by row c of the quarter
         if (masked) {
+          // (something that is not predicated, here and below: without it the selections were made for
+          // every tile)
+          __syncwarp();
           seen = 0;
 #pragma unroll
           for (int c = 0; c < C::kCols; c += 4) {
@@ -439,6 +451,7 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
           x[c + 3] = __float_as_uint(ex2_approx(b.y));
         }
         if (masked) {
+          __syncwarp();
 #pragma unroll
           for (int c = 0; c < C::kCols; ++c)
             if (!(seen & (1u << c))) x[c] = 0;
@@ -480,6 +493,7 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
           y[c + 3] = __float_as_uint(v.y);
         }
         if (masked) {
+          __syncwarp();
 #pragma unroll
           for (int c = 0; c < C::kCols; ++c)
             if (!(seen & (1u << c))) y[c] = 0;
@@ -754,7 +768,7 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
     const int q = warp >> 2, row = (warp & 3) * 32 + lane;
     const int token = token0 + row / p.y.per, head = group * p.y.per + row % p.y.per;
     const bool valid = row < p.y.tile_rows && token < p.y.n_q;
-    const float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * 4 * kTile + row;
+    const float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord + row;
     const float neg_lse = __ldcg(stat), neg_delta = __ldcg(stat + kTile);
     const int2 span = make_int2(__ldcg(reinterpret_cast<const int*>(stat) + 2 * kTile),
                                 __ldcg(reinterpret_cast<const int*>(stat) + 3 * kTile));
@@ -803,6 +817,7 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
         y[c + 1] = __float_as_uint(u.y);
       }
       if (masked) {
+        __syncwarp();  // (as above)
         const uint32_t seen = seen_word(span, key0);
 #pragma unroll
         for (int c = 0; c < 32; ++c)
@@ -923,7 +938,7 @@ BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   const size_t tiles = static_cast<size_t>(y.groups) * y.row_tiles;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   b.stat = 0;
-  b.limits = b.stat + tiles * 4 * kTile * sizeof(float);
+  b.limits = up(b.stat + tiles * kRecord * sizeof(float));
   b.most = b.limits + up(static_cast<size_t>(y.row_tiles) * sizeof(int4));
   b.part_q = b.most + up(tiles * sizeof(float));
   b.part_k = b.part_q + (b.q_parts > 1 ? tiles * b.q_parts * kTile * head_dim * sizeof(float) : 0);

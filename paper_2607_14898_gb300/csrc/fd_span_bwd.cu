@@ -141,12 +141,13 @@ __device__ __forceinline__ float down_scale(const float* most, int n) {
 // Lanes are keys and columns rows of the tile: X = K Q^T and Y = V dout^T into TMEM, P^T and dS^T
 // from there back into TMEM as the first operands of dv += P^T dout and dk += dS^T q.
 //   warps 0-15   P and dS: four groups of 128 threads (a key each), a quarter of a step's rows each
-//   warp 16      TMA: K and V, then q, dout and the rows' numbers by tiles
-//   warps 17-20  products: X, Y, dv, dk (a warp issues one per 104 to 158 cycles)
+//   warps 16-19  products: X, Y, dv, dk (a warp issues one per 104 to 158 cycles); the last one loads K and
+//                V, then q, dout and the rows' records by tiles, each when dk has gone into its place's
+//                last tile (a twenty-first warp would leave 80 registers a thread, not 96)
 // A step is a tile, or (D = 128, where TMEM has no room for more) half of one.
 template <int D>
 struct KeyCfg {
-  static constexpr int kThreads = 21 * 32;
+  static constexpr int kThreads = 20 * 32;
   static constexpr int kStep = D == 64 ? 128 : 64;  // rows of a step
   static constexpr int kSteps = kTile / kStep;      // of a tile
   static constexpr int kCols = kStep / 4;           // of a thread
@@ -290,41 +291,10 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
 
   if (count == 0) {
     // no row sees any of the keys
-  } else if (warp == 16) {
-    if (lane == 0) {
-      prefetch_tmap(&tmQ);
-      prefetch_tmap(&tmDo);
-      mbar_expect_tx(bar(C::kKV), 2 * C::kTileBytes);
-      for (int d = 0; d < D / 64; ++d) {
-        tma_load_4d(base + d * kSub, &tmK, bar(C::kKV), 64 * d, group, key0, 0);
-        tma_load_4d(base + C::kOffV + d * kSub, &tmV, bar(C::kKV), 64 * d, group, key0, 0);
-      }
-      int i = 0;
-      for (; i < count; ++i) {
-        const int st = i % C::kStages;
-        if (i >= C::kStages &&
-            !wait(bar(C::kFree + st), (i / C::kStages - 1) & 1, p.err, ERR_WAIT_MMA))
-          break;
-        const uint32_t b = bar(C::kFull + st), q = base + C::kOffRing + st * 2 * C::kTileBytes;
-        mbar_expect_tx(b, 2 * p.y.tile_rows * D * 2 + C::kStat);
-        const int token = (tile0 + i) * p.y.tile_tokens;
-        for (int d = 0; d < D / 64; ++d) {
-          tma_load_4d(q + d * kSub, &tmQ, b, 64 * d, group * p.y.per, token, 0);
-          tma_load_4d(q + C::kTileBytes + d * kSub, &tmDo, b, 64 * d, group * p.y.per, token, 0);
-        }
-        bulk_load(base + C::kOffStat + st * C::kStat,
-                  p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile0 + i) * kRecord,
-                  C::kStat, b);
-      }
-      // nothing may be in flight when the block exits
-      wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
-      for (int j = max(0, i - C::kStages); j < i; ++j)
-        wait(bar(C::kFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA, true);
-    }
-  } else if (warp == 17 || warp == 18) {
-    // ---- X = K Q^T (17), Y = V dout^T (18), and zeros for the rows of queries that see nothing:
+  } else if (warp == 16 || warp == 17) {
+    // ---- X = K Q^T (16), Y = V dout^T (17), and zeros for the rows of queries that see nothing:
     // their P and dS are 0, but 0 times NaN is NaN
-    const bool y = warp == 18;
+    const bool y = warp == 17;
     constexpr uint32_t idesc = Mma<F16, D>::idesc(C::kStep, false);
     const uint64_t a0 = sdesc_k_sw128(base + (y ? C::kOffV : 0));
     const uint32_t col = tmem + (y ? C::kColY : C::kColX);
@@ -365,14 +335,48 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
         mma_commit_w(bar(y ? C::kYFull : C::kXFull));
       }
     }
-  } else if (warp == 19 || warp == 20) {
-    // ---- dv += P^T dout (19), dk += dS^T q (20)
-    const bool dk = warp == 20;
+  } else if (warp >= 18) {
+    // ---- dv += P^T dout (18), dk += dS^T q and the loads (19)
+    const bool dk = warp == 19;
     constexpr uint32_t idesc = Mma<F16, D>::idesc(D, true);
     const uint32_t a = tmem + (dk ? C::kColDs : C::kColP), acc = tmem + (dk ? C::kColDk : C::kColDv);
+    auto load = [&](int i) {
+      const int st = i % C::kStages;
+      const uint32_t b = bar(C::kFull + st), q = base + C::kOffRing + st * 2 * C::kTileBytes;
+      mbar_expect_tx(b, 2 * p.y.tile_rows * D * 2 + C::kStat);
+      const int token = (tile0 + i) * p.y.tile_tokens;
+      for (int d = 0; d < D / 64; ++d) {
+        tma_load_4d(q + d * kSub, &tmQ, b, 64 * d, group * p.y.per, token, 0);
+        tma_load_4d(q + C::kTileBytes + d * kSub, &tmDo, b, 64 * d, group * p.y.per, token, 0);
+      }
+      bulk_load(base + C::kOffStat + st * C::kStat,
+                p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile0 + i) * kRecord, C::kStat, b);
+    };
+    int loaded = 0;
+    if (dk) {
+      if (lane == 0) {
+        mbar_expect_tx(bar(C::kKV), 2 * C::kTileBytes);
+        for (int d = 0; d < D / 64; ++d) {
+          tma_load_4d(base + d * kSub, &tmK, bar(C::kKV), 64 * d, group, key0, 0);
+          tma_load_4d(base + C::kOffV + d * kSub, &tmV, bar(C::kKV), 64 * d, group, key0, 0);
+        }
+        for (int i = 0; i < min(count, C::kStages); ++i) load(i);
+      }
+      loaded = min(count, C::kStages);
+      __syncwarp();
+    }
     bool ok = true;
     for (int i = 0; i < count && ok; ++i) {
       const int st = i % C::kStages;
+      if (dk && i > 0 && loaded < count) {
+        // the tile before is through: the next one to its place
+        ok = wait_warp(bar(C::kFree + (i - 1) % C::kStages), ((i - 1) / C::kStages) & 1, p.err,
+                       ERR_WAIT_MMA);
+        if (!ok) break;
+        if (lane == 0) load(loaded);
+        __syncwarp();
+        ++loaded;
+      }
       // (dv does not depend on Y, which waits for dout; dk on both)
       ok = wait_warp(bar(C::kReady + st), (i / C::kStages) & 1, p.err, ERR_WAIT_TMA);
       const uint32_t b = base + C::kOffRing + st * 2 * C::kTileBytes + (dk ? 0 : C::kTileBytes);
@@ -389,6 +393,12 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
         mma_commit_w(bar(dk ? C::kDsDone : C::kPDone));
       }
       if (ok) mma_commit_w(bar(C::kFree + st));
+    }
+    if (dk && lane == 0) {
+      // nothing may be in flight when the block exits
+      wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, loaded - C::kStages); j < loaded; ++j)
+        wait(bar(C::kFull + j % C::kStages), (j / C::kStages) & 1, p.err, ERR_WAIT_TMA, true);
     }
   }
   if (warp < 16) {
@@ -439,6 +449,18 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::kXRead));
+        uint32_t y[C::kCols];
+        auto read_y = [&]() {
+          wait_warp(bar(C::kYFull), k & 1, p.err, ERR_WAIT_MMA);
+          tc_fence_after();
+          tmem_ld(y_col, y);
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::kYRead));
+        };
+        // (at once where there are registers for both)
+        if (C::kCols == 16) read_y();
         uint32_t pk[C::kCols / 2];
 #pragma unroll
         for (int c = 0; c < C::kCols; c += 4) {
@@ -468,15 +490,7 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(C::kPFull));
-
-        wait_warp(bar(C::kYFull), k & 1, p.err, ERR_WAIT_MMA);
-        tc_fence_after();
-        uint32_t y[C::kCols];
-        tmem_ld(y_col, y);
-        tmem_ld_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C::kYRead));
+        if (C::kCols == 32) read_y();
 #pragma unroll
         for (int c = 0; c < C::kCols; c += 4) {
           const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(stat + kTile * 4 + c * 4);
@@ -795,12 +809,6 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kXRead));
-#pragma unroll
-      for (int c = 0; c < 32; c += 2) {
-        const float2 a = halves_of(fma2(pair_of(x[c], x[c + 1]), c2, l2));
-        x[c] = __float_as_uint(ex2_approx(a.x));
-        x[c + 1] = __float_as_uint(ex2_approx(a.y));
-      }
       wait_warp(bar(C::kYFull), i & 1, p.err, ERR_WAIT_MMA);
       tc_fence_after();
       tmem_ld_32x32b_x32(y_col, y);
@@ -808,6 +816,12 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kYRead));
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) {
+        const float2 a = halves_of(fma2(pair_of(x[c], x[c + 1]), c2, l2));
+        x[c] = __float_as_uint(ex2_approx(a.x));
+        x[c + 1] = __float_as_uint(ex2_approx(a.y));
+      }
 #pragma unroll
       for (int c = 0; c < 32; c += 2) {
         uint64_t a = pair_of(x[c], x[c + 1]);

@@ -17,6 +17,7 @@ namespace fd {
 namespace {
 
 constexpr int kMaxSpanTokens = 1 << 24;
+constexpr int64_t kMaxSpanRows = 1ll << 36;  // (a tile has 65 rows at least: fewer than 2^30 units)
 
 struct SpanShape {
   int n_q, n_k, heads, groups, per;
@@ -61,7 +62,8 @@ inline bool span_valid(const fd_span_attention* a) {
          a->heads % a->groups == 0 && a->heads / a->groups <= kTile && a->heads <= 65535 &&
          (a->head_dim == 64 || a->head_dim == 128) &&
          (a->dtype == FD_DTYPE_BF16 || a->dtype == FD_DTYPE_F16) && std::isfinite(a->scale) &&
-         a->scale > 0.f && a->n_q <= kMaxSpanTokens && a->n_k <= kMaxSpanTokens;
+         a->scale > 0.f && a->n_q <= kMaxSpanTokens && a->n_k <= kMaxSpanTokens &&
+         static_cast<int64_t>(a->n_q) * a->heads <= kMaxSpanRows;
 }
 inline bool span_rows_ok(const SpanRows& r, int tokens, int heads, int head_dim) {
   return span_ptr(r.p, 16) && r.token % 8 == 0 && r.head % 8 == 0 &&

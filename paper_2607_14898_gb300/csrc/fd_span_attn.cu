@@ -23,52 +23,41 @@ struct SpanFwd {
 
 constexpr float kSlack = 8.f;  // log2 by which a row's maximum may grow before O is rescaled
 
-// A block has a row tile of a group and a run of the key blocks, of 256 keys, that any of its queries
-// see.
-//
-// The softmax is the longest chain of a key block (scores out of TMEM, maximum, exponentials, P into
-// TMEM), so sixteen warps share it, four on every SM sub-partition: each of four groups of 128
-// threads has a quarter of the keys, a row (TMEM lane) per thread. The row's running maximum is
-// handed from quarter to quarter, which sets the groups a step apart: the exponentials of one run
-// beside the loads, masks and maxima of the others.
-//   warps 0-15    softmax: warps 4 q .. 4 q + 3 quarter q
-//   warp 16       TMA: Q, then K and V by half blocks (128 keys), through a ring each, so that a half
-//                 is fetched as soon as one has been used
-//   warps 17, 18  products (a thread issues one per 104 to 158 cycles whatever its size). D = 64:
-//                 those of the block's first and second half, each half with a running maximum and an
-//                 O of its own; D = 128: S of both halves, and P V into the one O that TMEM has
-//                 room for
-//   warp 19       zeros for the values of keys that no query of the tile sees (their probability is 0,
-//                 but 0 times NaN is NaN)
-// TMEM (512 columns): S 2 x 128, P 2 x 64 (two 16-bit values a column), O 2 x 64 or 128. S takes the
-// next scores once the softmax has it in registers.
+// A block has a row tile of a group and a run of the key blocks, of 128 keys, that any of its queries
+// see. Two blocks share an SM (half of TMEM and of shared memory each), so that the softmax of one runs
+// beside the products of the other, and its beginning and end beside the other's middle.
+//   warps 0-7   softmax: two threads a row (TMEM lane), half of the block's keys each; the row's maximum
+//               goes through shared memory
+//   warp 8      TMA: Q, then K and V by blocks, through a ring each
+//   warp 9      zeros for the values of keys that no query of the tile sees (their probability is 0, but
+//               0 times NaN is NaN)
+//   warp 10     products: S = Q K^T, O += P V
+// TMEM (256 columns): S 128, O at the end. D = 64: P has 64 of its own, so that the next scores begin when
+// the softmax has read the last. D = 128: each half's P takes the first columns of the scores it was made of; the
+// next scores are issued after the product that reads P, by the same thread, and products run in
+// their order.
 template <int D>
 struct FwdCfg {
-  static constexpr int kKeys = 256;
-  static constexpr int kThreads = 640;  // five warps a sub-partition: 96 registers
-  static constexpr int kTileBytes = kTile * D * 2;  // Q, and K or V of half a block
-  static constexpr int kSlots = D == 128 ? 3 : 6;   // of each ring; half 2 J + h is in slot (2 J + h) % kSlots
-  static constexpr bool kTwoO = D == 64;
-  // A parity tells a phase from its neighbours and no further, so whoever waits for a slot's
-  // barrier has to wait for every phase of it: one thread waits for all halves, or (D = 64) one
-  // for each half of the blocks, whose slots differ because the ring's length is even.
-  static_assert(!kTwoO || kSlots % 2 == 0, "waiters");
+  static constexpr int kThreads = 11 * 32;  // two blocks: six warps on a sub-partition, 80 registers
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr bool kOwnP = D == 64;
+  static constexpr int kSlotsK = D == 64 ? 3 : 1, kSlotsV = D == 64 ? 2 : 1;
   static constexpr int kOffK = kTileBytes;
-  static constexpr int kOffV = kOffK + kSlots * kTileBytes;
-  static constexpr int kOffMax = kOffV + kSlots * kTileBytes;
-  static constexpr int kOffBar = kOffMax + (kTwoO ? 4 : 1) * kTile * 4;  // D = 64: [half][m, l]
-  static constexpr uint32_t kColS = 0, kColP = 256, kColO = 384;
-  // barriers: kSFull, kSRead of the halves, kPFull, kPv of the quarters, kMax of each of their warps
-  static constexpr int kQFull = 0, kKFull = 1, kKFree = kKFull + kSlots, kVFull = kKFree + kSlots,
-                       kVFree = kVFull + kSlots, kVReady = kVFree + kSlots,
-                       kSFull = kVReady + kSlots, kSRead = kSFull + 2, kPFull = kSRead + 2,
-                       kPv = kPFull + 4, kMax = kPv + 4, kDone = kMax + 16, kBars = kDone + 2;
+  static constexpr int kOffV = kOffK + kSlotsK * kTileBytes;
+  static constexpr int kOffMax = kOffV + kSlotsV * kTileBytes;  // [2][half][row]
+  static constexpr int kOffBar = kOffMax + 4 * kTile * 4;
+  static constexpr int kQFull = 0, kKFull = 1, kKFree = kKFull + kSlotsK, kVFull = kKFree + kSlotsK,
+                       kVFree = kVFull + kSlotsV, kVReady = kVFree + kSlotsV,
+                       kSFull = kVReady + kSlotsV,
+                       kSRead = kSFull + 1, kPFull = kSRead + 1, kPv = kPFull + 1, kBars = kPv + 1;
   static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
-  static_assert(kSmem <= 227 * 1024, "shared memory");
+  static constexpr uint32_t kColS = 0, kColP = kOwnP ? 128 : 0, kColO = 256 - D;
+  static constexpr uint32_t kHalfP = kOwnP ? 32 : 64;  // columns from a half's P to the other's
+  static_assert(kSmem + 1024 <= 114 * 1024, "shared memory of two blocks");
 };
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
+__global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     span_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ SpanFwd p) {
   using C = FwdCfg<D>;
@@ -81,8 +70,6 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
   auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   volatile int* range = reinterpret_cast<volatile int*>(tmem_slot + 1);  // first key, blocks
-  // the rows' running maximum (D = 64: of each half); at the end their sums
-  volatile float* row_max = reinterpret_cast<volatile float*>(smem + C::kOffMax);
 
   // (later tokens first: under a causal mask they see most)
   const int part = blockIdx.x % p.parts;
@@ -92,37 +79,40 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
   const int tokens = min(p.y.tile_tokens, p.y.n_q - token0);
 
   // rows past tile_rows are never loaded
-  for (int i = threadIdx.x; i < C::kTileBytes / 16; i += C::kThreads)
-    reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
-  fence_proxy_async_smem();
+  if (p.y.tile_rows < kTile) {
+    for (int i = threadIdx.x; i < C::kTileBytes / 16; i += C::kThreads)
+      reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
   if (threadIdx.x == 0) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
     mbar_init(bar(C::kQFull), 1);
-    for (int i = 0; i < C::kSlots; ++i) {
+    for (int i = 0; i < C::kSlotsK; ++i) {
       mbar_init(bar(C::kKFull + i), 1);
       mbar_init(bar(C::kKFree + i), 1);
+    }
+    for (int i = 0; i < C::kSlotsV; ++i) {
       mbar_init(bar(C::kVFull + i), 1);
       mbar_init(bar(C::kVFree + i), 1);
       mbar_init(bar(C::kVReady + i), 1);
     }
-    for (int h = 0; h < 2; ++h) {
-      mbar_init(bar(C::kSFull + h), 1);
-      mbar_init(bar(C::kSRead + h), 8);
-      mbar_init(bar(C::kDone + h), 1);
-    }
-    for (int q = 0; q < 4; ++q) {
-      mbar_init(bar(C::kPFull + q), 4);
-      mbar_init(bar(C::kPv + q), 1);
-      for (int i = 0; i < 4; ++i) mbar_init(bar(C::kMax + 4 * q + i), 32);
-    }
+    mbar_init(bar(C::kSFull), 1);
+    mbar_init(bar(C::kSRead), 8);
+    mbar_init(bar(C::kPFull), 8);
+    mbar_init(bar(C::kPv), 1);
     fence_barrier_init();
   }
   grid_dep_wait();
   grid_dep_launch();
-  if (warp == 0) {
-    tmem_alloc(smem_u32(tmem_slot), 512);
+  if (warp == 10) {
+    tmem_alloc(smem_u32(tmem_slot), 256);
     tmem_relinquish();
-  } else if (warp == 1) {
+  } else if (warp == 8) {
+    if (lane == 0) {
+      prefetch_tmap(&tmQ);
+      prefetch_tmap(&tmK);
+      prefetch_tmap(&tmV);
+    }
     // the keys that any query of the tile sees, and this block's part of them
     int lo = 0x7fffffff, hi = 0;
     for (int i = lane; i < tokens; i += 32) {
@@ -135,11 +125,11 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
     const int key = hi > 0 ? lo / kTile * kTile : 0;
-    const int n = (hi - key + C::kKeys - 1) / C::kKeys;
+    const int n = (hi - key + kTile - 1) / kTile;
     const int first = static_cast<int>(static_cast<int64_t>(n) * part / p.parts);
     const int end = static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.parts);
     if (lane == 0) {
-      range[0] = key + first * C::kKeys;
+      range[0] = key + first * kTile;
       range[1] = aligned ? end - first : 0;
     }
   }
@@ -151,35 +141,33 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
 
   if (count == 0) {
     // nothing is seen: the softmax warps write that below
-  } else if (warp == 16) {
+  } else if (warp == 8) {
     if (lane == 0) {
-      prefetch_tmap(&tmK);
-      prefetch_tmap(&tmV);
       mbar_expect_tx(bar(C::kQFull), p.y.tile_rows * D * 2);
       for (int d = 0; d < D / 64; ++d)
         tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.y.per, token0, 0);
-      // the next half of K, or of V, as soon as its slot is free
-      int k = 0, v = 0, idle = 0;  // halves so far
+      // the next K, or V, as soon as its slot is free
+      int k = 0, v = 0, idle = 0;
       uint32_t idle_since = 0;
-      auto room = [&](int n, int free) {
-        return n < 2 * count && (n < C::kSlots ||
-                                 mbar_test_wait(bar(free + n % C::kSlots), (n / C::kSlots - 1) & 1));
+      auto room = [&](int n, int slots, int free) {
+        return n < count &&
+               (n < slots || mbar_test_wait(bar(free + n % slots), (n / slots - 1) & 1));
       };
-      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int full) {
-        const int slot = n % C::kSlots;
+      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full) {
+        const int slot = n % slots;
         mbar_expect_tx(bar(full + slot), C::kTileBytes);
         for (int d = 0; d < D / 64; ++d)
           tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
                       key_start + n * kTile, 0);
       };
-      while (k < 2 * count || v < 2 * count) {
+      while (k < count || v < count) {
         bool moved = false;
-        if (room(k, C::kKFree)) {
-          load(k++, &tmK, base + C::kOffK, C::kKFull);
+        if (room(k, C::kSlotsK, C::kKFree)) {
+          load(k++, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull);
           moved = true;
         }
-        if (room(v, C::kVFree)) {
-          load(v++, &tmV, base + C::kOffV, C::kVFull);
+        if (room(v, C::kSlotsV, C::kVFree)) {
+          load(v++, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull);
           moved = true;
         }
         if (moved)
@@ -189,20 +177,20 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
       }
       // nothing may be in flight when the block exits
       wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA, true);
-      for (int j = max(0, k - C::kSlots); j < k; ++j)
-        wait(bar(C::kKFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
-      for (int j = max(0, v - C::kSlots); j < v; ++j)
-        wait(bar(C::kVFull + j % C::kSlots), (j / C::kSlots) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, k - C::kSlotsK); j < k; ++j)
+        wait(bar(C::kKFull + j % C::kSlotsK), (j / C::kSlotsK) & 1, p.err, ERR_WAIT_TMA, true);
+      for (int j = max(0, v - C::kSlotsV); j < v; ++j)
+        wait(bar(C::kVFull + j % C::kSlotsV), (j / C::kSlotsV) & 1, p.err, ERR_WAIT_TMA, true);
     }
-  } else if (warp == 19) {
+  } else if (warp == 9) {
     // ---- values of keys that nothing sees
     int2 span[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       span[i] = lane + 32 * i < tokens ? span_of(p.spans, token0 + lane + 32 * i, p.y.n_k)
                                        : make_int2(0, 0);
-    for (int n = 0; n < 2 * count; ++n) {
-      const int key0 = key_start + n * kTile, slot = n % C::kSlots;
+    for (int n = 0; n < count; ++n) {
+      const int key0 = key_start + n * kTile, slot = n % C::kSlotsV;
       bool whole = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) whole |= span[i].x <= key0 && span[i].y >= key0 + kTile;
@@ -216,7 +204,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
           seen[w] = __reduce_or_sync(0xffffffffu, mine);
         }
       }
-      if (!wait_warp(bar(C::kVFull + slot), (n / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) break;
+      if (!wait_warp(bar(C::kVFull + slot), (n / C::kSlotsV) & 1, p.err, ERR_WAIT_TMA)) break;
       if ((seen[0] & seen[1] & seen[2] & seen[3]) != 0xffffffffu) {
 #pragma unroll 1
         for (int w = 0; w < 4; ++w) {
@@ -234,67 +222,44 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C::kVReady + slot));
     }
-  } else if (warp >= 17) {  // 17 and 18
-    if (lane == 0) {
-      constexpr uint32_t is = Mma<F16, D>::idesc(kTile, false), io = Mma<F16, D>::idesc(D, true);
-      const uint32_t s_col = tmem + C::kColS, p_col = tmem + C::kColP, o_col = tmem + C::kColO;
-      const uint64_t q0 = sdesc_k_sw128(base);
-      // S of half h of block J, once K is there
-      auto scores = [&](int J, int h) -> bool {
-        const int n = 2 * J + h, slot = n % C::kSlots;
-        if (!wait(bar(C::kKFull + slot), (n / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
-        tc_fence_after();
-        const uint64_t k0 = sdesc_k_sw128(base + C::kOffK + slot * C::kTileBytes);
+  } else if (warp == 10) {
+    constexpr uint32_t is = Mma<F16, D>::idesc(kTile, false), io = Mma<F16, D>::idesc(D, true);
+    const uint64_t q0 = sdesc_k_sw128(base);
+    auto scores = [&](int j) -> bool {
+      const int slot = j % C::kSlotsK;
+      if (!wait_warp(bar(C::kKFull + slot), (j / C::kSlotsK) & 1, p.err, ERR_WAIT_TMA)) return false;
+      tc_fence_after();
+      const uint64_t k0 = sdesc_k_sw128(base + C::kOffK + slot * C::kTileBytes);
 #pragma unroll
-        for (int d = 0; d < D / 64; ++d)
-          mma4_bf16_ss(s_col + 128u * h, q0 + static_cast<uint64_t>(d * (kSub >> 4)),
+      for (int d = 0; d < D / 64; ++d)
+        mma4_bf16_ss_w(tmem + C::kColS, q0 + static_cast<uint64_t>(d * (kSub >> 4)),
                        k0 + static_cast<uint64_t>(d * (kSub >> 4)), is, d > 0);
-        mma_commit(bar(C::kSFull + h));
-        mma_commit(bar(C::kKFree + slot));
-        return true;
-      };
-      // P V of half h of block J into O (the half's own for D = 64), quarter after quarter
-      auto values = [&](int J, int h) -> bool {
-        const int n = 2 * J + h, slot = n % C::kSlots;
-        if (!wait(bar(C::kVReady + slot), (n / C::kSlots) & 1, p.err, ERR_WAIT_TMA)) return false;
+      mma_commit_w(bar(C::kSFull));
+      mma_commit_w(bar(C::kKFree + slot));
+      return true;
+    };
+    bool ok = wait_warp(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA) && scores(0);
+    for (int j = 0; j < count && ok; ++j) {
+      const int slot = j % C::kSlotsV;
+      if (C::kOwnP && j + 1 < count)
+        ok = wait_warp(bar(C::kSRead), j & 1, p.err, ERR_WAIT_EPI) && scores(j + 1);
+      ok = ok && wait_warp(bar(C::kVReady + slot), (j / C::kSlotsV) & 1, p.err, ERR_WAIT_TMA) &&
+           wait_warp(bar(C::kPFull), j & 1, p.err, ERR_WAIT_EPI);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t v = base + C::kOffV + slot * C::kTileBytes;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int q = 2 * h + x;
-          if (!wait(bar(C::kPFull + q), J & 1, p.err, ERR_WAIT_EPI)) return false;
-          tc_fence_after();
-          const uint64_t v0 =
-              sdesc_mn_sw128(base + C::kOffV + slot * C::kTileBytes + x * (kSub / 2), kSub);
-          const bool fresh = J == 0 && x == 0 && (C::kTwoO || h == 0);
-          mma4_ts_mn(o_col + (C::kTwoO ? 64u * h : 0u), p_col + 32u * q, v0, io, !fresh);
-          mma_commit(bar(C::kPv + q));
-        }
-        mma_commit(bar(C::kVFree + slot));
-        return true;
-      };
-      const int h = warp - 17;
-      bool ok = true;
-      if (C::kTwoO) {
-        ok = wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA) && scores(0, h);
-        for (int J = 0; J < count && ok; ++J) {
-          if (J + 1 < count)
-            ok = wait(bar(C::kSRead + h), J & 1, p.err, ERR_WAIT_EPI) && scores(J + 1, h);
-          ok = ok && values(J, h);
-        }
-      } else if (h == 0) {
-        ok = wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA);
-        for (int J = 0; J < count && ok; ++J)
-          for (int x = 0; x < 2 && ok; ++x)
-            ok = (J == 0 || wait(bar(C::kSRead + x), (J - 1) & 1, p.err, ERR_WAIT_EPI)) && scores(J, x);
-      } else {
-        for (int J = 0; J < count && ok; ++J) ok = values(J, 0) && values(J, 1);
-      }
-      mma_commit(bar(C::kDone + h));
-      wait(bar(C::kDone + h), 0, p.err, ERR_WAIT_MMA, true);
+      for (int x = 0; x < 2; ++x)
+        mma4_ts_mn_w(tmem + C::kColO, tmem + C::kColP + C::kHalfP * x, sdesc_mn_sw128(v + x * 64 * 128, kSub), io,
+                     j > 0 || x > 0);
+      mma_commit_w(bar(C::kPv));
+      mma_commit_w(bar(C::kVFree + slot));
+      if (!C::kOwnP && j + 1 < count) ok = scores(j + 1);
     }
   }
-  if (warp < 16) {
-    // ---- softmax of quarter q of the blocks
-    const int q = warp >> 2, h = q >> 1, lanes = warp & 3;
+  if (warp < 8) {
+    // ---- softmax of half h of the blocks' keys
+    const int h = warp >> 2, lanes = warp & 3;
     const int row = lanes * 32 + lane;
     const int token = token0 + row / p.y.per;
     const bool valid = row < p.y.tile_rows && token < p.y.n_q;
@@ -304,91 +269,64 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
     const int all_from = __reduce_max_sync(0xffffffffu, sees ? span.x : 0);
     const int all_to = __reduce_min_sync(0xffffffffu, sees ? span.y : 0x7fffffff);
     const uint32_t lane_off = static_cast<uint32_t>(lanes * 32) << 16;
-    const uint32_t s_col = tmem + lane_off + C::kColS + 64u * q;
-    const uint32_t p_col = tmem + lane_off + C::kColP + 32u * q;
-    const uint32_t o_col = tmem + lane_off + C::kColO + (C::kTwoO ? 64u * h : 0u);
-    // the quarters that share an O and a running maximum: the one before this, in the same block
-    // or (the first one) the last in the block before
-    constexpr int kShare = C::kTwoO ? 2 : 4;
-    const bool lead = q % kShare == 0;
-    const int prev = lead ? q + kShare - 1 : q - 1;
-    volatile float* const my_max = row_max + (C::kTwoO ? 2 * h * kTile : 0) + row;
-    // (a per-thread copy: a kernel parameter costs the loop more instructions)
-    const float c = __shfl_sync(0xffffffffu, p.scale_log2, 0);
+    const uint32_t s_col = tmem + lane_off + C::kColS + 64u * h;
+    const uint32_t p_col = tmem + lane_off + C::kColP + C::kHalfP * h;
+    const uint32_t o_col = tmem + lane_off + C::kColO + D / 2 * h;
+    volatile float* const tops = reinterpret_cast<volatile float*>(smem + C::kOffMax) + row;
+    const float c = p.scale_log2;
     const uint64_t c2 = pack_f32x2(c, c);
     float m = -INFINITY, l = 0.f;
     // A wait that gives up has set the status word, and every wait after it returns at once: the warps
     // go on to the end.
 #pragma unroll 1
-    for (int J = 0; J < count; ++J) {
-      const int key0 = key_start + J * C::kKeys + 64 * q;
-      wait_warp(bar(C::kSFull + h), J & 1, p.err, ERR_WAIT_MMA);
+    for (int j = 0; j < count; ++j) {
+      const int key0 = key_start + j * kTile + 64 * h;
+      const bool masked = key0 < all_from || key0 + 64 > all_to;
+      wait_warp(bar(C::kSFull), j & 1, p.err, ERR_WAIT_MMA);
       tc_fence_after();
-      uint32_t sr[2][32];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) tmem_ld_32x32b_x32(s_col + 32 * i, sr[i]);
-      tmem_ld_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kSRead + h));
-      if (key0 < all_from || key0 + 64 > all_to) {
-        __syncwarp();  // (not predicated: else the selections are made for every block)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t seen = seen_word(span, key0 + 32 * i);
+      // 32 scores at a time; they are fetched again for their exponentials
+      uint32_t sr[32];
+      auto hide = [&](int x) {
+        if (masked) {
+          __syncwarp();  // (not predicated: else the selections are made for every block)
+          const uint32_t seen = seen_word(span, key0 + 32 * x);
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (!(seen & (1u << e))) sr[i][e] = 0xff800000u;
+            if (!(seen & (1u << e))) sr[e] = 0xff800000u;
         }
-      }
-      float mx[4];
+      };
+      float mx[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t* x = sr[i / 2] + 16 * (i % 2);
-        mx[i] = __uint_as_float(x[0]);
+      for (int x = 0; x < 2; ++x) {
+        tmem_ld_32x32b_x32(s_col + 32 * x, sr);
+        tmem_ld_wait();
+        hide(x);
+        float a = __uint_as_float(sr[0]), b = __uint_as_float(sr[16]);
 #pragma unroll
-        for (int e = 1; e < 15; e += 2)
-          mx[i] = fmax3(mx[i], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-        mx[i] = fmaxf(mx[i], __uint_as_float(x[15]));
-      }
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-      // the maximum that O stands for now
-      const bool fresh = J == 0 && lead;  // O holds nothing yet
-      float before = -INFINITY;
-      if (!fresh) {
-        wait_warp(bar(C::kMax + 4 * prev + lanes), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_EPI);
-        before = *my_max;
-      }
-      const bool grow = top > before + kSlack;
-      const float now = grow ? top : before;
-      const float off = now == -INFINITY ? 0.f : now;
-      *my_max = now;
-      mbar_arrive(bar(C::kMax + 4 * q + lanes));
-      const float f = grow ? ex2_approx(before - off) : 1.f;  // of O
-      l *= m == now ? 1.f : ex2_approx(m - off);
-      m = now;
-      const uint64_t off2 = pack_f32x2(-off, -off);
-      uint64_t sum2[2] = {0, 0};
-      // P in the inputs' type, which the product with V takes: 2^-9 (bf16) or 2^-12 (fp16) of each p at
-      // most. The sums are of P unrounded.
-      uint32_t pk[2][16];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-          const float2 x = halves_of(fma2(pair_of(sr[i][e], sr[i][e + 1]), c2, off2));
-          const float a = ex2_approx(x.x), b = ex2_approx(x.y);
-          sum2[e / 2 % 2] = add2(sum2[e / 2 % 2], pack_f32x2(a, b));
-          pk[i][e / 2] = pack16<F16>(a, b);
+        for (int e = 1; e < 15; e += 2) {
+          a = fmax3(a, __uint_as_float(sr[e]), __uint_as_float(sr[e + 1]));
+          b = fmax3(b, __uint_as_float(sr[16 + e]), __uint_as_float(sr[17 + e]));
         }
-      // the previous block's product has read this quarter's P
-      if (J > 0) wait_warp(bar(C::kPv + q), (J - 1) & 1, p.err, ERR_WAIT_MMA);
-      if (!fresh && __any_sync(0xffffffffu, grow)) {
-        // O as the products of all quarters before left it
-        wait_warp(bar(C::kPv + prev), (lead ? J - 1 : J) & 1, p.err, ERR_WAIT_MMA);
-        tc_fence_after();
+        mx[x] = fmax3(fmaxf(a, b), __uint_as_float(sr[15]), __uint_as_float(sr[31]));
+      }
+      // the row's maximum over both halves
+      float top = fmaxf(mx[0], mx[1]) * c;
+      volatile float* const at = tops + (j & 1) * 2 * kTile;
+      at[h * kTile] = top;
+      named_barrier(1 + lanes, 64);
+      top = fmaxf(top, at[(h ^ 1) * kTile]);
+      const bool grow = top > m + kSlack;
+      const float before = m;
+      if (grow) m = top;
+      const float off = m == -INFINITY ? 0.f : m;
+      // the last product has read P, and O is as it left it
+      if (j > 0) wait_warp(bar(C::kPv), (j - 1) & 1, p.err, ERR_WAIT_MMA);
+      tc_fence_after();
+      if (j > 0 && __any_sync(0xffffffffu, grow)) {
+        const float f = grow ? ex2_approx(before - off) : 1.f;
+        l *= f;
 #pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
+        for (int d = 0; d < D / 2; d += 16) {
           uint32_t o[16];
           tmem_ld_32x32b_x16(o_col + d, o);
           tmem_ld_wait();
@@ -397,121 +335,96 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 1)
           tmem_st_32x32b_x16(o_col + d, o);
         }
       }
-      tc_fence_after();
-      __syncwarp();
+      const uint64_t off2 = pack_f32x2(-off, -off);
+      uint64_t sum2[2] = {0, 0};
+      // P in the inputs' type, which the product with V takes: 2^-9 (bf16) or 2^-12 (fp16) of each p at
+      // most. The sums are of P unrounded.
 #pragma unroll
-      for (int i = 0; i < 2; ++i) tmem_st_32x32b_x16(p_col + 16 * i, pk[i]);
+      for (int x = 0; x < 2; ++x) {
+        tmem_ld_32x32b_x32(s_col + 32 * x, sr);
+        tmem_ld_wait();
+        if (C::kOwnP && x == 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C::kSRead));
+        }
+        hide(x);
+        uint32_t pk[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const float2 v = halves_of(fma2(pair_of(sr[e], sr[e + 1]), c2, off2));
+          const float a = ex2_approx(v.x), b = ex2_approx(v.y);
+          sum2[e / 2 % 2] = add2(sum2[e / 2 % 2], pack_f32x2(a, b));
+          pk[e / 2] = pack16<F16>(a, b);
+        }
+        tmem_st_32x32b_x16(p_col + 16 * x, pk);
+      }
       {
-        const float2 x = halves_of(sum2[0]), y = halves_of(sum2[1]);
-        l += (x.x + x.y) + (y.x + y.y);
+        const float2 a = halves_of(sum2[0]), b = halves_of(sum2[1]);
+        l += (a.x + a.y) + (b.x + b.y);
       }
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kPFull + q));
+      if (lane == 0) mbar_arrive(bar(C::kPFull));
     }
 
-    // ---- the result: this thread's quarter of the row's elements
-    float all = 0.f, f0 = 1.f, f1 = 1.f;
-    if (count > 0) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) wait_warp(bar(C::kPv + i), (count - 1) & 1, p.err, ERR_WAIT_MMA);
-      tc_fence_after();
-      // the sums on the last maximum, added up in the order of the quarters (named barriers of the
-      // row's four warps between the steps)
-      wait_warp(bar(C::kMax + 4 * (q / kShare * kShare + kShare - 1) + lanes), (count - 1) & 1, p.err,
-                ERR_WAIT_EPI);
-      const float last = *my_max;
-      l *= m == last ? 1.f : ex2_approx(m - last);
-      m = last;
-      // (the warp together at each of them)
-      auto meet = [&]() {
-        __syncwarp();
-        named_barrier(1 + lanes, 128);
-      };
-      meet();
-      if (C::kTwoO) {  // [half][m, l]: the halves on the larger maximum
-        volatile float* const my_sum = my_max + kTile;
-        if (lead) *my_sum = l;
-        meet();
-        if (!lead) *my_sum = *my_sum + l;
-        meet();
-        const float m0 = row_max[row], l0 = row_max[kTile + row];
-        const float m1 = row_max[2 * kTile + row], l1 = row_max[3 * kTile + row];
-        m = fmaxf(m0, m1);
-        const float at = m == -INFINITY ? 0.f : m;
-        f0 = ex2_approx(m0 - at);
-        f1 = ex2_approx(m1 - at);
-        all = fmaf(f0, l0, f1 * l1);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (q == i) *my_max = i == 0 ? l : *my_max + l;
-          meet();
-        }
-        all = *my_max;
-      }
-    }
-    if (!sees) all = 0.f;
-    if (all == 0.f) m = -INFINITY;
+    // ---- the result: half of the row's elements a thread
+    if (count > 0) wait_warp(bar(C::kPv), (count - 1) & 1, p.err, ERR_WAIT_MMA);
+    tc_fence_after();
+    volatile float* const at = tops + (count & 1) * 2 * kTile;
+    at[h * kTile] = l;
+    named_barrier(1 + lanes, 64);
+    l = at[0] + at[kTile];
+    if (!sees || count == 0) l = 0.f;
+    if (l == 0.f) m = -INFINITY;
     const bool whole = p.parts == 1;
-    const float inv = all == 0.f ? 0.f : 1.f / all;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int head = group * p.y.per + row % p.y.per;
     uint16_t* out = static_cast<uint16_t*>(p.out.p) + static_cast<int64_t>(token) * p.out.token +
                     static_cast<int64_t>(head) * p.out.head;
     const int64_t slot =
         ((static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.parts + part) * kTile + row;
 #pragma unroll 1
-    for (int d = q * (D / 4); d < (q + 1) * (D / 4); d += 16) {
-      uint32_t o[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[e] = 0;
+    for (int d = h * (D / 2); d < (h + 1) * (D / 2); d += 32) {
+      uint32_t o[32];
       if (count > 0) {
         __syncwarp();
-        tmem_ld_32x32b_x16(tmem + lane_off + C::kColO + d, o);
-        if (C::kTwoO) {
-          uint32_t o2[16];
-          tmem_ld_32x32b_x16(tmem + lane_off + C::kColO + 64 + d, o2);
-          tmem_ld_wait();
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            o[e] = __float_as_uint(fmaf(f0, __uint_as_float(o[e]), f1 * __uint_as_float(o2[e])));
-        } else {
-          tmem_ld_wait();
-        }
+        tmem_ld_32x32b_x32(tmem + lane_off + C::kColO + d, o);
+        tmem_ld_wait();
       }
       if (!valid) continue;
       if (whole) {
 #pragma unroll
-        for (int e = 0; e < 16; e += 8) {
+        for (int e = 0; e < 32; e += 8) {
           uint32_t v[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            v[i] = all == 0.f ? 0u
-                              : pack16<F16>(__uint_as_float(o[e + 2 * i]) * inv,
-                                            __uint_as_float(o[e + 2 * i + 1]) * inv);
+            v[i] = l == 0.f ? 0u
+                            : pack16<F16>(__uint_as_float(o[e + 2 * i]) * inv,
+                                          __uint_as_float(o[e + 2 * i + 1]) * inv);
           *reinterpret_cast<uint4*>(out + d + e) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-      } else if (all != 0.f) {
+      } else if (l != 0.f) {
 #pragma unroll
-        for (int e = 0; e < 16; e += 4)
+        for (int e = 0; e < 32; e += 4)
           *reinterpret_cast<uint4*>(p.part_o + slot * D + d + e) =
               make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
       }
     }
-    if (q == 0 && valid) {
+    if (h == 0 && valid) {
       if (whole)
         p.lse[static_cast<int64_t>(head) * p.y.n_q + token] =
-            all == 0.f ? -INFINITY : (m + log2f(all)) * kLn2;
+            l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       else
-        p.part_ml[slot] = make_float2(m, all);
+        p.part_ml[slot] = make_float2(m, l);
     }
     tc_fence_before();
   }
   __syncthreads();
-  if (warp == 0) {
+  if (warp == 10) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, 256);
   }
 }
 
@@ -574,12 +487,12 @@ __global__ void __launch_bounds__(256) span_join_kernel(const __grid_constant__ 
         l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Parts of every tile's key blocks: as many as fill the GPU where there are few tiles, but 512 keys (2 us)
-// each at least, since joining the parts takes 3 us.
+// Parts of every tile's key blocks: as many as fill the GPU (two blocks an SM) where there are few tiles,
+// but 256 keys each at least, since joining the parts takes 3 us.
 int fwd_parts(const SpanShape& y) {
   const int64_t units = static_cast<int64_t>(y.groups) * y.row_tiles;
   return static_cast<int>(
-      std::max<int64_t>(1, std::min<int64_t>(y.key_blocks / 4, num_sms() / units)));
+      std::max<int64_t>(1, std::min<int64_t>(y.key_blocks / 2, 2 * num_sms() / units)));
 }
 
 template <bool F16, int D>

@@ -667,34 +667,22 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
         tma_load_4d(base + d * kSub, &tmQ, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
         tma_load_4d(base + C::kOffDo + d * kSub, &tmDo, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
       }
-      // the next K, or V, as soon as its slot is free
-      int k = 0, v = 0, idle = 0;
-      uint32_t idle_since = 0;
-      auto room = [&](int n, int slots, int free) {
-        return n < count &&
-               (n < slots || mbar_test_wait(bar(free + n % slots), (n / slots - 1) & 1));
-      };
-      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full) {
-        const uint32_t b = bar(full + n % slots);
-        mbar_expect_tx(b, C::kTileBytes);
+      // K and V in turn, each when its slot is free (blocking waits: a loop that looked at both by turns
+      // took the other warps' issue slots)
+      int k = 0, v = 0;
+      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full, int free) {
+        const int slot = n % slots;
+        if (n >= slots && !wait(bar(free + slot), (n / slots - 1) & 1, p.err, ERR_WAIT_MMA)) return false;
+        mbar_expect_tx(bar(full + slot), C::kTileBytes);
         for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(to + n % slots * C::kTileBytes + d * kSub, map, b, 64 * d, group,
+          tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
                       (block0 + n) * kTile, 0);
+        return true;
       };
-      while (k < count || v < count) {
-        bool moved = false;
-        if (room(k, C::kSlotsK, C::kKFree)) {
-          load(k++, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull);
-          moved = true;
-        }
-        if (room(v, C::kSlotsV, C::kVFree)) {
-          load(v++, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull);
-          moved = true;
-        }
-        if (moved)
-          idle = 0;
-        else if (!poll_again(idle, idle_since, p.err, ERR_WAIT_MMA))
-          break;
+      while (v < count && load(k, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree)) {
+        ++k;
+        if (!load(v, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree)) break;
+        ++v;
       }
       // nothing may be in flight when the block exits
       wait(bar(C::kQ), 0, p.err, ERR_WAIT_TMA, true);

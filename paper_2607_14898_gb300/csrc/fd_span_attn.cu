@@ -83,9 +83,13 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     for (int i = threadIdx.x; i < C::kTileBytes / 16; i += C::kThreads)
       reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
+    __syncthreads();  // before Q is loaded
   }
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 8 * 32) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
     mbar_init(bar(C::kQFull), 1);
     for (int i = 0; i < C::kSlotsK; ++i) {
       mbar_init(bar(C::kKFull + i), 1);
@@ -104,15 +108,21 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
   }
   grid_dep_wait();
   grid_dep_launch();
+  int loads_k = 0, loads_v = 0;  // warp 8: so far
+  // K or V of block n; waits for its slot after the first ones
+  auto load = [&](int n, int first_key, const CUtensorMap* map, uint32_t to, int slots, int full, int free) {
+    const int slot = n % slots;
+    if (n >= slots && !wait(bar(free + slot), (n / slots - 1) & 1, p.err, ERR_WAIT_MMA)) return false;
+    mbar_expect_tx(bar(full + slot), C::kTileBytes);
+    for (int d = 0; d < D / 64; ++d)
+      tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
+                  first_key + n * kTile, 0);
+    return true;
+  };
   if (warp == 10) {
     tmem_alloc(smem_u32(tmem_slot), 256);
     tmem_relinquish();
   } else if (warp == 8) {
-    if (lane == 0) {
-      prefetch_tmap(&tmQ);
-      prefetch_tmap(&tmK);
-      prefetch_tmap(&tmV);
-    }
     // the keys that any query of the tile sees, and this block's part of them
     int lo = 0x7fffffff, hi = 0;
     for (int i = lane; i < tokens; i += 32) {
@@ -128,11 +138,25 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     const int n = (hi - key + kTile - 1) / kTile;
     const int first = static_cast<int>(static_cast<int64_t>(n) * part / p.parts);
     const int end = static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.parts);
+    const int first_key = key + first * kTile, blocks = aligned ? end - first : 0;
     if (lane == 0) {
-      range[0] = key + first * kTile;
-      range[1] = aligned ? end - first : 0;
+      range[0] = first_key;
+      range[1] = blocks;
+      if (blocks > 0) {  // what there is room for, while the others get ready
+        mbar_expect_tx(bar(C::kQFull), p.y.tile_rows * D * 2);
+        for (int d = 0; d < D / 64; ++d)
+          tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.y.per, token0, 0);
+        for (; loads_v < min(blocks, C::kSlotsV); ++loads_k, ++loads_v) {
+          load(loads_k, first_key, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree);
+          load(loads_v, first_key, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree);
+        }
+      }
     }
   }
+  // the softmax's rows
+  const int token = token0 + ((warp & 3) * 32 + lane) / p.y.per;
+  const bool valid = warp < 8 && (warp & 3) * 32 + lane < p.y.tile_rows && token < p.y.n_q;
+  const int2 span = valid ? span_of(p.spans, token, p.y.n_k) : make_int2(0, 0);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -143,24 +167,12 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     // nothing is seen: the softmax warps write that below
   } else if (warp == 8) {
     if (lane == 0) {
-      mbar_expect_tx(bar(C::kQFull), p.y.tile_rows * D * 2);
-      for (int d = 0; d < D / 64; ++d)
-        tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.y.per, token0, 0);
       // K and V in turn, each when its slot is free (the scores of a block are through before its P V:
-      // no K is kept waiting; a loop that looked at both by turns took the softmax's issue slots)
-      int k = 0, v = 0;
-      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full, int free) {
-        const int slot = n % slots;
-        if (n >= slots && !wait(bar(free + slot), (n / slots - 1) & 1, p.err, ERR_WAIT_MMA)) return false;
-        mbar_expect_tx(bar(full + slot), C::kTileBytes);
-        for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
-                      key_start + n * kTile, 0);
-        return true;
-      };
-      while (v < count && load(k, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree)) {
+      // no K is kept waiting)
+      int k = loads_k, v = loads_v;
+      while (v < count && load(k, key_start, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree)) {
         ++k;
-        if (!load(v, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree)) break;
+        if (!load(v, key_start, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree)) break;
         ++v;
       }
       // nothing may be in flight when the block exits
@@ -172,23 +184,23 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     }
   } else if (warp == 9) {
     // ---- values of keys that nothing sees
-    int2 span[4];
+    int2 spans[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      span[i] = lane + 32 * i < tokens ? span_of(p.spans, token0 + lane + 32 * i, p.y.n_k)
+      spans[i] = lane + 32 * i < tokens ? span_of(p.spans, token0 + lane + 32 * i, p.y.n_k)
                                        : make_int2(0, 0);
     for (int n = 0; n < count; ++n) {
       const int key0 = key_start + n * kTile, slot = n % C::kSlotsV;
       bool whole = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) whole |= span[i].x <= key0 && span[i].y >= key0 + kTile;
+      for (int i = 0; i < 4; ++i) whole |= spans[i].x <= key0 && spans[i].y >= key0 + kTile;
       uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
       if (!__any_sync(0xffffffffu, whole)) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           uint32_t mine = 0;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mine |= seen_word(span[i], key0 + 32 * w);
+          for (int i = 0; i < 4; ++i) mine |= seen_word(spans[i], key0 + 32 * w);
           seen[w] = __reduce_or_sync(0xffffffffu, mine);
         }
       }
@@ -249,9 +261,6 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     // ---- softmax of half h of the blocks' keys
     const int h = warp >> 2, lanes = warp & 3;
     const int row = lanes * 32 + lane;
-    const int token = token0 + row / p.y.per;
-    const bool valid = row < p.y.tile_rows && token < p.y.n_q;
-    const int2 span = valid ? span_of(p.spans, token, p.y.n_k) : make_int2(0, 0);
     const bool sees = span.x < span.y;
     // keys that all of the warp's rows see (rows that see none, or are none, are set right at the end)
     const int all_from = __reduce_max_sync(0xffffffffu, sees ? span.x : 0);

@@ -228,11 +228,17 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
   const int key0 = kb * kTile;
 
   // rows past tile_rows are never loaded
-  for (int i = threadIdx.x; i < C::kStages * 2 * C::kTileBytes / 16; i += C::kThreads)
-    reinterpret_cast<uint4*>(smem + C::kOffRing)[i] = make_uint4(0, 0, 0, 0);
-  fence_proxy_async_smem();
-  if (threadIdx.x == 0) {
+  if (p.y.tile_rows < kTile) {
+    for (int i = threadIdx.x; i < C::kStages * 2 * C::kTileBytes / 16; i += C::kThreads)
+      reinterpret_cast<uint4*>(smem + C::kOffRing)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  if (threadIdx.x == 19 * 32) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmDo);
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
     mbar_init(bar(C::kKV), 1);
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(bar(C::kFull + i), 1);
@@ -256,6 +262,12 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
   if (warp == 0) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
+  } else if (threadIdx.x == 19 * 32 && aligned) {
+    mbar_expect_tx(bar(C::kKV), 2 * C::kTileBytes);
+    for (int d = 0; d < D / 64; ++d) {
+      tma_load_4d(base + d * kSub, &tmK, bar(C::kKV), 64 * d, group, key0, 0);
+      tma_load_4d(base + C::kOffV + d * kSub, &tmV, bar(C::kKV), 64 * d, group, key0, 0);
+    }
   }
   __syncthreads();
   {
@@ -290,7 +302,8 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
   const float ds_down = F16 ? *down : 1.f;  // dS is kept times this
 
   if (count == 0) {
-    // no row sees any of the keys
+    // no row sees any of the keys (which may be on their way)
+    if (threadIdx.x == 19 * 32 && aligned) wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
   } else if (warp == 16 || warp == 17) {
     // ---- X = K Q^T (16), Y = V dout^T (17), and zeros for the rows of queries that see nothing:
     // their P and dS are 0, but 0 times NaN is NaN
@@ -354,14 +367,8 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
     };
     int loaded = 0;
     if (dk) {
-      if (lane == 0) {
-        mbar_expect_tx(bar(C::kKV), 2 * C::kTileBytes);
-        for (int d = 0; d < D / 64; ++d) {
-          tma_load_4d(base + d * kSub, &tmK, bar(C::kKV), 64 * d, group, key0, 0);
-          tma_load_4d(base + C::kOffV + d * kSub, &tmV, bar(C::kKV), 64 * d, group, key0, 0);
-        }
+      if (lane == 0)
         for (int i = 0; i < min(count, C::kStages); ++i) load(i);
-      }
       loaded = min(count, C::kStages);
       __syncwarp();
     }
@@ -614,11 +621,18 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
   const int token0 = tile * p.y.tile_tokens;
 
   // rows past tile_rows are never loaded
-  for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += C::kThreads)
-    reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
-  fence_proxy_async_smem();
-  if (threadIdx.x == 0) {
+  if (p.y.tile_rows < kTile) {
+    for (int i = threadIdx.x; i < 2 * C::kTileBytes / 16; i += C::kThreads)
+      reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+    __syncthreads();  // before q and dout are loaded
+  }
+  if (threadIdx.x == 16 * 32) {
     if (!aligned) atomicOr(p.err, ERR_SMEM_ALIGN);
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmDo);
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
     mbar_init(bar(C::kQ), 1);
     for (int i = 0; i < C::kSlotsK; ++i) {
       mbar_init(bar(C::kKFull + i), 1);
@@ -646,39 +660,44 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
     if (lane == 0) *down = f;
   }
   const int4 m = __ldcg(p.limits + tile);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
   const int b0 = m.y > 0 ? m.x / kTile : 0;
   const int n = aligned && m.y > 0 ? (m.y + kTile - 1) / kTile - b0 : 0;
   const int block0 = b0 + static_cast<int>(static_cast<int64_t>(n) * part / p.q_parts);
   const int count = b0 + static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.q_parts) - block0;
+  // K or V of block n; waits for its slot after the first ones
+  auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full, int free) {
+    const int slot = n % slots;
+    if (n >= slots && !wait(bar(free + slot), (n / slots - 1) & 1, p.err, ERR_WAIT_MMA)) return false;
+    mbar_expect_tx(bar(full + slot), C::kTileBytes);
+    for (int d = 0; d < D / 64; ++d)
+      tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
+                  (block0 + n) * kTile, 0);
+    return true;
+  };
+  int loads_k = 0, loads_v = 0;  // warp 16: so far
+  if (threadIdx.x == 16 * 32 && count > 0) {  // what there is room for, while the others get ready
+    mbar_expect_tx(bar(C::kQ), 2 * p.y.tile_rows * D * 2);
+    for (int d = 0; d < D / 64; ++d) {
+      tma_load_4d(base + d * kSub, &tmQ, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
+      tma_load_4d(base + C::kOffDo + d * kSub, &tmDo, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
+    }
+    for (; loads_v < min(count, C::kSlotsV); ++loads_k, ++loads_v) {
+      load(loads_k, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree);
+      load(loads_v, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
   const float ds_down = F16 ? *down : 1.f;
 
   if (count == 0) {
     // no row sees any key
   } else if (warp == 16) {
     if (lane == 0) {
-      prefetch_tmap(&tmK);
-      prefetch_tmap(&tmV);
-      mbar_expect_tx(bar(C::kQ), 2 * p.y.tile_rows * D * 2);
-      for (int d = 0; d < D / 64; ++d) {
-        tma_load_4d(base + d * kSub, &tmQ, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
-        tma_load_4d(base + C::kOffDo + d * kSub, &tmDo, bar(C::kQ), 64 * d, group * p.y.per, token0, 0);
-      }
-      // K and V in turn, each when its slot is free (blocking waits: a loop that looked at both by turns
-      // took the other warps' issue slots)
-      int k = 0, v = 0;
-      auto load = [&](int n, const CUtensorMap* map, uint32_t to, int slots, int full, int free) {
-        const int slot = n % slots;
-        if (n >= slots && !wait(bar(free + slot), (n / slots - 1) & 1, p.err, ERR_WAIT_MMA)) return false;
-        mbar_expect_tx(bar(full + slot), C::kTileBytes);
-        for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(to + slot * C::kTileBytes + d * kSub, map, bar(full + slot), 64 * d, group,
-                      (block0 + n) * kTile, 0);
-        return true;
-      };
+      // K and V in turn, each when its slot is free
+      int k = loads_k, v = loads_v;
       while (v < count && load(k, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree)) {
         ++k;
         if (!load(v, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree)) break;

@@ -59,7 +59,8 @@ struct FwdCfg {
 template <bool F16, int D>
 __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     span_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ SpanFwd p) {
+                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
+                    const __grid_constant__ SpanFwd p) {
   using C = FwdCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -90,6 +91,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     prefetch_tmap(&tmQ);
     prefetch_tmap(&tmK);
     prefetch_tmap(&tmV);
+    prefetch_tmap(&tmO);
     mbar_init(bar(C::kQFull), 1);
     for (int i = 0; i < C::kSlotsK; ++i) {
       mbar_init(bar(C::kKFull + i), 1);
@@ -123,6 +125,12 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     tmem_alloc(smem_u32(tmem_slot), 256);
     tmem_relinquish();
   } else if (warp == 8) {
+    if (lane == 0 && aligned) {
+      mbar_expect_tx(bar(C::kQFull), p.y.tile_rows * D * 2);
+      for (int d = 0; d < D / 64; ++d)
+        tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.y.per, token0, 0);
+    }
+    __syncwarp();
     // the keys that any query of the tile sees, and this block's part of them
     int lo = 0x7fffffff, hi = 0;
     for (int i = lane; i < tokens; i += 32) {
@@ -142,14 +150,10 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     if (lane == 0) {
       range[0] = first_key;
       range[1] = blocks;
-      if (blocks > 0) {  // what there is room for, while the others get ready
-        mbar_expect_tx(bar(C::kQFull), p.y.tile_rows * D * 2);
-        for (int d = 0; d < D / 64; ++d)
-          tma_load_4d(base + d * kSub, &tmQ, bar(C::kQFull), 64 * d, group * p.y.per, token0, 0);
-        for (; loads_v < min(blocks, C::kSlotsV); ++loads_k, ++loads_v) {
-          load(loads_k, first_key, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree);
-          load(loads_v, first_key, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree);
-        }
+      // what there is room for, while the others get ready
+      for (; loads_v < min(blocks, C::kSlotsV); ++loads_k, ++loads_v) {
+        load(loads_k, first_key, &tmK, base + C::kOffK, C::kSlotsK, C::kKFull, C::kKFree);
+        load(loads_v, first_key, &tmV, base + C::kOffV, C::kSlotsV, C::kVFull, C::kVFree);
       }
     }
   }
@@ -164,7 +168,8 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
   const int key_start = range[0], count = range[1];
 
   if (count == 0) {
-    // nothing is seen: the softmax warps write that below
+    // nothing is seen: the softmax warps write that below, where Q may be on its way to
+    if (threadIdx.x < 8 * 32 && aligned) wait_warp(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA);
   } else if (warp == 8) {
     if (lane == 0) {
       // K and V in turn, each when its slot is free (the scores of a block are through before its P V:
@@ -378,8 +383,6 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     const bool whole = p.parts == 1;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int head = group * p.y.per + row % p.y.per;
-    uint16_t* out = static_cast<uint16_t*>(p.out.p) + static_cast<int64_t>(token) * p.out.token +
-                    static_cast<int64_t>(head) * p.out.head;
     const int64_t slot =
         ((static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.parts + part) * kTile + row;
 #pragma unroll 1
@@ -390,8 +393,8 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
         tmem_ld_32x32b_x32(tmem + lane_off + C::kColO + d, o);
         tmem_ld_wait();
       }
-      if (!valid) continue;
       if (whole) {
+        // into Q's place, which the last scores have read
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
           uint32_t v[4];
@@ -400,9 +403,9 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
             v[i] = l == 0.f ? 0u
                             : pack16<F16>(__uint_as_float(o[e + 2 * i]) * inv,
                                           __uint_as_float(o[e + 2 * i + 1]) * inv);
-          *reinterpret_cast<uint4*>(out + d + e) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4*>(smem + tile_chunk(row, (d + e) / 8)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-      } else if (l != 0.f) {
+      } else if (valid && l != 0.f) {
 #pragma unroll
         for (int e = 0; e < 32; e += 4)
           *reinterpret_cast<uint4*>(p.part_o + slot * D + d + e) =
@@ -415,6 +418,16 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
             l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       else
         p.part_ml[slot] = make_float2(m, l);
+    }
+    if (whole) {
+      fence_proxy_async_smem();
+      named_barrier(5, 256);
+      if (threadIdx.x == 0 && aligned) {
+        for (int d = 0; d < D / 64; ++d)
+          tma_store_4d(&tmO, base + d * kSub, 64 * d, group * p.y.per, token0, 0);
+        bulk_commit();
+        bulk_wait_all();
+      }
     }
     tc_fence_before();
   }
@@ -496,8 +509,10 @@ template <bool F16, int D>
 cudaError_t launch_fwd(const SpanFwd& p, const SpanRows& q, const SpanRows& k, const SpanRows& v,
                        cudaStream_t s) {
   using C = FwdCfg<D>;
-  CUtensorMap tmQ, tmK, tmV;
-  if (!make_map(&tmQ, F16, q.p, D, p.y.heads, p.y.n_q, 1, q.head, q.token, 0, p.y.per, p.y.tile_tokens) ||
+  CUtensorMap tmQ, tmK, tmV, tmO;
+  if (!make_map(&tmO, F16, p.out.p, D, p.y.heads, p.y.n_q, 1, p.out.head, p.out.token, 0, p.y.per,
+                p.y.tile_tokens) ||
+      !make_map(&tmQ, F16, q.p, D, p.y.heads, p.y.n_q, 1, q.head, q.token, 0, p.y.per, p.y.tile_tokens) ||
       !make_map(&tmK, F16, k.p, D, p.y.groups, p.y.n_k, 1, k.head, k.token, 0, 1, kTile) ||
       !make_map(&tmV, F16, v.p, D, p.y.groups, p.y.n_k, 1, v.head, v.token, 0, 1, kTile))
     return cudaErrorInvalidValue;
@@ -511,7 +526,7 @@ cudaError_t launch_fwd(const SpanFwd& p, const SpanRows& q, const SpanRows& k, c
     });
   if (e != cudaSuccess) return e;
   e = launch_pdl(span_fwd_kernel<F16, D>, dim3(p.y.row_tiles * p.parts, p.y.groups), dim3(C::kThreads),
-                 C::kSmem, s, tmQ, tmK, tmV, p);
+                 C::kSmem, s, tmQ, tmK, tmV, tmO, p);
   if (e != cudaSuccess || p.parts == 1) return e;
   return launch_pdl(span_join_kernel<F16, D>, dim3(p.y.n_q, p.y.heads), dim3(256), 0, s, p);
 }

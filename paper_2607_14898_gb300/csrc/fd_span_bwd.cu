@@ -26,8 +26,8 @@ struct SpanBwd {
   float* stat;    // [group][row tile] records of kRecord: see below
   int4* limits;   // of each row tile, those of its records
   float* most;    // [group][row tile]: the largest |dout| (fp16)
-  float* part_q;  // [group][row tile][part][128][D]
-  float* part_k;  // [group][key block][part][dk, dv][128][D]
+  float* part_q;  // [group][row tile][part][D / 4][128 rows] of four
+  float* part_k;  // [group][key block][part][dk, dv][D / 4][128 keys] of four
   int* err;
 };
 
@@ -183,26 +183,38 @@ __device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
     tmem_st_32x32b_x8(at, r);
 }
 
-// 16 (or 32) columns of an accumulator times f to a row of a matrix of 16-bit elements or of floats
+// 16 columns of an accumulator times f, columns d.. of a row: into a tile in shared memory (rows that are not
+// `here` as zeros), or as floats to a part's place, [D / 4][128] of four.
 template <bool F16>
-__device__ __forceinline__ void leave16(uint32_t at, float f, uint16_t* to, float* part, bool here) {
+__device__ __forceinline__ void leave16(uint32_t at, float f, bool here, uint8_t* tile, float4* part, int row,
+                                        int d) {
   uint32_t a[16];
   tmem_ld_32x32b_x16(at, a);
   tmem_ld_wait();
-  if (!here) return;
   float o[16];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(a[e]) * f;
+  for (int e = 0; e < 16; ++e) o[e] = here ? __uint_as_float(a[e]) * f : 0.f;
   if (part == nullptr) {
 #pragma unroll
     for (int e = 0; e < 16; e += 8)
-      *reinterpret_cast<uint4*>(to + e) =
+      *reinterpret_cast<uint4*>(tile + tile_chunk(row, (d + e) / 8)) =
           make_uint4(pack16<F16>(o[e], o[e + 1]), pack16<F16>(o[e + 2], o[e + 3]),
                      pack16<F16>(o[e + 4], o[e + 5]), pack16<F16>(o[e + 6], o[e + 7]));
   } else {
 #pragma unroll
     for (int e = 0; e < 16; e += 4)
-      *reinterpret_cast<float4*>(part + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+      part[(d + e) / 4 * kTile + row] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+  }
+}
+// the same of zeros
+__device__ __forceinline__ void leave16_none(uint8_t* tile, float4* part, int row, int d) {
+  if (part == nullptr) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 8)
+      *reinterpret_cast<uint4*>(tile + tile_chunk(row, (d + e) / 8)) = make_uint4(0, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) part[(d + e) / 4 * kTile + row] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
 }
 
@@ -210,6 +222,7 @@ template <bool F16, int D>
 __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
     span_keys_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
                      const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ CUtensorMap tmDk, const __grid_constant__ CUtensorMap tmDv,
                      const __grid_constant__ SpanBwd p) {
   using C = KeyCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -302,8 +315,8 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
   const float ds_down = F16 ? *down : 1.f;  // dS is kept times this
 
   if (count == 0) {
-    // no row sees any of the keys (which may be on their way)
-    if (threadIdx.x == 19 * 32 && aligned) wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
+    // no row sees any of the keys (which may be on their way to where zeros leave from)
+    if (warp < 16 && aligned) wait_warp(bar(C::kKV), 0, p.err, ERR_WAIT_TMA);
   } else if (warp == 16 || warp == 17) {
     // ---- X = K Q^T (16), Y = V dout^T (17), and zeros for the rows of queries that see nothing:
     // their P and dS are 0, but 0 times NaN is NaN
@@ -536,32 +549,32 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
       wait_warp(bar(C::kDsDone), (k - 1) & 1, p.err, ERR_WAIT_MMA);
     }
     tc_fence_after();
-    const bool here = key < p.y.n_k;
-    const int64_t slot =
-        ((static_cast<int64_t>(group) * p.y.key_blocks + kb) * p.k_parts + part) * 2 * kTile +
-        (warp & 3) * 32 + lane;
+    // dk goes through K's place in shared memory, dv through V's: the last products are through
+    const int row = (warp & 3) * 32 + lane;
+    const int64_t slot = ((static_cast<int64_t>(group) * p.y.key_blocks + kb) * p.k_parts + part) * 2;
+    float4* part_k = p.k_parts > 1 ? reinterpret_cast<float4*>(p.part_k) + slot * (D / 4) * kTile : nullptr;
+    float4* part_v = p.k_parts > 1 ? part_k + D / 4 * kTile : nullptr;
     const float fk = p.scale / ds_down, fv = F16 ? 1.f / kPUp : 1.f;
 #pragma unroll 1
     for (int d = q * (D / 4); d < (q + 1) * (D / 4); d += 16) {
-      uint16_t* dk = static_cast<uint16_t*>(p.dk.p) + key * p.dk.token + group * p.dk.head + d;
-      uint16_t* dv = static_cast<uint16_t*>(p.dv.p) + key * p.dv.token + group * p.dv.head + d;
-      float* part_k = p.k_parts > 1 ? p.part_k + slot * D + d : nullptr;
-      float* part_v = p.k_parts > 1 ? p.part_k + (slot + kTile) * D + d : nullptr;
       if (count > 0) {
-        leave16<F16>(tmem + lane_off + C::kColDk + d, fk, dk, part_k, here);
-        leave16<F16>(tmem + lane_off + C::kColDv + d, fv, dv, part_v, here);
-      } else if (here) {
-#pragma unroll
-        for (int e = 0; e < 16; e += 8) {
-          const uint4 z = make_uint4(0, 0, 0, 0);
-          if (part_k == nullptr) {
-            *reinterpret_cast<uint4*>(dk + e) = z;
-            *reinterpret_cast<uint4*>(dv + e) = z;
-          } else {
-            *reinterpret_cast<uint4*>(part_k + e) = *reinterpret_cast<uint4*>(part_k + e + 4) = z;
-            *reinterpret_cast<uint4*>(part_v + e) = *reinterpret_cast<uint4*>(part_v + e + 4) = z;
-          }
+        leave16<F16>(tmem + lane_off + C::kColDk + d, fk, true, smem, part_k, row, d);
+        leave16<F16>(tmem + lane_off + C::kColDv + d, fv, true, smem + C::kOffV, part_v, row, d);
+      } else {
+        leave16_none(smem, part_k, row, d);
+        leave16_none(smem + C::kOffV, part_v, row, d);
+      }
+    }
+    if (p.k_parts == 1) {
+      fence_proxy_async_smem();
+      named_barrier(1, 512);
+      if (threadIdx.x == 0 && aligned) {
+        for (int d = 0; d < D / 64; ++d) {
+          tma_store_4d(&tmDk, base + d * kSub, 64 * d, group, key0, 0);
+          tma_store_4d(&tmDv, base + C::kOffV + d * kSub, 64 * d, group, key0, 0);
         }
+        bulk_commit();
+        bulk_wait_all();
       }
     }
     tc_fence_before();
@@ -603,7 +616,7 @@ template <bool F16, int D>
 __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
     span_query_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
                       const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                      const __grid_constant__ SpanBwd p) {
+                      const __grid_constant__ CUtensorMap tmDq, const __grid_constant__ SpanBwd p) {
   using C = QueryCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -787,8 +800,6 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
   if (warp < 16) {
     // ---- dS of a quarter of each block's keys
     const int q = warp >> 2, row = (warp & 3) * 32 + lane;
-    const int token = token0 + row / p.y.per, head = group * p.y.per + row % p.y.per;
-    const bool valid = row < p.y.tile_rows && token < p.y.n_q;
     const float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord + row;
     const float neg_lse = __ldcg(stat), neg_delta = __ldcg(stat + kTile);
     const int2 span = make_int2(__ldcg(reinterpret_cast<const int*>(stat) + 2 * kTile),
@@ -858,23 +869,25 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
     }
     if (count > 0) wait_warp(bar(C::kDsDone), (count - 1) & 1, p.err, ERR_WAIT_MMA);
     tc_fence_after();
-    const int64_t slot =
-        ((static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.q_parts + part) * kTile + row;
+    // dq goes through q's place in shared memory
+    const int64_t slot = (static_cast<int64_t>(group) * p.y.row_tiles + tile) * p.q_parts + part;
+    float4* part_q = p.q_parts > 1 ? reinterpret_cast<float4*>(p.part_q) + slot * (D / 4) * kTile : nullptr;
     const float f = p.scale / ds_down;
 #pragma unroll 1
     for (int d = q * (D / 4); d < (q + 1) * (D / 4); d += 16) {
-      uint16_t* dq = static_cast<uint16_t*>(p.dq.p) + token * p.dq.token + head * p.dq.head + d;
-      float* part_q = p.q_parts > 1 ? p.part_q + slot * D + d : nullptr;
-      if (count > 0) leave16<F16>(tmem + lane_off + C::kColDq + d, f, dq, part_q, valid && sees);
-      if (valid && (!sees || count == 0)) {
-#pragma unroll
-        for (int e = 0; e < 16; e += 8) {
-          const uint4 z = make_uint4(0, 0, 0, 0);
-          if (part_q == nullptr)
-            *reinterpret_cast<uint4*>(dq + e) = z;
-          else
-            *reinterpret_cast<uint4*>(part_q + e) = *reinterpret_cast<uint4*>(part_q + e + 4) = z;
-        }
+      if (count > 0)
+        leave16<F16>(tmem + lane_off + C::kColDq + d, f, sees, smem, part_q, row, d);
+      else
+        leave16_none(smem, part_q, row, d);
+    }
+    if (p.q_parts == 1) {
+      fence_proxy_async_smem();
+      named_barrier(1, 512);
+      if (threadIdx.x == 0 && aligned) {
+        for (int d = 0; d < D / 64; ++d)
+          tma_store_4d(&tmDq, base + d * kSub, 64 * d, group * p.y.per, token0, 0);
+        bulk_commit();
+        bulk_wait_all();
       }
     }
     tc_fence_before();
@@ -887,43 +900,43 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
 }
 
 // ------------------------------------------------------------------------------ parts added up
-// in their order: a thread per eight elements
+// in their order: a thread per row (neighbours in a warp) and eight elements
 template <bool F16, int D>
-__global__ void __launch_bounds__(256) span_sums_kernel(const __grid_constant__ SpanBwd p) {
+__global__ void __launch_bounds__(kTile) span_sums_kernel(const __grid_constant__ SpanBwd p) {
   grid_dep_wait();
   grid_dep_launch();
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 * 8 / D) + threadIdx.x / (D / 8);
-  const int d = threadIdx.x % (D / 8) * 8;
-  const float* from;
+  const int row = threadIdx.x, d = blockIdx.y * 8, which = blockIdx.z;  // dq, dk, dv
+  const float4* from;
   uint16_t* to;
   int parts;
   int64_t step;
-  if (blockIdx.y == 0) {
-    if (p.q_parts == 1 || i >= static_cast<int64_t>(p.y.n_q) * p.y.heads) return;
-    const int token = static_cast<int>(i / p.y.heads), head = static_cast<int>(i % p.y.heads);
-    const int tile = token / p.y.tile_tokens;
-    const int row = (token - tile * p.y.tile_tokens) * p.y.per + head % p.y.per;
+  if (which == 0) {
+    if (p.q_parts == 1) return;
+    const int tile = static_cast<int>(blockIdx.x) / p.y.groups, group = static_cast<int>(blockIdx.x) % p.y.groups;
+    const int token = tile * p.y.tile_tokens + row / p.y.per, head = group * p.y.per + row % p.y.per;
+    if (tile >= p.y.row_tiles || row >= p.y.tile_rows || token >= p.y.n_q) return;
     parts = p.q_parts;
-    step = kTile * D;
-    from = p.part_q + ((static_cast<int64_t>(head / p.y.per) * p.y.row_tiles + tile) * parts * kTile + row) * D + d;
+    step = D / 4 * kTile;
+    from = reinterpret_cast<const float4*>(p.part_q) +
+           (static_cast<int64_t>(group) * p.y.row_tiles + tile) * parts * step;
     to = static_cast<uint16_t*>(p.dq.p) + token * p.dq.token + head * p.dq.head + d;
   } else {
-    if (p.k_parts == 1 || i >= static_cast<int64_t>(p.y.n_k) * p.y.groups) return;
-    const bool v = blockIdx.y == 2;
-    const int key = static_cast<int>(i / p.y.groups), group = static_cast<int>(i % p.y.groups);
+    if (p.k_parts == 1) return;
+    const int kb = static_cast<int>(blockIdx.x) / p.y.groups, group = static_cast<int>(blockIdx.x) % p.y.groups;
+    const int key = kb * kTile + row;
+    if (kb >= p.y.key_blocks || key >= p.y.n_k) return;
     parts = p.k_parts;
-    step = 2 * kTile * D;
-    from = p.part_k +
-           ((static_cast<int64_t>(group) * p.y.key_blocks + key / kTile) * parts * 2 * kTile +
-            (v ? kTile : 0) + key % kTile) * D + d;
-    const SpanRows& r = v ? p.dv : p.dk;
+    step = 2 * (D / 4) * kTile;
+    from = reinterpret_cast<const float4*>(p.part_k) +
+           (static_cast<int64_t>(group) * p.y.key_blocks + kb) * parts * step + (which == 2 ? D / 4 * kTile : 0);
+    const SpanRows& r = which == 2 ? p.dv : p.dk;
     to = static_cast<uint16_t*>(r.p) + key * r.token + group * r.head + d;
   }
+  from += d / 4 * kTile + row;
   float sum[8] = {};
 #pragma unroll 4
   for (int c = 0; c < parts; ++c) {
-    const float4 a = __ldcg(reinterpret_cast<const float4*>(from + c * step));
-    const float4 b = __ldcg(reinterpret_cast<const float4*>(from + c * step + 4));
+    const float4 a = __ldcg(from + c * step), b = __ldcg(from + c * step + kTile);
     sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w;
     sum[4] += b.x, sum[5] += b.y, sum[6] += b.z, sum[7] += b.w;
   }
@@ -972,12 +985,16 @@ BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
 template <bool F16, int D>
 cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, const SpanRows& v,
                        cudaStream_t s) {
-  CUtensorMap tmQ, tmDo, tmK, tmV;
+  CUtensorMap tmQ, tmDo, tmK, tmV, tmDq, tmDk, tmDv;
   if (!make_map(&tmQ, F16, q.p, D, p.y.heads, p.y.n_q, 1, q.head, q.token, 0, p.y.per, p.y.tile_tokens) ||
       !make_map(&tmDo, F16, p.dout.p, D, p.y.heads, p.y.n_q, 1, p.dout.head, p.dout.token, 0, p.y.per,
                 p.y.tile_tokens) ||
       !make_map(&tmK, F16, k.p, D, p.y.groups, p.y.n_k, 1, k.head, k.token, 0, 1, kTile) ||
-      !make_map(&tmV, F16, v.p, D, p.y.groups, p.y.n_k, 1, v.head, v.token, 0, 1, kTile))
+      !make_map(&tmV, F16, v.p, D, p.y.groups, p.y.n_k, 1, v.head, v.token, 0, 1, kTile) ||
+      !make_map(&tmDq, F16, p.dq.p, D, p.y.heads, p.y.n_q, 1, p.dq.head, p.dq.token, 0, p.y.per,
+                p.y.tile_tokens) ||
+      !make_map(&tmDk, F16, p.dk.p, D, p.y.groups, p.y.n_k, 1, p.dk.head, p.dk.token, 0, 1, kTile) ||
+      !make_map(&tmDv, F16, p.dv.p, D, p.y.groups, p.y.n_k, 1, p.dv.head, p.dv.token, 0, 1, kTile))
     return cudaErrorInvalidValue;
   static OncePerDevice once;
   int dev = 0;
@@ -995,16 +1012,14 @@ cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, c
     e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles, p.y.groups), dim3(256), 0, s, p);
   if (e == cudaSuccess)
     e = launch_pdl(span_keys_kernel<F16, D>, dim3(p.y.key_blocks * p.k_parts, p.y.groups),
-                   dim3(KeyCfg<D>::kThreads), KeyCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, p);
+                   dim3(KeyCfg<D>::kThreads), KeyCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, tmDk, tmDv, p);
   if (e == cudaSuccess)
     e = launch_pdl(span_query_kernel<F16, D>, dim3(p.y.row_tiles * p.q_parts, p.y.groups),
-                   dim3(QueryCfg<D>::kThreads), QueryCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, p);
+                   dim3(QueryCfg<D>::kThreads), QueryCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, tmDq, p);
   if (e != cudaSuccess || (p.q_parts == 1 && p.k_parts == 1)) return e;
-  const int64_t rows = std::max(p.q_parts > 1 ? static_cast<int64_t>(p.y.n_q) * p.y.heads : 0,
-                                p.k_parts > 1 ? static_cast<int64_t>(p.y.n_k) * p.y.groups : 0);
-  constexpr int kRows = 256 * 8 / D;
-  return launch_pdl(span_sums_kernel<F16, D>, dim3(static_cast<unsigned>((rows + kRows - 1) / kRows), 3),
-                    dim3(256), 0, s, p);
+  const int64_t tiles = std::max(p.q_parts > 1 ? p.y.row_tiles : 0, p.k_parts > 1 ? p.y.key_blocks : 0);
+  return launch_pdl(span_sums_kernel<F16, D>, dim3(static_cast<unsigned>(tiles * p.y.groups), D / 8, 3),
+                    dim3(kTile), 0, s, p);
 }
 
 }  // namespace

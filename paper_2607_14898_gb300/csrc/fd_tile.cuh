@@ -156,6 +156,13 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* er
 constexpr int kTile = 128;      // rows of a tile, slots of a block
 constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swizzled sub-tile
 
+// Where 16 bytes, elements 8 chunk .. 8 chunk + 7 of a row, are in a tile of swizzled sub-tiles. A tile
+// that goes to memory by TMA is put together there: a row is a thread's, and rows stored by threads
+// take a cycle of the SM for every 32 bytes of each (4200 cycles at the end of every tile of 128 x 128).
+__device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) {
+  return static_cast<uint32_t>((chunk >> 3) * kSub + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+}
+
 // 4D map over 16-bit elements, strides in elements, boxes of 64 x b1 x b2 x 1
 inline bool make_map(CUtensorMap* m, bool f16, const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
               uint64_t d3, int64_t s1, int64_t s2, int64_t s3, uint32_t b1, uint32_t b2) {

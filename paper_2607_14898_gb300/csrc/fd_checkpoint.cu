@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads)
   for (int j = 0; j < kPerThread; ++j) {
     float v[8];
     widen(raw[j], v);
-    const uint32_t byte = kept_exponent(block_top(v));
+    const uint32_t byte = kept_exponent(block_top(raw[j]));
     if (unit[j] < 0) continue;
     if (unit[j] < p.width / 8)
       *reinterpret_cast<uint2*>(codes + row[j] * p.width + unit[j] * 8) = kept_codes(v, byte);
@@ -101,19 +101,19 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// Transposed: x[column][row]. A block turns 256 rows by 64 columns over in shared memory: codes are
-// read by whole sectors of a row, and a column's values leave as aligned 16-byte stores. Columns begin
-// at any address (rows may be odd), so a vector may reach over the tile's end: it is the tile's that has
-// its first element, which has the next rows too for that. Only a column's own two ends are stored by
-// elements. (Tiles of 128 x 128 that stored their ends by elements took 74 us for 16001 x 4096.)
-constexpr int kTileRows = 256, kTileCols = 64;
+// Transposed: x[column][row]. A block turns 128 rows by 64 columns over in shared memory (256 rows, of
+// which an SM holds fewer blocks, took 64 us instead of 50 for 16001 x 4096): codes are read by whole sectors of a row, two rows a thread (whose 16-bit values go into shared memory as one
+// word), and a column's values leave as aligned 16-byte stores. Columns begin at any address (rows may be
+// odd), so a vector may reach over the tile's end: it is the tile's that has its first element, which
+// has the next rows too for that. Only a column's own two ends are stored by elements.
+constexpr int kTileRows = 128, kTileCols = 64;
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
     load_transposed_kernel(int rows, int width, const int8_t* codes, const uint8_t* exps, T* x,
                            int64_t stride) {
   constexpr int kVec = 16 / sizeof(T);
-  constexpr int kAll = kTileRows + 8;             // with the next tile's first rows
+  constexpr int kAll = kTileRows + 16;            // with the next tile's first rows
   constexpr int kPitch = kAll + 4 / sizeof(T);    // an odd number of 32-bit words
   extern __shared__ __align__(16) uint8_t smem[];
   T* tile = reinterpret_cast<T*>(smem);  // [column][row]
@@ -122,35 +122,49 @@ __global__ void __launch_bounds__(kThreads)
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileRows;
   const int col0 = blockIdx.y * kTileCols;
   const int blocks = (width + kKeptBlock - 1) / kKeptBlock;
-  // lanes: 4 groups of eight columns (a sector) by 8 rows
+  // lanes: 4 groups of eight columns (a sector) by 8 pairs of rows; warps: runs of 16 rows by 32 columns
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int r_in = lane >> 2, u_in = lane & 3;
-  constexpr int kRuns = kAll / 8 * (kTileCols / 32);  // 33 runs of 8 rows by 2 of 32 columns
+  const int u_in = lane & 3;
+  constexpr int kRuns = kAll / 16 * (kTileCols / 32);
   constexpr int kSteps = (kRuns + kThreads / 32 - 1) / (kThreads / 32);
-  uint2 raw[kSteps];
-  uint32_t byte[kSteps];
+  const int col = col0 + (warp & 1) * 32 + u_in * 8;  // (an even number of warps)
+  const int64_t first_row = row0 + (warp >> 1) * 16 + (lane >> 2) * 2;
+  const int8_t* from = codes + first_row * width + col;
+  const uint8_t* exp_from = exps + first_row * blocks + col / kKeptBlock;
+  constexpr int kRowStep = kThreads / 64 * 16;  // rows from a warp's run to its next
+  uint2 raw[kSteps][2];
+  uint32_t byte[kSteps][2];
 #pragma unroll
-  for (int j = 0; j < kSteps; ++j) {
-    const int step = j * (kThreads / 32) + warp;
-    const int64_t row = row0 + (step >> 1) * 8 + r_in;
-    const int col = col0 + (step & 1) * 32 + u_in * 8;
-    raw[j] = make_uint2(0u, 0u);
-    byte[j] = 1u;
-    if (step < kRuns && row < rows && col < width) {
-      raw[j] = __ldg(reinterpret_cast<const uint2*>(codes + row * width + col));
-      byte[j] = __ldg(exps + row * blocks + col / kKeptBlock);
+  for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      raw[j][i] = make_uint2(0u, 0u);
+      byte[j][i] = 1u;
+      if (j * (kThreads / 32) + warp < kRuns && first_row + j * kRowStep + i < rows && col < width) {
+        raw[j][i] = __ldg(reinterpret_cast<const uint2*>(from + static_cast<int64_t>(j * kRowStep + i) * width));
+        byte[j][i] = __ldg(exp_from + static_cast<int64_t>(j * kRowStep + i) * blocks);
+      }
     }
-  }
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {
-    const int step = j * (kThreads / 32) + warp;
-    if (step >= kRuns) break;
-    const int r = (step >> 1) * 8 + r_in, c = (step & 1) * 32 + u_in * 8;
-    float v[8];
-    kept_values(raw[j], byte[j], v);
-    into_range<T>(v);
+    if (j * (kThreads / 32) + warp >= kRuns) break;
+    const int r = (warp >> 1) * 16 + (lane >> 2) * 2 + j * kRowStep, c = (warp & 1) * 32 + u_in * 8;
+    float v[2][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) tile[(c + i) * kPitch + r] = T(v[i]);
+    for (int i = 0; i < 2; ++i) {
+      kept_values(raw[j][i], byte[j][i], v[i]);
+      into_range<T>(v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      T* to = tile + (c + i) * kPitch + r;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint32_t*>(to) = pack2(v[0][i], v[1][i], T());
+      } else {
+        to[0] = v[0][i];
+        to[1] = v[1][i];
+      }
+    }
   }
   __syncthreads();
   // elements there are from row0 on, with those of the next tile that a vector may need
@@ -159,36 +173,35 @@ __global__ void __launch_bounds__(kThreads)
   const bool starts = blockIdx.x == 0;
   const int cols = min(kTileCols, width - col0);
   constexpr int kChunks = kTileRows / kVec;
-  // lanes are neighbouring vectors of a column
-  for (int it = threadIdx.x; it < cols * kChunks; it += kThreads) {
-    const int c = it / kChunks, chunk = it % kChunks;
-    T* column = x + static_cast<int64_t>(col0 + c) * stride + row0;
+  constexpr int kColStep = kThreads / kChunks;
+  // neighbouring threads have neighbouring vectors of a column
+  const int chunk = threadIdx.x % kChunks;
+  int c = threadIdx.x / kChunks;
+  T* column = x + static_cast<int64_t>(col0 + c) * stride + row0;
+  const T* in = tile + c * kPitch;
+#pragma unroll 4
+  for (; c < cols; c += kColStep, column += kColStep * stride, in += kColStep * kPitch) {
     const int lead =  // elements up to the first aligned address
-        static_cast<int>((0 - reinterpret_cast<uintptr_t>(column) / sizeof(T)) % kVec);
+        static_cast<int>((0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(column)) / sizeof(T)) % kVec);
     const int first = lead + chunk * kVec;
-    const T* from = tile + c * kPitch;
     if (starts && chunk == 0)
-      for (int e = 0; e < min(lead, count); ++e) column[e] = from[e];
-    if (first >= mine) continue;
+      for (int e = 0; e < min(lead, count); ++e) column[e] = in[e];
     if (first + kVec <= count) {
+      if (first >= mine) continue;
       uint4 v;
       if constexpr (sizeof(T) == 2) {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(from) + (first >> 1);
-        if (first & 1) {
-          v.x = __funnelshift_r(w[0], w[1], 16);
-          v.y = __funnelshift_r(w[1], w[2], 16);
-          v.z = __funnelshift_r(w[2], w[3], 16);
-          v.w = __funnelshift_r(w[3], w[4], 16);
-        } else {
-          v = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(in) + (first >> 1);
+        const uint32_t shift = (first & 1) * 16;
+        const uint32_t a = w[0], b = w[1], d = w[2], e = w[3], f = w[4];
+        v = make_uint4(__funnelshift_r(a, b, shift), __funnelshift_r(b, d, shift),
+                       __funnelshift_r(d, e, shift), __funnelshift_r(e, f, shift));
       } else {
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(from) + first;
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(in) + first;
         v = make_uint4(w[0], w[1], w[2], w[3]);
       }
       *reinterpret_cast<uint4*>(column + first) = v;
-    } else {  // the column's end
-      for (int e = first; e < count; ++e) column[e] = from[e];
+    } else if (first < mine) {  // the column's end
+      for (int e = first; e < count; ++e) column[e] = in[e];
     }
   }
 }
@@ -209,7 +222,7 @@ cudaError_t load_type(bool transposed, int rows, int width, const int8_t* codes,
     return launch_pdl(load_kernel<T>, grid_of(p), dim3(kThreads), 0, s, p, codes, exps,
                       static_cast<T*>(x), stride);
   }
-  constexpr size_t kSmem = kTileCols * (kTileRows + 8 + 4 / sizeof(T)) * sizeof(T);
+  constexpr size_t kSmem = kTileCols * (kTileRows + 16 + 4 / sizeof(T)) * sizeof(T);
   static OncePerDevice once;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -1,6 +1,8 @@
 // Rows of activations for the kernels that work on them element by element (fd_block.cu,
 // fd_checkpoint.cu): eight neighbours at once, as floats, and their 8-bit form.
 #pragma once
+#include <type_traits>
+
 #include "fd_internal.h"
 #include "fd_ptx.cuh"
 
@@ -124,16 +126,18 @@ __device__ __forceinline__ uint2 kept_codes(const float (&x)[8], uint32_t byte) 
   uint32_t c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    float v = x[i];
-    // 64 steps of 2^122 are 2^128: the largest floats stay finite
-    if (byte >= 249u) v = fminf(fmaxf(v, -63.f * 0x1p122f), 63.f * 0x1p122f);
-    c[i] = __float_as_uint(fmaf(v, per_step, 12582912.f));
+    c[i] = __float_as_uint(fmaf(x[i], per_step, 12582912.f));
   }
   auto four = [&](int i) {
     return __byte_perm(__byte_perm(c[i], c[i + 1], 0x0040), __byte_perm(c[i + 2], c[i + 3], 0x0040),
                        0x5410);
   };
-  return make_uint2(four(0), four(4));
+  uint2 r = make_uint2(four(0), four(4));
+  if (byte >= 249u) {  // 64 steps of 2^122 are 2^128: the largest floats stay finite
+    r.x = __vmins4(__vmaxs4(r.x, 0xc1c1c1c1u), 0x3f3f3f3fu);
+    r.y = __vmins4(__vmaxs4(r.y, 0xc1c1c1c1u), 0x3f3f3f3fu);
+  }
+  return r;
 }
 // What eight codes stand for: code + 128 goes into the last bits of 2^23, which is taken off again. (A
 // byte of 255 makes the step infinite and the block NaN: 0 times it.)
@@ -157,13 +161,27 @@ __device__ __forceinline__ Pairs kept_values2(uint2 codes, uint32_t byte) {
                   step2);
   return r;
 }
-// the largest magnitude's bits over the four neighbouring lanes that hold a block (NaN above all)
-__device__ __forceinline__ uint32_t block_top(const float (&x)[8]) {
+// The largest magnitude's bits, as fp32's, over the four neighbouring lanes that hold a block (NaN above
+// all); 16-bit elements are compared two by two as they lie in memory.
+__device__ __forceinline__ uint32_t block_top(const Raw8<float>& r) {
+  const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  for (int i = 0; i < 8; ++i) top = max(top, w[i] & 0x7fffffffu);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   return max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t block_top(const Raw8<T>& r) {
+  const uint32_t m = 0x7fff7fffu;
+  uint32_t top = __vmaxu2(__vmaxu2(r.a.x & m, r.a.y & m), __vmaxu2(r.a.z & m, r.a.w & m));
+  top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  top = max(top & 0xffffu, top >> 16);
+  if constexpr (std::is_same<T, __half>::value)
+    return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(top))));
+  else
+    return top << 16;
 }
 
 }  // namespace fd

@@ -364,7 +364,7 @@ fd_status fd_op_cache_compact(const fd_cache* src, int used, const fd_cache* dst
  * (NaN too). Keys and values that some query sees, and the queries (and their gradients) that see some,
  * are finite. */
 typedef struct {
-  int32_t n_q, n_k;         /* 0..16,777,216; n_q heads <= 2^36                               */
+  int32_t n_q, n_k;         /* 0..16,777,216; n_q heads, n_k groups <= 2^36                   */
   int32_t heads, groups;    /* heads % groups == 0, heads / groups <= 128, heads <= 65,535    */
   int32_t head_dim;         /* 64 or 128                                                      */
   int32_t dtype;            /* FD_DTYPE_BF16 or FD_DTYPE_F16                                  */

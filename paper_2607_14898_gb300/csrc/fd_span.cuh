@@ -63,7 +63,8 @@ inline bool span_valid(const fd_span_attention* a) {
          (a->head_dim == 64 || a->head_dim == 128) &&
          (a->dtype == FD_DTYPE_BF16 || a->dtype == FD_DTYPE_F16) && std::isfinite(a->scale) &&
          a->scale > 0.f && a->n_q <= kMaxSpanTokens && a->n_k <= kMaxSpanTokens &&
-         static_cast<int64_t>(a->n_q) * a->heads <= kMaxSpanRows;
+         static_cast<int64_t>(a->n_q) * a->heads <= kMaxSpanRows &&
+         static_cast<int64_t>(a->n_k) * a->groups <= kMaxSpanRows;
 }
 inline bool span_rows_ok(const SpanRows& r, int tokens, int heads, int head_dim) {
   return span_ptr(r.p, 16) && r.token % 8 == 0 && r.head % 8 == 0 &&

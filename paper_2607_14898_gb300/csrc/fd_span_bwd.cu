@@ -4,8 +4,8 @@
 //   dv = P^T dout,  dk = scale dS^T q  (over the rows of a group's heads),  dq = scale dS k
 //
 //   span_rows   each row's lse and delta, each row tile's limits
-//   span_keys   dk and dv: a block has 128 keys and walks over the row tiles that see some of them
-//   span_query  dq: a block has a row tile and walks over its key blocks
+//   span_grad   keys_block: dk and dv of 128 keys, a walk over the row tiles that see some of them
+//               query_block: dq of a row tile, a walk over its key blocks
 // Scores and dout v^T are computed twice, 7 products for the 5 that are needed, so that every sum stays
 // in one block's TMEM: no atomics, the same bits every time.
 #include <algorithm>
@@ -219,11 +219,10 @@ __device__ __forceinline__ void leave16_none(uint8_t* tile, float4* part, int ro
 }
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
-    span_keys_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
-                     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                     const __grid_constant__ CUtensorMap tmDk, const __grid_constant__ CUtensorMap tmDv,
-                     const __grid_constant__ SpanBwd p) {
+__device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtensorMap& tmDo,
+                                           const CUtensorMap& tmK, const CUtensorMap& tmV,
+                                           const CUtensorMap& tmDk, const CUtensorMap& tmDv,
+                                           const SpanBwd& p, int unit) {
   using C = KeyCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -236,8 +235,8 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
   int* range = reinterpret_cast<int*>(tmem_slot + 1);  // first row tile, the one past the last
   volatile float* down = reinterpret_cast<volatile float*>(tmem_slot + 3);
 
-  const int part = blockIdx.x % p.k_parts, kb = static_cast<int>(blockIdx.x) / p.k_parts;
-  const int group = blockIdx.y;
+  const int part = unit % p.k_parts, kb = unit / p.k_parts % p.y.key_blocks;
+  const int group = unit / (p.k_parts * p.y.key_blocks);
   const int key0 = kb * kTile;
 
   // rows past tile_rows are never loaded
@@ -613,10 +612,9 @@ struct QueryCfg {
 };
 
 template <bool F16, int D>
-__global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
-    span_query_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
-                      const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                      const __grid_constant__ CUtensorMap tmDq, const __grid_constant__ SpanBwd p) {
+__device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtensorMap& tmDo,
+                                            const CUtensorMap& tmK, const CUtensorMap& tmV,
+                                            const CUtensorMap& tmDq, const SpanBwd& p, int unit) {
   using C = QueryCfg<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -628,9 +626,9 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   volatile float* down = reinterpret_cast<volatile float*>(tmem_slot + 1);
 
-  const int part = blockIdx.x % p.q_parts;
-  const int tile = p.y.row_tiles - 1 - static_cast<int>(blockIdx.x) / p.q_parts;
-  const int group = blockIdx.y;
+  const int part = unit % p.q_parts;
+  const int tile = p.y.row_tiles - 1 - unit / p.q_parts % p.y.row_tiles;
+  const int group = unit / (p.q_parts * p.y.row_tiles);
   const int token0 = tile * p.y.tile_tokens;
 
   // rows past tile_rows are never loaded
@@ -899,6 +897,22 @@ __global__ void __launch_bounds__(QueryCfg<D>::kThreads, 1)
   }
 }
 
+// The blocks of keys, which take longest, then those of queries: in one launch the second ones fill the end of
+// the first.
+template <bool F16, int D>
+__global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
+    span_grad_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmDo,
+                     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                     const __grid_constant__ CUtensorMap tmDq, const __grid_constant__ CUtensorMap tmDk,
+                     const __grid_constant__ CUtensorMap tmDv, const __grid_constant__ SpanBwd p) {
+  static_assert(KeyCfg<D>::kThreads == QueryCfg<D>::kThreads, "one launch");
+  const int keys = p.k_parts * p.y.key_blocks * p.y.groups;
+  if (static_cast<int>(blockIdx.x) < keys)
+    keys_block<F16, D>(tmQ, tmDo, tmK, tmV, tmDk, tmDv, p, blockIdx.x);
+  else
+    query_block<F16, D>(tmQ, tmDo, tmK, tmV, tmDq, p, static_cast<int>(blockIdx.x) - keys);
+}
+
 // ------------------------------------------------------------------------------ parts added up
 // in their order: a thread per row (neighbours in a warp) and eight elements
 template <bool F16, int D>
@@ -996,26 +1010,21 @@ cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, c
       !make_map(&tmDk, F16, p.dk.p, D, p.y.groups, p.y.n_k, 1, p.dk.head, p.dk.token, 0, 1, kTile) ||
       !make_map(&tmDv, F16, p.dv.p, D, p.y.groups, p.y.n_k, 1, p.dv.head, p.dv.token, 0, 1, kTile))
     return cudaErrorInvalidValue;
+  constexpr int kSmem = std::max(KeyCfg<D>::kSmem, QueryCfg<D>::kSmem);
   static OncePerDevice once;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess)
     e = once.run(dev, [&] {
-      const cudaError_t a = cudaFuncSetAttribute(
-          span_keys_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, KeyCfg<D>::kSmem);
-      return a != cudaSuccess ? a
-                              : cudaFuncSetAttribute(span_query_kernel<F16, D>,
-                                                     cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     QueryCfg<D>::kSmem);
+      return cudaFuncSetAttribute(span_grad_kernel<F16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  kSmem);
     });
   if (e == cudaSuccess)
     e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles, p.y.groups), dim3(256), 0, s, p);
   if (e == cudaSuccess)
-    e = launch_pdl(span_keys_kernel<F16, D>, dim3(p.y.key_blocks * p.k_parts, p.y.groups),
-                   dim3(KeyCfg<D>::kThreads), KeyCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, tmDk, tmDv, p);
-  if (e == cudaSuccess)
-    e = launch_pdl(span_query_kernel<F16, D>, dim3(p.y.row_tiles * p.q_parts, p.y.groups),
-                   dim3(QueryCfg<D>::kThreads), QueryCfg<D>::kSmem, s, tmQ, tmDo, tmK, tmV, tmDq, p);
+    e = launch_pdl(span_grad_kernel<F16, D>,
+                   dim3((p.y.key_blocks * p.k_parts + p.y.row_tiles * p.q_parts) * p.y.groups),
+                   dim3(KeyCfg<D>::kThreads), kSmem, s, tmQ, tmDo, tmK, tmV, tmDq, tmDk, tmDv, p);
   if (e != cudaSuccess || (p.q_parts == 1 && p.k_parts == 1)) return e;
   const int64_t tiles = std::max(p.q_parts > 1 ? p.y.row_tiles : 0, p.k_parts > 1 ? p.y.key_blocks : 0);
   return launch_pdl(span_sums_kernel<F16, D>, dim3(static_cast<unsigned>(tiles * p.y.groups), D / 8, 3),

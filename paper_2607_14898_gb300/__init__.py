@@ -2,3 +2,4 @@
 from . import flashdec  # noqa: F401
 from .flashdec import Decoder, Weights, decode_chunks, lib, make_config, pack_blob  # noqa: F401
 from .bounded import BoundedStream  # noqa: F401
+from .residual import ResidualAttention  # noqa: F401

@@ -16,7 +16,11 @@
 namespace fd {
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
 constexpr int kMaxSpanTokens = 1 << 24;
+constexpr int64_t kMaxSpanStride = 1ll << 38;  // elements (a tensor map's strides are below 2^40 bytes)
 constexpr int64_t kMaxSpanRows = 1ll << 36;  // (a tile has 65 rows at least: fewer than 2^30 units)
 
 struct SpanShape {
@@ -61,18 +65,22 @@ inline bool span_valid(const fd_span_attention* a) {
   return a != nullptr && a->n_q >= 0 && a->n_k >= 0 && a->groups >= 1 && a->heads >= a->groups &&
          a->heads % a->groups == 0 && a->heads / a->groups <= kTile && a->heads <= 65535 &&
          (a->head_dim == 64 || a->head_dim == 128) &&
-         (a->dtype == FD_DTYPE_BF16 || a->dtype == FD_DTYPE_F16) && std::isfinite(a->scale) &&
+         (a->dtype == FD_DTYPE_BF16 || a->dtype == FD_DTYPE_F16) && std::isfinite(a->scale * kLog2e) &&
          a->scale > 0.f && a->n_q <= kMaxSpanTokens && a->n_k <= kMaxSpanTokens &&
          static_cast<int64_t>(a->n_q) * a->heads <= kMaxSpanRows &&
          static_cast<int64_t>(a->n_k) * a->groups <= kMaxSpanRows;
 }
 inline bool span_rows_ok(const SpanRows& r, int tokens, int heads, int head_dim) {
-  return span_ptr(r.p, 16) && r.token % 8 == 0 && r.head % 8 == 0 &&
+  return span_ptr(r.p, 16) && r.token % 8 == 0 && r.head % 8 == 0 && r.token < kMaxSpanStride &&
+         r.head < kMaxSpanStride &&
          (tokens == 1 || r.token >= head_dim) && (heads == 1 || r.head >= head_dim);
 }
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+// rows that are written: no two share elements (a token's heads lie between tokens, or the other way round)
+inline bool span_out_ok(const SpanRows& r, int tokens, int heads, int head_dim) {
+  return span_rows_ok(r, tokens, heads, head_dim) &&
+         (tokens == 1 || heads == 1 || r.token >= (heads - 1) * r.head + head_dim ||
+          r.head >= (tokens - 1) * r.token + head_dim);
+}
 
 }  // namespace
 

@@ -49,7 +49,8 @@ struct FwdCfg {
   static constexpr int kQFull = 0, kKFull = 1, kKFree = kKFull + kSlotsK, kVFull = kKFree + kSlotsK,
                        kVFree = kVFull + kSlotsV, kVReady = kVFree + kSlotsV,
                        kSFull = kVReady + kSlotsV,
-                       kSRead = kSFull + 1, kPFull = kSRead + 1, kPv = kPFull + 1, kBars = kPv + 1;
+                       kSRead = kSFull + 1, kPFull = kSRead + 1, kPv = kPFull + 1,
+                       kDone = kPv + 1, kBars = kDone + 1;
   static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
   static constexpr uint32_t kColS = 0, kColP = kOwnP ? 128 : 0, kColO = 256 - D;
   static constexpr uint32_t kHalfP = kOwnP ? 32 : 64;  // columns from a half's P to the other's
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     mbar_init(bar(C::kSRead), 8);
     mbar_init(bar(C::kPFull), 8);
     mbar_init(bar(C::kPv), 1);
+    mbar_init(bar(C::kDone), 1);
     fence_barrier_init();
   }
   grid_dep_wait();
@@ -261,6 +263,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
       mma_commit_w(bar(C::kVFree + slot));
       if (!C::kOwnP && j + 1 < count) ok = scores(j + 1);
     }
+    products_done(bar(C::kDone), p.err);
   }
   if (warp < 8) {
     // ---- softmax of half h of the blocks' keys
@@ -286,7 +289,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
       const bool masked = key0 < all_from || key0 + 64 > all_to;
       wait_warp(bar(C::kSFull), j & 1, p.err, ERR_WAIT_MMA);
       tc_fence_after();
-      // 32 scores at a time; they are fetched again for their exponentials
+      // 32 scores at a time; the second 32 are fetched again for their exponentials
       uint32_t sr[32];
       auto hide = [&](int x) {
         if (masked) {
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
       };
       float mx[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 1; x >= 0; --x) {
         tmem_ld_32x32b_x32(s_col + 32 * x, sr);
         tmem_ld_wait();
         hide(x);
@@ -343,14 +346,16 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
       // most. The sums are of P unrounded.
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        tmem_ld_32x32b_x32(s_col + 32 * x, sr);
-        tmem_ld_wait();
-        if (C::kOwnP && x == 1) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(C::kSRead));
+        if (x == 1) {
+          tmem_ld_32x32b_x32(s_col + 32, sr);
+          tmem_ld_wait();
+          if (C::kOwnP) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::kSRead));
+          }
+          hide(1);
         }
-        hide(x);
         uint32_t pk[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
@@ -586,7 +591,7 @@ fd_status fd_op_span_attention(const fd_span_attention* a, const void* q, int64_
       vr{const_cast<void*>(v), v_token_stride, v_head_stride},
       outr{out, out_token_stride, out_head_stride};
   if (!fd::span_rows_ok(qr, a->n_q, a->heads, a->head_dim) ||
-      !fd::span_rows_ok(outr, a->n_q, a->heads, a->head_dim) ||
+      !fd::span_out_ok(outr, a->n_q, a->heads, a->head_dim) ||
       (a->n_k > 0 && (!fd::span_rows_ok(kr, a->n_k, a->groups, a->head_dim) ||
                       !fd::span_rows_ok(vr, a->n_k, a->groups, a->head_dim))) ||
       !fd::span_ptr(spans, 8) || !fd::span_ptr(lse, 4) || !fd::span_ptr(err_dev, 4))

@@ -161,7 +161,7 @@ struct KeyCfg {
   static constexpr int kKV = 0, kFull = 1, kFree = kFull + kStages, kReady = kFree + kStages,
                        kXFull = kReady + kStages, kYFull = kXFull + 1, kXRead = kYFull + 1,
                        kYRead = kXRead + 1, kPFull = kYRead + 1, kDsFull = kPFull + 1,
-                       kPDone = kDsFull + 1, kDsDone = kPDone + 1, kBars = kDsDone + 1;
+                       kPDone = kDsFull + 1, kDsDone = kPDone + 1, kDone = kDsDone + 1, kBars = kDone + 4;
   static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
   static constexpr uint32_t kColX = 0, kColY = kStep, kColP = 2 * kStep, kColDs = kColP + kStep / 2,
                             kColDv = 512 - 2 * D, kColDk = 512 - D;
@@ -264,6 +264,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
     mbar_init(bar(C::kPFull), 16);
     mbar_init(bar(C::kDsFull), 16);
     mbar_init(bar(C::kPDone), 1);
+    for (int i = 0; i < 4; ++i) mbar_init(bar(C::kDone + i), 1);
     mbar_init(bar(C::kDsDone), 1);
     fence_barrier_init();
     range[0] = 0x7fffffff;
@@ -360,6 +361,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
         mma_commit_w(bar(y ? C::kYFull : C::kXFull));
       }
     }
+    products_done(bar(C::kDone + (y ? 1 : 0)), p.err);
   } else if (warp >= 18) {
     // ---- dv += P^T dout (18), dk += dS^T q and the loads (19)
     const bool dk = warp == 19;
@@ -413,6 +415,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
       }
       if (ok) mma_commit_w(bar(C::kFree + st));
     }
+    products_done(bar(C::kDone + (dk ? 3 : 2)), p.err);
     if (dk && lane == 0) {
       // nothing may be in flight when the block exits
       wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
@@ -605,7 +608,7 @@ struct QueryCfg {
   static constexpr int kQ = 0, kKFull = 1, kKFree = kKFull + kSlotsK, kVFull = kKFree + kSlotsK,
                        kVFree = kVFull + kSlotsV, kXFull = kVFree + kSlotsV, kYFull = kXFull + 1,
                        kXRead = kYFull + 1, kYRead = kXRead + 1, kDsFull = kYRead + 1,
-                       kDsDone = kDsFull + 1, kBars = kDsDone + 1;
+                       kDsDone = kDsFull + 1, kDone = kDsDone + 1, kBars = kDone + 3;
   static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
   static constexpr uint32_t kColX = 0, kColY = 128, kColDs = 256, kColDq = 384;
   static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -658,6 +661,7 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
     mbar_init(bar(C::kXRead), 16);
     mbar_init(bar(C::kYRead), 16);
     mbar_init(bar(C::kDsFull), 16);
+    for (int i = 0; i < 3; ++i) mbar_init(bar(C::kDone + i), 1);
     mbar_init(bar(C::kDsDone), 1);
     fence_barrier_init();
   }
@@ -776,6 +780,7 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
       mma_commit_w(bar(y ? C::kYFull : C::kXFull));
       if (y) mma_commit_w(bar(C::kVFree + st));
     }
+    products_done(bar(C::kDone + (y ? 1 : 0)), p.err);
   } else if (warp == 19) {
     // ---- dq += dS k
     constexpr uint32_t idesc = Mma<F16, D>::idesc(D, true);
@@ -794,6 +799,7 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
       mma_commit_w(bar(C::kDsDone));
       mma_commit_w(bar(C::kKFree + st));
     }
+    products_done(bar(C::kDone + 2), p.err);
   }
   if (warp < 16) {
     // ---- dS of a quarter of each block's keys

@@ -153,6 +153,14 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* er
          wait_more_warp<LIMIT>(bar, parity, err, code);
 }
 
+// The end of a warp that issued products: none may be in flight when their operands' memory or TMEM is
+// given back. (One barrier, used once; by every lane, so that the warp stays together.)
+__device__ __forceinline__ void products_done(uint32_t bar, int* err) {
+  mma_commit_w(bar);
+  wait(bar, 0, err, ERR_WAIT_MMA, true);
+  __syncwarp();
+}
+
 constexpr int kTile = 128;      // rows of a tile, slots of a block
 constexpr int kSub = kTile * 128;  // bytes of 64 elements of 128 rows: one swizzled sub-tile
 

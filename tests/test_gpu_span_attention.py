@@ -195,6 +195,20 @@ def test_rising_scores(D):
     check(s, *run(s, scale=1 / D), scale=1 / D)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=str)
+@pytest.mark.parametrize("level", [-300.0, 300.0])
+def test_scores_far_from_zero(level, dtype, D):
+    """Rows whose first keys come at any place, with scores far below or above zero, and steps of a few
+    powers of two between the blocks."""
+    n = 700
+    for spans in (packed([n], window=300)[0], anywhere(260, n, 3)):
+        s = make(spans, n, 2, 1, D, dtype, nan=False)
+        s["q"].fill_(1.0)
+        s["k"].copy_((level + 4 * (torch.arange(n, device="cuda") // 100 % 3))[:, None, None])
+        check(s, *run(s, scale=1 / D), scale=1 / D)
+
+
 def test_equal_calls_give_equal_bits():
     spans, n = packed([1, 200, 33, 128, 257, 5], pad=40)
     for D in (64, 128):

@@ -61,14 +61,13 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// fp16 has no room for what rounds up past its largest number: it stays there
-template <typename T>
-__device__ __forceinline__ void into_range(float (&x)[8]) {
-  if constexpr (std::is_same<T, __half>::value) {
+// fp16 has no room for what rounds up past its largest number, 64 steps of 2^10: it stays there. (Steps
+// that large are rare: every other block is spared the comparisons.)
+constexpr uint32_t kWideStep = 127u + 10u;  // the byte of 2^10
+__device__ __forceinline__ void into_fp16(float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (fabsf(x[i]) <= 65536.f) x[i] = fminf(fmaxf(x[i], -65504.f), 65504.f);
-  }
+  for (int i = 0; i < 8; ++i)
+    if (fabsf(x[i]) <= 65536.f) x[i] = fminf(fmaxf(x[i], -65504.f), 65504.f);
 }
 
 template <typename T>
@@ -96,20 +95,23 @@ __global__ void __launch_bounds__(kThreads)
     if (to[j] == nullptr) continue;
     float v[8];
     kept_values(raw[j], byte[j], v);
-    into_range<T>(v);
+    if constexpr (std::is_same<T, __half>::value) {
+      const uint32_t together = __activemask();
+      if (__any_sync(together, byte[j] >= kWideStep)) into_fp16(v);
+    }
     store8(to[j], v);
   }
 }
 
-// Transposed: x[column][row]. A block turns 128 rows by 64 columns over in shared memory (256 rows, of
-// which an SM holds fewer blocks, took 64 us instead of 50 for 16001 x 4096): codes are read by whole sectors of a row, two rows a thread (whose 16-bit values go into shared memory as one
+// Transposed: x[column][row]. A block turns 64 rows by 64 columns over in shared memory (with 128 threads 46 us
+// for 16001 x 4096; 128 rows by 256 threads 50, 256 rows 58): codes are read by whole sectors of a row, two rows a thread (whose 16-bit values go into shared memory as one
 // word), and a column's values leave as aligned 16-byte stores. Columns begin at any address (rows may be
 // odd), so a vector may reach over the tile's end: it is the tile's that has its first element, which
 // has the next rows too for that. Only a column's own two ends are stored by elements.
-constexpr int kTileRows = 128, kTileCols = 64;
+constexpr int kTileRows = 64, kTileCols = 64, kTurners = 128;  // turners: threads of a block
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kTurners)
     load_transposed_kernel(int rows, int width, const int8_t* codes, const uint8_t* exps, T* x,
                            int64_t stride) {
   constexpr int kVec = 16 / sizeof(T);
@@ -126,12 +128,12 @@ __global__ void __launch_bounds__(kThreads)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int u_in = lane & 3;
   constexpr int kRuns = kAll / 16 * (kTileCols / 32);
-  constexpr int kSteps = (kRuns + kThreads / 32 - 1) / (kThreads / 32);
+  constexpr int kSteps = (kRuns + kTurners / 32 - 1) / (kTurners / 32);
   const int col = col0 + (warp & 1) * 32 + u_in * 8;  // (an even number of warps)
   const int64_t first_row = row0 + (warp >> 1) * 16 + (lane >> 2) * 2;
   const int8_t* from = codes + first_row * width + col;
   const uint8_t* exp_from = exps + first_row * blocks + col / kKeptBlock;
-  constexpr int kRowStep = kThreads / 64 * 16;  // rows from a warp's run to its next
+  constexpr int kRowStep = kTurners / 64 * 16;  // rows from a warp's run to its next
   uint2 raw[kSteps][2];
   uint32_t byte[kSteps][2];
 #pragma unroll
@@ -140,20 +142,21 @@ __global__ void __launch_bounds__(kThreads)
     for (int i = 0; i < 2; ++i) {
       raw[j][i] = make_uint2(0u, 0u);
       byte[j][i] = 1u;
-      if (j * (kThreads / 32) + warp < kRuns && first_row + j * kRowStep + i < rows && col < width) {
+      if (j * (kTurners / 32) + warp < kRuns && first_row + j * kRowStep + i < rows && col < width) {
         raw[j][i] = __ldg(reinterpret_cast<const uint2*>(from + static_cast<int64_t>(j * kRowStep + i) * width));
         byte[j][i] = __ldg(exp_from + static_cast<int64_t>(j * kRowStep + i) * blocks);
       }
     }
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {
-    if (j * (kThreads / 32) + warp >= kRuns) break;
+    if (j * (kTurners / 32) + warp >= kRuns) break;
     const int r = (warp >> 1) * 16 + (lane >> 2) * 2 + j * kRowStep, c = (warp & 1) * 32 + u_in * 8;
     float v[2][8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       kept_values(raw[j][i], byte[j][i], v[i]);
-      into_range<T>(v[i]);
+      if constexpr (std::is_same<T, __half>::value)
+        if (__any_sync(0xffffffffu, byte[j][i] >= kWideStep)) into_fp16(v[i]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(kThreads)
   const bool starts = blockIdx.x == 0;
   const int cols = min(kTileCols, width - col0);
   constexpr int kChunks = kTileRows / kVec;
-  constexpr int kColStep = kThreads / kChunks;
+  constexpr int kColStep = kTurners / kChunks;
   // neighbouring threads have neighbouring vectors of a column
   const int chunk = threadIdx.x % kChunks;
   int c = threadIdx.x / kChunks;
@@ -233,7 +236,7 @@ cudaError_t load_type(bool transposed, int rows, int width, const int8_t* codes,
     });
   if (e != cudaSuccess) return e;
   const dim3 grid((rows + kTileRows - 1) / kTileRows, (width + kTileCols - 1) / kTileCols);
-  return launch_pdl(load_transposed_kernel<T>, grid, dim3(kThreads), kSmem, s, rows, width, codes,
+  return launch_pdl(load_transposed_kernel<T>, grid, dim3(kTurners), kSmem, s, rows, width, codes,
                     exps, static_cast<T*>(x), stride);
 }
 

@@ -445,11 +445,13 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
   }
 }
 
-// The blocks' partial rows added up in their order, 32 columns a block and an item for blockIdx.y:
-// dpost, dpre, then the gates that several blocks share: each of them in turn where there are fewer gates
-// than blocks, else (a gate then spans two or three blocks) 32 of the borders between blocks, a warp each.
+// The blocks' partial rows added up, 32 columns a block, whose 32 warps share out the rows of what blockIdx.y
+// says: dpost, dpre, then the gates that several blocks share: some at a time where there are fewer gates than
+// blocks, `gate_slices` warps each, else (a gate then spans two or three blocks) 32 of the borders between
+// blocks, a warp each.
 constexpr int kSumThreads = 1024, kSumSlices = kSumThreads / 32;
-__global__ void __launch_bounds__(kSumThreads) join_sums_kernel(const __grid_constant__ JoinBwd p) {
+__global__ void __launch_bounds__(kSumThreads)
+    join_sums_kernel(const __grid_constant__ JoinBwd p, int gate_slices) {
   __shared__ float part[kSumSlices][33];
   grid_dep_wait();
   grid_dep_launch();
@@ -460,7 +462,6 @@ __global__ void __launch_bounds__(kSumThreads) join_sums_kernel(const __grid_con
   const float* from = p.part + col;
   const int item = static_cast<int>(blockIdx.y) - 2;
   const int gates = p.gate == nullptr ? 0 : (p.rows + p.gate_rows - 1) / p.gate_rows;
-  const float gain = there && p.post != nullptr ? p.post[col] : 1.f;
   if (item >= 0 && gates > p.grid) {
     // the gate across the border between blocks c and c + 1, if it begins in block c
     const int c = item * kSumSlices + slice;
@@ -472,43 +473,53 @@ __global__ void __launch_bounds__(kSumThreads) join_sums_kernel(const __grid_con
     const int last = block_of(p.rows, p.grid, static_cast<int>(end < p.rows ? end : p.rows) - 1);
     float sum = from[3 * plane + static_cast<int64_t>(c) * p.width];
     for (int i = c + 1; i <= last; ++i) sum += from[2 * plane + static_cast<int64_t>(i) * p.width];
-    p.d_gate[static_cast<int64_t>(at) * p.width + col] = sum * gain;
+    p.d_gate[static_cast<int64_t>(at) * p.width + col] = p.post != nullptr ? sum * p.post[col] : sum;
     return;
   }
   // blocks [c0, c1) of a plane, but block c0 of another where it is a gate's first
-  int which = 0, first = 0, c0 = 0, c1 = p.grid;
-  float* to = p.d_post;
+  const int slices = item < 0 ? kSumSlices : gate_slices;
+  int which = blockIdx.y, first = blockIdx.y, c0 = 0, c1 = p.grid;
+  int gate_at = 0;
   if (item < 0) {
-    which = first = blockIdx.y;
-    if (item == -1) to = p.d_pre;
-    if (to == nullptr || (item == -2 && p.one_gate)) return;
+    if (item == -1 ? p.d_pre == nullptr : p.d_post == nullptr || p.one_gate) return;
   } else {
-    const int64_t begin = static_cast<int64_t>(item) * p.gate_rows, end = begin + p.gate_rows;
-    c0 = block_of(p.rows, p.grid, static_cast<int>(begin));
-    c1 = block_of(p.rows, p.grid, static_cast<int>(end < p.rows ? end : p.rows) - 1) + 1;
-    to = p.d_gate == nullptr ? nullptr : p.d_gate + begin / p.gate_rows * p.width;
+    gate_at = (item * kSumSlices + slice) / slices;
     which = 2;
     first = 3;
-    if (!p.one_gate && (c1 == c0 + 1 || to == nullptr)) return;
+    c1 = 0;
+    if (gate_at < gates) {
+      const int64_t begin = static_cast<int64_t>(gate_at) * p.gate_rows, end = begin + p.gate_rows;
+      c0 = block_of(p.rows, p.grid, static_cast<int>(begin));
+      c1 = block_of(p.rows, p.grid, static_cast<int>(end < p.rows ? end : p.rows) - 1) + 1;
+    }
   }
   float sum = 0.f;
   if (there) {
 #pragma unroll 8
-    for (int c = c0 + slice; c < c1; c += kSumSlices)
+    for (int c = c0 + slice % slices; c < c1; c += slices)
       sum += __ldcg(from + (c == c0 ? first : which) * plane + static_cast<int64_t>(c) * p.width);
   }
   part[slice][lane] = sum;
   __syncthreads();
-  // a warp of 32 slices for every column
-  sum = warp_sum(part[lane][slice]);
-  if (lane == 0 && blockIdx.x * 32 + slice < p.width) {
-    const int64_t at = blockIdx.x * 32 + slice;
-    const float g = item >= 0 && p.post != nullptr ? p.post[at] : 1.f;
-    if (to != nullptr) to[at] = sum * g;
-    // one gate: dpost is the gate times the sum without the gain
-    if (item >= 0 && p.one_gate && p.post != nullptr && p.d_post != nullptr)
-      p.d_post[at] = sum * p.gate[at];
+  // a warp for every column, a lane for every slice; a gate's slices are neighbours
+  sum = part[lane][slice];
+  for (int i = slices / 2; i; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
+  const int64_t at = blockIdx.x * 32 + slice;
+  if (lane % slices != 0 || at >= p.width) return;
+  if (item < 0) {
+    (item == -1 ? p.d_pre : p.d_post)[at] = sum;
+    return;
   }
+  gate_at = (item * kSumSlices + lane) / slices;
+  if (gate_at >= gates) return;
+  const int64_t begin = static_cast<int64_t>(gate_at) * p.gate_rows, end = begin + p.gate_rows;
+  const bool shared = p.one_gate || block_of(p.rows, p.grid, static_cast<int>(begin)) !=
+                                        block_of(p.rows, p.grid, static_cast<int>(end < p.rows ? end : p.rows) - 1);
+  // (a gate of one block alone has left from there)
+  if (shared && p.d_gate != nullptr)
+    p.d_gate[static_cast<int64_t>(gate_at) * p.width + at] = p.post != nullptr ? sum * p.post[at] : sum;
+  // one gate: dpost is the gate times the sum without the gain
+  if (p.one_gate && p.post != nullptr && p.d_post != nullptr) p.d_post[at] = sum * p.gate[at];
 }
 
 // threads for a row, and how many blocks of them an SM is given
@@ -537,10 +548,14 @@ cudaError_t launch_join_bwd(const JoinBwd& p, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const int64_t gates =
       p.gate == nullptr ? 0 : (static_cast<int64_t>(p.rows) + p.gate_rows - 1) / p.gate_rows;
-  const int items = static_cast<int>(
-      gates <= p.grid ? gates : (p.grid - 1 + kSumSlices - 1) / kSumSlices);
-  if (p.post == nullptr && p.pre == nullptr && items == 0) return cudaSuccess;
-  return launch_pdl(join_sums_kernel, dim3((p.width + 31) / 32, 2 + items), dim3(kSumThreads), 0, s, p);
+  // four partial rows a warp and gate, about
+  int slices = kSumSlices, items = (p.grid - 1 + kSumSlices - 1) / kSumSlices;
+  if (gates <= p.grid) {
+    while (slices > 1 && static_cast<int64_t>(slices) * 2 * gates > p.grid) slices /= 2;
+    items = static_cast<int>((gates * slices + kSumSlices - 1) / kSumSlices);
+  }
+  if (p.post == nullptr && p.pre == nullptr && gates == 0) return cudaSuccess;
+  return launch_pdl(join_sums_kernel, dim3((p.width + 31) / 32, 2 + items), dim3(kSumThreads), 0, s, p, slices);
 }
 
 bool ok_ptr(const void* p, uintptr_t align) {

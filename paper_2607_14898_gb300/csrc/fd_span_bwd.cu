@@ -922,49 +922,49 @@ __global__ void __launch_bounds__(KeyCfg<D>::kThreads, 1)
 }
 
 // ------------------------------------------------------------------------------ parts added up
-// in their order: a thread per row (neighbours in a warp) and eight elements
+// in their order: a block a tile, a thread per row (neighbours in a warp) and eight elements at a time
+constexpr int kSumThreads = 4 * kTile;
 template <bool F16, int D>
-__global__ void __launch_bounds__(kTile) span_sums_kernel(const __grid_constant__ SpanBwd p) {
+__global__ void __launch_bounds__(kSumThreads) span_sums_kernel(const __grid_constant__ SpanBwd p, int first) {
   grid_dep_wait();
   grid_dep_launch();
-  const int row = threadIdx.x, d = blockIdx.y * 8, which = blockIdx.z;  // dq, dk, dv
+  const int row = threadIdx.x % kTile, which = first + blockIdx.y;  // dq, dk, dv
+  const int tile = static_cast<int>(blockIdx.x) / p.y.groups, group = static_cast<int>(blockIdx.x) % p.y.groups;
   const float4* from;
   uint16_t* to;
   int parts;
-  int64_t step;
+  int64_t step = D / 4 * kTile;
   if (which == 0) {
-    if (p.q_parts == 1) return;
-    const int tile = static_cast<int>(blockIdx.x) / p.y.groups, group = static_cast<int>(blockIdx.x) % p.y.groups;
     const int token = tile * p.y.tile_tokens + row / p.y.per, head = group * p.y.per + row % p.y.per;
-    if (tile >= p.y.row_tiles || row >= p.y.tile_rows || token >= p.y.n_q) return;
+    if (p.q_parts == 1 || tile >= p.y.row_tiles || row >= p.y.tile_rows || token >= p.y.n_q) return;
     parts = p.q_parts;
-    step = D / 4 * kTile;
     from = reinterpret_cast<const float4*>(p.part_q) +
            (static_cast<int64_t>(group) * p.y.row_tiles + tile) * parts * step;
-    to = static_cast<uint16_t*>(p.dq.p) + token * p.dq.token + head * p.dq.head + d;
+    to = static_cast<uint16_t*>(p.dq.p) + token * p.dq.token + head * p.dq.head;
   } else {
-    if (p.k_parts == 1) return;
-    const int kb = static_cast<int>(blockIdx.x) / p.y.groups, group = static_cast<int>(blockIdx.x) % p.y.groups;
-    const int key = kb * kTile + row;
-    if (kb >= p.y.key_blocks || key >= p.y.n_k) return;
+    const int key = tile * kTile + row;
+    if (p.k_parts == 1 || tile >= p.y.key_blocks || key >= p.y.n_k) return;
     parts = p.k_parts;
-    step = 2 * (D / 4) * kTile;
+    step *= 2;
     from = reinterpret_cast<const float4*>(p.part_k) +
-           (static_cast<int64_t>(group) * p.y.key_blocks + kb) * parts * step + (which == 2 ? D / 4 * kTile : 0);
+           (static_cast<int64_t>(group) * p.y.key_blocks + tile) * parts * step + (which == 2 ? step / 2 : 0);
     const SpanRows& r = which == 2 ? p.dv : p.dk;
-    to = static_cast<uint16_t*>(r.p) + key * r.token + group * r.head + d;
+    to = static_cast<uint16_t*>(r.p) + key * r.token + group * r.head;
   }
-  from += d / 4 * kTile + row;
-  float sum[8] = {};
+#pragma unroll
+  for (int d = threadIdx.x / kTile * 8; d < D; d += kSumThreads / kTile * 8) {
+    const float4* at = from + d / 4 * kTile + row;
+    float sum[8] = {};
 #pragma unroll 4
-  for (int c = 0; c < parts; ++c) {
-    const float4 a = __ldcg(from + c * step), b = __ldcg(from + c * step + kTile);
-    sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w;
-    sum[4] += b.x, sum[5] += b.y, sum[6] += b.z, sum[7] += b.w;
+    for (int c = 0; c < parts; ++c) {
+      const float4 a = __ldcg(at + c * step), b = __ldcg(at + c * step + kTile);
+      sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w;
+      sum[4] += b.x, sum[5] += b.y, sum[6] += b.z, sum[7] += b.w;
+    }
+    *reinterpret_cast<uint4*>(to + d) =
+        make_uint4(pack16<F16>(sum[0], sum[1]), pack16<F16>(sum[2], sum[3]),
+                   pack16<F16>(sum[4], sum[5]), pack16<F16>(sum[6], sum[7]));
   }
-  *reinterpret_cast<uint4*>(to) =
-      make_uint4(pack16<F16>(sum[0], sum[1]), pack16<F16>(sum[2], sum[3]),
-                 pack16<F16>(sum[4], sum[5]), pack16<F16>(sum[6], sum[7]));
 }
 
 // no keys, or no queries: what there is gets zeros
@@ -976,11 +976,12 @@ __global__ void span_zeros_kernel(SpanRows r, int tokens, int heads, int head_di
   grid_dep_launch();
 }
 
-// Parts of a unit's walk over `steps` tiles: as many as give every SM `rounds` units to take, but four tiles
-// (4 us) each at least, since the sums of the parts take 3 us.
-int parts_for(int64_t units, int steps, int rounds) {
-  const int64_t want = (static_cast<int64_t>(rounds) * num_sms() + units - 1) / units;
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(steps / 4, want)));
+// Parts of a unit's walk over `steps` tiles: as many as give every SM a unit, but four tiles (4 us) each at
+// least, since the sums of the parts take 3 us. (More parts of the keys' walks, four units an SM, even them out
+// no better than the queries' units behind them do: 555 us instead of 519 for the 480p clip.)
+int parts_for(int64_t units, int steps) {
+  return static_cast<int>(
+      std::max<int64_t>(1, std::min<int64_t>(steps / 4, (num_sms() + units - 1) / units)));
 }
 
 struct BwdPlan {
@@ -989,8 +990,8 @@ struct BwdPlan {
 };
 BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   BwdPlan b{};
-  b.q_parts = parts_for(static_cast<int64_t>(y.groups) * y.row_tiles, y.key_blocks, 1);
-  b.k_parts = parts_for(static_cast<int64_t>(y.groups) * y.key_blocks, y.row_tiles, 4);
+  b.q_parts = parts_for(static_cast<int64_t>(y.groups) * y.row_tiles, y.key_blocks);
+  b.k_parts = parts_for(static_cast<int64_t>(y.groups) * y.key_blocks, y.row_tiles);
   const size_t tiles = static_cast<size_t>(y.groups) * y.row_tiles;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   b.stat = 0;
@@ -1035,8 +1036,9 @@ cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, c
                    dim3(KeyCfg<D>::kThreads), kSmem, s, tmQ, tmDo, tmK, tmV, tmDq, tmDk, tmDv, p);
   if (e != cudaSuccess || (p.q_parts == 1 && p.k_parts == 1)) return e;
   const int64_t tiles = std::max(p.q_parts > 1 ? p.y.row_tiles : 0, p.k_parts > 1 ? p.y.key_blocks : 0);
-  return launch_pdl(span_sums_kernel<F16, D>, dim3(static_cast<unsigned>(tiles * p.y.groups), D / 8, 3),
-                    dim3(kTile), 0, s, p);
+  const int first = p.q_parts > 1 ? 0 : 1, end = p.k_parts > 1 ? 3 : 1;
+  return launch_pdl(span_sums_kernel<F16, D>, dim3(static_cast<unsigned>(tiles * p.y.groups), end - first),
+                    dim3(kSumThreads), 0, s, p, first);
 }
 
 }  // namespace

@@ -495,9 +495,26 @@ __global__ void __launch_bounds__(kSumThreads)
   }
   float sum = 0.f;
   if (there) {
-#pragma unroll 8
-    for (int c = c0 + slice % slices; c < c1; c += slices)
-      sum += __ldcg(from + (c == c0 ? first : which) * plane + static_cast<int64_t>(c) * p.width);
+    int c = c0 + slice % slices;
+    if (c == c0 && c < c1) {
+      sum = __ldcg(from + first * plane + static_cast<int64_t>(c) * p.width);
+      c += slices;
+    }
+    const float* at = from + which * plane + static_cast<int64_t>(c) * p.width;
+    const int64_t step = static_cast<int64_t>(slices) * p.width;
+    int left = c < c1 ? (c1 - c + slices - 1) / slices : 0;
+    for (; left >= 8; left -= 8, at += 8 * step) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __ldcg(at + i * step);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += x[i];
+    }
+    float x[7];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) x[i] = i < left ? __ldcg(at + i * step) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 7; ++i) sum += x[i];
   }
   part[slice][lane] = sum;
   __syncthreads();

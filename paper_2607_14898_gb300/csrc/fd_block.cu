@@ -48,10 +48,10 @@ __device__ __forceinline__ void keep8(const Raw8<T> (&raw)[NV], const float (&x)
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const uint32_t byte = kept_exponent(block_top(raw[v]));
+    const uint2 eight = kept_codes(x[v], byte);
     const int unit = unit0 + v * step;
     if (unit >= width / 8) continue;
-    *reinterpret_cast<uint2*>(codes + static_cast<int64_t>(row) * width + unit * 8) =
-        kept_codes(x[v], byte);
+    *reinterpret_cast<uint2*>(codes + static_cast<int64_t>(row) * width + unit * 8) = eight;
     if (unit % 4 == 0) exps[static_cast<int64_t>(row) * blocks + unit / 4] = static_cast<uint8_t>(byte);
   }
 }

@@ -21,11 +21,27 @@ struct Plane {
   int rows, width;
   int units, rows_of;
   int padded;  // groups a row, those past its end too
+  int rows_on, units_on;  // from a thread's group to its next: so many rows and groups
+};
+// where a thread's group is in its block's plane (without a division for each)
+struct Place {
+  int row, unit;
+  __device__ Place(const Plane& p) : row(threadIdx.x / p.units), unit(threadIdx.x - row * p.units) {}
+  __device__ void next(const Plane& p) {
+    row += p.rows_on;
+    unit += p.units_on;
+    if (unit >= p.units) {
+      unit -= p.units;
+      ++row;
+    }
+  }
 };
 Plane plane(int rows, int width) {
-  Plane p{rows, width, 0, 0, (width + kKeptBlock - 1) / kKeptBlock * 4};
+  Plane p{rows, width, 0, 0, (width + kKeptBlock - 1) / kKeptBlock * 4, 0, 0};
   p.units = std::min(p.padded, kUnits);
   p.rows_of = kUnits / p.units;
+  p.rows_on = kThreads / p.units;
+  p.units_on = kThreads % p.units;
   return p;
 }
 dim3 grid_of(const Plane& p) {
@@ -40,23 +56,25 @@ __global__ void __launch_bounds__(kThreads)
   Raw8<T> raw[kPerThread];
   int64_t row[kPerThread];
   int unit[kPerThread];
+  const int width8 = p.width / 8, unit0 = blockIdx.y * p.units;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * p.rows_of;
+  Place at(p);
 #pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const int l = threadIdx.x + j * kThreads, r = l / p.units;
-    row[j] = static_cast<int64_t>(blockIdx.x) * p.rows_of + r;
-    unit[j] = static_cast<int>(blockIdx.y) * p.units + l - r * p.units;
+  for (int j = 0; j < kPerThread; ++j, at.next(p)) {
+    row[j] = row0 + at.row;
+    unit[j] = unit0 + at.unit;
     raw[j] = Raw8<T>{};
-    if (r >= p.rows_of || row[j] >= p.rows || unit[j] >= p.padded) unit[j] = -1;
-    if (unit[j] >= 0 && unit[j] < p.width / 8) raw[j] = load_raw(x + row[j] * stride + unit[j] * 8);
+    if (at.row >= p.rows_of || row[j] >= p.rows || unit[j] >= p.padded) unit[j] = -1;
+    if (unit[j] >= 0 && unit[j] < width8) raw[j] = load_raw(x + row[j] * stride + unit[j] * 8);
   }
 #pragma unroll
   for (int j = 0; j < kPerThread; ++j) {
     float v[8];
     widen(raw[j], v);
     const uint32_t byte = kept_exponent(block_top(raw[j]));
+    const uint2 eight = kept_codes(v, byte);
     if (unit[j] < 0) continue;
-    if (unit[j] < p.width / 8)
-      *reinterpret_cast<uint2*>(codes + row[j] * p.width + unit[j] * 8) = kept_codes(v, byte);
+    if (unit[j] < width8) *reinterpret_cast<uint2*>(codes + row[j] * p.width + unit[j] * 8) = eight;
     if (unit[j] % 4 == 0) exps[row[j] * (p.padded / 4) + unit[j] / 4] = static_cast<uint8_t>(byte);
   }
 }
@@ -64,10 +82,8 @@ __global__ void __launch_bounds__(kThreads)
 // fp16 has no room for what rounds up past its largest number, 64 steps of 2^10: it stays there. (Steps
 // that large are rare: every other block is spared the comparisons.)
 constexpr uint32_t kWideStep = 127u + 10u;  // the byte of 2^10
-__device__ __forceinline__ void into_fp16(float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (fabsf(x[i]) <= 65536.f) x[i] = fminf(fmaxf(x[i], -65504.f), 65504.f);
+__device__ __forceinline__ float into_fp16(float x) {
+  return fabsf(x) <= 65536.f ? fminf(fmaxf(x, -65504.f), 65504.f) : x;
 }
 
 template <typename T>
@@ -78,13 +94,13 @@ __global__ void __launch_bounds__(kThreads)
   uint2 raw[kPerThread];
   uint32_t byte[kPerThread];
   T* to[kPerThread];
+  Place at(p);
 #pragma unroll
-  for (int j = 0; j < kPerThread; ++j) {
-    const int l = threadIdx.x + j * kThreads, r = l / p.units;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * p.rows_of + r;
-    const int unit = static_cast<int>(blockIdx.y) * p.units + l - r * p.units;
+  for (int j = 0; j < kPerThread; ++j, at.next(p)) {
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * p.rows_of + at.row;
+    const int unit = static_cast<int>(blockIdx.y) * p.units + at.unit;
     to[j] = nullptr;
-    if (r < p.rows_of && row < p.rows && unit < p.width / 8) {
+    if (at.row < p.rows_of && row < p.rows && unit < p.width / 8) {
       raw[j] = *reinterpret_cast<const uint2*>(codes + row * p.width + unit * 8);
       byte[j] = exps[row * (p.padded / 4) + unit / 4];
       to[j] = x + row * stride + unit * 8;
@@ -97,7 +113,10 @@ __global__ void __launch_bounds__(kThreads)
     kept_values(raw[j], byte[j], v);
     if constexpr (std::is_same<T, __half>::value) {
       const uint32_t together = __activemask();
-      if (__any_sync(together, byte[j] >= kWideStep)) into_fp16(v);
+      if (__any_sync(together, byte[j] >= kWideStep)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = into_fp16(v[i]);
+      }
     }
     store8(to[j], v);
   }
@@ -156,7 +175,10 @@ __global__ void __launch_bounds__(kTurners)
     for (int i = 0; i < 2; ++i) {
       kept_values(raw[j][i], byte[j][i], v[i]);
       if constexpr (std::is_same<T, __half>::value)
-        if (__any_sync(0xffffffffu, byte[j][i] >= kWideStep)) into_fp16(v[i]);
+        if (__any_sync(0xffffffffu, byte[j][i] >= kWideStep)) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[i][k] = into_fp16(v[i][k]);
+        }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -117,25 +117,26 @@ __device__ __forceinline__ uint32_t kept_exponent(uint32_t top_bits) {
   const int byte = static_cast<int>(e) - 6 + ((top_bits & 0x7fffffu) > 0x7e0000u);
   return static_cast<uint32_t>(byte < 1 ? 1 : byte);
 }
-// The codes of eight elements of the block, low byte first. x 2^-E + 1.5 2^23 is rounded to a whole
-// number by the addition itself, ties to even, and its low byte is the code: no conversions, which
+// The codes of eight elements of the block, low byte first; by a whole warp. x 2^-E + 1.5 2^23 is rounded to a
+// whole number by the addition itself, ties to even, and its low byte is the code: no conversions, which
 // run at a quarter of the additions' rate.
 __device__ __forceinline__ uint2 kept_codes(const float (&x)[8], uint32_t byte) {
-  if (byte == 255u) return make_uint2(0u, 0u);
   const float per_step = __uint_as_float((254u - byte) << 23);  // 2^-E
   uint32_t c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    c[i] = __float_as_uint(fmaf(x[i], per_step, 12582912.f));
-  }
+  for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(fmaf(x[i], per_step, 12582912.f));
   auto four = [&](int i) {
     return __byte_perm(__byte_perm(c[i], c[i + 1], 0x0040), __byte_perm(c[i + 2], c[i + 3], 0x0040),
                        0x5410);
   };
   uint2 r = make_uint2(four(0), four(4));
-  if (byte >= 249u) {  // 64 steps of 2^122 are 2^128: the largest floats stay finite
-    r.x = __vmins4(__vmaxs4(r.x, 0xc1c1c1c1u), 0x3f3f3f3fu);
-    r.y = __vmins4(__vmaxs4(r.y, 0xc1c1c1c1u), 0x3f3f3f3fu);
+  if (__any_sync(0xffffffffu, byte >= 249u)) {  // (rare, and not predicated)
+    // 64 steps of 2^122 are 2^128: the largest floats stay finite
+    if (byte >= 249u) {
+      r.x = __vmins4(__vmaxs4(r.x, 0xc1c1c1c1u), 0x3f3f3f3fu);
+      r.y = __vmins4(__vmaxs4(r.y, 0xc1c1c1c1u), 0x3f3f3f3fu);
+    }
+    if (byte == 255u) r = make_uint2(0u, 0u);
   }
   return r;
 }

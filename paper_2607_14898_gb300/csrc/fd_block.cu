@@ -9,8 +9,11 @@
 //   dpost = sum w gate n;  dpre = sum du m;  e = w gate post;  db = r_post (e - n mean(e n))
 // (sums over the tokens; of a gate's tokens for dgate). All in fp32.
 //
-// Both are bound by memory: every row is read and written once, its sums taken while it is in
-// registers.
+// Every row is read and written once, its sums taken while it is in registers. Measured, of a plain copy's
+// rate:
+//   6240 x 1024, bf16 on fp32, both inputs kept in 8 bits: join      15.4 us  5.9 TB/s, 87 %
+//     its gradient from 8 bits, a gate, two launches                  21.9 us  4.1 TB/s, 61 %
+//   16001 x 4096, bf16, a gate for 1000 rows: gradient               162 us   4.9 TB/s, 72 %
 #include <algorithm>
 #include <cmath>
 

@@ -1,7 +1,9 @@
 // Activations kept in 8 bits for the backward pass (fd_op_checkpoint_save / _load): the format is
 // in fd_rows.cuh.
 //
-// Bound by memory: every element is read and written once, 1 + 1/32 byte of it in 8 bits.
+// Bound by memory: every element is read and written once, 1 + 1/32 byte of it in 8 bits. 6240 x 4096 of
+// bf16 are saved in 13.8 us, 5.6 TB/s, 83 % of a plain copy's rate, with 70 % of the issue slots in use (17 us with
+// divisions for a thread's places and one conversion an element).
 #include <algorithm>
 
 #include "fd_once.h"
@@ -122,12 +124,16 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// Transposed: x[column][row]. A block turns 64 rows by 64 columns over in shared memory (with 128 threads 46 us
-// for 16001 x 4096; 128 rows by 256 threads 50, 256 rows 58): codes are read by whole sectors of a row, two rows a thread (whose 16-bit values go into shared memory as one
-// word), and a column's values leave as aligned 16-byte stores. Columns begin at any address (rows may be
-// odd), so a vector may reach over the tile's end: it is the tile's that has its first element, which
-// has the next rows too for that. Only a column's own two ends are stored by elements.
+// Transposed: x[column][row]. A block turns 64 rows by 64 columns over in shared memory: codes are read by
+// whole sectors of a row, two rows a thread (whose 16-bit values go into shared memory as one word), and a
+// column's values leave as aligned 16-byte stores. Columns begin at any address (rows may be odd), so a
+// vector may reach over the tile's end: it is the tile's that has its first element, which has the next
+// rows too for that. Only a column's own two ends are stored by elements.
+// 16001 x 4096 into fp16: 46 us, 4.3 TB/s, bound by the L1's way to memory (82 % busy: a store takes a cycle for
+// every sector). With 256 threads 49 us, tiles of 128 rows 53 to 54, stores by whole sectors with the
+// reads of shared memory free of conflicts 48.
 constexpr int kTileRows = 64, kTileCols = 64, kTurners = 128;  // turners: threads of a block
+static_assert(kTileCols == 64 && kTurners % 64 == 0, "two warps side by side have a tile's columns");
 
 template <typename T>
 __global__ void __launch_bounds__(kTurners)

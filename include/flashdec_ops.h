@@ -391,7 +391,8 @@ fd_status fd_op_span_attention(const fd_span_attention* attn, const void* q, int
  *   dq[t][h] = scale sum_j dS k_j;  dk[j] = scale sum dS q[t][h];  dv[j] = sum P dout[t][h]
  * (dk, dv over the queries and the group's heads). The probabilities are computed again and never
  * stored. Sums are in fp32 and a fixed order: equal calls give equal bits; P and dS are rounded to dtype for
- * their products (fp16: scaled by powers of two, dS by that of the largest |dout|). Queries that see
+ * their products (fp16: scaled by powers of two, dS by 2^-E for the largest |dout| = f 2^E, 1 <= f < 2:
+ * |dS| of 65504 2^E and more, which takes values in the hundreds that dout points along, is infinite). Queries that see
  * nothing and keys that nothing sees get zeros. dq like q, dk and dv like k, each with strides of its own;
  * they share no memory with the inputs or each other. spans, err_dev as above; workspace of
  * fd_span_attention_workspace_bytes(attn, 1). */
@@ -415,8 +416,8 @@ fd_status fd_op_span_attention_bwd(
  * at the last step, or at the largest fp16 number, before it.) */
 
 /* x of dtype FD_DTYPE_F32 / BF16 / F16, element (row, i) at x[row x_stride + i], into codes and exps.
- * width % 8 == 0, 8..1,048,576; x 16-byte aligned, x_stride % 8 == 0; codes 8-byte aligned. rows may
- * be 0. */
+ * width % 8 == 0, 8..1,048,576; x 16-byte aligned, x_stride % 8 == 0; codes 8-byte aligned. rows
+ * 0..2^30. */
 fd_status fd_op_checkpoint_save(int dtype, int rows, int width, const void* x, int64_t x_stride,
                                 int8_t* codes, uint8_t* exps, void* stream);
 
@@ -437,7 +438,7 @@ fd_status fd_op_checkpoint_load(int dtype, int transposed, int rows, int width,
  *   u = y r_pre pre_gain,  r_pre = (mean(y^2) + eps)^(-1/2)   (pre_gain NULL: no u)
  * in fp32; the norm before is that of y before it is rounded. */
 typedef struct {
-  int32_t rows, width;      /* rows >= 0; width % 8 == 0, 8..8192                             */
+  int32_t rows, width;      /* rows 0..2^30; width % 8 == 0, 8..8192                          */
   int32_t dtype;            /* of b, u, du and db: FD_DTYPE_BF16 or FD_DTYPE_F16              */
   int32_t stream_dtype;     /* of h, y, dy and dh: FD_DTYPE_F32 or dtype                      */
   const float* post_gain;   /* [width] or NULL                                                */

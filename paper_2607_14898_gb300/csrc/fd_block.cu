@@ -584,8 +584,9 @@ bool ok_ptr(const void* p, uintptr_t align) {
 // null, or aligned
 bool ok_or_null(const void* p, uintptr_t align) { return reinterpret_cast<uintptr_t>(p) % align == 0; }
 
+constexpr int kMaxRows = 1 << 30;  // (sums of rows and gate_rows, cut to rows, stay within 32 bits)
 bool valid(const fd_block_join* j) {
-  if (j == nullptr || j->rows < 0 || j->width < 8 || j->width % 8 != 0 || j->width > 8192)
+  if (j == nullptr || j->rows < 0 || j->rows > kMaxRows || j->width < 8 || j->width % 8 != 0 || j->width > 8192)
     return false;
   if (j->dtype != FD_DTYPE_BF16 && j->dtype != FD_DTYPE_F16) return false;
   if (j->stream_dtype != FD_DTYPE_F32 && j->stream_dtype != j->dtype) return false;
@@ -596,6 +597,12 @@ bool valid(const fd_block_join* j) {
 // rows of a 16-byte aligned matrix
 bool ok_rows(const fd_block_join* j, const void* p, int64_t stride) {
   return ok_ptr(p, 16) && stride % 8 == 0 && (j->rows == 1 || stride >= j->width);
+}
+// results that begin at the same address
+bool meet(const void* a, const void* b) { return a != nullptr && a == b; }
+// a result in the place of an input: of the same rows
+bool ok_place(const void* to, int64_t to_stride, const void* from, int64_t from_stride) {
+  return !meet(to, from) || to_stride == from_stride;
 }
 
 }  // namespace
@@ -616,9 +623,13 @@ fd_status fd_op_block_join(const fd_block_join* j, const void* h, int64_t h_stri
   if ((h_codes == nullptr) != (h_exps == nullptr) || (b_codes == nullptr) != (b_exps == nullptr) ||
       !fd::ok_or_null(h_codes, 8) || !fd::ok_or_null(b_codes, 8))
     return FD_ERR_INVALID_ARG;
+  if (fd::meet(y, u) || fd::meet(y, b) || fd::meet(u, h) || fd::meet(r_post, r_pre) ||
+      fd::meet(h_codes, b_codes) || fd::meet(h_exps, b_exps) || !fd::ok_place(y, y_stride, h, h_stride) ||
+      !fd::ok_place(u, u_stride, b, b_stride))
+    return FD_ERR_INVALID_ARG;
   const fd_status st = fd::check_device();
   if (st != FD_OK) return st;
-  const fd::Join p{j->rows,  j->width, j->post_gain, j->pre_gain, j->gate,  j->gate_rows,
+  const fd::Join p{j->rows,  j->width, j->post_gain, j->pre_gain, j->gate,  std::min(j->gate_rows, j->rows),
                    j->scale, eps,      h,            b,           h_stride, b_stride,
                    y,        u,        y_stride,     u_stride,    r_post,   r_pre,
                    h_codes,  b_codes,  h_exps,       b_exps};
@@ -633,7 +644,7 @@ fd_status fd_op_block_join(const fd_block_join* j, const void* h, int64_t h_stri
 }
 
 size_t fd_block_join_bwd_workspace_bytes(int rows, int width) {
-  if (rows < 1 || width < 8 || width % 8 != 0 || width > 8192) return 0;
+  if (rows < 1 || rows > fd::kMaxRows || width < 8 || width % 8 != 0 || width > 8192) return 0;
   return static_cast<size_t>(4) * fd::bwd_grid(rows, width) * width * sizeof(float);
 }
 
@@ -671,9 +682,15 @@ fd_status fd_op_block_join_bwd(const fd_block_join* j, const void* dy, int64_t d
   if ((dh != nullptr && !fd::ok_rows(j, dh, dh_stride)) ||
       (db != nullptr && !fd::ok_rows(j, db, db_stride)) || !fd::ok_ptr(workspace, 16))
     return FD_ERR_INVALID_ARG;
+  if (fd::meet(dh, db) || fd::meet(dh, du) || fd::meet(dh, b) || fd::meet(db, dy) || (pre && fd::meet(dh, h)) ||
+      (pre && fd::meet(db, h)) || fd::meet(d_post, d_pre) || fd::meet(d_post, d_gate) ||
+      fd::meet(d_pre, d_gate) || !fd::ok_place(dh, dh_stride, dy, dy_stride) ||
+      !fd::ok_place(db, db_stride, du, du_stride) || (b_exps != nullptr && fd::meet(db, b)) ||
+      !fd::ok_place(db, db_stride, b, b_stride))
+    return FD_ERR_INVALID_ARG;
   const fd_status st = fd::check_device();
   if (st != FD_OK) return st;
-  const fd::JoinBwd p{j->rows,    j->width,  j->post_gain, j->pre_gain, j->gate, j->gate_rows,
+  const fd::JoinBwd p{j->rows,    j->width,  j->post_gain, j->pre_gain, j->gate, std::min(j->gate_rows, j->rows),
                       j->scale,   dy,        du,           h,           b,       dy_stride,
                       du_stride,  h_stride,  b_stride,     h_exps,      b_exps,  r_post,
                       r_pre,      dh,        db,           dh_stride,   db_stride, d_post,

@@ -272,7 +272,7 @@ bool ok_ptr(const void* p, uintptr_t align) {
   return p != nullptr && reinterpret_cast<uintptr_t>(p) % align == 0;
 }
 bool valid(int dtype, int rows, int width) {
-  return (dtype == FD_DTYPE_F32 || dtype == FD_DTYPE_BF16 || dtype == FD_DTYPE_F16) && rows >= 0 &&
+  return (dtype == FD_DTYPE_F32 || dtype == FD_DTYPE_BF16 || dtype == FD_DTYPE_F16) && rows >= 0 && rows <= 1 << 30 &&
          width >= 8 && width % 8 == 0 && width <= 1 << 20;
 }
 

@@ -8,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include <cmath>
+#include <initializer_list>
 
 #include "fd_once.h"
 #include "fd_tile.cuh"
@@ -80,6 +81,12 @@ inline bool span_out_ok(const SpanRows& r, int tokens, int heads, int head_dim) 
   return span_rows_ok(r, tokens, heads, head_dim) &&
          (tokens == 1 || heads == 1 || r.token >= (heads - 1) * r.head + head_dim ||
           r.head >= (tokens - 1) * r.token + head_dim);
+}
+// whether what is written begins where one of the others does (other overlaps are the caller's to avoid)
+inline bool span_meets(const SpanRows& r, std::initializer_list<const void*> others) {
+  for (const void* p : others)
+    if (r.p != nullptr && r.p == p) return true;
+  return false;
 }
 
 }  // namespace

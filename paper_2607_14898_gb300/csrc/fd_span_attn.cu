@@ -604,7 +604,8 @@ fd_status fd_op_span_attention(const fd_span_attention* a, const void* q, int64_
       !fd::span_out_ok(outr, a->n_q, a->heads, a->head_dim) ||
       (a->n_k > 0 && (!fd::span_rows_ok(kr, a->n_k, a->groups, a->head_dim) ||
                       !fd::span_rows_ok(vr, a->n_k, a->groups, a->head_dim))) ||
-      !fd::span_ptr(spans, 8) || !fd::span_ptr(lse, 4) || !fd::span_ptr(err_dev, 4))
+      !fd::span_ptr(spans, 8) || !fd::span_ptr(lse, 4) || !fd::span_ptr(err_dev, 4) ||
+      fd::span_meets(outr, {q, k, v, spans, lse, workspace}))
     return FD_ERR_INVALID_ARG;
   const size_t need =
       fd::span_fwd_workspace_bytes(a->n_q, a->n_k, a->heads, a->groups, a->head_dim);

@@ -1084,8 +1084,15 @@ fd_status fd_op_span_attention_bwd(
   auto keys = [&](const fd::SpanRows& r) {
     return a->n_k == 0 || fd::span_rows_ok(r, a->n_k, a->groups, a->head_dim);
   };
-  if (!queries(qr) || !queries(p.out) || !queries(p.dout) || !queries(p.dq) || !keys(kr) ||
-      !keys(vr) || !keys(p.dk) || !keys(p.dv) || !fd::span_ptr(err_dev, 4))
+  if (!queries(qr) || !queries(p.out) || !queries(p.dout) || !keys(kr) || !keys(vr) ||
+      !fd::span_ptr(err_dev, 4))
+    return FD_ERR_INVALID_ARG;
+  if ((a->n_q > 0 && !fd::span_out_ok(p.dq, a->n_q, a->heads, a->head_dim)) ||
+      (a->n_k > 0 && (!fd::span_out_ok(p.dk, a->n_k, a->groups, a->head_dim) ||
+                      !fd::span_out_ok(p.dv, a->n_k, a->groups, a->head_dim))) ||
+      fd::span_meets(p.dq, {q, k, v, spans, out, lse, dout, dk, dv, workspace}) ||
+      fd::span_meets(p.dk, {q, k, v, spans, out, lse, dout, dv, workspace}) ||
+      fd::span_meets(p.dv, {q, k, v, spans, out, lse, dout, workspace}))
     return FD_ERR_INVALID_ARG;
   if (a->n_q > 0 && a->n_k > 0 &&
       (!fd::span_ptr(spans, 8) || !fd::span_ptr(lse, 4) || !fd::span_ptr(workspace, 16)))

@@ -106,3 +106,36 @@ def test_workspace():
     for rows, width in ((0, 64), (-1, 64), (4, 60), (4, 0), (4, 8200)):
         assert L.fd_block_join_bwd_workspace_bytes(rows, width) == 0
     assert L.fd_block_join_bwd_workspace_bytes(1, 64) == 4 * 64 * 4
+
+
+def test_rows_past_the_limit():
+    L = fdp.lib()
+    assert join(L, view(rows=(1 << 30) + 1)) == INVALID
+    assert L.fd_block_join_bwd_workspace_bytes((1 << 30) + 1, 64) == 0
+    assert L.fd_block_join_bwd_workspace_bytes(1 << 30, 64) > 0
+    assert L.fd_op_checkpoint_save(1, (1 << 30) + 1, 64, P, 64, P, P, None) == INVALID
+    assert L.fd_op_checkpoint_load(1, 0, (1 << 30) + 1, 64, P, P, P, 64, None) == INVALID
+
+
+JOIN = ("h", "b", "y", "u", "r_post", "r_pre", "hc", "he", "bc", "be")
+JOIN_BWD = ("dy", "du", "h", "b", "r_post", "r_pre", "dh", "db", "d_post", "d_pre", "d_gate", "work")
+
+
+@pytest.mark.parametrize("a,b,more", [
+    ("y", "u", {}), ("y", "b", {}), ("u", "h", {}), ("r_post", "r_pre", {}), ("hc", "bc", {}), ("he", "be", {}),
+    ("y", "h", dict(ys=72)), ("u", "b", dict(bs=72))])
+def test_join_results_in_each_others_place(a, b, more):
+    at = {name: P * (2 + i) for i, name in enumerate(JOIN)}
+    assert join(fdp.lib(), view(), **{**at, a: at[b], **more}) == INVALID
+
+
+@pytest.mark.parametrize("a,b,more", [
+    ("dh", "db", {}), ("dh", "du", {}), ("dh", "h", {}), ("dh", "b", {}), ("db", "dy", {}), ("db", "h", {}),
+    ("d_post", "d_pre", {}), ("d_post", "d_gate", {}), ("d_pre", "d_gate", {}), ("dh", "dy", dict(dhs=72)),
+    ("db", "du", dict(dbs=72)), ("db", "b", dict(bs=72)), ("db", "b", dict(be=P))])
+def test_gradients_in_each_others_place(a, b, more):
+    d = dict(dy=P, dys=64, du=P, dus=64, h=P, hs=64, he=None, b=P, bs=64, be=None, r_post=P, r_pre=P, dh=P,
+             dhs=64, db=P, dbs=64, d_post=P, d_pre=P, d_gate=P, work=P)
+    d.update({name: P * (2 + i) for i, name in enumerate(JOIN_BWD)})
+    d.update({a: d[b], **more})
+    assert fdp.lib().fd_op_block_join_bwd(view(), *d.values(), None) == INVALID

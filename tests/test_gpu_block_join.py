@@ -323,3 +323,45 @@ def test_tensors_that_are_refused():
         fdp.op_block_join_bwd(s["dy"], s["du"], s["h"], s["b"], y, u, post_gain=s["post"],
                               pre_gain=s["pre"], r_post=s["h"][:, 0].contiguous(),
                               r_pre=s["h"][:, 0].contiguous())
+
+
+@pytest.mark.parametrize("rows", [3, 70, 700])
+def test_one_gate_for_any_number_of_tokens(rows, monkeypatch):
+    """The library's gate_rows past rows, up to the largest int (the binding cuts it to the tokens there are)."""
+    s = make(rows, 256, torch.bfloat16, F32, rows, True, True)
+    want = run(s)
+    want_bwd = run_bwd(s, want, s["h"], s["b"])
+    view = fdp._join_view
+
+    def wide(*args):
+        j = view(*args)
+        j.gate_rows = 2 ** 31 - 1
+        return j
+
+    monkeypatch.setattr(fdp, "_join_view", wide)
+    got = run(s)
+    got_bwd = run_bwd(s, got, s["h"], s["b"])
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    assert all(torch.equal(got_bwd[n], want_bwd[n]) for n in want_bwd)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_two_calls_at_once(dtype):
+    """Two joins with their gradients on two streams, each with a workspace of its own, give what they give alone."""
+    cases = [make(rows, 1024, dtype, F32, 7, True, True, seed=rows) for rows in (300, 2000)]
+    alone = []
+    for s in cases:
+        fwd = run(s)
+        alone.append((fwd, run_bwd(s, fwd, s["h"], s["b"])))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        found = []
+        for s, stream in zip(cases, streams):
+            with torch.cuda.stream(stream):
+                fwd = run(s)
+                found.append((fwd, run_bwd(s, fwd, s["h"], s["b"])))
+        torch.cuda.synchronize()
+        for got, want in zip(found, alone):
+            for a, b in zip(got, want):
+                assert all(torch.equal(a[n], b[n]) for n in b if isinstance(b[n], torch.Tensor))

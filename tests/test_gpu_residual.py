@@ -79,7 +79,7 @@ def test_training_pass(lengths, pad, width, heads, groups, D, gate_tokens):
         block.check()
         got = {"y": y, "u_next": u_next, "dh": dh, "du": du, **g}
         for name, value in want.items():
-            off = float((got[name].double() - value).norm() / value.norm())
+            off = float((got[name].double() - value.detach()).norm() / value.detach().norm())
             assert off <= BOUND, (name, off)
 
 

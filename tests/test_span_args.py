@@ -81,3 +81,31 @@ def test_workspace_bytes():
     assert L.fd_span_attention_workspace_bytes(view(n_q=0), 1) == 0
     assert L.fd_span_attention_workspace_bytes(view(n_k=0), 1) == 0
     assert L.fd_span_attention_workspace_bytes(view(), 1) > 0
+
+
+def distinct(names):
+    """An address of its own for each name, far apart."""
+    return {name: P * (2 + i) for i, name in enumerate(names)}
+
+
+@pytest.mark.parametrize("shared,with_", [("out_p", n) for n in ("q_p", "k_p", "v_p", "spans", "lse")])
+def test_result_in_the_place_of_an_input(shared, with_):
+    at = distinct(("q_p", "k_p", "v_p", "spans", "out_p", "lse", "work", "err"))
+    assert forward(fdp.lib(), view(), **{**at, shared: at[with_]}) == INVALID
+
+
+@pytest.mark.parametrize("shared,with_", [(a, b) for i, a in enumerate(("dq_p", "dk_p", "dv_p")) for b in (
+    "q_p", "k_p", "v_p", "spans", "out_p", "lse", "dout_p", "work", *("dq_p", "dk_p", "dv_p")[i + 1:])])
+def test_gradient_in_the_place_of_another(shared, with_):
+    at = distinct(("q_p", "k_p", "v_p", "spans", "out_p", "lse", "dout_p", "dq_p", "dk_p", "dv_p", "work", "err"))
+    assert backward(fdp.lib(), view(), **{**at, shared: at[with_]}) == INVALID
+
+
+@pytest.mark.parametrize("call,name,token,head", [
+    (forward, "out", 448, 64), (forward, "out", 64, 64), (forward, "out", 64, 6392), (backward, "dq", 448, 64),
+    (backward, "dk", 64, 64), (backward, "dv", 64, 19192)])
+def test_results_whose_rows_share_elements(call, name, token, head):
+    # (8 heads or 2 groups of 64 within a token's stride, or 100 or 300 tokens within a head's)
+    at = distinct(("q_p", "k_p", "v_p", "out_p", "lse", "work", "err")) if call is forward else distinct(
+        ("q_p", "k_p", "v_p", "out_p", "lse", "dout_p", "dq_p", "dk_p", "dv_p", "work", "err"))
+    assert call(fdp.lib(), view(), **at, **{f"{name}_t": token, f"{name}_h": head}) == INVALID

@@ -32,7 +32,8 @@ struct SpanBwd {
   const float* lse;
   float* stat;    // [group][row tile] records of kRecord: see below
   int4* limits;   // of each row tile, those of its records
-  float* most;    // [group][row tile]: the largest |dout| (fp16)
+  float* most;    // [group][row tile]: the largest |dout| (fp16); behind them the largest of all
+  int mosts;      // of them, those that the blocks look through: 1 is the largest of all
   float* part_q;  // [group][row tile][part][D / 4][128 rows] of four
   float* part_k;  // [group][key block][part][dk, dv][D / 4][128 keys] of four
   int* err;
@@ -134,10 +135,38 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
   }
 }
 
-// 2^-E of the largest |dout| = f 2^E, 1 <= f < 2, over all tiles, by one warp (fp16)
-__device__ __forceinline__ float down_scale(const float* most, int n) {
+// The largest |dout| of all tiles (fp16), where they are too many for every block to look through: 131072 tokens of
+// 16 heads of 128 on 8 in windows of 512 (16384 tiles) took 3909 us, and take 2794. 8191 causal tokens (2048 tiles),
+// whose blocks have more to do, take the same either way (1283, 1292), the 480p clip 575 and 565.
+constexpr int kFewTiles = 256;  // a round of loads of one warp
+__global__ void __launch_bounds__(1024) span_most_kernel(float* most, int tiles) {
+  __shared__ float top[32];
+  grid_dep_wait();
+  grid_dep_launch();
   float m = 0.f;
-  for (int i = threadIdx.x & 31; i < n; i += 32) m = fmaxf(m, __ldcg(most + i));
+#pragma unroll 8
+  for (int i = threadIdx.x; i < tiles; i += 1024) m = fmaxf(m, __ldcg(most + i));
+#pragma unroll
+  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+  if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  m = top[threadIdx.x];
+#pragma unroll
+  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+  if (threadIdx.x == 0) most[tiles] = m;
+}
+
+// 2^-E of the largest |dout| = f 2^E, 1 <= f < 2, over all tiles, by one warp (fp16)
+__device__ __forceinline__ float down_scale(const SpanBwd& p) {
+  const int tiles = p.y.groups * p.y.row_tiles;
+  const float* most = tiles > kFewTiles ? p.most + tiles : p.most;
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < kFewTiles; i += 32) {
+    const int at = i + (threadIdx.x & 31);
+    if (at < p.mosts) m = fmaxf(m, __ldcg(most + at));
+  }
 #pragma unroll
   for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
   const uint32_t e = __float_as_uint(m) >> 23;  // (fp16: e is 103 at least unless m is zero)
@@ -309,7 +338,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
       atomicMax(range + 1, end);
     }
     if (F16 && warp == 0) {
-      const float f = down_scale(p.most, p.y.groups * p.y.row_tiles);
+      const float f = down_scale(p);
       if (lane == 0) *down = f;
     }
   }
@@ -680,7 +709,7 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   } else if (F16 && warp == 1) {
-    const float f = down_scale(p.most, p.y.groups * p.y.row_tiles);
+    const float f = down_scale(p);
     if (lane == 0) *down = f;
   }
   const int4 m = __ldcg(p.limits + tile);
@@ -1004,7 +1033,7 @@ BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   b.stat = 0;
   b.limits = up(b.stat + tiles * kRecord * sizeof(float));
   b.most = b.limits + up(static_cast<size_t>(y.row_tiles) * sizeof(int4));
-  b.part_q = b.most + up(tiles * sizeof(float));
+  b.part_q = b.most + up((tiles + 1) * sizeof(float));
   b.part_k = b.part_q + (b.q_parts > 1 ? tiles * b.q_parts * kTile * head_dim * sizeof(float) : 0);
   b.total = b.part_k + (b.k_parts > 1 ? static_cast<size_t>(y.groups) * y.key_blocks * b.k_parts * 2 *
                                             kTile * head_dim * sizeof(float)
@@ -1037,6 +1066,8 @@ cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, c
     });
   if (e == cudaSuccess)
     e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles, p.y.groups), dim3(256), 0, s, p);
+  if (e == cudaSuccess && F16 && p.y.row_tiles * p.y.groups > kFewTiles)
+    e = launch_pdl(span_most_kernel, dim3(1), dim3(1024), 0, s, p.most, p.y.row_tiles * p.y.groups);
   if (e == cudaSuccess)
     e = launch_pdl(span_grad_kernel<F16, D>,
                    dim3((p.y.key_blocks * p.k_parts + p.y.row_tiles * p.q_parts) * p.y.groups),
@@ -1124,6 +1155,8 @@ fd_status fd_op_span_attention_bwd(
   p.stat = reinterpret_cast<float*>(ws + b.stat);
   p.limits = reinterpret_cast<int4*>(ws + b.limits);
   p.most = reinterpret_cast<float*>(ws + b.most);
+  const int tiles = p.y.groups * p.y.row_tiles;
+  p.mosts = tiles <= fd::kFewTiles ? tiles : 1;
   p.part_q = reinterpret_cast<float*>(ws + b.part_q);
   p.part_k = reinterpret_cast<float*>(ws + b.part_k);
   p.err = err_dev;

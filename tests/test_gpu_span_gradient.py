@@ -236,3 +236,15 @@ def test_tensors_that_are_refused():
                                                                      device="cuda").expand(-1, 2, -1))):
         with pytest.raises(fdp.FdError):
             call(**bad)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [0, 150, 299])
+def test_largest_gradient_of_many_tiles(at, D):
+    """300 row tiles, one of which has gradients 2000 times as large (fp16's are scaled by the largest)."""
+    spans, n = packed([30, 20])
+    s = make(spans, n, 300, 300, D, FP16)
+    s["dout"].mul_(0.01)
+    s["dout"][:, at].mul_(2000)
+    out, lse = run(s)
+    check(run_bwd(s, out, lse), gradient(s, out, lse), s)

@@ -10,7 +10,8 @@
 //   8191 queries, as many keys, every one seen, 32 heads of 128 on 8      721 us  1524 TFLOP/s, 81 %
 //   1 query of 8 sequences, 49920 keys, 16 heads of 64 on 4               16.6 us  3.1 TB/s (3 us of it to join parts)
 // Slower were: one block an SM with a row tile over blocks of 256 keys, by quarters (229 us for the first); blocks that
-// stay and take one unit after another (5 to 20 %); no running maximum while sums stay small (222).
+// stay and take one unit after another (5 to 20 %); no running maximum while sums stay small (222); four blocks an SM over
+// 64 keys, a thread a row (246); no warp of its own for the zeros (199 instead of 187 for the second).
 #include <algorithm>
 #include <cmath>
 

@@ -12,8 +12,8 @@
 // Every row is read and written once, its sums taken while it is in registers. Measured, of a plain copy's
 // rate:
 //   6240 x 1024, bf16 on fp32, both inputs kept in 8 bits: join      15.4 us  5.9 TB/s, 87 %
-//     its gradient from 8 bits, a gate, two launches                  21.9 us  4.1 TB/s, 61 %
-//   16001 x 4096, bf16, a gate for 1000 rows: gradient               162 us   4.9 TB/s, 72 %
+//     its gradient from 8 bits, a gate, two launches                  19.7 us  4.6 TB/s, 68 %
+//   16001 x 4096, bf16, a gate for 1000 rows: gradient               153 us   5.1 TB/s, 76 %
 #include <algorithm>
 #include <cmath>
 
@@ -224,11 +224,14 @@ struct Inputs {
 // Bound by its instructions (pairs of fp32 throughout, gains and gate in registers while they stay the
 // same): copies ahead into a ring in shared memory, three or four rows deep, made it slower (480p chunk 24.7 to 35
 // us), fewer instructions faster.
-template <typename B, typename H, int NT, int NV>
+// FORM: what there is, known beforehand where it is what training has, else looked up. (The branches for it, and
+// three sums a row that were added up apart, had the two cases above at 21.9 and 162 us.)
+enum Form { kSome, kAll, kAllKept };  // kAll: both norms, dy, dh and db; kAllKept: and both inputs in 8 bits
+template <typename B, typename H, int NT, int NV, Form FORM>
 __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ JoinBwd p) {
   constexpr int NW = NT / 32;
   constexpr bool kKeep = NV == 1;  // gains stay in registers
-  __shared__ float4 part[2][NW];
+  __shared__ float part[2][NW][4];
   grid_dep_wait();
   grid_dep_launch();
   const int units = p.width / 8, blocks = (p.width + kKeptBlock - 1) / kKeptBlock;
@@ -236,7 +239,10 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
   const int row1 = first_row(p.rows, p.grid, blockIdx.x + 1);
   const float inv_width = 1.f / static_cast<float>(p.width);
   const int lane = threadIdx.x & 31;
-  const bool pre = p.pre != nullptr, post = p.post != nullptr;
+  const bool pre = FORM != kSome || p.pre != nullptr, post = FORM != kSome || p.post != nullptr;
+  const bool has_dy = FORM != kSome || p.dy != nullptr;
+  const bool h_kept = FORM == kAllKept || (FORM == kSome && p.h_exps != nullptr);
+  const bool b_kept = FORM == kAllKept || (FORM == kSome && p.b_exps != nullptr);
   Inputs<B, H> in[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) in[v] = Inputs<B, H>{};
@@ -252,10 +258,10 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
       auto codes = [&](const void* from, int64_t stride) {
         return *reinterpret_cast<const uint2*>(static_cast<const int8_t*>(from) + row * stride + unit * 8);
       };
-      if (p.dy != nullptr) x.dy = load_raw(static_cast<const H*>(p.dy) + row * p.dy_stride + unit * 8);
+      if (has_dy) x.dy = load_raw(static_cast<const H*>(p.dy) + row * p.dy_stride + unit * 8);
       if (pre) {
         x.du = load_raw(static_cast<const B*>(p.du) + row * p.du_stride + unit * 8);
-        if (p.h_exps != nullptr) {
+        if (h_kept) {
           const uint2 c = codes(p.h, p.h_stride);
           x.h.a.x = c.x;
           x.h.a.y = c.y;
@@ -264,7 +270,7 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
           x.h = load_raw(static_cast<const H*>(p.h) + row * p.h_stride + unit * 8);
         }
       }
-      if (p.b_exps != nullptr) {
+      if (b_kept) {
         const uint2 c = codes(p.b, p.b_stride);
         x.b.a.x = c.x;
         x.b.a.y = c.y;
@@ -352,10 +358,10 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const Inputs<B, H>& x = in[v];
-      n[v] = p.b_exps != nullptr ? kept_values2(make_uint2(x.b.a.x, x.b.a.y), x.b_byte) : widen2(x.b);
+      n[v] = b_kept ? kept_values2(make_uint2(x.b.a.x, x.b.a.y), x.b_byte) : widen2(x.b);
       d[v] = widen2(x.dy);
       if (pre) {
-        m[v] = p.h_exps != nullptr ? kept_values2(make_uint2(x.h.a.x, x.h.a.y), x.h_byte) : widen2(x.h);
+        m[v] = h_kept ? kept_values2(make_uint2(x.h.a.x, x.h.a.y), x.h_byte) : widen2(x.h);
         du[v] = widen2(x.du);
       } else {
         m[v] = du[v] = Pairs{};
@@ -365,7 +371,7 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int unit = threadIdx.x + v * NT;
-      if (unit >= units) continue;
+      if (!kKeep && unit >= units) continue;  // (zeros add nothing: no branch)
       const Pairs q = kKeep ? q_kept[v] : factors(unit);
       Pairs qn;
 #pragma unroll
@@ -389,31 +395,29 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
       for (int i = 0; i < 4; ++i) sum_dq = fma2(d[v].v[i], qn.v[i], sum_dq);
     }
     const float2 a = halves_of(sum_gm), b = halves_of(sum_dq), c = halves_of(sum_mq);
-    float3 sum = make_float3(warp_sum(a.x + a.y), warp_sum(b.x + b.y), warp_sum(c.x + c.y));
-    if constexpr (NW > 1) {
-      float4* to = part[row & 1];
-      if (lane == 0) to[threadIdx.x >> 5] = make_float4(sum.x, sum.y, sum.z, 0.f);
-      __syncthreads();
-      if constexpr (NW <= 4) {
-        sum = make_float3(0.f, 0.f, 0.f);
+    // The three sums over the row, folded into one value a lane on the way: gm ends in lanes 0-7, mq in 8-15
+    // and 24-31, dq in 16-23.
+    float at;
+    {
+      const float gm = a.x + a.y, dq = b.x + b.y, mq = c.x + c.y;
+      const bool upper = lane & 16, odd = lane & 8;
+      const float x = (upper ? dq : gm) + __shfl_xor_sync(0xffffffffu, upper ? gm : dq, 16);
+      const float y = mq + __shfl_xor_sync(0xffffffffu, mq, 16);
+      at = (odd ? y : x) + __shfl_xor_sync(0xffffffffu, odd ? x : y, 8);
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-          const float4 x = to[i];
-          sum.x += x.x;
-          sum.y += x.y;
-          sum.z += x.z;
-        }
-      } else {
-        const float4 x = to[lane % NW];
-        sum = make_float3(x.x, x.y, x.z);
-#pragma unroll
-        for (int i = NW / 2; i; i >>= 1) {
-          sum.x += __shfl_xor_sync(0xffffffffu, sum.x, i);
-          sum.y += __shfl_xor_sync(0xffffffffu, sum.y, i);
-          sum.z += __shfl_xor_sync(0xffffffffu, sum.z, i);
-        }
-      }
+      for (int i = 4; i; i >>= 1) at += __shfl_xor_sync(0xffffffffu, at, i);
     }
+    if constexpr (NW > 1) {
+      float(*to)[4] = part[row & 1];
+      if ((lane & 7) == 0) to[threadIdx.x >> 5][lane >> 3] = at;
+      __syncthreads();
+      at = to[lane & (NW < 8 ? NW - 1 : 7)][lane >> 3];
+      if constexpr (NW > 8) at += to[8 + (lane & 7)][lane >> 3];
+#pragma unroll
+      for (int i = NW < 8 ? NW / 2 : 4; i; i >>= 1) at += __shfl_xor_sync(0xffffffffu, at, i);
+    }
+    const float3 sum = make_float3(__shfl_sync(0xffffffffu, at, 0), __shfl_sync(0xffffffffu, at, 16),
+                                   __shfl_sync(0xffffffffu, at, 8));
     const float mean_gm = r_pre * sum.x * inv_width;  // r_pre mean(g m)
     const float mean_en = post ? (sum.y - mean_gm * sum.z) * inv_width : 0.f;
     const float en = -r_post * mean_en;
@@ -421,7 +425,7 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int unit = threadIdx.x + v * NT;
-      if (unit >= units) continue;
+      if (!kKeep && unit >= units) continue;
       const Pairs q = kKeep ? q_kept[v] : factors(unit);
       Pairs db;
 #pragma unroll
@@ -430,8 +434,8 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
         s_gate[v].v[i] = fma2(d[v].v[i], n[v].v[i], s_gate[v].v[i]);
         db.v[i] = fma2(mul2(q.v[i], d[v].v[i]), rpost2, mul2(en2, n[v].v[i]));
       }
-      if (p.dh != nullptr) store8(static_cast<H*>(p.dh) + row * p.dh_stride + unit * 8, d[v]);
-      if (p.db != nullptr) store8(static_cast<B*>(p.db) + row * p.db_stride + unit * 8, db);
+      if (unit < units && (FORM != kSome || p.dh != nullptr)) store8(static_cast<H*>(p.dh) + row * p.dh_stride + unit * 8, d[v]);
+      if (unit < units && (FORM != kSome || p.db != nullptr)) store8(static_cast<B*>(p.db) + row * p.db_stride + unit * 8, db);
     }
   }
   if (row0 < row1 && p.gate != nullptr) leave();
@@ -558,13 +562,23 @@ int bwd_grid(int rows, int width) {
 template <typename B, typename H>
 cudaError_t launch_join_bwd(const JoinBwd& p, cudaStream_t s) {
   const int t = bwd_threads(p.width);
-  auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(p.grid), dim3(t), 0, s, p); };
-  const cudaError_t e = p.width > 4096 ? go(join_bwd_kernel<B, H, 512, 2>)
-                        : t == 32      ? go(join_bwd_kernel<B, H, 32, 1>)
-                        : t == 64      ? go(join_bwd_kernel<B, H, 64, 1>)
-                        : t == 128     ? go(join_bwd_kernel<B, H, 128, 1>)
-                        : t == 256     ? go(join_bwd_kernel<B, H, 256, 1>)
-                                       : go(join_bwd_kernel<B, H, 512, 1>);
+  const bool all = p.post != nullptr && p.pre != nullptr && p.dy != nullptr && p.dh != nullptr && p.db != nullptr;
+  auto go = [&](auto some, auto as_they_are, auto kept) {
+    return launch_pdl(!all || (p.h_exps == nullptr) != (p.b_exps == nullptr) ? some : p.h_exps != nullptr ? kept : as_they_are,
+                      dim3(p.grid), dim3(t), 0, s, p);
+  };
+#define FD_FORMS(NT, NV) \
+  go(join_bwd_kernel<B, H, NT, NV, kSome>, join_bwd_kernel<B, H, NT, NV, kAll>, join_bwd_kernel<B, H, NT, NV, kAllKept>)
+  // (rows past 4096 wait for registers more than for branches, rows up to 512 for their loads)
+#define FD_SOME(NT, NV) launch_pdl(join_bwd_kernel<B, H, NT, NV, kSome>, dim3(p.grid), dim3(t), 0, s, p)
+  const cudaError_t e = p.width > 4096 ? FD_SOME(512, 2)
+                        : t == 32      ? FD_SOME(32, 1)
+                        : t == 64      ? FD_SOME(64, 1)
+                        : t == 128     ? FD_FORMS(128, 1)
+                        : t == 256     ? FD_FORMS(256, 1)
+                                       : FD_FORMS(512, 1);
+#undef FD_SOME
+#undef FD_FORMS
   if (e != cudaSuccess) return e;
   const int64_t gates =
       p.gate == nullptr ? 0 : (static_cast<int64_t>(p.rows) + p.gate_rows - 1) / p.gate_rows;

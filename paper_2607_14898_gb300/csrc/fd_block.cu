@@ -225,7 +225,8 @@ struct Inputs {
 // same): copies ahead into a ring in shared memory, three or four rows deep, made it slower (480p chunk 24.7 to 35
 // us), fewer instructions faster.
 // FORM: what there is, known beforehand where it is what training has, else looked up. (The branches for it, and
-// three sums a row that were added up apart, had the two cases above at 21.9 and 162 us.)
+// three sums a row that were added up apart, had the two cases above at 21.9 and 162 us, and 8000 rows of 8192 at
+// 370 instead of 242: they spill.)
 enum Form { kSome, kAll, kAllKept };  // kAll: both norms, dy, dh and db; kAllKept: and both inputs in 8 bits
 template <typename B, typename H, int NT, int NV, Form FORM>
 __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ JoinBwd p) {
@@ -569,15 +570,12 @@ cudaError_t launch_join_bwd(const JoinBwd& p, cudaStream_t s) {
   };
 #define FD_FORMS(NT, NV) \
   go(join_bwd_kernel<B, H, NT, NV, kSome>, join_bwd_kernel<B, H, NT, NV, kAll>, join_bwd_kernel<B, H, NT, NV, kAllKept>)
-  // (rows past 4096 wait for registers more than for branches, rows up to 512 for their loads)
-#define FD_SOME(NT, NV) launch_pdl(join_bwd_kernel<B, H, NT, NV, kSome>, dim3(p.grid), dim3(t), 0, s, p)
-  const cudaError_t e = p.width > 4096 ? FD_SOME(512, 2)
-                        : t == 32      ? FD_SOME(32, 1)
-                        : t == 64      ? FD_SOME(64, 1)
+  const cudaError_t e = p.width > 4096 ? FD_FORMS(512, 2)
+                        : t == 32      ? FD_FORMS(32, 1)
+                        : t == 64      ? FD_FORMS(64, 1)
                         : t == 128     ? FD_FORMS(128, 1)
                         : t == 256     ? FD_FORMS(256, 1)
                                        : FD_FORMS(512, 1);
-#undef FD_SOME
 #undef FD_FORMS
   if (e != cudaSuccess) return e;
   const int64_t gates =

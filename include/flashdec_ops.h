@@ -392,8 +392,9 @@ fd_status fd_op_span_attention(const fd_span_attention* attn, const void* q, int
  * (dk, dv over the queries and the group's heads). The probabilities are computed again and never
  * stored. Sums are in fp32 and a fixed order: equal calls give equal bits; P and dS are rounded to dtype for
  * their products (fp16: scaled by powers of two, dS by 2^-E for the largest |dout| = f 2^E, 1 <= f < 2:
- * |dS| of 65504 2^E and more, which takes values in the hundreds that dout points along, is infinite). Queries that see
- * nothing and keys that nothing sees get zeros. dq like q, dk and dv like k, each with strides of its own;
+ * |dS| of 65504 2^E and more, which takes values in the hundreds that dout points along, is infinite).
+ * Queries that see nothing and keys that nothing sees get zeros. dq like q, dk and dv like k, each with
+ * strides of its own;
  * they share no memory with the inputs or each other. spans, err_dev as above; workspace of
  * fd_span_attention_workspace_bytes(attn, 1). */
 fd_status fd_op_span_attention_bwd(
@@ -467,8 +468,8 @@ fd_status fd_op_block_join(const fd_block_join* join, const void* h, int64_t h_s
  *   e = w gate post_gain;  db = r_post (e - n mean(e n))
  * (without the norms: d = dy, db = w gate). h_exps not NULL: h points to codes of rows of `width` (h_stride =
  * width), their exponents at h_exps; b the same. h is not read without a pre_gain. dh may be dy, db may
- * be du or a b that is not in codes (same pointer and strides); dh, db, d_post, d_pre, d_gate may be NULL: not wanted. Sums over tokens are in a fixed
- * order: equal calls give equal bits. workspace: fd_block_join_bwd_workspace_bytes(...) bytes of device
+ * be du or a b that is not in codes (same pointer and strides); dh, db, d_post, d_pre, d_gate may be NULL: not
+ * wanted. Sums over tokens are in a fixed order: equal calls give equal bits. workspace: fd_block_join_bwd_workspace_bytes(...) bytes of device
  * memory (16-byte aligned) that the call overwrites; calls that may overlap need one each. With rows
  * = 0 d_post and d_pre are zeros. */
 size_t fd_block_join_bwd_workspace_bytes(int rows, int width);

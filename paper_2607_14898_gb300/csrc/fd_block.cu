@@ -435,8 +435,10 @@ __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ Jo
         s_gate[v].v[i] = fma2(d[v].v[i], n[v].v[i], s_gate[v].v[i]);
         db.v[i] = fma2(mul2(q.v[i], d[v].v[i]), rpost2, mul2(en2, n[v].v[i]));
       }
-      if (unit < units && (FORM != kSome || p.dh != nullptr)) store8(static_cast<H*>(p.dh) + row * p.dh_stride + unit * 8, d[v]);
-      if (unit < units && (FORM != kSome || p.db != nullptr)) store8(static_cast<B*>(p.db) + row * p.db_stride + unit * 8, db);
+      if (unit < units && (FORM != kSome || p.dh != nullptr))
+        store8(static_cast<H*>(p.dh) + row * p.dh_stride + unit * 8, d[v]);
+      if (unit < units && (FORM != kSome || p.db != nullptr))
+        store8(static_cast<B*>(p.db) + row * p.db_stride + unit * 8, db);
     }
   }
   if (row0 < row1 && p.gate != nullptr) leave();
@@ -565,11 +567,13 @@ cudaError_t launch_join_bwd(const JoinBwd& p, cudaStream_t s) {
   const int t = bwd_threads(p.width);
   const bool all = p.post != nullptr && p.pre != nullptr && p.dy != nullptr && p.dh != nullptr && p.db != nullptr;
   auto go = [&](auto some, auto as_they_are, auto kept) {
-    return launch_pdl(!all || (p.h_exps == nullptr) != (p.b_exps == nullptr) ? some : p.h_exps != nullptr ? kept : as_they_are,
-                      dim3(p.grid), dim3(t), 0, s, p);
+    const bool mixed = (p.h_exps == nullptr) != (p.b_exps == nullptr);
+    return launch_pdl(!all || mixed ? some : p.h_exps != nullptr ? kept : as_they_are, dim3(p.grid),
+                      dim3(t), 0, s, p);
   };
 #define FD_FORMS(NT, NV) \
-  go(join_bwd_kernel<B, H, NT, NV, kSome>, join_bwd_kernel<B, H, NT, NV, kAll>, join_bwd_kernel<B, H, NT, NV, kAllKept>)
+  go(join_bwd_kernel<B, H, NT, NV, kSome>, join_bwd_kernel<B, H, NT, NV, kAll>,  \
+     join_bwd_kernel<B, H, NT, NV, kAllKept>)
   const cudaError_t e = p.width > 4096 ? FD_FORMS(512, 2)
                         : t == 32      ? FD_FORMS(32, 1)
                         : t == 64      ? FD_FORMS(64, 1)

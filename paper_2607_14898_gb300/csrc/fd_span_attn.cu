@@ -2,16 +2,17 @@
 //   s = scale q k^T within the span, lse = log sum exp s, out = exp(s - lse) v
 // by blocks of 128 keys with a running maximum and sum, kept in fp32 with O in TMEM.
 //
-// Bound by the chain from a block's scores through their softmax to the product that waits for it, and
-// by the softmax's instructions: of a 4680-token clip's heads of 64, 57 % of the issue slots, 39 % of the tensor cores;
-// of 4096 causal tokens' heads of 128, 43 % and 55 %. Measured, of the measured cuBLAS rate:
+// Bound by the chain from a block's scores through their softmax to the product that waits for it, and by
+// the softmax's instructions: heads of 64 (a clip of 4680 tokens) use 57 % of the issue slots and 39 % of the
+// tensor cores, heads of 128 (4096 causal tokens) 43 % and 55 %. Measured, of the measured cuBLAS rate:
 //   9360 queries in chunks of 1560, each sees up to 4; 16 heads of 64 on 4   201 us   892 TFLOP/s, 47 %
 //   8191 packed causal tokens, 32 heads of 128 on 8                       187 us   914 TFLOP/s, 48 %
 //   8191 queries, as many keys, every one seen, 32 heads of 128 on 8      721 us  1524 TFLOP/s, 81 %
-//   1 query of 8 sequences, 49920 keys, 16 heads of 64 on 4               16.6 us  3.1 TB/s (3 us of it to join parts)
-// Slower were: one block an SM with a row tile over blocks of 256 keys, by quarters (229 us for the first); blocks that
-// stay and take one unit after another (5 to 20 %); no running maximum while sums stay small (222); four blocks an SM over
-// 64 keys, a thread a row (246); no warp of its own for the zeros (199 instead of 187 for the second).
+//   1 query of 8 sequences, 49920 keys, 16 heads of 64 on 4               16.6 us  3.1 TB/s, 3 us to join parts
+// Slower were: one block an SM with a row tile over blocks of 256 keys, by quarters (229 us for the first);
+// blocks that stay and take one unit after another (5 to 20 %); no running maximum while sums stay small
+// (222); four blocks an SM over 64 keys, a thread a row (246); no warp of its own for the zeros (199 instead
+// of 187 for the second).
 #include <algorithm>
 #include <cmath>
 

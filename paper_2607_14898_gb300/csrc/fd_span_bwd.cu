@@ -13,8 +13,8 @@
 // of the measured cuBLAS rate:
 //   9360 queries in chunks of 1560, each sees up to 4; 16 heads of 64 on 4   520 us  1208 TFLOP/s, 64 %
 //   8191 causal tokens, 32 heads of 128 on 8                               1.2 ms  1600 TFLOP/s, 84 %
-// (a smaller clip: tensor cores 50 % busy, issue slots 58 %; smaller causal tokens: 66 % and 50 %). Dropped: X and Y read
-// together, with dS told a step later (688 us to 1056 for the first).
+// (a smaller clip: tensor cores 50 % busy, issue slots 58 %; fewer causal tokens: 66 % and 50 %). Dropped: X
+// and Y read together, with dS told a step later (688 us to 1056 for the first).
 #include <algorithm>
 #include <cmath>
 

@@ -76,6 +76,8 @@ class ResidualAttention:
     def forward(self, h, u, spans):
         """(y, u_next) of the residual stream h float32 [tokens][width] and the block's normed input u bfloat16;
         spans int32 [tokens][2]: the keys that each token sees."""
+        if u.dtype != torch.bfloat16 or not u.is_contiguous():
+            raise TypeError("u: a contiguous bfloat16 tensor is required")  # (the products read it as it lies)
         self.spans = spans
         fdp.op_checkpoint_save(u, self.u_kept)
         self._linear(u, self.w_qkv, self.qkv)

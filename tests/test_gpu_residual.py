@@ -156,3 +156,21 @@ def test_example_runs_and_its_gradients():
             want = (sides[0] - sides[1]) / 2e-4
             found = float((t.grad.double() * way).sum())
             assert abs(found - want) <= 2 * BOUND * float(t.grad.double().norm()) * float(way.norm()), (i, name)
+
+
+def test_inputs_that_are_refused():
+    T, w, x, spans = make([90, 38], 0, 256, 4, 2, 64, 64)
+    block = ResidualAttention(T, 256, 4, 2, 64, w["w_qkv"], w["w_out"], w["post_gain"], w["pre_gain"], w["gate"], 64)
+    wide = torch.zeros(T, 512, dtype=torch.bfloat16, device="cuda")[:, :256]
+    for u in (x["u"].float(), x["u"].half(), wide, x["u"][:-8], x["u"].cpu(), x["u"][:, :128].contiguous()):
+        with pytest.raises((TypeError, ValueError)):
+            block.forward(x["h"], u, spans)
+    for s in (spans.long(), spans[:-8], spans.cpu(), spans.flatten()):
+        with pytest.raises((TypeError, ValueError)):
+            block.forward(x["h"], x["u"], s)
+    for h in (x["h"].half(), x["h"][:, :128], x["h"].cpu()):
+        with pytest.raises((TypeError, ValueError, RuntimeError)):  # (the library refuses a mix of types)
+            block.forward(h, x["u"], spans)
+    y, u_next = block.forward(x["h"], x["u"], spans)  # works as before
+    want = block.forward(x["h"], x["u"], spans)
+    assert torch.equal(y, want[0]) and torch.equal(u_next, want[1])

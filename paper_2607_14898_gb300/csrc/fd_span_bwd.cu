@@ -12,7 +12,7 @@
 // Bound by the chain from the scores through P and dS to the products that wait for them; all 7 products
 // of the measured cuBLAS rate:
 //   9360 queries in chunks of 1560, each sees up to 4; 16 heads of 64 on 4   520 us  1208 TFLOP/s, 64 %
-//   8191 causal tokens, 32 heads of 128 on 8                               1.2 ms  1600 TFLOP/s, 84 %
+//   8191 causal tokens, 32 heads of 128 on 8                              1190 us  1615 TFLOP/s, 85 %
 // (a smaller clip: tensor cores 50 % busy, issue slots 58 %; fewer causal tokens: 66 % and 50 %). Dropped: X
 // and Y read together, with dS told a step later (688 us to 1056 for the first).
 #include <algorithm>
@@ -46,7 +46,8 @@ constexpr float kPUpLog2 = 14.f;
 
 // What a row tile's record holds, 16 bytes in line: -lse log2(e), -delta and the ends of the span (int) of
 // each row, [4][128], then the tile's limits: {first key, end of the keys} that some query sees, {first, end}
-// of those that all queries see which see any; the third is negative (~) where some query sees none.
+// of those that all queries see which see any; the third is negative (~) where some query sees none, the fourth
+// where some query sees one.
 constexpr int kRecord = 4 * kTile + 4;
 
 // ------------------------------------------------------------------------------ rows
@@ -111,7 +112,7 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
   }
   if (threadIdx.x < 32) {
     int4 m = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
-    bool none = false;
+    bool none = false, one = false;
     for (int i = threadIdx.x; i < p.y.tile_tokens && token0 + i < p.y.n_q; i += 32) {
       const int2 s = span_of(p.spans, token0 + i, p.y.n_k);
       if (s.x < s.y) {
@@ -119,6 +120,7 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
         m.y = max(m.y, s.y);
         m.z = max(m.z, s.x);
         m.w = min(m.w, s.y);
+        one |= s.x + 1 == s.y;
       } else {
         none = true;
       }
@@ -128,6 +130,7 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
     m.z = __reduce_max_sync(0xffffffffu, m.z);
     m.w = __reduce_min_sync(0xffffffffu, m.w);
     if (__any_sync(0xffffffffu, none)) m.z = ~m.z;
+    if (__any_sync(0xffffffffu, one)) m.w = ~m.w;
     if (threadIdx.x == 0) {
       *reinterpret_cast<int4*>(stat + 4 * kTile) = m;
       if (group == 0) p.limits[tile] = m;
@@ -476,7 +479,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
       const int st = i % C::kStages;
-      bool masked = false;
+      bool masked = false, one = false;
 #pragma unroll 1
       for (int s = 0; s < C::kSteps; ++s, ++k) {
         const uint8_t* stat = smem + C::kOffStat + st * C::kStat + (s * C::kStep + q * C::kCols) * 4;
@@ -487,7 +490,8 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
         if (s == 0) {
           // (a tile between others may see nothing of the block, or nothing at all)
           const int4 m = *reinterpret_cast<const int4*>(smem + C::kOffStat + st * C::kStat + 16 * kTile);
-          masked = m.x > key0 || (m.z < 0 ? ~m.z : m.z) > key0 || m.w < key0 + kTile;
+          masked = m.x > key0 || (m.z < 0 ? ~m.z : m.z) > key0 || (m.w < 0 ? ~m.w : m.w) < key0 + kTile;
+          one = m.w < 0;
         }
         uint32_t seen = 0xffffffffu;  // bit c: the key is seen by row c of the quarter
         if (masked) {
@@ -568,6 +572,19 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
         }
         if (masked) {
           __syncwarp();
+          // And where a row sees one key only: P is 1 whatever the scores, so dS is 0, not what rounding
+          // leaves of a difference. (A loop: unrolled it took registers from every step, 535 us instead of
+          // 520 for the 480p clip.)
+          if (one) {
+#pragma unroll 1
+            for (int c = 0; c < C::kCols; c += 4) {
+              const int4 lo = *reinterpret_cast<const int4*>(stat + 2 * kTile * 4 + c * 4);
+              const int4 hi = *reinterpret_cast<const int4*>(stat + 3 * kTile * 4 + c * 4);
+              const uint32_t four = (lo.x + 1 == hi.x ? 1u : 0u) | (lo.y + 1 == hi.y ? 2u : 0u) |
+                                    (lo.z + 1 == hi.z ? 4u : 0u) | (lo.w + 1 == hi.w ? 8u : 0u);
+              seen &= ~(four << c);
+            }
+          }
 #pragma unroll
           for (int c = 0; c < C::kCols; ++c)
             if (!(seen & (1u << c))) y[c] = 0;
@@ -892,7 +909,7 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
       }
       if (masked) {
         __syncwarp();  // (as above)
-        const uint32_t seen = seen_word(span, key0);
+        const uint32_t seen = span.y - span.x > 1 ? seen_word(span, key0) : 0u;
 #pragma unroll
         for (int c = 0; c < 32; ++c)
           if (!(seen & (1u << c))) y[c] = 0;

@@ -248,3 +248,24 @@ def test_largest_gradient_of_many_tiles(at, D):
     s["dout"][:, at].mul_(2000)
     out, lse = run(s)
     check(run_bwd(s, out, lse), gradient(s, out, lse), s)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [BF16, FP16], ids=str)
+def test_queries_that_see_one_key(dtype, D):
+    """Their probability is 1 whatever the score: dq is zero, dk has nothing of them, dv their dout."""
+    T = 300
+    one = [(t, t + 1) for t in range(T)]
+    s = make(one, T, 6, 2, D, dtype)
+    out, lse = run(s)
+    got = run_bwd(s, out, lse)
+    assert not bool(got["dq"].any()) and not bool(got["dk"].any())
+    check(got, gradient(s, out, lse), s)
+    # among others: every third query sees one key, another one sees those and more
+    mixed = [(t, t + 1) if t % 3 else (max(0, t - 40), t + 1) for t in range(T)]
+    s = make(mixed, T, 6, 2, D, dtype)
+    out, lse = run(s)
+    got = run_bwd(s, out, lse)
+    check(got, gradient(s, out, lse), s)
+    alone = [t for t in range(T) if t % 3] + [0]
+    assert not bool(got["dq"][alone].any()) and bool(got["dq"][3:][::3].any(-1).all())

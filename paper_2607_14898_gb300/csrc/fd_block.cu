@@ -9,10 +9,10 @@
 //   dpost = sum w gate n;  dpre = sum du m;  e = w gate post;  db = r_post (e - n mean(e n))
 // (sums over the tokens; of a gate's tokens for dgate). All in fp32.
 //
-// Every row is read and written once, its sums taken while it is in registers. Measured, of a plain copy's
-// rate:
-//   6240 x 1024, bf16 on fp32, both inputs kept in 8 bits: join      15.4 us  5.9 TB/s, 87 %
-//     its gradient from 8 bits, a gate, two launches                  19.7 us  4.6 TB/s, 68 %
+// Every row is read and written once, its sums taken while it is in registers. Measured on inputs that are
+// not in L2, of a plain copy's rate:
+//   6240 x 1024, bf16 on fp32, both inputs kept in 8 bits: join      18.5 us  4.9 TB/s, 72 %
+//     its gradient from 8 bits, a gate, two launches                  24.7 us  3.6 TB/s, 54 %
 //   16001 x 4096, bf16, a gate for 1000 rows: gradient               153 us   5.1 TB/s, 76 %
 #include <algorithm>
 #include <cmath>
@@ -168,12 +168,13 @@ cudaError_t launch_join(const Join& p, cudaStream_t s) {
     return launch_pdl(kernel, dim3((p.rows + per_block - 1) / per_block),
                       dim3(warps == 1 ? 128 : warps * 32), 0, s, p);
   };
-  // Two groups of eight elements a thread: with four, a warp a row, the 480p chunk took 19.8 us instead
-  // of 15.4. Few rows are spread over more warps, for which a row is a shorter chain.
+  // Up to 1024 elements a group of eight a thread (6240 x 1024: 18.3 us, two groups 19.4, four 22.8), past that
+  // two (8000 x 4096: 78 us, one group 90). Few rows are spread over more warps, for which a row is a
+  // shorter chain.
   const bool few = p.rows < 4 * num_sms();
   if (units <= 32) return go(join_kernel<B, H, 1, 1>, 1);
-  if (units <= 64) return go(join_kernel<B, H, 1, 2>, 1);
-  if (units <= 128) return few ? go(join_kernel<B, H, 4, 1>, 4) : go(join_kernel<B, H, 2, 2>, 2);
+  if (units <= 64) return go(join_kernel<B, H, 2, 1>, 2);
+  if (units <= 128) return go(join_kernel<B, H, 4, 1>, 4);
   if (units <= 256) return few ? go(join_kernel<B, H, 8, 1>, 8) : go(join_kernel<B, H, 4, 2>, 4);
   if (units <= 512) return few ? go(join_kernel<B, H, 16, 1>, 16) : go(join_kernel<B, H, 8, 2>, 8);
   return go(join_kernel<B, H, 16, 2>, 16);
@@ -225,8 +226,8 @@ struct Inputs {
 // same): copies ahead into a ring in shared memory, three or four rows deep, made it slower (480p chunk 24.7 to 35
 // us), fewer instructions faster.
 // FORM: what there is, known beforehand where it is what training has, else looked up. (The branches for it, and
-// three sums a row that were added up apart, had the two cases above at 21.9 and 162 us, and 8000 rows of 8192 at
-// 370 instead of 242: they spill.)
+// three sums a row that were added up apart, cost 2 and 9 us of the two cases above; 8000 rows of 8192, which spill
+// more for them, took 370 us instead of 242.)
 enum Form { kSome, kAll, kAllKept };  // kAll: both norms, dy, dh and db; kAllKept: and both inputs in 8 bits
 template <typename B, typename H, int NT, int NV, Form FORM>
 __global__ void __launch_bounds__(NT) join_bwd_kernel(const __grid_constant__ JoinBwd p) {

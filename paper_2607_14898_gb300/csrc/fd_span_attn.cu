@@ -8,7 +8,7 @@
 //   9360 queries in chunks of 1560, each sees up to 4; 16 heads of 64 on 4   201 us   892 TFLOP/s, 47 %
 //   8191 packed causal tokens, 32 heads of 128 on 8                       187 us   914 TFLOP/s, 48 %
 //   8191 queries, as many keys, every one seen, 32 heads of 128 on 8      721 us  1524 TFLOP/s, 81 %
-//   1 query of 8 sequences, 49920 keys, 16 heads of 64 on 4               14.5 us  3.5 TB/s, 3 us to join parts
+//   1 query of 8 sequences, 49920 keys, 16 heads of 64 on 4               17.3 us  3.0 TB/s, 3 us to join parts
 // Slower were: one block an SM with a row tile over blocks of 256 keys, by quarters (229 us for the first);
 // blocks that stay and take one unit after another (5 to 20 %); no running maximum while sums stay small
 // (222); four blocks an SM over 64 keys, a thread a row (246); no warp of its own for the zeros (199 instead
@@ -295,8 +295,8 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     float m = -INFINITY, l = 0.f;
     // A wait that gives up has set the status word, and every wait after it returns at once: the warps
     // go on to the end. Warps without a row that sees any key (a tile of few queries has such) leave the
-    // others their issue slots, 16.5 us to 14.5 for the one query of 8 sequences; what is in their rows of TMEM
-    // goes nowhere.
+    // others their issue slots, which saves 2 us for the one query of 8 sequences; what is in their rows of
+    // TMEM goes nowhere.
     const bool idle = !__any_sync(0xffffffffu, sees);
 #pragma unroll 1
     for (int j = 0; j < count; ++j) {

@@ -377,8 +377,9 @@ size_t fd_span_attention_workspace_bytes(const fd_span_attention* attn, int back
 
 /* out[t][h] = sum_j exp(s_j - lse) v_j,  s_j = scale q[t][h] . k_j,  lse[h][t] = log sum_j exp(s_j)
  * (fp32, natural logarithm). A query that sees nothing gets zeros and -inf. Softmax and sums are in fp32, the
- * probabilities are rounded to dtype for their product with V. The order of every sum is fixed: equal
- * calls give equal bits. out shares no memory with the inputs. err_dev as for fd_op_linear. */
+ * probabilities are rounded to dtype for their product with V (fp16: times a power of two that keeps its digits
+ * down to 2^-25 of the row's largest; smaller ones are off by 2^-36 of that each). The order of every sum is
+ * fixed: equal calls give equal bits. out shares no memory with the inputs. err_dev as for fd_op_linear. */
 fd_status fd_op_span_attention(const fd_span_attention* attn, const void* q, int64_t q_token_stride,
                                int64_t q_head_stride, const void* k, int64_t k_token_stride,
                                int64_t k_head_stride, const void* v, int64_t v_token_stride,

@@ -33,7 +33,14 @@ struct SpanFwd {
   int* err;
 };
 
-constexpr float kSlack = 8.f;  // log2 by which a row's maximum may grow before O is rescaled
+// P is made as 2^Up exp(s - m), where m, the row's maximum (log2), may be Slack behind before O is rescaled.
+// fp16 ends at 2^16 and has steps of 2^-24 below 2^-14: with 11 and 4 P stays below 2^15 and keeps its digits down
+// to 2^-25 of the row's largest; smaller ones are off by 2^-36 of it each, those of all 2^24 keys by
+// 2^-12. (Sums of exponentials and O have the factor alike.) bf16 has fp32's range.
+template <bool F16>
+struct Lift {
+  static constexpr float kUp = F16 ? 11.f : 0.f, kSlack = F16 ? 4.f : 8.f;
+};
 
 // A block has a row tile of a group and a run of the key blocks, of 128 keys, that any of its queries
 // see. Two blocks share an SM (half of TMEM and of shared memory each), so that the softmax of one runs
@@ -344,7 +351,7 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
       at[h * kTile] = top;
       named_barrier(1 + lanes, 64);
       top = fmaxf(top, at[(h ^ 1) * kTile]);
-      const bool grow = top > m + kSlack;
+      const bool grow = top > m + Lift<F16>::kSlack;
       const float before = m;
       if (grow) m = top;
       const float off = m == -INFINITY ? 0.f : m;
@@ -364,10 +371,11 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
           tmem_st_32x32b_x16(o_col + d, o);
         }
       }
-      const uint64_t off2 = pack_f32x2(-off, -off);
+      const float lift = Lift<F16>::kUp - off;
+      const uint64_t off2 = pack_f32x2(lift, lift);
       uint64_t sum2[2] = {0, 0};
-      // P in the inputs' type, which the product with V takes: 2^-9 (bf16) or 2^-12 (fp16) of each p at
-      // most. The sums are of P unrounded.
+      // P in the inputs' type, which the product with V takes: half a step of each, 2^-8 (bf16) or 2^-11
+      // (fp16, down to 2^-25 of the row's largest) of it at most. The sums are of P unrounded.
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         if (x == 1) {
@@ -444,9 +452,9 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
     if (h == 0 && valid) {
       if (whole)
         p.lse[static_cast<int64_t>(head) * p.y.n_q + token] =
-            l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+            l == 0.f ? -INFINITY : (m - Lift<F16>::kUp + log2f(l)) * kLn2;
       else
-        p.part_ml[slot] = make_float2(m, l);
+        p.part_ml[slot] = make_float2(m - Lift<F16>::kUp, l);
     }
     if (whole) {
       fence_proxy_async_smem();

@@ -32,15 +32,20 @@ struct SpanBwd {
   const float* lse;
   float* stat;    // [group][row tile] records of kRecord: see below
   int4* limits;   // of each row tile, those of its records
-  float* most;    // [group][row tile]: the largest |dout| (fp16); behind them the largest of all
-  int mosts;      // of them, those that the blocks look through: 1 is the largest of all
+  // fp16: the largest |dout| of each row, [group][row tile][128]; of the heads of each token, {its span, that, 0},
+  // [group][token]; of each row tile, [group][row tile]
+  float* size_row;
+  float4* size_token;
+  float* size_tile;
   float* part_q;  // [group][row tile][part][D / 4][128 rows] of four
   float* part_k;  // [group][key block][part][dk, dv][D / 4][128 keys] of four
   int* err;
 };
 
-// fp16 has few exponents: P goes into its product times 2^14, and dS divided by the power of two in the
-// largest |dout|, so that small gradients keep their digits. bf16 has fp32's range.
+// fp16 has few exponents: P goes into its product times 2^14, and dS divided by the power of two in a largest
+// |dout|, so that small gradients keep their digits: for dq the row's own, for dk that of the rows that see
+// the key (a lane has one row or key, and with it one scale). Nothing of another sequence comes in.
+// bf16 has fp32's range.
 constexpr float kPUp = 16384.f;
 constexpr float kPUpLog2 = 14.f;
 
@@ -50,26 +55,31 @@ constexpr float kPUpLog2 = 14.f;
 // where some query sees one.
 constexpr int kRecord = 4 * kTile + 4;
 
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int i = 16; i; i >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, i));
+  return x;
+}
+
 // ------------------------------------------------------------------------------ rows
 // D / 8 lanes a row. A row that sees nothing, or is none, gets P = 0 by an infinite lse.
 template <bool F16, int D>
 __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ SpanBwd p) {
   constexpr int kLanes = D / 8;
-  __shared__ float top[8];
+  __shared__ float size[kTile];
   grid_dep_wait();
   grid_dep_launch();
   const int tile = blockIdx.x, group = blockIdx.y;
   const int token0 = tile * p.y.tile_tokens;
   const int lane = threadIdx.x % kLanes;
   float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord;
-  float most = 0.f;
 #pragma unroll
   for (int row = threadIdx.x / kLanes; row < kTile; row += 256 / kLanes) {
     const int token = token0 + row / p.y.per, head = group * p.y.per + row % p.y.per;
     const bool valid = row < p.y.tile_rows && token < p.y.n_q;
     const int2 span = valid ? span_of(p.spans, token, p.y.n_k) : make_int2(0, 0);
     const bool sees = span.x < span.y;
-    float sum = 0.f;
+    float sum = 0.f, most = 0.f;
     if (sees) {
       const uint4 a = __ldg(reinterpret_cast<const uint4*>(
           static_cast<const uint16_t*>(p.out.p) + token * p.out.token + head * p.out.head + lane * 8));
@@ -91,7 +101,14 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
       }
     }
 #pragma unroll
-    for (int i = kLanes / 2; i; i >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, i);
+    for (int i = kLanes / 2; i; i >>= 1) {
+      sum += __shfl_xor_sync(0xffffffffu, sum, i);
+      if (F16) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, i));
+    }
+    if (F16 && lane == 0) {
+      size[row] = most;
+      p.size_row[(static_cast<int64_t>(group) * p.y.row_tiles + tile) * kTile + row] = most;
+    }
     if (lane == 0) {
       const float l = sees ? __ldg(p.lse + static_cast<int64_t>(head) * p.y.n_q + token) : 0.f;
       stat[row] = sees ? fmaf(-l, kLog2e, F16 ? kPUpLog2 : 0.f) : -INFINITY;
@@ -100,21 +117,20 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
       reinterpret_cast<int*>(stat)[3 * kTile + row] = span.y;
     }
   }
-  if (F16) {
-#pragma unroll
-    for (int i = 16; i; i >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, i));
-    if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int i = 1; i < 8; ++i) most = fmaxf(most, top[i]);
-      p.most[group * p.y.row_tiles + tile] = most;
-    }
-  }
+  if (F16) __syncthreads();
   if (threadIdx.x < 32) {
     int4 m = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
     bool none = false, one = false;
+    float most = 0.f;  // of the tile
     for (int i = threadIdx.x; i < p.y.tile_tokens && token0 + i < p.y.n_q; i += 32) {
       const int2 s = span_of(p.spans, token0 + i, p.y.n_k);
+      if (F16) {
+        float of_token = 0.f;
+        for (int h = 0; h < p.y.per; ++h) of_token = fmaxf(of_token, size[i * p.y.per + h]);
+        p.size_token[static_cast<int64_t>(group) * p.y.n_q + token0 + i] =
+            make_float4(__int_as_float(s.x), __int_as_float(s.y), of_token, 0.f);
+        most = fmaxf(most, of_token);
+      }
       if (s.x < s.y) {
         m.x = min(m.x, s.x);
         m.y = max(m.y, s.y);
@@ -131,49 +147,19 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
     m.w = __reduce_min_sync(0xffffffffu, m.w);
     if (__any_sync(0xffffffffu, none)) m.z = ~m.z;
     if (__any_sync(0xffffffffu, one)) m.w = ~m.w;
+    if (F16) most = warp_max(most);
     if (threadIdx.x == 0) {
+      if (F16) p.size_tile[group * p.y.row_tiles + tile] = most;
       *reinterpret_cast<int4*>(stat + 4 * kTile) = m;
       if (group == 0) p.limits[tile] = m;
     }
   }
 }
 
-// The largest |dout| of all tiles (fp16), where they are too many for every block to look through: 131072 tokens of
-// 16 heads of 128 on 8 in windows of 512 (16384 tiles) took 3909 us, and take 2794. 8191 causal tokens (2048 tiles),
-// whose blocks have more to do, take the same either way (1283, 1292), the 480p clip 575 and 565.
-constexpr int kFewTiles = 256;  // a round of loads of one warp
-__global__ void __launch_bounds__(1024) span_most_kernel(float* most, int tiles) {
-  __shared__ float top[32];
-  grid_dep_wait();
-  grid_dep_launch();
-  float m = 0.f;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < tiles; i += 1024) m = fmaxf(m, __ldcg(most + i));
-#pragma unroll
-  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-  if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = m;
-  __syncthreads();
-  if (threadIdx.x >= 32) return;
-  m = top[threadIdx.x];
-#pragma unroll
-  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-  if (threadIdx.x == 0) most[tiles] = m;
-}
-
-// 2^-E of the largest |dout| = f 2^E, 1 <= f < 2, over all tiles, by one warp (fp16)
-__device__ __forceinline__ float down_scale(const SpanBwd& p) {
-  const int tiles = p.y.groups * p.y.row_tiles;
-  const float* most = tiles > kFewTiles ? p.most + tiles : p.most;
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < kFewTiles; i += 32) {
-    const int at = i + (threadIdx.x & 31);
-    if (at < p.mosts) m = fmaxf(m, __ldcg(most + at));
-  }
-#pragma unroll
-  for (int i = 16; i; i >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
-  const uint32_t e = __float_as_uint(m) >> 23;  // (fp16: e is 103 at least unless m is zero)
-  return m > 0.f && e < 255u ? __uint_as_float((254u - e) << 23) : 1.f;
+// 2^-E for a largest |dout| = f 2^E, 1 <= f < 2
+__device__ __forceinline__ float down_scale(float most) {
+  const uint32_t e = __float_as_uint(most) >> 23;  // (fp16: 103 at least unless it is zero)
+  return most > 0.f && e < 255u ? __uint_as_float((254u - e) << 23) : 1.f;
 }
 
 // ------------------------------------------------------------------------------ keys: dk and dv
@@ -203,7 +189,9 @@ struct KeyCfg {
                        kXFull = kReady + kStages, kYFull = kXFull + 1, kXRead = kYFull + 1,
                        kYRead = kXRead + 1, kPFull = kYRead + 1, kDsFull = kPFull + 1,
                        kPDone = kDsFull + 1, kDsDone = kPDone + 1, kDone = kDsDone + 1, kBars = kDone + 4;
-  static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
+  static constexpr int kOffSize = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;  // fp16: [16 warps][32 tokens]
+  static constexpr int kOffAll = kOffSize + 16 * 32 * 16;  // [4][128]
+  static constexpr int kSmem = kOffAll + 4 * kTile * 4;
   static constexpr uint32_t kColX = 0, kColY = kStep, kColP = 2 * kStep, kColDs = kColP + kStep / 2,
                             kColDv = 512 - 2 * D, kColDk = 512 - D;
   static_assert(kSmem <= 227 * 1024 && kColDs + kStep / 2 <= kColDv, "room");
@@ -259,6 +247,81 @@ __device__ __forceinline__ void leave16_none(uint8_t* tile, float4* part, int ro
   }
 }
 
+// The largest |dout| of the rows that see a thread's key (fp16), by warps 0-15: the four warps of a key share the
+// tokens out, 32 at a time, and leave what they find in shared memory.
+template <int D>
+struct KeySizes {
+  const SpanBwd& p;
+  const int group, lane, q, at, key;  // at: the key's place in the block
+  float4* const mine;
+  float* const all;  // [quarter][key]
+  float size = 0.f;
+
+  __device__ __forceinline__ KeySizes(const SpanBwd& p, uint8_t* smem, int group, int key0)
+      : p(p), group(group), lane(threadIdx.x & 31), q(threadIdx.x >> 7), at(threadIdx.x & 127), key(key0 + at),
+        mine(reinterpret_cast<float4*>(smem + KeyCfg<D>::kOffSize) + (threadIdx.x >> 5) * 32),
+        all(reinterpret_cast<float*>(smem + KeyCfg<D>::kOffAll)) {}
+  __device__ __forceinline__ float4 token(int t, int end) const {
+    return t + lane < end ? __ldcg(p.size_token + static_cast<int64_t>(group) * p.y.n_q + t + lane)
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void look_at(const float4& tokens, int count) {
+    mine[lane] = tokens;
+    __syncwarp();
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += 8)
+#pragma unroll
+      for (int i = i0; i < i0 + 8; ++i) {
+        const float4 x = mine[i];
+        if (__float_as_int(x.x) <= key && key < __float_as_int(x.y)) size = fmaxf(size, x.z);
+      }
+    __syncwarp();
+  }
+  // Row tiles [first, end), every fourth of them. A tile whose rows see all of the block's keys, or none, counts as a
+  // whole; of the others every token is looked at, the next ones on their way meanwhile.
+  __device__ __forceinline__ void look_at_tiles(int first, int end) {
+    const int key0 = key - at, keys_end = min(key0 + kTile, p.y.n_k);
+    float of_tiles = 0.f;
+    int held = 0;
+    float4 x;
+#pragma unroll 1
+    for (int i0 = first + q; i0 < end; i0 += 128) {
+      const int tile = i0 + 4 * lane;
+      bool some = false;
+      if (tile < end) {
+        const int4 m = __ldcg(p.limits + tile);
+        const float of_tile = __ldcg(p.size_tile + group * p.y.row_tiles + tile);
+        if (m.x < keys_end && m.y > key0) {
+          some = (m.z < 0 ? ~m.z : m.z) > key0 || (m.w < 0 ? ~m.w : m.w) < keys_end;
+          if (!some) of_tiles = fmaxf(of_tiles, of_tile);
+        }
+      }
+#pragma unroll 1
+      for (uint32_t left = __ballot_sync(0xffffffffu, some); left; left &= left - 1) {
+        const int token0 = (i0 + 4 * (__ffs(left) - 1)) * p.y.tile_tokens;
+        const int token1 = min(token0 + p.y.tile_tokens, p.y.n_q);
+#pragma unroll 1
+        for (int t = token0; t < token1; t += 32) {
+          const float4 next = token(t, token1);
+          if (held > 0) look_at(x, held);
+          x = next;
+          held = min(32, token1 - t);
+        }
+      }
+    }
+    if (held > 0) look_at(x, held);
+    size = fmaxf(size, warp_max(of_tiles));
+  }
+  __device__ __forceinline__ void leave() const { all[q * kTile + at] = size; }
+  // of all four, after a barrier
+  __device__ __forceinline__ float found() const {
+    return fmaxf(fmaxf(all[at], all[kTile + at]), fmaxf(all[2 * kTile + at], all[3 * kTile + at]));
+  }
+};
+// So few tokens are all looked at, while the limits of the tiles are on their way (2 sequences of 77, forward and
+// backward launches in a stream: 17.4 us, by tiles 17.9).
+constexpr int kFewTokens = 256;
+
 template <bool F16, int D>
 __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtensorMap& tmDo,
                                            const CUtensorMap& tmK, const CUtensorMap& tmV,
@@ -274,7 +337,6 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
   auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
   int* range = reinterpret_cast<int*>(tmem_slot + 1);  // first row tile, the one past the last
-  volatile float* down = reinterpret_cast<volatile float*>(tmem_slot + 3);
 
   const int part = unit % p.k_parts, kb = unit / p.k_parts % p.y.key_blocks;
   const int group = unit / (p.k_parts * p.y.key_blocks);
@@ -324,9 +386,16 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
     }
   }
   __syncthreads();
+  KeySizes<D> sizes(p, smem, group, key0);
+  const bool few = p.y.n_q <= kFewTokens;
   {
     // the row tiles that see some of the keys: from the first to the last
     int first = 0x7fffffff, end = 0;
+    float4 tokens[kFewTokens / 128];
+    if (F16 && few && warp < 16) {
+#pragma unroll
+      for (int i = 0; i < kFewTokens / 128; ++i) tokens[i] = sizes.token((4 * i + sizes.q) * 32, p.y.n_q);
+    }
     for (int i = threadIdx.x; i < p.y.row_tiles; i += C::kThreads) {
       const int4 m = __ldcg(p.limits + i);
       if (m.x < key0 + kTile && m.y > key0) {
@@ -340,9 +409,11 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
       atomicMin(range, first);
       atomicMax(range + 1, end);
     }
-    if (F16 && warp == 0) {
-      const float f = down_scale(p);
-      if (lane == 0) *down = f;
+    if (F16 && few && warp < 16) {
+#pragma unroll
+      for (int i = 0; i < kFewTokens / 128; ++i)
+        sizes.look_at(tokens[i], min(32, p.y.n_q - (4 * i + sizes.q) * 32));
+      sizes.leave();
     }
   }
   tc_fence_before();
@@ -353,7 +424,15 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
   const int tile0 = range[0] + static_cast<int>(static_cast<int64_t>(n) * part / p.k_parts);
   const int count = static_cast<int>(static_cast<int64_t>(n) * (part + 1) / p.k_parts) -
                     static_cast<int>(static_cast<int64_t>(n) * part / p.k_parts);
-  const float ds_down = F16 ? *down : 1.f;  // dS is kept times this
+  float ds_down = 1.f;  // the key's dS are kept times this
+  if (F16 && warp < 16) {
+    if (!few) {
+      sizes.look_at_tiles(range[0], range[1]);
+      sizes.leave();
+      named_barrier(1, 512);
+    }
+    ds_down = down_scale(sizes.found());
+  }
 
   if (count == 0) {
     // no row sees any of the keys (which may be on their way to where zeros leave from)
@@ -682,7 +761,6 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
-  volatile float* down = reinterpret_cast<volatile float*>(tmem_slot + 1);
 
   const int part = unit % p.q_parts;
   const int tile = p.y.row_tiles - 1 - unit / p.q_parts % p.y.row_tiles;
@@ -725,9 +803,6 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
   if (warp == 0) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
-  } else if (F16 && warp == 1) {
-    const float f = down_scale(p);
-    if (lane == 0) *down = f;
   }
   const int4 m = __ldcg(p.limits + tile);
   const int b0 = m.y > 0 ? m.x / kTile : 0;
@@ -760,7 +835,6 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const float ds_down = F16 ? *down : 1.f;
 
   if (count == 0) {
     // no row sees any key
@@ -859,7 +933,9 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
   if (warp < 16) {
     // ---- dS of a quarter of each block's keys
     const int q = warp >> 2, row = (warp & 3) * 32 + lane;
-    const float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord + row;
+    const int64_t at = static_cast<int64_t>(group) * p.y.row_tiles + tile;
+    const float* stat = p.stat + at * kRecord + row;
+    const float ds_down = F16 ? down_scale(__ldcg(p.size_row + at * kTile + row)) : 1.f;  // dS is kept times this
     const float neg_lse = __ldcg(stat), neg_delta = __ldcg(stat + kTile);
     const int2 span = make_int2(__ldcg(reinterpret_cast<const int*>(stat) + 2 * kTile),
                                 __ldcg(reinterpret_cast<const int*>(stat) + 3 * kTile));
@@ -1039,7 +1115,7 @@ int parts_for(int64_t units, int steps) {
 
 struct BwdPlan {
   int q_parts, k_parts;
-  size_t stat, limits, most, part_q, part_k, total;  // byte offsets
+  size_t stat, limits, size_row, size_token, size_tile, part_q, part_k, total;  // byte offsets
 };
 BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   BwdPlan b{};
@@ -1049,8 +1125,11 @@ BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   b.stat = 0;
   b.limits = up(b.stat + tiles * kRecord * sizeof(float));
-  b.most = b.limits + up(static_cast<size_t>(y.row_tiles) * sizeof(int4));
-  b.part_q = b.most + up((tiles + 1) * sizeof(float));
+  // (for either type: the plan has none)
+  b.size_row = b.limits + up(static_cast<size_t>(y.row_tiles) * sizeof(int4));
+  b.size_token = b.size_row + up(tiles * kTile * sizeof(float));
+  b.size_tile = b.size_token + up(static_cast<size_t>(y.groups) * y.n_q * sizeof(float4));
+  b.part_q = b.size_tile + up(tiles * sizeof(float));
   b.part_k = b.part_q + (b.q_parts > 1 ? tiles * b.q_parts * kTile * head_dim * sizeof(float) : 0);
   b.total = b.part_k + (b.k_parts > 1 ? static_cast<size_t>(y.groups) * y.key_blocks * b.k_parts * 2 *
                                             kTile * head_dim * sizeof(float)
@@ -1083,8 +1162,6 @@ cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, c
     });
   if (e == cudaSuccess)
     e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles, p.y.groups), dim3(256), 0, s, p);
-  if (e == cudaSuccess && F16 && p.y.row_tiles * p.y.groups > kFewTiles)
-    e = launch_pdl(span_most_kernel, dim3(1), dim3(1024), 0, s, p.most, p.y.row_tiles * p.y.groups);
   if (e == cudaSuccess)
     e = launch_pdl(span_grad_kernel<F16, D>,
                    dim3((p.y.key_blocks * p.k_parts + p.y.row_tiles * p.q_parts) * p.y.groups),
@@ -1171,9 +1248,9 @@ fd_status fd_op_span_attention_bwd(
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.stat = reinterpret_cast<float*>(ws + b.stat);
   p.limits = reinterpret_cast<int4*>(ws + b.limits);
-  p.most = reinterpret_cast<float*>(ws + b.most);
-  const int tiles = p.y.groups * p.y.row_tiles;
-  p.mosts = tiles <= fd::kFewTiles ? tiles : 1;
+  p.size_row = reinterpret_cast<float*>(ws + b.size_row);
+  p.size_token = reinterpret_cast<float4*>(ws + b.size_token);
+  p.size_tile = reinterpret_cast<float*>(ws + b.size_tile);
   p.part_q = reinterpret_cast<float*>(ws + b.part_q);
   p.part_k = reinterpret_cast<float*>(ws + b.part_k);
   p.err = err_dev;

@@ -1,13 +1,16 @@
 """Attention in spans of keys in fp16 where its range could cost digits: few large probabilities beside many
-small ones.
+small ones, gradients of very different sizes beside each other.
 
-Tolerances are those of test_gpu_span_attention.py without what it allows fp16 for each key that a query sees:
-probabilities keep half a step, 2^-11, down to 2^-25 of the row's largest."""
+Tolerances are those of test_gpu_span_attention.py and test_gpu_span_gradient.py without what these allow fp16 for
+each key that a query sees. Forward: probabilities keep half a step, 2^-11, down to 2^-25 of the row's largest.
+Gradient: dS is off by 2^-25 of the largest |dout| of its own row (dq) or of the rows that see the key (dk)."""
 import math
 
 import pytest
 import torch
-from test_gpu_span_attention import FP16, U, check, make, run
+from test_gpu_span_attention import FP16, U, check, heads_of, make, packed, run
+from test_gpu_span_gradient import check as check_bwd
+from test_gpu_span_gradient import run_bwd
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +71,76 @@ def test_rising_scores(step, D):
     for way in (1, -1):
         s["k"].copy_(((torch.arange(n, device="cuda") * step) * way)[:, None, None])
         check(s, *run(s, scale=1 / D), scale=1 / D)
+
+
+def gradient(s, out, lse, scale=None):
+    """{name: (value, tolerance)} of the formula in 64 bits from out and lse as they are."""
+    T, H, D = s["q"].shape
+    S, G = s["k"].shape[:2]
+    f64 = {"dtype": torch.float64, "device": "cuda"}
+    c, u = D ** -0.5 if scale is None else scale, U[FP16]
+    found = {n: [torch.zeros(shape, **f64) for _ in range(2)]
+             for n, shape in (("dq", (T, H, D)), ("dk", (S, G, D)), ("dv", (S, G, D)))}
+    rows = s["seen"].any(1)[:, None]
+    seen = s["seen"].double()
+    top = torch.where(rows, s["dout"].abs().amax(2), 0).double()  # of a row
+    of_key = torch.stack([(seen * t[:, None]).amax(0) for t in top.view(T, G, -1).amax(2).t()], 1)
+    for h, g, q, k, v, x, size in heads_of(s, scale):
+        do = torch.where(rows, s["dout"][:, h], 0).double()
+        l = torch.where(rows[:, 0], lse[h], 0).double()[:, None]
+        p = torch.exp(x - l)
+        e = (2 * (D + 8) * 2.0 ** -23 * size + 2.0 ** -18 + 2.0 ** -22 * float(l.abs().max())
+             + (D + 8) * 2.0 ** -23 + max(S, T * (H // G)) * 2.0 ** -24)
+        o = out[:, h].double()
+        ds = p * (do @ v.t() - (do * o).sum(1, keepdim=True))
+        off = (u + e) * p * (do.abs() @ v.abs().t() + (do * o).abs().sum(1, keepdim=True))
+        for n, at, value, tol in (
+                ("dq", h, c * ds @ k, c * (off + 2.0 ** -25 * top[:, h:h + 1] * seen) @ k.abs()),
+                ("dk", g, c * ds.t() @ q, c * (off + 2.0 ** -25 * of_key[:, g] * seen).t() @ q.abs()),
+                ("dv", g, p.t() @ do, ((u + e) * p + 2.0 ** -39 * seen).t() @ do.abs())):
+            found[n][0][:, at] += value
+            found[n][1][:, at] += tol
+    return {n: (a, b + (u * a.abs()).clamp_min(2.0 ** -25)) for n, (a, b) in found.items()}
+
+
+def owner(lengths):
+    return torch.cat([torch.full((n,), i) for i, n in enumerate(lengths)]).cuda()
+
+
+@pytest.mark.parametrize("heads,groups,D", [(4, 1, 64), (2, 2, 128)])
+@pytest.mark.parametrize("small", [1, 0.01, 0.001])
+@pytest.mark.parametrize("lengths", [[1700, 2500], [2500, 1700], [60, 50] * 8, [1, 130, 700, 5, 129]], ids=str)
+def test_sequences_with_gradients_far_apart(lengths, small, heads, groups, D):
+    """Packed sequences, every other one with gradients 1000, the rest with small ones: none takes digits from
+    another, wherever they meet in a tile."""
+    spans, n = packed(lengths, pad=3)
+    s = make(spans, n, heads, groups, D, FP16, seed=len(lengths))
+    far = torch.cat([owner(lengths) % 2 == 1, torch.ones(3, dtype=torch.bool, device="cuda")])
+    s["dout"][far] *= 1000
+    s["dout"][~far] *= small
+    out, lse = run(s)
+    check_bwd(run_bwd(s, out, lse), gradient(s, out, lse), s)
+
+
+@pytest.mark.parametrize("heads,groups,D", [(6, 2, 64), (3, 3, 128)])
+def test_rows_with_gradients_far_apart(heads, groups, D):
+    """Every query and head has gradients of another size, chunks and windows between them."""
+    spans, n = packed([900, 333], chunk=7, window=40)
+    s = make(spans, n, heads, groups, D, FP16, seed=D)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    power = torch.randint(-8, 10, (len(spans), heads, 1), generator=gen, device="cuda")
+    s["dout"].copy_(torch.ldexp(s["dout"].float(), power))
+    out, lse = run(s)
+    check_bwd(run_bwd(s, out, lse), gradient(s, out, lse), s)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_few_keys_of_many_rows_with_gradients_far_apart(D):
+    """Keys walked in parts: 300 keys and 6000 rows, whose gradients grow 2^16-fold from the first to the last;
+    each row sees the keys around its place."""
+    rows, n = 6000, 300
+    spans = [(t * n // rows - 2, t * n // rows + 3) for t in range(rows)]
+    s = make(spans, n, 2, 1, D, FP16)
+    s["dout"].copy_(torch.ldexp(s["dout"].float(), (torch.arange(rows, device="cuda") * 16 // rows - 6)[:, None, None]))
+    out, lse = run(s)
+    check_bwd(run_bwd(s, out, lse), gradient(s, out, lse), s)

@@ -427,7 +427,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
   float ds_down = 1.f;  // the key's dS are kept times this
   if (F16 && warp < 16) {
     if (!few) {
-      sizes.look_at_tiles(range[0], range[1]);
+      if (range[1] > 0) sizes.look_at_tiles(range[0], range[1]);  // (else the first one is the largest int)
       sizes.leave();
       named_barrier(1, 512);
     }

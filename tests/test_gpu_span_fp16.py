@@ -144,3 +144,23 @@ def test_few_keys_of_many_rows_with_gradients_far_apart(D):
     s["dout"].copy_(torch.ldexp(s["dout"].float(), (torch.arange(rows, device="cuda") * 16 // rows - 6)[:, None, None]))
     out, lse = run(s)
     check_bwd(run_bwd(s, out, lse), gradient(s, out, lse), s)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, FP16], ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_what_nothing_sees_has_no_effect(D, dtype):
+    """Whatever is in keys that no query sees and in queries that see nothing, the results are the same bits."""
+    layouts = [([(0, 200)] * 32 + [(0, 0)] * 64 + [(300, 310)] * 32 + [(100, 200)] * 40, 400),
+               ([(40, 41), (7, 7), (130, 250)] + [(251 + t, 255 + t) for t in range(20)], 600),
+               ([(5, 70)] * 300, 20000)]
+    for spans, n in layouts:
+        found = []
+        for fill in (0.0, math.inf, math.nan, torch.finfo(dtype).max, -1000.0):
+            s = make(spans, n, 6, 2, D, dtype, nan=False)
+            for name, there in (("q", s["seen"].any(1)), ("dout", s["seen"].any(1)), ("k", s["seen"].any(0)),
+                                ("v", s["seen"].any(0))):
+                s[name][~there] = fill
+            out, lse = run(s)
+            found.append([out, lse, *run_bwd(s, out, lse).values()])
+        for got in found[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(got, found[0]))

@@ -28,24 +28,27 @@ struct SpanBwd {
   int q_parts, k_parts;
   const int32_t* spans;
   float scale, scale_log2;
-  SpanRows out, dout, dq, dk, dv;
+  SpanRows v, out, dout, dq, dk, dv;
   const float* lse;
   float* stat;    // [group][row tile] records of kRecord: see below
   int4* limits;   // of each row tile, those of its records
-  // fp16: the largest |dout| of each row, [group][row tile][128]; of the heads of each token, {its span, that, 0},
-  // [group][token]; of each row tile, [group][row tile]
-  float* size_row;
+  // fp16: A = sum |dout_i| and A max |out_i| of each row, [group][row tile][128]; the largest of a token's heads behind
+  // its span, [group][token]; those of a row tile, [group][row tile]; exponents (a byte) of each key's
+  // max |v_i|, [group][key block][128], and the largest of a key block, [group][key block]
+  float2* size_row;
   float4* size_token;
-  float* size_tile;
+  float2* size_tile;
+  uint8_t *v_exp, *v_most;
   float* part_q;  // [group][row tile][part][D / 4][128 rows] of four
   float* part_k;  // [group][key block][part][dk, dv][D / 4][128 keys] of four
   int* err;
 };
 
-// fp16 has few exponents: P goes into its product times 2^14, and dS divided by the power of two in a largest
-// |dout|, so that small gradients keep their digits: for dq the row's own, for dk that of the rows that see
-// the key (a lane has one row or key, and with it one scale). Nothing of another sequence comes in.
-// bf16 has fp32's range.
+// fp16 has few exponents: P goes into its product times 2^14, and dS times a power of two by which its bound
+// |dS_tj| <= sum_i |dout_ti| (max |v_ji| + max |out_ti|) comes between 2^14 and 2^15: none is infinite, and small ones
+// keep their digits down to 2^-28 of the bound. The bound is that of the row for dq, over the keys that it sees, and that
+// of the key for dk, over the rows that see it (a lane has one row or key, and with it one scale): nothing of
+// another sequence comes in. bf16 has fp32's range.
 constexpr float kPUp = 16384.f;
 constexpr float kPUpLog2 = 14.f;
 
@@ -61,17 +64,64 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
+__device__ __forceinline__ float2 larger(float2 a, float2 b) {
+  return make_float2(fmaxf(a.x, b.x), fmaxf(a.y, b.y));
+}
+
 // ------------------------------------------------------------------------------ rows
+// The largest magnitude of eight numbers, and that of both halves of such a pair, as bits
+__device__ __forceinline__ uint32_t top_of(const uint4& a) {
+  const uint32_t m = 0x7fff7fffu;
+  return __vmaxu2(__vmaxu2(a.x & m, a.y & m), __vmaxu2(a.z & m, a.w & m));
+}
+__device__ __forceinline__ float top_half(uint32_t x) {
+  return __half2float(__ushort_as_half(static_cast<unsigned short>(max(x & 0xffffu, x >> 16))));
+}
+
+// The exponents of a key block's max |v_i|, D / 8 lanes a key (those of keys that nothing sees are not looked at).
+template <int D>
+__device__ __forceinline__ void key_sizes(const SpanBwd& p, int kb, int group) {
+  constexpr int kLanes = D / 8;
+  __shared__ uint32_t top[8];
+  const int lane = threadIdx.x % kLanes;
+  const int64_t block = static_cast<int64_t>(group) * p.y.key_blocks + kb;
+  uint32_t most = 0;
+#pragma unroll
+  for (int row = threadIdx.x / kLanes; row < kTile; row += 256 / kLanes) {
+    const int key = kb * kTile + row;
+    uint32_t of_v = 0;
+    if (key < p.y.n_k)
+      of_v = top_of(__ldg(reinterpret_cast<const uint4*>(
+          static_cast<const uint16_t*>(p.v.p) + key * p.v.token + group * p.v.head + lane * 8)));
+#pragma unroll
+    for (int i = kLanes / 2; i; i >>= 1) of_v = __vmaxu2(of_v, __shfl_xor_sync(0xffffffffu, of_v, i));
+    const uint32_t e = __float_as_uint(top_half(of_v)) >> 23;
+    if (lane == 0) p.v_exp[block * kTile + row] = static_cast<uint8_t>(e);
+    most = max(most, e);
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((threadIdx.x & 31) == 0) top[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 8; ++i) most = max(most, top[i]);
+    p.v_most[block] = static_cast<uint8_t>(most);
+  }
+}
+
 // D / 8 lanes a row. A row that sees nothing, or is none, gets P = 0 by an infinite lse.
 template <bool F16, int D>
 __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ SpanBwd p) {
   constexpr int kLanes = D / 8;
-  __shared__ float size[kTile];
+  __shared__ float2 size[kTile];
   grid_dep_wait();
   grid_dep_launch();
   const int tile = blockIdx.x, group = blockIdx.y;
-  const int token0 = tile * p.y.tile_tokens;
   const int lane = threadIdx.x % kLanes;
+  if (F16 && tile >= p.y.row_tiles) {
+    key_sizes<D>(p, tile - p.y.row_tiles, group);
+    return;
+  }
+  const int token0 = tile * p.y.tile_tokens;
   float* stat = p.stat + (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord;
 #pragma unroll
   for (int row = threadIdx.x / kLanes; row < kTile; row += 256 / kLanes) {
@@ -79,20 +129,22 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
     const bool valid = row < p.y.tile_rows && token < p.y.n_q;
     const int2 span = valid ? span_of(p.spans, token, p.y.n_k) : make_int2(0, 0);
     const bool sees = span.x < span.y;
-    float sum = 0.f, most = 0.f;
+    float sum = 0.f, of_dout = 0.f;
+    uint32_t of_out = 0;
     if (sees) {
       const uint4 a = __ldg(reinterpret_cast<const uint4*>(
           static_cast<const uint16_t*>(p.out.p) + token * p.out.token + head * p.out.head + lane * 8));
       const uint4 b = __ldg(reinterpret_cast<const uint4*>(
           static_cast<const uint16_t*>(p.dout.p) + token * p.dout.token + head * p.dout.head + lane * 8));
       const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+      if (F16) of_out = top_of(a);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float2 u, v;
         if (F16) {
           u = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
           v = __half22float2(*reinterpret_cast<const __half2*>(&y[i]));
-          most = fmaxf(most, fmaxf(fabsf(v.x), fabsf(v.y)));
+          of_dout += fabsf(v.x) + fabsf(v.y);
         } else {
           u = make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
           v = make_float2(__uint_as_float(y[i] << 16), __uint_as_float(y[i] & 0xffff0000u));
@@ -103,11 +155,15 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
 #pragma unroll
     for (int i = kLanes / 2; i; i >>= 1) {
       sum += __shfl_xor_sync(0xffffffffu, sum, i);
-      if (F16) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, i));
+      if (F16) {
+        of_dout += __shfl_xor_sync(0xffffffffu, of_dout, i);
+        of_out = __vmaxu2(of_out, __shfl_xor_sync(0xffffffffu, of_out, i));
+      }
     }
     if (F16 && lane == 0) {
-      size[row] = most;
-      p.size_row[(static_cast<int64_t>(group) * p.y.row_tiles + tile) * kTile + row] = most;
+      const float2 both = make_float2(of_dout, of_dout * top_half(of_out));
+      size[row] = both;
+      p.size_row[(static_cast<int64_t>(group) * p.y.row_tiles + tile) * kTile + row] = both;
     }
     if (lane == 0) {
       const float l = sees ? __ldg(p.lse + static_cast<int64_t>(head) * p.y.n_q + token) : 0.f;
@@ -121,15 +177,15 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
   if (threadIdx.x < 32) {
     int4 m = make_int4(0x7fffffff, 0, 0, 0x7fffffff);
     bool none = false, one = false;
-    float most = 0.f;  // of the tile
+    float2 most = make_float2(0.f, 0.f);  // of the tile
     for (int i = threadIdx.x; i < p.y.tile_tokens && token0 + i < p.y.n_q; i += 32) {
       const int2 s = span_of(p.spans, token0 + i, p.y.n_k);
       if (F16) {
-        float of_token = 0.f;
-        for (int h = 0; h < p.y.per; ++h) of_token = fmaxf(of_token, size[i * p.y.per + h]);
+        float2 of_token = make_float2(0.f, 0.f);
+        for (int h = 0; h < p.y.per; ++h) of_token = larger(of_token, size[i * p.y.per + h]);
         p.size_token[static_cast<int64_t>(group) * p.y.n_q + token0 + i] =
-            make_float4(__int_as_float(s.x), __int_as_float(s.y), of_token, 0.f);
-        most = fmaxf(most, of_token);
+            make_float4(__int_as_float(s.x), __int_as_float(s.y), of_token.x, of_token.y);
+        most = larger(most, of_token);
       }
       if (s.x < s.y) {
         m.x = min(m.x, s.x);
@@ -147,7 +203,7 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
     m.w = __reduce_min_sync(0xffffffffu, m.w);
     if (__any_sync(0xffffffffu, none)) m.z = ~m.z;
     if (__any_sync(0xffffffffu, one)) m.w = ~m.w;
-    if (F16) most = warp_max(most);
+    if (F16) most = make_float2(warp_max(most.x), warp_max(most.y));
     if (threadIdx.x == 0) {
       if (F16) p.size_tile[group * p.y.row_tiles + tile] = most;
       *reinterpret_cast<int4*>(stat + 4 * kTile) = m;
@@ -156,10 +212,13 @@ __global__ void __launch_bounds__(256) span_rows_kernel(const __grid_constant__ 
   }
 }
 
-// 2^-E for a largest |dout| = f 2^E, 1 <= f < 2
-__device__ __forceinline__ float down_scale(float most) {
-  const uint32_t e = __float_as_uint(most) >> 23;  // (fp16: 103 at least unless it is zero)
-  return most > 0.f && e < 255u ? __uint_as_float((254u - e) << 23) : 1.f;
+// The power of two that brings the bound of a lane's dS between 2^14 and 2^15, from its rows' sizes and the exponent
+// of its keys' (1 where nothing is seen, or all is zero).
+__device__ __forceinline__ float down_scale(float2 size, uint32_t v_exp) {
+  // |v_i| < 2^(v_exp - 126)
+  const float bound = size.x > 0.f ? fmaf(size.x, __uint_as_float((v_exp + 1) << 23), size.y) : 0.f;
+  const uint32_t e = __float_as_uint(bound) >> 23;  // (of fp16 numbers: 79 to 167 unless it is zero)
+  return e > 14u && e < 255u ? __uint_as_float((268u - e) << 23) : 1.f;
 }
 
 // ------------------------------------------------------------------------------ keys: dk and dv
@@ -191,7 +250,7 @@ struct KeyCfg {
                        kPDone = kDsFull + 1, kDsDone = kPDone + 1, kDone = kDsDone + 1, kBars = kDone + 4;
   static constexpr int kOffSize = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;  // fp16: [16 warps][32 tokens]
   static constexpr int kOffAll = kOffSize + 16 * 32 * 16;  // [4][128]
-  static constexpr int kSmem = kOffAll + 4 * kTile * 4;
+  static constexpr int kSmem = kOffAll + 4 * kTile * 8;
   static constexpr uint32_t kColX = 0, kColY = kStep, kColP = 2 * kStep, kColDs = kColP + kStep / 2,
                             kColDv = 512 - 2 * D, kColDk = 512 - D;
   static_assert(kSmem <= 227 * 1024 && kColDs + kStep / 2 <= kColDv, "room");
@@ -247,20 +306,20 @@ __device__ __forceinline__ void leave16_none(uint8_t* tile, float4* part, int ro
   }
 }
 
-// The largest |dout| of the rows that see a thread's key (fp16), by warps 0-15: the four warps of a key share the
+// The largest sizes of the rows that see a thread's key (fp16), by warps 0-15: the four warps of a key share the
 // tokens out, 32 at a time, and leave what they find in shared memory.
 template <int D>
 struct KeySizes {
   const SpanBwd& p;
   const int group, lane, q, at, key;  // at: the key's place in the block
   float4* const mine;
-  float* const all;  // [quarter][key]
-  float size = 0.f;
+  float2* const all;  // [quarter][key]
+  float2 size = make_float2(0.f, 0.f);
 
   __device__ __forceinline__ KeySizes(const SpanBwd& p, uint8_t* smem, int group, int key0)
       : p(p), group(group), lane(threadIdx.x & 31), q(threadIdx.x >> 7), at(threadIdx.x & 127), key(key0 + at),
         mine(reinterpret_cast<float4*>(smem + KeyCfg<D>::kOffSize) + (threadIdx.x >> 5) * 32),
-        all(reinterpret_cast<float*>(smem + KeyCfg<D>::kOffAll)) {}
+        all(reinterpret_cast<float2*>(smem + KeyCfg<D>::kOffAll)) {}
   __device__ __forceinline__ float4 token(int t, int end) const {
     return t + lane < end ? __ldcg(p.size_token + static_cast<int64_t>(group) * p.y.n_q + t + lane)
                           : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -273,7 +332,8 @@ struct KeySizes {
 #pragma unroll
       for (int i = i0; i < i0 + 8; ++i) {
         const float4 x = mine[i];
-        if (__float_as_int(x.x) <= key && key < __float_as_int(x.y)) size = fmaxf(size, x.z);
+        if (__float_as_int(x.x) <= key && key < __float_as_int(x.y))
+          size = larger(size, make_float2(x.z, x.w));
       }
     __syncwarp();
   }
@@ -281,7 +341,7 @@ struct KeySizes {
   // whole; of the others every token is looked at, the next ones on their way meanwhile.
   __device__ __forceinline__ void look_at_tiles(int first, int end) {
     const int key0 = key - at, keys_end = min(key0 + kTile, p.y.n_k);
-    float of_tiles = 0.f;
+    float2 of_tiles = make_float2(0.f, 0.f);
     int held = 0;
     float4 x;
 #pragma unroll 1
@@ -290,10 +350,10 @@ struct KeySizes {
       bool some = false;
       if (tile < end) {
         const int4 m = __ldcg(p.limits + tile);
-        const float of_tile = __ldcg(p.size_tile + group * p.y.row_tiles + tile);
+        const float2 of_tile = __ldcg(p.size_tile + group * p.y.row_tiles + tile);
         if (m.x < keys_end && m.y > key0) {
           some = (m.z < 0 ? ~m.z : m.z) > key0 || (m.w < 0 ? ~m.w : m.w) < keys_end;
-          if (!some) of_tiles = fmaxf(of_tiles, of_tile);
+          if (!some) of_tiles = larger(of_tiles, of_tile);
         }
       }
 #pragma unroll 1
@@ -310,12 +370,12 @@ struct KeySizes {
       }
     }
     if (held > 0) look_at(x, held);
-    size = fmaxf(size, warp_max(of_tiles));
+    size = larger(size, make_float2(warp_max(of_tiles.x), warp_max(of_tiles.y)));
   }
   __device__ __forceinline__ void leave() const { all[q * kTile + at] = size; }
   // of all four, after a barrier
-  __device__ __forceinline__ float found() const {
-    return fmaxf(fmaxf(all[at], all[kTile + at]), fmaxf(all[2 * kTile + at], all[3 * kTile + at]));
+  __device__ __forceinline__ float2 found() const {
+    return larger(larger(all[at], all[kTile + at]), larger(all[2 * kTile + at], all[3 * kTile + at]));
   }
 };
 // So few tokens are all looked at, while the limits of the tiles are on their way (2 sequences of 77, forward and
@@ -388,6 +448,9 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
   __syncthreads();
   KeySizes<D> sizes(p, smem, group, key0);
   const bool few = p.y.n_q <= kFewTokens;
+  uint32_t v_exp = 0;
+  if (F16 && warp < 16)
+    v_exp = __ldcg(p.v_exp + (static_cast<int64_t>(group) * p.y.key_blocks + kb) * kTile + sizes.at);
   {
     // the row tiles that see some of the keys: from the first to the last
     int first = 0x7fffffff, end = 0;
@@ -431,7 +494,7 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
       sizes.leave();
       named_barrier(1, 512);
     }
-    ds_down = down_scale(sizes.found());
+    ds_down = down_scale(sizes.found(), v_exp);
   }
 
   if (count == 0) {
@@ -743,9 +806,65 @@ struct QueryCfg {
                        kVFree = kVFull + kSlotsV, kXFull = kVFree + kSlotsV, kYFull = kXFull + 1,
                        kXRead = kYFull + 1, kYRead = kXRead + 1, kDsFull = kYRead + 1,
                        kDsDone = kDsFull + 1, kDone = kDsDone + 1, kBars = kDone + 3;
-  static constexpr int kSmem = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;
+  static constexpr int kOffAll = kOffBar + (kBars * 8 + 32 + 127) / 128 * 128;  // fp16: [4][128]
+  static constexpr int kSmem = kOffAll + 4 * kTile;
   static constexpr uint32_t kColX = 0, kColY = 128, kColDs = 256, kColDq = 384;
   static_assert(kSmem <= 227 * 1024, "shared memory");
+};
+
+// The largest exponent of max |v_i| among the keys that a thread's row sees (fp16), by warps 0-15: the four warps of
+// a row share out 32 keys each of its first and of its last block, and the blocks between, which most rows of a
+// warp have in common.
+struct SeenKeys {
+  int first, last;  // blocks
+  int2 span;
+  uint4 exps[4];              // of a quarter of the first block, of the last
+  uint32_t all, before, behind;  // of the blocks that the warp's rows have in common, of those before and behind them
+
+  // (Nothing waits for these loads here but the ends of the span. One for each place in line is enough
+  // for most rows.)
+  __device__ __forceinline__ void load(const SpanBwd& p, int group, const int* ends) {
+    const int q = threadIdx.x >> 7, lane = threadIdx.x & 31;
+    span = make_int2(__ldcg(ends), __ldcg(ends + kTile));
+    const bool sees = span.x < span.y;
+    first = sees ? span.x / kTile : 0;
+    last = sees ? (span.y - 1) / kTile : 0;
+    const int64_t block0 = static_cast<int64_t>(group) * p.y.key_blocks;
+    const uint4* from = reinterpret_cast<const uint4*>(p.v_exp + block0 * kTile) + 2 * q;
+    exps[0] = __ldcg(from + first * 8);
+    exps[1] = __ldcg(from + first * 8 + 1);
+    exps[2] = __ldcg(from + last * 8);
+    exps[3] = __ldcg(from + last * 8 + 1);
+    int lo = __reduce_max_sync(0xffffffffu, sees ? first + 1 : 0);
+    int hi = __reduce_min_sync(0xffffffffu, sees ? last : 0x7fffffff);
+    if (lo >= hi || hi == 0x7fffffff) lo = hi = 0;
+    auto largest = [&](int b, int end, int step) {
+      uint32_t x = b < end ? __ldcg(p.v_most + block0 + b) : 0u;
+#pragma unroll 1
+      for (b += step; b < end; b += step) x = max(x, static_cast<uint32_t>(__ldcg(p.v_most + block0 + b)));
+      return x;
+    };
+    all = largest(lo + 32 * q + lane, hi, 128);
+    before = largest(first + 1 + q, min(lo, last), 4);
+    behind = largest(max(hi, first + 1) + q, last, 4);
+  }
+  __device__ __forceinline__ uint32_t found() const {
+    const int q = threadIdx.x >> 7;
+    const uint32_t most = max(__reduce_max_sync(0xffffffffu, all), max(before, behind));
+    uint32_t four = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t seen = seen_word(span, (i < 2 ? first : last) * kTile + 32 * q) >> (i & 1) * 16;
+      const uint32_t w[4] = {exps[i].x, exps[i].y, exps[i].z, exps[i].w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t bits = seen >> 4 * c & 15u;
+        four = __vmaxu4(four, w[c] & (bits * 0x00204081u & 0x01010101u) * 255u);  // a byte for every bit
+      }
+    }
+    four = __vmaxu4(four, four >> 16);
+    return max(most, __vmaxu4(four, four >> 8) & 255u);
+  }
 };
 
 template <bool F16, int D>
@@ -819,6 +938,10 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
                   (block0 + n) * kTile, 0);
     return true;
   };
+  SeenKeys keys;
+  if (F16 && warp < 16)
+    keys.load(p, group, reinterpret_cast<const int*>(p.stat) + 2 * kTile + threadIdx.x % kTile +
+                            (static_cast<int64_t>(group) * p.y.row_tiles + tile) * kRecord);
   int loads_k = 0, loads_v = 0;  // warp 16: so far
   if (threadIdx.x == 16 * 32 && count > 0) {  // what there is room for, while the others get ready
     mbar_expect_tx(bar(C::kQ), 2 * p.y.tile_rows * D * 2);
@@ -935,11 +1058,18 @@ __device__ __forceinline__ void query_block(const CUtensorMap& tmQ, const CUtens
     const int q = warp >> 2, row = (warp & 3) * 32 + lane;
     const int64_t at = static_cast<int64_t>(group) * p.y.row_tiles + tile;
     const float* stat = p.stat + at * kRecord + row;
-    const float ds_down = F16 ? down_scale(__ldcg(p.size_row + at * kTile + row)) : 1.f;  // dS is kept times this
     const float neg_lse = __ldcg(stat), neg_delta = __ldcg(stat + kTile);
     const int2 span = make_int2(__ldcg(reinterpret_cast<const int*>(stat) + 2 * kTile),
                                 __ldcg(reinterpret_cast<const int*>(stat) + 3 * kTile));
     const bool sees = span.x < span.y;
+    float ds_down = 1.f;  // the row's dS are kept times this
+    if (F16) {
+      const float2 size = __ldcg(p.size_row + at * kTile + row);
+      uint8_t* const v_exps = smem + C::kOffAll + row;  // by quarters
+      v_exps[q * kTile] = static_cast<uint8_t>(keys.found());
+      named_barrier(1, 512);
+      ds_down = down_scale(size, max(max(v_exps[0], v_exps[kTile]), max(v_exps[2 * kTile], v_exps[3 * kTile])));
+    }
     const int all_from = __reduce_max_sync(0xffffffffu, sees ? span.x : 0);
     const int all_to = __reduce_min_sync(0xffffffffu, sees ? span.y : 0x7fffffff);
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -1115,7 +1245,7 @@ int parts_for(int64_t units, int steps) {
 
 struct BwdPlan {
   int q_parts, k_parts;
-  size_t stat, limits, size_row, size_token, size_tile, part_q, part_k, total;  // byte offsets
+  size_t stat, limits, size_row, size_token, size_tile, v_exp, v_most, part_q, part_k, total;  // byte offsets
 };
 BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   BwdPlan b{};
@@ -1127,9 +1257,11 @@ BwdPlan bwd_plan(const SpanShape& y, int head_dim) {
   b.limits = up(b.stat + tiles * kRecord * sizeof(float));
   // (for either type: the plan has none)
   b.size_row = b.limits + up(static_cast<size_t>(y.row_tiles) * sizeof(int4));
-  b.size_token = b.size_row + up(tiles * kTile * sizeof(float));
+  b.size_token = b.size_row + up(tiles * kTile * sizeof(float2));
   b.size_tile = b.size_token + up(static_cast<size_t>(y.groups) * y.n_q * sizeof(float4));
-  b.part_q = b.size_tile + up(tiles * sizeof(float));
+  b.v_exp = b.size_tile + up(tiles * sizeof(float2));
+  b.v_most = b.v_exp + up(static_cast<size_t>(y.groups) * y.key_blocks * kTile);
+  b.part_q = b.v_most + up(static_cast<size_t>(y.groups) * y.key_blocks);
   b.part_k = b.part_q + (b.q_parts > 1 ? tiles * b.q_parts * kTile * head_dim * sizeof(float) : 0);
   b.total = b.part_k + (b.k_parts > 1 ? static_cast<size_t>(y.groups) * y.key_blocks * b.k_parts * 2 *
                                             kTile * head_dim * sizeof(float)
@@ -1161,7 +1293,8 @@ cudaError_t launch_bwd(const SpanBwd& p, const SpanRows& q, const SpanRows& k, c
                                   kSmem);
     });
   if (e == cudaSuccess)
-    e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles, p.y.groups), dim3(256), 0, s, p);
+    e = launch_pdl(span_rows_kernel<F16, D>, dim3(p.y.row_tiles + (F16 ? p.y.key_blocks : 0), p.y.groups), dim3(256),
+                   0, s, p);
   if (e == cudaSuccess)
     e = launch_pdl(span_grad_kernel<F16, D>,
                    dim3((p.y.key_blocks * p.k_parts + p.y.row_tiles * p.q_parts) * p.y.groups),
@@ -1198,6 +1331,7 @@ fd_status fd_op_span_attention_bwd(
       kr{const_cast<void*>(k), k_token_stride, k_head_stride},
       vr{const_cast<void*>(v), v_token_stride, v_head_stride};
   fd::SpanBwd p{};
+  p.v = vr;
   p.out = {const_cast<void*>(out), out_token_stride, out_head_stride};
   p.dout = {const_cast<void*>(dout), dout_token_stride, dout_head_stride};
   p.dq = {dq, dq_token_stride, dq_head_stride};
@@ -1248,9 +1382,11 @@ fd_status fd_op_span_attention_bwd(
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.stat = reinterpret_cast<float*>(ws + b.stat);
   p.limits = reinterpret_cast<int4*>(ws + b.limits);
-  p.size_row = reinterpret_cast<float*>(ws + b.size_row);
+  p.size_row = reinterpret_cast<float2*>(ws + b.size_row);
   p.size_token = reinterpret_cast<float4*>(ws + b.size_token);
-  p.size_tile = reinterpret_cast<float*>(ws + b.size_tile);
+  p.size_tile = reinterpret_cast<float2*>(ws + b.size_tile);
+  p.v_exp = ws + b.v_exp;
+  p.v_most = ws + b.v_most;
   p.part_q = reinterpret_cast<float*>(ws + b.part_q);
   p.part_k = reinterpret_cast<float*>(ws + b.part_k);
   p.err = err_dev;

@@ -3,7 +3,8 @@ small ones, gradients of very different sizes beside each other.
 
 Tolerances are those of test_gpu_span_attention.py and test_gpu_span_gradient.py without what these allow fp16 for
 each key that a query sees. Forward: probabilities keep half a step, 2^-11, down to 2^-25 of the row's largest.
-Gradient: dS is off by 2^-25 of the largest |dout| of its own row (dq) or of the rows that see the key (dk)."""
+Gradient: dS is off by 2^-25 of the largest |dout| of its own row (dq) or of the rows that see the key (dk). (Where
+values are so large that 2^-39 of dS's bound is more than that, half a step of P M is, too.)"""
 import math
 
 import pytest
@@ -144,6 +145,42 @@ def test_few_keys_of_many_rows_with_gradients_far_apart(D):
     s["dout"].copy_(torch.ldexp(s["dout"].float(), (torch.arange(rows, device="cuda") * 16 // rows - 6)[:, None, None]))
     out, lse = run(s)
     check_bwd(run_bwd(s, out, lse), gradient(s, out, lse), s)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("keys", [2, 3, 150])
+@pytest.mark.parametrize("size", [500.0, 4000.0])
+def test_large_values_along_the_gradient(size, keys, D):
+    """Values of some size with signs that dout shares: dS = P (dout . v - dout . out) is past fp16's largest number,
+    dq and dk (scores' factors are small) are not."""
+    spans, n = packed([keys] * 40)
+    s = make(spans, n, 4, 2, D, FP16, seed=keys, size=0.05)
+    s["k"].mul_(0.05)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    sign = torch.randint(0, 2, (1, 1, D), generator=gen, device="cuda") * 2 - 1
+    s["v"].copy_(sign * size * (torch.arange(n, device="cuda") % 2 * 2 - 1)[:, None, None])
+    s["dout"].copy_((1.5 + 0.4 * torch.rand(s["dout"].shape, generator=gen, device="cuda")) * sign)
+    out, lse = run(s)
+    want = gradient(s, out, lse)
+    assert all(float(v.abs().max()) < 60000 for v, _ in want.values())
+    check_bwd(run_bwd(s, out, lse), want, s)
+
+
+@pytest.mark.parametrize("heads,groups,D", [(4, 1, 64), (2, 2, 128)])
+@pytest.mark.parametrize("lengths", [[700, 900, 3], [60, 50] * 8, [1, 130, 700, 5, 129]], ids=str)
+@pytest.mark.parametrize("first", [0, 1])
+def test_sequences_with_values_far_apart(first, lengths, heads, groups, D):
+    """Packed sequences, every other one with values of thousands, the rest with small ones."""
+    spans, n = packed(lengths)
+    s = make(spans, n, heads, groups, D, FP16, seed=len(lengths))
+    far = owner(lengths) % 2 == first
+    s["v"][far] *= 3000
+    s["v"][~far] *= 0.01
+    s["dout"].mul_(4)
+    out, lse = run(s)
+    # (a result past 65504 is an infinity of fp16, whatever computes it)
+    want = {m: (v, torch.where(v.abs() < 65000, t, math.inf)) for m, (v, t) in gradient(s, out, lse).items()}
+    check_bwd(run_bwd(s, out, lse), want, s)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, FP16], ids=str)

@@ -189,8 +189,12 @@ __global__ void __launch_bounds__(FwdCfg<D>::kThreads, 2)
   const int key_start = range[0], count = range[1];
 
   if (count == 0) {
-    // nothing is seen: the softmax warps write that below, where Q may be on its way to
-    if (threadIdx.x < 8 * 32 && aligned) wait_warp(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA);
+    // nothing is seen: the softmax warps write that below, where Q may be on its way to (and nothing may be in
+    // flight when the block exits)
+    if (threadIdx.x < 8 * 32 && aligned) {
+      wait(bar(C::kQFull), 0, p.err, ERR_WAIT_TMA, true);
+      __syncwarp();
+    }
   } else if (warp == 8) {
     if (lane == 0) {
       // K and V in turn, each when its slot is free (the scores of a block are through before its P V:

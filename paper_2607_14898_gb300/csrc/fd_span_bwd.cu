@@ -498,8 +498,12 @@ __device__ __forceinline__ void keys_block(const CUtensorMap& tmQ, const CUtenso
   }
 
   if (count == 0) {
-    // no row sees any of the keys (which may be on their way to where zeros leave from)
-    if (warp < 16 && aligned) wait_warp(bar(C::kKV), 0, p.err, ERR_WAIT_TMA);
+    // no row sees any of the keys (which may be on their way to where zeros leave from; and nothing may be in flight
+    // when the block exits)
+    if (warp < 16 && aligned) {
+      wait(bar(C::kKV), 0, p.err, ERR_WAIT_TMA, true);
+      __syncwarp();
+    }
   } else if (warp == 16 || warp == 17) {
     // ---- X = K Q^T (16), Y = V dout^T (17), and zeros for the rows of queries that see nothing:
     // their P and dS are 0, but 0 times NaN is NaN

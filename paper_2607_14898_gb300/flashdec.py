@@ -1167,29 +1167,38 @@ def _input_rows(x, what, shape, dtype, dev):
 def op_block_join_bwd(dy, du, h, b, dh, db, post_gain=None, pre_gain=None, gate=None,
                       gate_tokens=0, scale=1.0, r_post=None, r_pre=None, d_post=None, d_pre=None,
                       d_gate=None, workspace=None, stream=None) -> None:
-    """The gradient of op_block_join from dy (None: zero) and du (None without a pre_gain): dh (may be
-    None), db, and d_post, d_pre float32 [width], d_gate like gate (None: not wanted). h and b: the inputs of
+    """The gradient of op_block_join from dy (None: zero) and du (None without a pre_gain): dh, db (may be
+    None), and d_post, d_pre float32 [width], d_gate like gate (None: not wanted). h and b: the inputs of
     the forward call, or the Checkpoint8 that hold them; r_post, r_pre as that call left them
     (fd_op_block_join_bwd)."""
-    shape, dev = db.shape, db.get_device()
-    if dev < 0 or len(shape) != 2:
-        raise TypeError("db: a CUDA tensor [tokens][width] is required")
+    f32 = _torch_types()[2]
+    stream_dtype = f32  # (where nothing of the stream's type is read or written)
+    for t in (dh, dy, h):
+        if t is not None and not isinstance(t, Checkpoint8):
+            stream_dtype = t.dtype
+            break
+    if db is None and isinstance(b, Checkpoint8):
+        import torch
+        shape, dev = b.shape, b.device  # (without du nothing of the blocks' type is read or written)
+        dtype = du.dtype if du is not None else torch.bfloat16 if stream_dtype is f32 else stream_dtype
+    else:
+        like, what = (b, "b") if db is None else (db, "db")
+        if getattr(like, "ndim", 0) != 2 or like.get_device() < 0:
+            raise TypeError(f"{what}: a CUDA tensor [tokens][width] is required")
+        shape, dev, dtype = like.shape, like.get_device(), like.dtype
     rows, width = shape
-    stream_dtype = dh.dtype if dh is not None else dy.dtype if dy is not None else h.dtype
-    bp, bs = _rows(db, "db", shape, db.dtype, dev)
+    bp, bs = (0, (0, 0)) if db is None else _rows(db, "db", shape, dtype, dev)
     yp, ys = (0, (0, 0)) if dy is None else _rows(dy, "dy", shape, stream_dtype, dev)
     hp, hs = (0, (0, 0)) if dh is None else _rows(dh, "dh", shape, stream_dtype, dev)
     if (du is None) != (pre_gain is None):
         raise ValueError("du and pre_gain come together")
-    up, us = (0, (0, 0)) if du is None else _rows(du, "du", shape, db.dtype, dev)
+    up, us = (0, (0, 0)) if du is None else _rows(du, "du", shape, dtype, dev)
     h_in = (0, 0, 0) if pre_gain is None else _input_rows(h, "h", shape, stream_dtype, dev)
-    b_in = _input_rows(b, "b", shape, db.dtype, dev)
-    f32 = _torch_types()[2]
+    b_in = _input_rows(b, "b", shape, dtype, dev)
     sums = [0 if t is None else _dense(t, n, s, f32, dev) for t, n, s in (
         (d_post, "d_post", (width,)), (d_pre, "d_pre", (width,)),
         (d_gate, "d_gate", () if gate is None else gate.shape))]
-    j = _join_view(rows, width, db.dtype, stream_dtype, dev, post_gain, pre_gain, gate, gate_tokens,
-                   scale)
+    j = _join_view(rows, width, dtype, stream_dtype, dev, post_gain, pre_gain, gate, gate_tokens, scale)
     need = _join_workspace.get((rows, width))
     if need is None:
         if len(_join_workspace) > 1000:

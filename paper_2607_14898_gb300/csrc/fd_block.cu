@@ -170,8 +170,10 @@ cudaError_t launch_join(const Join& p, cudaStream_t s) {
   };
   // Up to 1024 elements a group of eight a thread (6240 x 1024: 18.3 us, two groups 19.4, four 22.8), past that
   // two (8000 x 4096: 78 us, one group 90). Few rows are spread over more warps, for which a row is a
-  // shorter chain.
-  const bool few = p.rows < 4 * num_sms();
+  // shorter chain: 2048 elements, 300 rows 2.5 us instead of 2.7, 400 either way 3.0, 600 rows 5.1 instead of 4.4;
+  // 2056 elements, 150 rows 2.4 instead of 2.5, 300 rows 3.5 instead of 2.9 (4096: 2.8 either way, 5.7 instead of 4.8).
+  const int few_halves = units <= 256 ? 5 : 2;  // of a wave of a block an SM
+  const bool few = 2 * static_cast<int64_t>(p.rows) <= few_halves * num_sms();
   if (units <= 32) return go(join_kernel<B, H, 1, 1>, 1);
   if (units <= 64) return go(join_kernel<B, H, 2, 1>, 2);
   if (units <= 128) return go(join_kernel<B, H, 4, 1>, 4);

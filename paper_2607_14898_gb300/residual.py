@@ -25,8 +25,10 @@ class ResidualAttention:
 
     def __init__(self, tokens, width, heads, groups, head_dim, w_qkv, w_out, post_gain, pre_gain, gate=None,
                  gate_tokens=0, scale=1.0, eps=1e-6):
-        if tokens % 8 or width % 32 or heads * head_dim % 32:
-            raise ValueError("tokens in multiples of 8, width and heads * head_dim of 32 are required")
+        if tokens < 8 or tokens % 8 or not 32 <= width <= 8192 or width % 32:
+            raise ValueError("tokens in multiples of 8 and a width of 32 to 8192 in multiples of 32 are required")
+        if head_dim not in (64, 128) or not 1 <= groups <= heads or heads % groups or heads > 128 * groups:
+            raise ValueError("head_dim 64 or 128 and heads in equal groups of 128 at most are required")
         self.tokens, self.width, self.heads, self.groups, self.head_dim = tokens, width, heads, groups, head_dim
         self.post_gain, self.pre_gain, self.gate, self.gate_tokens = post_gain, pre_gain, gate, gate_tokens
         self.scale, self.eps = scale, eps

@@ -201,3 +201,38 @@ def test_what_nothing_sees_has_no_effect(D, dtype):
             found.append([out, lse, *run_bwd(s, out, lse).values()])
         for got in found[1:]:
             assert all(torch.equal(a, b) for a, b in zip(got, found[0]))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lengths", [[77, 60], [400, 300]], ids=str)
+def test_captured_gradient_with_other_inputs(lengths, D):
+    """Scales are of the inputs at every replay: a captured gradient with gradients, values and spans of other sizes
+    gives the bits of a call of its own."""
+    spans, n = packed(lengths)
+    s = make(spans, n, 6, 2, D, FP16, nan=False)
+    out, lse = run(s)
+    got = {"d" + m: torch.empty_like(s[m]) for m in "qkv"}
+    work = torch.empty(fdp.span_attention_workspace_bytes(n, n, 6, 2, D, backward=True), dtype=torch.uint8,
+                       device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fdp.op_span_attention_bwd(s["q"], s["k"], s["v"], s["spans"], out, lse, s["dout"], *got.values(),
+                                  workspace=work, err=err)
+    for change in range(4):
+        if change == 1:
+            s["dout"][::2] *= 1000
+        elif change == 2:
+            s["v"][:n // 2] *= 2000
+        elif change == 3:
+            s["spans"][:, 0] = (s["spans"][:, 1] - 9).clamp_min(0)
+        fresh = run(s)
+        out.copy_(fresh[0])
+        lse.copy_(fresh[1])
+        want = run_bwd(s, out, lse)
+        for x in got.values():
+            x.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[m], want[m]) for m in got), change
+    assert int(err) == 0

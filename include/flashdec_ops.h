@@ -392,9 +392,10 @@ fd_status fd_op_span_attention(const fd_span_attention* attn, const void* q, int
  *   dq[t][h] = scale sum_j dS k_j;  dk[j] = scale sum dS q[t][h];  dv[j] = sum P dout[t][h]
  * (dk, dv over the queries and the group's heads). The probabilities are computed again and never
  * stored. Sums are in fp32 and a fixed order: equal calls give equal bits; P and dS are rounded to dtype for
- * their products (fp16: scaled by powers of two, so that dS keeps its digits down to 2^-28 of its bound, the largest
- * sum_i |dout_i| (max |v_i| + max |out_i|) of its query over the keys that it sees for dq, of its key over the
- * queries and heads that see it for dk; smaller ones are off by 2^-39 of the bound each).
+ * their products. (fp16: scaled by powers of two, so that P keeps its digits down to 2^-28, and dS down to 2^-28 of
+ * its bound, the largest sum_i |dout_i| (max |v_i| + max |out_i|): for dq that of its query over the keys that it
+ * sees, for dk that of its key over the queries and heads that see it. Smaller ones are off by 2^-39 each, or by
+ * that of the bound.)
  * Queries that see nothing and keys that nothing sees get zeros; a query that sees one key (P = 1 whatever
  * the scores) gets dq = 0 and adds nothing to dk. dq like q, dk and dv like k, each with
  * strides of its own;

@@ -3,7 +3,7 @@
 //   P = exp(scale q k^T - lse),  delta = rowsum(dout o out),  dS = P (dout v^T - delta)
 //   dv = P^T dout,  dk = scale dS^T q  (over the rows of a group's heads),  dq = scale dS k
 //
-//   span_rows   each row's lse and delta, each row tile's limits
+//   span_rows   each row's lse and delta, each row tile's limits; in fp16 the sizes that dS is scaled by
 //   span_grad   keys_block: dk and dv of 128 keys, a walk over the row tiles that see some of them
 //               query_block: dq of a row tile, a walk over its key blocks
 // Scores and dout v^T are computed twice, 7 products for the 5 that are needed, so that every sum stays
@@ -11,8 +11,9 @@
 //
 // Bound by the chain from the scores through P and dS to the products that wait for them; all 7 products
 // of the measured cuBLAS rate:
-//   9360 queries in chunks of 1560, each sees up to 4; 16 heads of 64 on 4   520 us  1208 TFLOP/s, 64 %
-//   8191 causal tokens, 32 heads of 128 on 8                              1190 us  1615 TFLOP/s, 85 %
+//   9360 queries in chunks of 1560, each sees up to 4; 16 heads of 64 on 4   522 us  1203 TFLOP/s, 64 %
+//   8191 causal tokens, 32 heads of 128 on 8                    1177 to 1195 us  1633 TFLOP/s, 86 %
+//   the same in fp16, whose scales cost a look at sizes in every block        560 us, 1297 us
 // (a smaller clip: tensor cores 50 % busy, issue slots 58 %; fewer causal tokens: 66 % and 50 %). Dropped: X
 // and Y read together, with dS told a step later (688 us to 1056 for the first).
 #include <algorithm>
@@ -378,8 +379,8 @@ struct KeySizes {
     return larger(larger(all[at], all[kTile + at]), larger(all[2 * kTile + at], all[3 * kTile + at]));
   }
 };
-// So few tokens are all looked at, while the limits of the tiles are on their way (2 sequences of 77, forward and
-// backward launches in a stream: 17.4 us, by tiles 17.9).
+// So few tokens are all looked at, while the limits of the tiles are on their way (2 sequences of 77 each, 6 heads of 64
+// on 2: 17.4 us, by tiles 17.9).
 constexpr int kFewTokens = 256;
 
 template <bool F16, int D>
@@ -1240,7 +1241,7 @@ __global__ void span_zeros_kernel(SpanRows r, int tokens, int heads, int head_di
 }
 
 // Parts of a unit's walk over `steps` tiles: as many as give every SM a unit, but four tiles (4 us) each at
-// least, since the sums of the parts take 3 us. (More parts of the keys' walks, four units an SM, even them out
+// least where every tile is walked (spans are not known here), since the sums of the parts take 3 us. (More parts of the keys' walks, four units an SM, even them out
 // no better than the queries' units behind them do: 555 us instead of 519 for the 480p clip.)
 int parts_for(int64_t units, int steps) {
   return static_cast<int>(
